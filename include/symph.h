@@ -346,6 +346,111 @@ int32_t symph_debug_check_tables(const symph_kv_cache* cache, const int32_t* d_b
                                  const int32_t* d_lens, int32_t n_sessions, int32_t is_destination, void* stream,
                                  int32_t* h_first_bad_session);
 
+/*
+ * A speculative decoding step over the paged cache.  A draft of a few tokens per session, arranged as a tree, is scored by
+ * the model in one pass, and the path the model agrees with is kept (many tokens per read of a long cache, where a decode
+ * step of Sec. 2.2 reads it all for one).  Drafted tokens are numbered like new tokens: session s owns rows cu_new_lens[s]
+ * .. cu_new_lens[s+1]-1, its nodes 0 .. N_s-1; node 0 is the tree's root, the last token the session has emitted (its K,V
+ * are not in the cache yet); a parent comes before its children.  A step is
+ *   symph_build_tables   blocks for the drafted tokens, where each would lie in the pools
+ *   symph_tree_mask      who sees whom, and the positions (for rotary embeddings) of the drafted tokens
+ *   symph_tree_attn      per layer
+ *   symph_tree_accept    the accepted path, the next root
+ *   symph_kv_commit      its K,V rows, all layers, into the cache
+ * after which the lengths that symph_tree_accept wrote are the next step's prefix lengths.
+ */
+
+/*
+ * Block tables and slot maps from lengths.  Session s has P_s cached tokens (d_prefix_lens [n_sessions]) and the first H_s
+ * entries of its row of d_block_table, which are kept: H_s = ceil(P_s / block_size), or d_held_blocks[s] where that is given
+ * and more (blocks taken for drafted tokens that were not accepted stay the session's).  It gets room for N_s more tokens
+ * (d_new_lens):
+ *   table entries H_s .. ceil((P_s + N_s) / block_size) - 1 become the next ids of d_free_blocks [n_free], taken in session
+ *   order from entry *d_free_begin on (NULL: from 0); -1 where the list has ended;
+ *   d_cu_new_lens  int32 [n_sessions+1], d_token_offsets int64 [n_sessions+1]: exclusive prefix sums of N (what the attention
+ *                  and append calls and what the pack / unpack calls take);
+ *   d_slot_map     int64 [total_new_tokens]: block id * block_size + place in the block of every new token, -1 for one without
+ *                  a block (list ended, row of the table ended, id outside [0, n_blocks));
+ *   d_positions    int32 [total_new_tokens]: P_s + i of new token i;
+ *   d_blocks_taken int32 [1]: *d_free_begin + the ids all sessions need, i.e. the next call's *d_free_begin; more than n_free
+ *                  says that the list was too short;
+ *   d_held_after   int32 [n_sessions]: entries of the row that the session holds now (entries of -1 counted).
+ * The last six may be NULL each, d_held_blocks and d_free_begin too; an output must not be the input it belongs to
+ * (d_held_after and d_held_blocks, d_blocks_taken and d_free_begin).  With P_s = 0 this is the table of an arriving session
+ * (symph_kv_unpack), with N_s = its drafted tokens that of a step.  total_new_tokens = sum of N (host copy) sizes the grid:
+ * tokens past it get neither slot nor block; entries past the true sum are -1.  Lengths below 0 count as 0.
+ */
+int32_t symph_build_tables(const int32_t* d_prefix_lens, const int32_t* d_new_lens, const int32_t* d_held_blocks,
+                           int32_t n_sessions, int32_t* d_block_table, int32_t table_stride, const int32_t* d_free_blocks,
+                           int32_t n_free, const int32_t* d_free_begin, int32_t block_size, int32_t n_blocks,
+                           int64_t total_new_tokens, int32_t* d_cu_new_lens, int64_t* d_token_offsets, int64_t* d_slot_map,
+                           int32_t* d_positions, int32_t* d_blocks_taken, int32_t* d_held_after, void* stream);
+
+/*
+ * Masks of trees from parent links: bit j of row i (word j / 64 of d_mask [total_new_tokens][mask_words], bit j % 64) is set
+ * where node j of the session is node i itself or an ancestor of it.  d_parents int32 [total_new_tokens]: index of the parent
+ * within the session; any value outside 0 .. i-1 makes node i a root.  d_positions (int32 [total_new_tokens], may be NULL)
+ * becomes P_s + number of ancestors (P_s from d_prefix_lens, 0 where that is NULL).
+ * max_new_len >= max N_s; at most 64 * mask_words and SYMPH_TREE_MAX_NODES.  Rows of nodes past max_new_len are not written.
+ */
+#define SYMPH_TREE_MAX_NODES 4096
+int32_t symph_tree_mask(const int32_t* d_parents, const int32_t* d_cu_new_lens, const int32_t* d_prefix_lens,
+                        int32_t n_sessions, int32_t total_new_tokens, int32_t max_new_len, uint64_t* d_mask,
+                        int32_t mask_words, int32_t* d_positions, void* stream);
+
+/*
+ * Attention of one layer for drafted tokens (the attention definition of Sec. 2.1 with a mask over the new tokens).  For
+ * session s, query head h, new token i:
+ *   out[cu[s]+i][h][:] = sum_j softmax_j(scale * <q, k_j>) v_j,   j over the P_s cached keys (paged, kv-head
+ *   h / (n_q_heads / n_kv_heads)) followed by those new keys whose bit is set in row cu[s]+i of d_tree_mask.
+ * The mask is the caller's: symph_tree_mask builds the one of a tree, any other bits do as well (bits at or past N_s are
+ * ignored; a token does not see itself unless its own bit is set).  A row that sees no key (P_s = 0 and no bit) is zero.
+ * K,V of masked tokens may hold anything, infinities and NaN too: they reach no row that does not see them.
+ * Arguments as for symph_prefix_prefill_attn; d_tree_mask uint64 [total_new_tokens][mask_words], 64 * mask_words >=
+ * max_new_len.  max_new_len and max_prefix_len choose how the work is divided and are not relied on for memory safety or
+ * results.  d_out may be d_q.  d_workspace: at least symph_tree_attn_workspace_bytes(...) bytes, 256-byte aligned (may be
+ * NULL where that is 0); nothing has to be cleared.
+ * Arithmetic: fp32 sums and softmax state.  bf16: products on the matrix cores, probabilities as two bf16 values whose sum
+ * keeps 16 bits of each, output rounded to nearest even.  fp32 throughout for fp32.
+ * Supported: head_dim 64 or 128, n_q_heads a multiple of n_kv_heads, any block size.
+ */
+int32_t symph_tree_attn(const symph_kv_cache* cache, int32_t layer, const void* d_q, const void* d_k_new,
+                        const void* d_v_new, void* d_out, const uint64_t* d_tree_mask, int32_t mask_words,
+                        const int32_t* d_cu_new_lens, const int32_t* d_prefix_lens, const int32_t* d_block_table,
+                        int32_t table_stride, int32_t n_sessions, int32_t n_q_heads, int32_t total_new_tokens,
+                        int32_t max_new_len, int32_t max_prefix_len, float scale, void* d_workspace,
+                        int64_t workspace_bytes, void* stream);
+/* Scratch bytes symph_tree_attn needs for these host-side values (the same as in the call; 0 is possible).  Negative on bad
+ * input. */
+int64_t symph_tree_attn_workspace_bytes(const symph_kv_cache* cache, int32_t n_sessions, int32_t n_q_heads,
+                                        int32_t total_new_tokens, int32_t max_new_len, int32_t max_prefix_len);
+
+/*
+ * The accepted path of every session's tree.  d_target_tokens int32 [total_new_tokens]: the token that the model puts behind
+ * each node (the arg-max of its logits, or a sample).  The root is accepted; behind an accepted node, of its children whose
+ * drafted token (d_draft_tokens, int32) equals the node's target token, the one with the lowest index.  Written:
+ *   d_rows        int32 [total_new_tokens]: entry cu[s]+k is the row (cu[s] + node) of the k-th accepted node, -1 past the last;
+ *   d_n_accepted  int32 [n_sessions], the root counted (0 for a session without nodes);
+ *   d_next_tokens int32 [n_sessions]: the target token of the last accepted node, the next root (-1 without nodes);
+ *   d_new_prefix_lens int32 [n_sessions], may be NULL: P_s + n_accepted (may be d_prefix_lens itself; that may be NULL only
+ *                 where this is).
+ * d_parents as for symph_tree_mask.
+ */
+int32_t symph_tree_accept(const int32_t* d_draft_tokens, const int32_t* d_parents, const int32_t* d_target_tokens,
+                          const int32_t* d_cu_new_lens, const int32_t* d_prefix_lens, int32_t n_sessions,
+                          int32_t total_new_tokens, int32_t* d_rows, int32_t* d_n_accepted, int32_t* d_next_tokens,
+                          int32_t* d_new_prefix_lens, void* stream);
+
+/*
+ * Writes K,V rows of all layers through a slot map: for every t with 0 <= d_rows[t] < n_rows and a slot d_slot_map[t] inside
+ * the cache, row d_rows[t] of d_k_new / d_v_new [n_layers][n_rows][n_kv_heads][head_dim] (cache dtype) goes to that slot of
+ * every layer; other t are skipped and no other byte of the pools changes.  With the rows of symph_tree_accept and the slots
+ * of symph_build_tables: the accepted path, node k of it behind the prefix at place k.  n_entries: length of d_rows and
+ * d_slot_map.  A slot named twice has two writers and is undefined.  Alignment as for symph_kv_pack.
+ */
+int32_t symph_kv_commit(const symph_kv_cache* cache, const void* d_k_new, const void* d_v_new, int32_t n_rows,
+                        const int32_t* d_rows, const int64_t* d_slot_map, int32_t n_entries, void* stream);
+
 /* Plain contiguous device copy with the same 16-byte-per-lane access shape as pack / unpack: the practical
  * HBM ceiling the migration kernels are compared with, and the known-size kernel used to calibrate hardware
  * traffic counters.  bytes must be a multiple of 16, pointers 16-byte aligned. */

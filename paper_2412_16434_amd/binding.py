@@ -20,7 +20,8 @@ EXPORTED_SYMBOLS = (
     "symph_prefix_prefill_attn", "symph_prefix_prefill_attn_workspace_bytes", "symph_prefix_prefill_attn_tuned",
     "symph_prefix_prefill_attn_workspace_bytes_tuned", "symph_prefix_prefill_attn_static", "symph_debug_attn_flags", "symph_stage_to_host",
     "symph_stage_to_device", "symph_stage_layer_to_host", "symph_stage_layer_to_device", "symph_device_copy",
-    "symph_mfma_reference", "symph_debug_check_tables",
+    "symph_build_tables", "symph_tree_mask", "symph_tree_attn", "symph_tree_attn_workspace_bytes", "symph_tree_accept",
+    "symph_kv_commit", "symph_mfma_reference", "symph_debug_check_tables",
     "symph_status_string",
     # symph_pool.h (host code only)
     "symph_pool_create", "symph_pool_destroy", "symph_pool_advise", "symph_pool_drop", "symph_pool_claim",
@@ -107,6 +108,18 @@ def load_library():
     lib.symph_prefix_prefill_attn_static.argtypes = lib.symph_prefix_prefill_attn.argtypes[:16] + [vp]
     lib.symph_debug_attn_flags.restype = i32
     lib.symph_debug_attn_flags.argtypes = [vp, vp, C.POINTER(i32)]
+    lib.symph_build_tables.restype = i32
+    lib.symph_build_tables.argtypes = [vp, vp, vp, i32, vp, i32, vp, i32, vp, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp]
+    lib.symph_tree_mask.restype = i32
+    lib.symph_tree_mask.argtypes = [vp, vp, vp, i32, i32, i32, vp, i32, vp, vp]
+    lib.symph_tree_attn.restype = i32
+    lib.symph_tree_attn.argtypes = [cp, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, i32, i32, i32, i32, i32, i32, f32, vp, i64, vp]
+    lib.symph_tree_attn_workspace_bytes.restype = i64
+    lib.symph_tree_attn_workspace_bytes.argtypes = [cp, i32, i32, i32, i32, i32]
+    lib.symph_tree_accept.restype = i32
+    lib.symph_tree_accept.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+    lib.symph_kv_commit.restype = i32
+    lib.symph_kv_commit.argtypes = [cp, vp, vp, i32, vp, vp, i32, vp]
     for fn in (lib.symph_stage_to_host, lib.symph_stage_to_device):
         fn.restype = i32
         fn.argtypes = [vp, vp, i64, vp, vp, vp]
@@ -484,6 +497,117 @@ def prefix_prefill_attn_static(cache: KVCache, layer: int, q, k_new, v_new, out,
                       max_prefix_len, scale)
     _check(load_library().symph_prefix_prefill_attn_static(C.byref(st), *args, _stream_ptr(stream)),
            "symph_prefix_prefill_attn_static")
+
+
+def _vector(t, name: str, dtype, length: Optional[int] = None, allow_none: bool = False):
+    """Pointer of a 1-D device tensor of ``dtype`` with at least ``length`` entries."""
+    if t is None and allow_none:
+        return None
+    ptr = _dev(t, name, dtype)
+    if t.dim() != 1:
+        raise ValueError(f"{name} must be 1-D")
+    if length is not None and t.shape[0] < length:
+        raise ValueError(f"{name} must have {length} entries, not {t.shape[0]}")
+    return ptr
+
+
+def build_tables(prefix_lens, new_lens, block_table, free_blocks, block_size: int, n_blocks: int, total_new_tokens: int,
+                 cu_new_lens=None, token_offsets=None, slot_map=None, positions=None, blocks_taken=None, held_blocks=None,
+                 held_after=None, free_begin=None, stream=None) -> None:
+    """Block table entries for ``new_lens`` more tokens of every session, taken from ``free_blocks`` in session order, and
+    what is asked for of: prefix sums (``cu_new_lens`` int32, ``token_offsets`` int64), the slot of every new token in a
+    layer's pool (``slot_map`` int64, -1: none), ``positions`` and the entries of the free list used up so far."""
+    torch = _torch()
+    i32, i64 = torch.int32, torch.int64
+    n, t = prefix_lens.shape[0], int(total_new_tokens)
+    tp, stride = _table(block_table)
+    if tp is not None and block_table.shape[0] < n:
+        raise ValueError(f"block_table must have {n} rows, not {block_table.shape[0]}")
+    _check(load_library().symph_build_tables(
+        _vector(prefix_lens, "prefix_lens", i32), _vector(new_lens, "new_lens", i32, n),
+        _vector(held_blocks, "held_blocks", i32, n, True), n, tp, stride, _vector(free_blocks, "free_blocks", i32),
+        free_blocks.shape[0], _vector(free_begin, "free_begin", i32, 1, True), int(block_size), int(n_blocks), t,
+        _vector(cu_new_lens, "cu_new_lens", i32, n + 1, True), _vector(token_offsets, "token_offsets", i64, n + 1, True),
+        _vector(slot_map, "slot_map", i64, t, True), _vector(positions, "positions", i32, t, True),
+        _vector(blocks_taken, "blocks_taken", i32, 1, True), _vector(held_after, "held_after", i32, n, True),
+        _stream_ptr(stream)), "symph_build_tables")
+
+
+def _mask_words(mask, rows: int, name: str):
+    """(pointer, words of a row) of an int64 [rows][words] mask."""
+    if mask is None or mask.dim() != 2 or mask.shape[0] < rows:
+        raise ValueError(f"{name} must be an int64 tensor [{rows}][words]")
+    return _dev(mask, name, _torch().int64), mask.shape[1]
+
+
+def tree_mask(parents, cu_new_lens, max_new_len: int, mask, prefix_lens=None, positions=None, stream=None) -> None:
+    """mask[T][words] (int64, 64 bits a word) <- bit j of row i: node j is node i or an ancestor of it.  ``parents`` holds
+    indices within the session (anything outside 0 .. i-1: a root); ``positions`` <- prefix length + number of ancestors."""
+    i32 = _torch().int32
+    n, t = cu_new_lens.shape[0] - 1, parents.shape[0]
+    mp, words = _mask_words(mask, t, "mask")
+    _check(load_library().symph_tree_mask(
+        _vector(parents, "parents", i32), _vector(cu_new_lens, "cu_new_lens", i32),
+        _vector(prefix_lens, "prefix_lens", i32, n, True), n, t, int(max_new_len), mp, words,
+        _vector(positions, "positions", i32, t, True), _stream_ptr(stream)), "symph_tree_mask")
+
+
+def tree_attn_workspace_bytes(cache: KVCache, n_sessions: int, n_q_heads: int, total_new_tokens: int, max_new_len: int,
+                              max_prefix_len: int) -> int:
+    st = cache.struct()
+    n = load_library().symph_tree_attn_workspace_bytes(C.byref(st), n_sessions, n_q_heads, total_new_tokens, max_new_len,
+                                                       max_prefix_len)
+    if n < 0:
+        raise SymphError(-1, "symph_tree_attn_workspace_bytes")
+    return int(n)
+
+
+def tree_attn(cache: KVCache, layer: int, q, k_new, v_new, out, tree_mask, cu_new_lens, prefix_lens, block_table,
+              max_new_len: int, max_prefix_len: int, scale: float, workspace=None, stream=None) -> None:
+    """out[T][H_q][d] <- attention of drafted tokens over [cached prefix ; the drafted tokens whose bit is set in
+    ``tree_mask`` (int64 [T][words])] for one layer.  A row that sees nothing is zero."""
+    st = cache.struct()
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    args = _attn_args(cache, layer, q, k_new, v_new, out, cu_new_lens, prefix_lens, block_table, max_new_len,
+                      max_prefix_len, scale)
+    n, (hkv, d) = prefix_lens.shape[0], cache.k_pool.shape[3:]
+    if q.shape[2] != d or k_new.shape != (q.shape[0], hkv, d):
+        raise ValueError(f"q must be [T][H_q][{d}] and k_new / v_new [T][{hkv}][{d}]")
+    if cu_new_lens.shape[0] < n + 1 or (block_table is not None and block_table.shape[0] < n):
+        raise ValueError(f"cu_new_lens must have {n + 1} entries and block_table {n} rows")
+    mp, words = _mask_words(tree_mask, q.shape[0], "tree_mask")
+    _check(load_library().symph_tree_attn(C.byref(st), *args[:5], mp, words, *args[5:],
+                                          _dev(workspace, "workspace", allow_none=True), ws_bytes, _stream_ptr(stream)),
+           "symph_tree_attn")
+
+
+def tree_accept(draft_tokens, parents, target_tokens, cu_new_lens, prefix_lens, rows, n_accepted, next_tokens,
+                new_prefix_lens=None, stream=None) -> None:
+    """The path of every session's tree that agrees with ``target_tokens`` (the model's token behind each node): ``rows`` <-
+    rows of the accepted nodes from entry cu[s] on, then -1; ``n_accepted``, ``next_tokens`` and the new lengths per session."""
+    i32 = _torch().int32
+    n, t = cu_new_lens.shape[0] - 1, draft_tokens.shape[0]
+    _check(load_library().symph_tree_accept(
+        _vector(draft_tokens, "draft_tokens", i32), _vector(parents, "parents", i32, t),
+        _vector(target_tokens, "target_tokens", i32, t), _vector(cu_new_lens, "cu_new_lens", i32),
+        _vector(prefix_lens, "prefix_lens", i32, n, True), n, t, _vector(rows, "rows", i32, t),
+        _vector(n_accepted, "n_accepted", i32, n), _vector(next_tokens, "next_tokens", i32, n),
+        _vector(new_prefix_lens, "new_prefix_lens", i32, n, True), _stream_ptr(stream)), "symph_tree_accept")
+
+
+def kv_commit(cache: KVCache, k_new, v_new, rows, slot_map, stream=None) -> None:
+    """Row ``rows[t]`` of ``k_new`` / ``v_new`` [L][n_rows][H_kv][d] into slot ``slot_map[t]`` of every layer, for every t where
+    both are valid (>= 0 and in range)."""
+    st = cache.struct()
+    k = cache.k_pool
+    if k_new.dim() != 4 or v_new.shape != k_new.shape or (k_new.shape[0], *k_new.shape[2:]) != (k.shape[0], *k.shape[3:]):
+        raise ValueError("k_new / v_new must be [L][n_rows][H_kv][d]")
+    torch = _torch()
+    n = rows.shape[0]
+    _check(load_library().symph_kv_commit(
+        C.byref(st), _dev(k_new, "k_new", k.dtype), _dev(v_new, "v_new", k.dtype), k_new.shape[1],
+        _vector(rows, "rows", torch.int32), _vector(slot_map, "slot_map", torch.int64, n), n, _stream_ptr(stream)),
+        "symph_kv_commit")
 
 
 def debug_attn_flags(workspace, stream=None) -> int:

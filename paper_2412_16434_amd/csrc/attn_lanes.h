@@ -1,4 +1,4 @@
-// What the attention kernels share: operand layouts of the 32x32x16 bf16 matrix instruction, exchanges between lanes.
+// What the attention kernels share: operand layouts of the 32x32x16 bf16 matrix instruction, exchanges between lanes, sums over them.
 #pragma once
 
 #include "common.h"
@@ -42,6 +42,23 @@ __device__ __forceinline__ float sum_across_halves(float x) {
   float lo, hi;
   swap_halves(x, lo, hi);
   return lo + hi;
+}
+
+// Inclusive scan over the 64 lanes of a wave with data-parallel moves: shifts by 1, 2, 4, 8 inside each row of 16
+// lanes (a lane without a source adds 0), then the last lane of rows 0 and 2 added to rows 1 and 3, then lane 31 to
+// rows 2 and 3.  (A shuffle per step goes through the LDS crossbar and takes ten times as long.)
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int dpp_from(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xF, true);
+}
+__device__ __forceinline__ int wave_inclusive_scan(int v) {
+  v += dpp_from<0x111, 0xF>(v);  // row_shr:1
+  v += dpp_from<0x112, 0xF>(v);  // row_shr:2
+  v += dpp_from<0x114, 0xF>(v);  // row_shr:4
+  v += dpp_from<0x118, 0xF>(v);  // row_shr:8
+  v += dpp_from<0x142, 0xA>(v);  // row_bcast:15
+  v += dpp_from<0x143, 0xC>(v);  // row_bcast:31
+  return v;
 }
 
 }  // namespace symph

@@ -81,23 +81,6 @@ __device__ __forceinline__ int unit_tiles(int P, int N, int t0, int bmt) {
   return (P + min(N, t0 + bmt) + kBN - 1) / kBN;
 }
 
-// Inclusive scan over the 64 lanes of a wave with data-parallel moves: shifts by 1, 2, 4, 8 inside each row of 16
-// lanes (a lane without a source adds 0), then the last lane of rows 0 and 2 added to rows 1 and 3, then lane 31 to
-// rows 2 and 3.  (A shuffle per step goes through the LDS crossbar and takes ten times as long.)
-template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ int dpp_from(int v) {
-  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xF, true);
-}
-__device__ __forceinline__ int wave_inclusive_scan(int v) {
-  v += dpp_from<0x111, 0xF>(v);  // row_shr:1
-  v += dpp_from<0x112, 0xF>(v);  // row_shr:2
-  v += dpp_from<0x114, 0xF>(v);  // row_shr:4
-  v += dpp_from<0x118, 0xF>(v);  // row_shr:8
-  v += dpp_from<0x142, 0xA>(v);  // row_bcast:15
-  v += dpp_from<0x143, 0xC>(v);  // row_bcast:31
-  return v;
-}
-
 // Maximum over the 64 lanes of a wave of values >= 0 (the same moves as the scan; a lane without a source sees 0);
 // lane 63 holds the result.
 __device__ __forceinline__ int wave_inclusive_max(int v) {

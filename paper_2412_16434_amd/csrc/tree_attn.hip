@@ -1,0 +1,922 @@
+// tree_attn: drafted tokens against [paged cached prefix ; the drafted tokens themselves under a bit mask].
+//
+// The N drafted tokens of a session and the G query heads of a kv-head are N * G query rows that read the same keys; a tile
+// is up to 32 * RW of them (bf16; 16 * RW in fp32).  One workgroup of eight waves has one tile, one kv-head and one range of
+// keys: RW waves side by side on the rows, 8 / RW on the keys, each with a softmax of its own, joined through LDS at the end.
+// Trees are small and prefixes long, so the key axis is cut (a piece per workgroup) until the chip is full; the pieces of a
+// tile leave (maximum, sum, unnormalised rows) in the workspace and a second launch joins them.
+//   * Scores are computed transposed, S^T = K Q^T: a query per lane, so the softmax state is a scalar of the lane, and the
+//     probabilities a lane holds are the operand of O^T += V^T P^T as they are.
+//   * K goes from memory into operand registers; V through LDS (bf16: the transposing read) or registers (fp32).
+//   * Every key block has one 32-bit word per query row that says which of its keys the row sees: all ones inside the prefix,
+//     the low bits in its last block, the caller's mask in the blocks of the tree, which start at the tree's first token.
+#include "attn_lanes.h"
+
+namespace symph {
+
+struct TreeParams {
+  const void* k_layer;
+  const void* v_layer;
+  int64_t block_stride;  // elements
+  int32_t n_blocks, block_size, bs_shift, n_kv_heads, n_q_heads;  // bs_shift: log2(block_size) or -1
+  const void* q;
+  const void* k_new;
+  const void* v_new;
+  void* out;
+  const uint32_t* mask;
+  int32_t mask_words;  // 32-bit words of a row
+  const int32_t* cu_new_lens;
+  const int32_t* prefix_lens;
+  const int32_t* table;
+  int32_t table_stride, n_sessions, total;
+  float scale;
+  uint32_t group_bytes;  // bytes between blocks where 16 consecutive keys lie in one block and a block fits 32 bits; else 0
+  int32_t max_pieces;    // per kv-head: what the grid and the workspace have room for
+  int32_t c_min;         // key blocks of a tile that are not cut further
+  int32_t cut;           // 0: one piece per tile
+  float* parts;
+};
+
+template <typename T>
+struct TreeTile;
+template <>
+struct TreeTile<__bf16> {
+  static constexpr int R = 32;  // query rows of a wave, and keys of a block
+};
+template <>
+struct TreeTile<float> {
+  static constexpr int R = 16;
+};
+constexpr int kTreeWaves = 8;
+
+static __device__ __attribute__((aligned(256))) const unsigned kNoRow[128] = {};  // a head's row of zeros
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(__bf16 x) { return (float)x; }
+
+// Scores are kept in units of the exponential that the type uses: base 2 in bf16, e in fp32.
+template <typename T>
+__device__ __forceinline__ float exp_of(float x) {
+  if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(x);
+  return expf(x);
+}
+template <typename T>
+__device__ __forceinline__ float score_scale(float scale) {
+  return sizeof(T) == 2 ? scale * 1.4426950408889634f : scale;
+}
+
+// ---- which piece of which tile a workgroup has --------------------------------------------------------------------
+struct TreePiece {
+  int s, cu, P, N;
+  int tile, index, count;  // tile of the session, piece of the tile, pieces of each of its tiles
+  int block0, block1;      // key blocks: the prefix's first, then the tree's
+  int stride;              // between the numbers of a tile's consecutive pieces
+};
+
+template <int BM, int KB>
+__device__ __forceinline__ void tree_session(const TreeParams& p, int G, int i, int& cu, int& P, int& N, int& tiles,
+                                             int& blocks) {
+  cu = P = N = tiles = blocks = 0;
+  if (i >= p.n_sessions) return;
+  cu = max(p.cu_new_lens[i], 0);
+  N = max(min(p.cu_new_lens[i + 1], p.total) - cu, 0);
+  P = max(p.prefix_lens[i], 0);
+  if (N == 0) return;
+  tiles = (N * G + BM - 1) / BM;
+  blocks = P / KB + (P % KB != 0) + (N + KB - 1) / KB;
+}
+
+// Piece `g` of the batch.  A tile of b key blocks is cut into ceil(b / c) near-equal pieces, c being the smallest length for
+// which the batch's pieces fit; the tiles of a session have their pieces of the same keys beside each other.  Every wave works
+// this out by itself, a session per lane: no scheduling launch, no barrier.
+template <int BM, int KB>
+__device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, TreePiece& it) {
+  const int lane = threadIdx.x & 63;
+  int cu, P, N, tiles, blocks;
+  int c = 0x7FFFFFFF;
+  tree_session<BM, KB>(p, G, lane, cu, P, N, tiles, blocks);
+  if (p.cut) {
+    int64_t work = (int64_t)tiles * blocks;
+    int n_tiles = tiles;
+    for (int i = 64 + lane; i < p.n_sessions; i += 64) {
+      int a, b, d, t, k;
+      tree_session<BM, KB>(p, G, i, a, b, d, t, k);
+      work += (int64_t)t * k;
+      n_tiles += t;
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+      work += __shfl_xor((long long)work, o);
+      n_tiles += __shfl_xor(n_tiles, o);
+    }
+    const int64_t room = p.max_pieces - n_tiles;
+    if (room > 0) {
+      const int64_t even =  // (a 32-bit division where that is enough: a quarter of the instructions)
+          work + room <= 0x7FFFFFFFLL ? ((unsigned)work + (unsigned)room - 1) / (unsigned)room : (work + room - 1) / room;
+      c = (int)min(max(even, (int64_t)p.c_min), (int64_t)0x7FFFFFFF);
+    }
+  }
+  int before = 0;
+  for (int i0 = 0; i0 < p.n_sessions; i0 += 64) {
+    if (i0 > 0) tree_session<BM, KB>(p, G, i0 + lane, cu, P, N, tiles, blocks);
+    const int count = blocks / c + (blocks % c != 0), mine = tiles * count;
+    const int incl = wave_inclusive_scan(mine);
+    const uint64_t holds = __ballot(before + incl > g);
+    if (holds) {
+      const int at = __builtin_ctzll(holds);
+      it.s = i0 + at;
+      it.cu = __builtin_amdgcn_readlane(cu, at);
+      it.P = __builtin_amdgcn_readlane(P, at);
+      it.N = __builtin_amdgcn_readlane(N, at);
+      it.count = __builtin_amdgcn_readlane(count, at);
+      it.stride = __builtin_amdgcn_readlane(tiles, at);
+      const int local = g - before - __builtin_amdgcn_readlane(incl - mine, at), b = __builtin_amdgcn_readlane(blocks, at);
+      it.index = local / it.stride;
+      it.tile = local - it.index * it.stride;
+      it.block0 = (int)((int64_t)b * it.index / it.count);
+      it.block1 = (int)((int64_t)b * (it.index + 1) / it.count);
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
+// What a row without any probability gets: zero if it sees no key, NaN if all its scores are minus infinity (0 / 0).
+__device__ __forceinline__ float nothing_seen(const TreeParams& p, const TreePiece& it, int tok) {
+  bool sees = it.P > 0;
+  const uint32_t* row = p.mask + (int64_t)(it.cu + tok) * p.mask_words;
+  for (int w = 0; w < p.mask_words && w * 32 < it.N && !sees; ++w)
+    sees = (row[w] & (it.N - w * 32 >= 32 ? ~0u : (1u << (it.N - w * 32)) - 1u)) != 0;
+  return sees ? NAN : 0.f;
+}
+
+// ---- one row by one wave, lanes over the keys of blocks block0 .. block1 - 1, fp32 on the vector unit.  Keys that the row does
+// not see are not read.  The result (unnormalised, relative to the maximum m) is left in lds[D .. 2 D - 1]; lds: 2 * D floats of
+// the wave's own.  CH columns at a time, the scores worked out again for each.
+template <typename T, int D, int KB, int CH>
+__device__ __forceinline__ void row_by_lanes(const TreeParams& p, const TreePiece& it, int tok, int h, float* lds, float& m_row,
+                                             float& l_row) {
+  const int lane = threadIdx.x & 63;
+  const int g = h / (p.n_q_heads / p.n_kv_heads);
+  const int prefix_blocks = it.P / KB + (it.P % KB != 0);
+  const T* const q = (const T*)p.q + ((int64_t)(it.cu + tok) * p.n_q_heads + h) * D;
+  for (int c = lane; c < D; c += 64) lds[c] = widen(q[c]);
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const uint32_t* const mask = p.mask + (int64_t)(it.cu + tok) * p.mask_words;
+  const float cs = score_scale<T>(p.scale);
+  for (int c0 = 0; c0 < D; c0 += CH) {
+    float m = -INFINITY, l = 0.f;
+    float acc[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) acc[c] = 0.f;
+    for (int64_t v = (int64_t)it.block0 * KB + lane; v < (int64_t)it.block1 * KB; v += 64) {
+      const T* kp = nullptr;
+      const T* vp = nullptr;
+      if (v < (int64_t)prefix_blocks * KB) {
+        const int key = (int)v;
+        if (key >= it.P) continue;
+        const int b = key / p.block_size;
+        const int id = b < p.table_stride ? p.table[(int64_t)it.s * p.table_stride + b] : -1;
+        if (id >= 0 && id < p.n_blocks) {  // (else a row of zeros: score 0, value 0)
+          const int64_t e = (int64_t)id * p.block_stride + ((int64_t)(key - b * p.block_size) * p.n_kv_heads + g) * D;
+          kp = (const T*)p.k_layer + e;
+          vp = (const T*)p.v_layer + e;
+        }
+      } else {
+        const int j = (int)(v - (int64_t)prefix_blocks * KB);
+        if (j >= it.N || (j >> 5) >= p.mask_words || !((mask[j >> 5] >> (j & 31)) & 1)) continue;
+        const int64_t e = ((int64_t)(it.cu + j) * p.n_kv_heads + g) * D;
+        kp = (const T*)p.k_new + e;
+        vp = (const T*)p.v_new + e;
+      }
+      float dot = 0.f;
+      if (kp) {
+#pragma unroll 8
+        for (int c = 0; c < D; ++c) dot = fmaf(lds[c], widen(kp[c]), dot);
+      }
+      float x = cs * dot;
+      asm("" : "+v"(x));  // (rounded before the maximum is taken off, so that the largest score's exponent is 0 at any size)
+      const float m_new = fmaxf(m, x);
+      const float ref = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = exp_of<T>(m - ref);
+      const float w = exp_of<T>(x - ref);
+      l = l * alpha + w;
+      if (vp) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) acc[c] = fmaf(w, widen(vp[c0 + c]), acc[c] * alpha);
+      } else {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) acc[c] *= alpha;
+      }
+      m = m_new;
+    }
+    float M = m;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    const float f = m == -INFINITY ? (l == l ? 0.f : 1.f) : exp_of<T>(m - M);
+    float lt = l * f;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) lt += __shfl_xor(lt, o);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      float a = acc[c] * f;
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) a += __shfl_xor(a, o);
+      if (lane == 0) lds[D + c0 + c] = a;  // (a store by lane c each would keep CH lane masks in scalar registers)
+    }
+    m_row = M;
+    l_row = lt;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Addresses that the tiled kernel cannot load 16 bytes wide from: a wave per (token, head), all keys.
+template <typename T, int D>
+__global__ __launch_bounds__(64) void tree_row_kernel(const TreeParams p) {
+  constexpr int KB = TreeTile<T>::R;
+  __shared__ float lds[2 * D];
+  const int lane = threadIdx.x;
+  const int tok_all = (int)(blockIdx.x / (unsigned)p.n_q_heads), h = (int)(blockIdx.x % (unsigned)p.n_q_heads);
+  int lo = 0, hi = p.n_sessions;  // the last session that begins at or before the token
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (p.cu_new_lens[mid] <= tok_all)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  TreePiece it;
+  int tiles, blocks;
+  tree_session<1, KB>(p, 1, lo, it.cu, it.P, it.N, tiles, blocks);
+  const int tok = tok_all - it.cu;
+  if (tok < 0 || tok >= it.N) return;
+  it.s = lo;
+  it.block0 = 0;
+  it.block1 = blocks;
+  float m, l;
+  row_by_lanes<T, D, KB, D>(p, it, tok, h, lds, m, l);
+  const float none = l == 0.f ? nothing_seen(p, it, tok) : 0.f;
+  T* const out = (T*)p.out + ((int64_t)tok_all * p.n_q_heads + h) * D;
+  for (int c = lane; c < D; c += 64) out[c] = (T)(l == 0.f ? none : lds[D + c] * (1.0f / l));
+}
+
+// The part of a float that a bf16 value holds without rounding, and two such parts as neighbours of an operand
+__device__ __forceinline__ float upper_part(float x) {
+  return __builtin_bit_cast(float, __builtin_bit_cast(unsigned, x) & 0xFFFF0000u);
+}
+__device__ __forceinline__ void put_pair(bf16x8& v, int at, float x, float y) {
+  u32x4 words = __builtin_bit_cast(u32x4, v);
+  words[at >> 1] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, y), __builtin_bit_cast(unsigned, x), 0x07060302u);
+  v = __builtin_bit_cast(bf16x8, words);
+}
+
+template <int BM, int D>
+__device__ __forceinline__ float* part_slot(const TreeParams& p, int64_t g, int kvh) {
+  return p.parts + (g * p.n_kv_heads + kvh) * (int64_t)(BM * (D + 2));
+}
+
+// ---- the tiled kernel ----------------------------------------------------------------------------------------------
+template <typename T, int D, int RW>
+__global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const TreeParams p) {
+  constexpr bool kBf16 = sizeof(T) == 2;
+  constexpr int R = TreeTile<T>::R, BM = R * RW, W = kTreeWaves, KW = W / RW;
+  constexpr int kVRow = D * 2 + 64;  // bytes between V rows in LDS (bf16): the transposing read then has no conflicts
+  constexpr int kVBytes = kBf16 ? W * 32 * kVRow : 0;
+  constexpr int kStride = D + 4;  // floats between rows of the results
+  constexpr int kJoinBytes = W * R * kStride * 4;
+  __shared__ __attribute__((aligned(16))) char lds[kVBytes > kJoinBytes ? kVBytes : kJoinBytes];
+  __shared__ float wave_m[W][R], wave_l[W][R];
+  __shared__ unsigned bad_rows[RW];
+
+  const int Hkv = p.n_kv_heads;
+  const int G = p.n_q_heads / Hkv;
+  const int kvh = blockIdx.x % Hkv;
+  const int piece = blockIdx.x / Hkv;
+  TreePiece it;
+  if (!find_piece<BM, R>(p, G, piece, it)) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = wave % RW, kw = wave / RW;
+  const int n = lane & (R - 1);  // query row of this lane within its wave's; also its row of the K operand
+  const int kg = lane / R;       // its share of the contraction index: half (bf16) or quarter (fp32) of the wave
+  const int cu = it.cu, P = it.P, N = it.N;
+  const unsigned row0 = (unsigned)it.tile * BM;
+  const int n_rows = (int)min((unsigned)BM, (unsigned)N * (unsigned)G - row0);
+  const int prefix_blocks = P / R + (P % R != 0);
+  if (tid < RW) bad_rows[tid] = 0;
+
+  const unsigned my_row = row0 + min(rw * R + n, n_rows - 1);
+  const int tok = (int)(my_row / (unsigned)G);
+  const T* const qp = (const T*)p.q + ((int64_t)(cu + tok) * p.n_q_heads + kvh * G + (int)(my_row - (unsigned)tok * G)) * D;
+  const uint32_t* const mask_row = p.mask + (int64_t)(cu + tok) * p.mask_words;
+
+  auto block_of = [&](int key) { return p.bs_shift >= 0 ? key >> p.bs_shift : key / p.block_size; };
+  const int32_t* const table_row = p.table + (int64_t)it.s * p.table_stride;
+  // Block ids one per lane (lane i: key i of the block), passed between lanes
+  auto fetch_id = [&](int blk) {
+    const int key = blk * R + n;
+    if (blk >= min(prefix_blocks, it.block1) || key >= P) return -1;
+    const int j = block_of(key);
+    return j < p.table_stride ? table_row[j] : -1;
+  };
+  // Row r of key block blk
+  auto row_of = [&](const void* pool, const void* fresh, int blk, int r, int id) {
+    if (blk < prefix_blocks) {
+      const int key = blk * R + r;
+      if (key >= P || id < 0 || id >= p.n_blocks) return (const T*)kNoRow;
+      return (const T*)pool + (int64_t)id * p.block_stride + ((int64_t)(key - block_of(key) * p.block_size) * Hkv + kvh) * D;
+    }
+    const int j = (blk - prefix_blocks) * R + r;
+    return j < N ? (const T*)fresh + ((int64_t)(cu + j) * Hkv + kvh) * D : (const T*)kNoRow;
+  };
+  // The keys of a block that the lane's row sees, a bit each
+  auto seen_of = [&](int blk) -> uint32_t {
+    constexpr uint32_t kAll = R == 32 ? ~0u : 0xFFFFu;
+    const int left = blk < prefix_blocks ? P - blk * R : N - (blk - prefix_blocks) * R;
+    uint32_t bits = left >= R ? kAll : (1u << left) - 1u;
+    if (blk >= prefix_blocks) {
+      const int at = (blk - prefix_blocks) * R;
+      bits &= (at >> 5) < p.mask_words ? mask_row[at >> 5] >> (at & 31) : 0u;
+    }
+    return bits;
+  };
+  // Blocks that lie whole in the prefix, their 16-key groups in a block of the cache each: a group's rows start at a scalar
+  // address and a lane adds a constant.
+  const bool grouped = p.group_bytes != 0;
+  auto group_id = [&](int id, int g) { return __builtin_amdgcn_readlane(id, 16 * g); };
+  auto in_cache = [&](int id) { return (unsigned)id < (unsigned)p.n_blocks; };
+  const unsigned row_bytes = (unsigned)(Hkv * D * (int)sizeof(T));
+  auto group_off = [&](int key, int id) {
+    return (uint64_t)(unsigned)id * p.group_bytes + (unsigned)(key & (p.block_size - 1)) * row_bytes;
+  };
+  auto load_vec = [](const void* at) { return *(const u32x4 __attribute__((address_space(1)))*)(uintptr_t)at; };
+  auto load16 = [&](const char* base, unsigned lane_off) {
+    if constexpr (kBf16 || D == 128) asm("" : "+s"(base), "+v"(lane_off));
+    return load_vec(base + lane_off);
+  };
+  const char* const k_head = (const char*)((const T*)p.k_layer + kvh * D);
+  const char* const v_head = (const char*)((const T*)p.v_layer + kvh * D);
+
+  const int first = it.block0 + kw;
+  const int last = rw * R < n_rows ? it.block1 : it.block0;  // (waves without a row have no blocks)
+  const float cs = score_scale<T>(p.scale);
+  float m = -INFINITY, l = 0.f;
+  float* const mine = reinterpret_cast<float*>(lds) + (rw * KW + kw) * R * kStride;  // the wave's part of the results
+
+  // Between the loop and the results: the row's maximum over the KW waves, this wave's factor
+  auto share_state = [&](float l_row) {
+    if (lane < R) wave_m[rw * KW + kw][n] = m;
+    __syncthreads();  // (also: no wave reads its V tile any more, the buffer is free)
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < KW; ++w) M = fmaxf(M, wave_m[rw * KW + w][n]);
+    const float f = m == -INFINITY ? 0.f : exp_of<T>(m - M);
+    if (lane < R) wave_l[rw * KW + kw][n] = m == -INFINITY ? l_row : l_row * f;  // (no maximum: 0, or NaN scores)
+    return f;
+  };
+
+  if constexpr (kBf16) {
+    constexpr int NS = D / 16;            // contraction steps of the first product
+    constexpr int NT = D / 32;            // 32-column tiles of the output
+    constexpr int LPR = D / 8, RPI = 64 / LPR, NV = 32 / RPI;  // lanes per V row, rows per load, loads
+    char* const v_lds = lds + wave * 32 * kVRow;
+    bf16x8 q[NS];
+#pragma unroll
+    for (int st = 0; st < NS; ++st) q[st] = *reinterpret_cast<const bf16x8*>(qp + 16 * st + 8 * kg);
+    const int krow = key_of_row(n);
+    const int vlane_row = lane / LPR, vlane_col = (lane % LPR) * 16;
+    bf16x8 kr[NS];
+    u32x4 vr[NV];
+    const unsigned k_off = (krow & 15) * row_bytes + 16 * kg;
+    unsigned v_off_mem[NV / 2];
+#pragma unroll
+    for (int i = 0; i < NV / 2; ++i) v_off_mem[i] = (unsigned)(i * RPI + vlane_row) * row_bytes + vlane_col;
+    auto load_block = [&](int blk, int id) {
+      const int id0 = group_id(id, 0), id1 = group_id(id, 1);
+      if (grouped && blk < prefix_blocks && (blk + 1) * 32 <= P && in_cache(id0) && in_cache(id1)) {
+        const uint64_t off0 = group_off(blk * 32, id0), off1 = group_off(blk * 32 + 16, id1);
+        const char* const k_row = k_head + (krow < 16 ? off0 : off1) + k_off;
+#pragma unroll
+        for (int st = 0; st < NS; ++st) kr[st] = __builtin_bit_cast(bf16x8, load_vec(k_row + 32 * st));
+        const char* const v0 = v_head + off0;
+        const char* const v1 = v_head + off1;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) vr[i] = load16(i < NV / 2 ? v0 : v1, v_off_mem[i % (NV / 2)]);
+        return;
+      }
+      const T* const k_row = row_of(p.k_layer, p.k_new, blk, krow, __shfl(id, krow)) + 8 * kg;
+#pragma unroll
+      for (int st = 0; st < NS; ++st) kr[st] = __builtin_bit_cast(bf16x8, load_vec(k_row + 16 * st));
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int r = i * RPI + vlane_row;
+        const T* const v_row = row_of(p.v_layer, p.v_new, blk, r, __shfl(id, r));
+        vr[i] = load_vec(reinterpret_cast<const char*>(v_row) + vlane_col);
+      }
+    };
+    const int i16 = lane & 15;
+    const int v_off = (8 * kg + (i16 >> 2)) * kVRow + 32 * ((lane >> 4) & 1) + 8 * (i16 & 3);
+    f32x16 o[NT];
+#pragma unroll
+    for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+    int id_next = first < last ? fetch_id(first) : -1;
+    if (first < last) load_block(first, id_next);
+    id_next = fetch_id(first + KW);
+    for (int blk = first; blk < last; blk += KW) {
+      f32x16 x;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = 0.f;
+#pragma unroll
+      for (int st = 0; st < NS; ++st) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[st], q[st], x, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        *reinterpret_cast<u32x4*>(v_lds + (i * RPI + vlane_row) * kVRow + vlane_col) = vr[i];
+      if (blk + KW < last) load_block(blk + KW, id_next);
+      id_next = fetch_id(blk + 2 * KW);
+      if (blk >= prefix_blocks || (blk + 1) * 32 > P) {
+        const uint32_t bits = seen_of(blk) >> (8 * kg);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!((bits >> (16 * (e >> 3) + (e & 7))) & 1)) x[e] = -INFINITY;
+      }
+      float mx = x[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
+      const float m_new = fmaxf(m, max_across_halves(mx) * cs);
+      if (__any(m_new > m)) {
+        const float a = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        l *= a;
+#pragma unroll
+        for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[dt][e] *= a;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      // One multiplication and subtraction without a rounding between them: the rounding of `ref` itself is common to all keys
+      // and cancels, unless scores are so large that it is more than an exponent's range.
+      float to_log2 = cs;
+      if (__any(fabsf(ref) > 0x1p20f)) {
+        to_log2 = 1.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float y = x[e] * cs;
+          asm("" : "+v"(y));
+          x[e] = y;
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // (here, so that V operands can be read beside the exponentials)
+      __builtin_amdgcn_wave_barrier();
+      // the probabilities as two bf16 values each, w = hi + lo with 16 bits in all: the leading bits, then those of what is left
+      bf16x8 hi[2], lo[2];
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        float w[2], rest[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          w[k] = __builtin_amdgcn_exp2f(fmaf(x[e + k], to_log2, -ref));
+          sum += w[k];
+          rest[k] = w[k] - upper_part(w[k]);
+        }
+        put_pair(hi[e >> 3], e & 7, w[0], w[1]);
+        put_pair(lo[e >> 3], e & 7, rest[0], rest[1]);
+      }
+      l += sum;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int dt = 0; dt < NT; ++dt) {
+          const char* vp = v_lds + v_off + 16 * u * kVRow + 64 * dt;
+          const s16x4 a0 = lds_read_tr16(reinterpret_cast<const __bf16*>(vp));
+          const s16x4 a1 = lds_read_tr16(reinterpret_cast<const __bf16*>(vp + 4 * kVRow));
+          const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, hi[u], o[dt], 0, 0, 0);
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, lo[u], o[dt], 0, 0, 0);
+        }
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      __builtin_amdgcn_wave_barrier();  // the tile has been read before the next one is written
+    }
+    const float f = share_state(sum_across_halves(l));
+    if (rw * R < n_rows) {
+#pragma unroll
+      for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<f32x4*>(mine + n * kStride + 32 * dt + 4 * kg + 8 * i) =
+              f32x4{o[dt][4 * i] * f, o[dt][4 * i + 1] * f, o[dt][4 * i + 2] * f, o[dt][4 * i + 3] * f};
+    }
+  } else {
+    constexpr int NS = D / 16;  // 16-byte loads of a row per lane
+    constexpr int NH = D / 64;  // groups of 64 output columns
+    f32x4 q[NS];
+#pragma unroll
+    for (int j = 0; j < NS; ++j) q[j] = *reinterpret_cast<const f32x4*>(qp + 16 * j + 4 * kg);
+    f32x4 kr[NS], vr[4][NH];
+    const unsigned k_off = n * row_bytes + 16 * kg, v_off_mem = 4 * kg * row_bytes + 16 * n;
+    auto load_block = [&](int blk, int id) {
+      const int id0 = group_id(id, 0);
+      if (grouped && blk < prefix_blocks && (blk + 1) * 16 <= P && in_cache(id0)) {
+        const uint64_t off = group_off(blk * 16, id0);
+#pragma unroll
+        for (int j = 0; j < NS; ++j) kr[j] = __builtin_bit_cast(f32x4, load16(k_head + off + 64 * j, k_off));
+        const char* const v_rows = v_head + off;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int h = 0; h < NH; ++h)
+            vr[e][h] = __builtin_bit_cast(f32x4, load16(v_rows + e * row_bytes + 256 * h, v_off_mem));
+        return;
+      }
+      const T* const k_row = row_of(p.k_layer, p.k_new, blk, n, id) + 4 * kg;
+#pragma unroll
+      for (int j = 0; j < NS; ++j) kr[j] = __builtin_bit_cast(f32x4, load_vec(k_row + 16 * j));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {  // key 4 * kg + e: values 64 * h + 4 * n .. + 3 of its row
+        const T* const v_row = row_of(p.v_layer, p.v_new, blk, 4 * kg + e, __shfl(id, 4 * kg + e)) + 4 * n;
+#pragma unroll
+        for (int h = 0; h < NH; ++h) vr[e][h] = __builtin_bit_cast(f32x4, load_vec(v_row + 64 * h));
+      }
+    };
+    // o[h][c][e]: column 64 * h + 16 * kg + 4 * e + c of row n.  A sum over thousands of keys in one chain loses bits: kRun blocks
+    // are added up by themselves (o_run, l_run) before they join the rest.
+    constexpr int kRun = 8;
+    f32x4 o[NH][4], o_run[NH][4];
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[h][c] = o_run[h][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float l_run = 0.f;
+    auto join_run = [&]() {
+      l += l_run;
+      l_run = 0.f;
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          o[h][c] += o_run[h][c];
+          o_run[h][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    int run = 0;
+    int id_next = first < last ? fetch_id(first) : -1;
+    if (first < last) load_block(first, id_next);
+    id_next = fetch_id(first + KW);
+    for (int blk = first; blk < last; blk += KW) {
+      f32x4 sc[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < NS; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j][e], q[j][e], sc[e], 0, 0, 0);
+      f32x4 v[4][NH];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int h = 0; h < NH; ++h) v[e][h] = vr[e][h];
+      if (blk + KW < last) load_block(blk + KW, id_next);
+      id_next = fetch_id(blk + 2 * KW);
+      float x[4];  // key 4 * kg + e
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = cs * ((sc[0][e] + sc[1][e]) + (sc[2][e] + sc[3][e]));
+        asm("" : "+v"(x[e]));  // (rounded before the maximum is taken off, so that the largest score's exponent is 0 at any size)
+      }
+      if (blk >= prefix_blocks || (blk + 1) * 16 > P) {
+        const uint32_t bits = seen_of(blk) >> (4 * kg);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!((bits >> e) & 1)) x[e] = -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float m_new = fmaxf(m, mx);
+      if (__any(m_new > m)) {
+        const float a = m == -INFINITY ? 0.f : expf(m - m_new);
+        m = m_new;
+        l *= a;
+        l_run *= a;
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            o[h][c] *= a;
+            o_run[h][c] *= a;
+          }
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float w = expf(x[e] - ref);
+        l_run += w;
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            o_run[h][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][h][c], w, o_run[h][c], 0, 0, 0);
+      }
+      if (++run == kRun) {
+        join_run();
+        run = 0;
+      }
+    }
+    join_run();
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    const float f = share_state(l);
+    if (rw * R < n_rows) {
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<f32x4*>(mine + n * kStride + 64 * h + 16 * kg + 4 * e) =
+              f32x4{o[h][0][e] * f, o[h][1][e] * f, o[h][2][e] * f, o[h][3][e] * f};
+    }
+  }
+  __syncthreads();
+
+  // ---- results of the tile: a thread adds up four columns of a row at a time over the KW waves.  A row with a value that is not
+  // finite (an infinity or a NaN among the values, which the matrix product spreads to rows that do not see it) is worked out
+  // again by itself.  Its q is read again for that, so nothing is written before: out may be q.
+  constexpr int kQuads = BM * D / 4, kTurns = (kQuads + 64 * W - 1) / (64 * W);
+  typedef T vec __attribute__((ext_vector_type(4)));
+  const float* const all = reinterpret_cast<const float*>(lds);
+  const bool whole = it.count == 1;
+  float* const slot = whole ? nullptr : part_slot<BM, D>(p, piece, kvh);
+  f32x4 x[kTurns];
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    const int i = tid + t * 64 * W, r = i / (D / 4), c0 = 4 * (i % (D / 4));
+    if (i >= kQuads || r >= n_rows) break;
+    const int w0 = (r / R) * KW;
+    float L = 0.f, M = -INFINITY;
+    f32x4 sum{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < KW; ++w) {
+      L += wave_l[w0 + w][r % R];
+      M = fmaxf(M, wave_m[w0 + w][r % R]);
+      sum += *reinterpret_cast<const f32x4*>(all + ((w0 + w) * R + r % R) * kStride + c0);
+    }
+    if (L == 0.f) sum = f32x4{0.f, 0.f, 0.f, 0.f};  // (no probability: whatever values the product brought in are not the row's)
+    bool bad = false;
+    float scale = 1.0f, none = 0.f;
+    if (whole) {
+      scale = L == 0.f ? 0.f : 1.0f / L;
+      if (L == 0.f) none = nothing_seen(p, it, (int)((row0 + r) / (unsigned)G));
+    } else if (c0 == 0) {
+      slot[BM * D + r] = M;
+      slot[BM * D + BM + r] = L;
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      sum[v] = sum[v] * scale + none;
+      bad = bad || !(fabsf(sum[v]) < INFINITY);
+    }
+    x[t] = sum;
+    // (a sum that is NaN comes from a score that is: every value of the row is NaN either way; so is 0 / 0)
+    if (bad && L == L && L != 0.f) atomicOr(&bad_rows[r / R], 1u << (r % R));
+  }
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    const int i = tid + t * 64 * W, r = i / (D / 4), c0 = 4 * (i % (D / 4));
+    if (i >= kQuads || r >= n_rows) break;
+    if ((bad_rows[r / R] >> (r % R)) & 1) continue;
+    if (whole) {
+      const unsigned row = row0 + r, tk = row / (unsigned)G;
+      T* const op = (T*)p.out + ((int64_t)(cu + (int)tk) * p.n_q_heads + kvh * G + (int)(row - tk * G)) * D;
+      vec y;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) y[v] = (T)x[t][v];
+      *reinterpret_cast<vec*>(op + c0) = y;
+    } else {
+      *reinterpret_cast<f32x4*>(slot + r * D + c0) = x[t];
+    }
+  }
+  int turn = 0;
+  for (int grp = 0; grp < RW; ++grp)
+    for (unsigned left = __builtin_amdgcn_readfirstlane(bad_rows[grp]); left; left &= left - 1) {
+      if (turn++ % W != wave) continue;
+      const int r = grp * R + __builtin_ctz(left);
+      const unsigned row = row0 + r, tk = row / (unsigned)G;
+      const int h = kvh * G + (int)(row - tk * G);
+      float* const own = reinterpret_cast<float*>(lds) + wave * 2 * D;
+      float rm, rl;
+      row_by_lanes<T, D, R, 64>(p, it, (int)tk, h, own, rm, rl);
+      if (whole) {
+        T* const op = (T*)p.out + ((int64_t)(cu + (int)tk) * p.n_q_heads + h) * D;
+        const float none = rl == 0.f ? nothing_seen(p, it, (int)tk) : 0.f;
+        for (int c = lane; c < D; c += 64) op[c] = (T)(rl == 0.f ? none : own[D + c] * (1.0f / rl));
+      } else {
+        for (int c = lane; c < D; c += 64) slot[r * D + c] = own[D + c];
+        if (lane == 0) {
+          slot[BM * D + r] = rm;
+          slot[BM * D + BM + r] = rl;
+        }
+      }
+    }
+}
+
+// ---- joins the pieces of cut tiles: out = sum_c f_c O_c / sum_c f_c l_c, f_c = e^(m_c - max_c m_c).  Each of a tile's pieces
+// has a workgroup here too, which joins an equal share of the tile's rows, a wave per row.
+template <typename T, int D, int RW>
+__global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
+  constexpr int R = TreeTile<T>::R, BM = R * RW, LPR = D / 4, SUB = 64 / LPR;  // lanes per row, pieces side by side
+  const int Hkv = p.n_kv_heads;
+  const int G = p.n_q_heads / Hkv;
+  const int kvh = blockIdx.x % Hkv, piece = blockIdx.x / Hkv;
+  TreePiece it;
+  if (!find_piece<BM, R>(p, G, piece, it) || it.count == 1) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const unsigned row0 = (unsigned)it.tile * BM;
+  const int n_rows = (int)min((unsigned)BM, (unsigned)it.N * (unsigned)G - row0);
+  const int r0 = (int)((int64_t)n_rows * it.index / it.count), r1 = (int)((int64_t)n_rows * (it.index + 1) / it.count);
+  const int64_t first = piece - (int64_t)it.index * it.stride;
+  const int sub = lane / LPR, c0 = 4 * (lane % LPR);
+  for (int r = r0 + wave; r < r1; r += 4) {
+    float M = -INFINITY, L = 0.f;
+    for (int c = lane; c < it.count; c += 64) M = fmaxf(M, part_slot<BM, D>(p, first + (int64_t)c * it.stride, kvh)[BM * D + r]);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    f32x4 sum{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < it.count; b += 64) {
+      const int c = b + lane;
+      float f = 0.f;
+      if (c < it.count) {
+        const float* const slot = part_slot<BM, D>(p, first + (int64_t)c * it.stride, kvh);
+        const float m = slot[BM * D + r], l = slot[BM * D + BM + r];
+        f = m == -INFINITY ? (l == l ? 0.f : 1.f) : exp_of<T>(m - M);
+        L += l * f;
+      }
+      const int here = min(64, it.count - b);
+      for (int k = 0; k < here; k += SUB) {
+        const int at = k + sub;
+        const float fc = __shfl(f, min(at, 63));
+        if (at < here) {
+          const float* const slot = part_slot<BM, D>(p, first + (int64_t)(b + at) * it.stride, kvh);
+          sum += *reinterpret_cast<const f32x4*>(slot + r * D + c0) * fc;
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) L += __shfl_xor(L, o);
+#pragma unroll
+    for (int o = 32; o >= LPR; o >>= 1)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) sum[v] += __shfl_xor(sum[v], o);
+    const unsigned row = row0 + r, tok = row / (unsigned)G;
+    const float none = L == 0.f ? nothing_seen(p, it, (int)tok) : 0.f;
+    typedef T vec __attribute__((ext_vector_type(4)));
+    vec y;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) y[v] = (T)(L == 0.f ? none : sum[v] * (1.0f / L));
+    if (sub == 0) {
+      T* const op = (T*)p.out + ((int64_t)(it.cu + (int)tok) * p.n_q_heads + kvh * G + (int)(row - tok * G)) * D;
+      *reinterpret_cast<vec*>(op + c0) = y;
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// host side
+// ------------------------------------------------------------------------------------------------------------
+constexpr int kTreePieces = 1024;  // workgroups that the key axis is cut for, all kv-heads together
+constexpr int kTreeMinBlocks = 16; // key blocks below which a tile is not cut
+
+struct TreePlan {
+  int rw;              // waves side by side on the rows
+  int64_t pieces;      // per kv-head
+  bool cut;
+  int64_t bytes;
+};
+
+// Everything that follows from host-side values alone; the workspace query and the call agree on it.
+static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions, int32_t n_q_heads, int32_t total,
+                      int32_t max_new, int32_t max_prefix) {
+  const int R = c->dtype == SYMPH_BF16 ? 32 : 16;
+  const int64_t G = n_q_heads / c->n_kv_heads;
+  const int64_t rows = (int64_t)max_new * G;
+  pl.rw = rows <= R ? 1 : rows <= 2 * R ? 2 : 4;
+  const int64_t BM = (int64_t)R * pl.rw;
+  const int64_t tiles = (int64_t)total * G / BM + n_sessions;  // at least as many as there are
+  const int64_t blocks = ceil_div64(max_prefix, R) + ceil_div64(max_new, R);
+  const int64_t per_tile = ceil_div64(blocks, kTreeMinBlocks);
+  const int64_t target = ceil_div64(kTreePieces, c->n_kv_heads);
+  const int64_t more = per_tile <= 1 ? 0 : (tiles > target ? target : (tiles * (per_tile - 1) < target ? tiles * (per_tile - 1) : target));
+  pl.cut = more > 0;
+  pl.pieces = tiles + more;
+  pl.bytes = pl.cut ? pl.pieces * c->n_kv_heads * BM * (c->head_dim + 2) * 4 : 0;
+  return pl.pieces * c->n_kv_heads <= 0x7FFFFFFFLL;
+}
+
+template <typename T, int D, int RW>
+static void launch_tree(const TreeParams& p, unsigned groups, hipStream_t stream) {
+  hipLaunchKernelGGL((tree_attn_kernel<T, D, RW>), dim3(groups), dim3(64 * kTreeWaves), 0, stream, p);
+  if (p.cut) hipLaunchKernelGGL((tree_join_kernel<T, D, RW>), dim3(groups), dim3(256), 0, stream, p);
+}
+
+template <typename T, int D>
+static int32_t launch_tree(TreeParams& p, const TreePlan& pl, bool wide, hipStream_t stream) {
+  if (!wide) {
+    hipLaunchKernelGGL((tree_row_kernel<T, D>), dim3((unsigned)p.total * (unsigned)p.n_q_heads), dim3(64), 0, stream, p);
+  } else {
+    const unsigned groups = (unsigned)(pl.pieces * p.n_kv_heads);
+    if (pl.rw == 1)
+      launch_tree<T, D, 1>(p, groups, stream);
+    else if (pl.rw == 2)
+      launch_tree<T, D, 2>(p, groups, stream);
+    else
+      launch_tree<T, D, 4>(p, groups, stream);
+  }
+  return hipGetLastError() == hipSuccess ? SYMPH_OK : SYMPH_ELAUNCH;
+}
+
+}  // namespace symph
+
+using namespace symph;
+
+extern "C" {
+
+int64_t symph_tree_attn_workspace_bytes(const symph_kv_cache* cache, int32_t n_sessions, int32_t n_q_heads,
+                                        int32_t total_new_tokens, int32_t max_new_len, int32_t max_prefix_len) {
+  if (validate_cache(cache) != SYMPH_OK || n_sessions < 0 || n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0 ||
+      total_new_tokens < 0 || max_new_len < 0 || max_prefix_len < 0)
+    return -1;
+  TreePlan pl;
+  if (!plan_tree(pl, cache, n_sessions, n_q_heads, total_new_tokens, max_new_len, max_prefix_len)) return -1;
+  return pl.bytes;
+}
+
+int32_t symph_tree_attn(const symph_kv_cache* cache, int32_t layer, const void* d_q, const void* d_k_new,
+                        const void* d_v_new, void* d_out, const uint64_t* d_tree_mask, int32_t mask_words,
+                        const int32_t* d_cu_new_lens, const int32_t* d_prefix_lens, const int32_t* d_block_table,
+                        int32_t table_stride, int32_t n_sessions, int32_t n_q_heads, int32_t total_new_tokens,
+                        int32_t max_new_len, int32_t max_prefix_len, float scale, void* d_workspace,
+                        int64_t workspace_bytes, void* stream) {
+  const int32_t rc = validate_cache(cache);
+  if (rc != SYMPH_OK) return rc;
+  if (layer < 0 || layer >= cache->n_layers) return SYMPH_EINVAL;
+  if (n_sessions < 0 || total_new_tokens < 0 || max_new_len < 0 || max_prefix_len < 0 || table_stride < 0 ||
+      workspace_bytes < 0 || mask_words < 0)
+    return SYMPH_EINVAL;
+  if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0) return SYMPH_EINVAL;
+  if (!(scale > 0.0f) || !(scale < INFINITY)) return SYMPH_EINVAL;
+  if (max_new_len > total_new_tokens || (int64_t)mask_words * 64 < max_new_len || mask_words > 0x3FFFFFFF) return SYMPH_EINVAL;
+  if (n_sessions == 0 || total_new_tokens == 0) return SYMPH_OK;
+  if (!d_q || !d_k_new || !d_v_new || !d_out || !d_tree_mask || mask_words == 0 || !d_cu_new_lens || !d_prefix_lens)
+    return SYMPH_EINVAL;
+  if (max_prefix_len > 0 && (!d_block_table || table_stride == 0)) return SYMPH_EINVAL;
+  if (max_prefix_len > 0 && (int64_t)table_stride * cache->block_size < max_prefix_len) return SYMPH_EINVAL;
+  if (cache->head_dim != 64 && cache->head_dim != 128) return SYMPH_EUNSUPPORTED;
+  if ((int64_t)total_new_tokens * n_q_heads > 0x7FFFFFFFLL) return SYMPH_EUNSUPPORTED;
+  TreePlan pl;
+  if (!plan_tree(pl, cache, n_sessions, n_q_heads, total_new_tokens, max_new_len, max_prefix_len)) return SYMPH_EUNSUPPORTED;
+  const int eb = elem_bytes_of(cache->dtype);
+  TreeParams p;
+  p.k_layer = (const char*)cache->k_base + (int64_t)layer * cache->layer_stride * eb;
+  p.v_layer = (const char*)cache->v_base + (int64_t)layer * cache->layer_stride * eb;
+  p.block_stride = cache->block_stride;
+  p.n_blocks = cache->n_blocks;
+  p.block_size = cache->block_size;
+  p.bs_shift = (cache->block_size & (cache->block_size - 1)) == 0 ? __builtin_ctz((unsigned)cache->block_size) : -1;
+  p.n_kv_heads = cache->n_kv_heads;
+  p.n_q_heads = n_q_heads;
+  p.q = d_q;
+  p.k_new = d_k_new;
+  p.v_new = d_v_new;
+  p.out = d_out;
+  p.mask = (const uint32_t*)d_tree_mask;
+  p.mask_words = 2 * mask_words;
+  p.cu_new_lens = d_cu_new_lens;
+  p.prefix_lens = d_prefix_lens;
+  p.table = d_block_table;
+  p.table_stride = d_block_table ? table_stride : 0;
+  p.n_sessions = n_sessions;
+  p.total = total_new_tokens;
+  p.scale = scale;
+  const int64_t block_bytes = cache->block_stride * (int64_t)eb;
+  p.group_bytes = p.bs_shift >= 4 && block_bytes <= 0x7FFFFFFFLL ? (uint32_t)block_bytes : 0;
+  p.max_pieces = (int32_t)pl.pieces;
+  p.c_min = kTreeMinBlocks;
+  p.cut = pl.cut;
+  p.parts = (float*)d_workspace;
+  const uintptr_t address_bits = (uintptr_t)p.k_layer | (uintptr_t)p.v_layer | (uintptr_t)d_q | (uintptr_t)d_k_new |
+                                 (uintptr_t)d_v_new | (uintptr_t)d_out | (uintptr_t)block_bytes;
+  const bool wide = (address_bits & 15) == 0;
+  if (pl.bytes > 0 && (!d_workspace || workspace_bytes < pl.bytes)) return SYMPH_EWORKSPACE;
+  if (pl.bytes > 0 && ((uintptr_t)d_workspace & 15) != 0) return SYMPH_EUNSUPPORTED;
+  if (cache->dtype == SYMPH_BF16)
+    return cache->head_dim == 64 ? launch_tree<__bf16, 64>(p, pl, wide, (hipStream_t)stream)
+                                 : launch_tree<__bf16, 128>(p, pl, wide, (hipStream_t)stream);
+  return cache->head_dim == 64 ? launch_tree<float, 64>(p, pl, wide, (hipStream_t)stream)
+                               : launch_tree<float, 128>(p, pl, wide, (hipStream_t)stream);
+}
+
+}  // extern "C"
