@@ -12,6 +12,8 @@
 //     the low bits in its last block, the caller's mask in the blocks of the tree, which start at the tree's first token.
 #include "attn_lanes.h"
 
+#include <type_traits>
+
 namespace symph {
 
 struct TreeParams {
@@ -131,10 +133,11 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
       it.count = __builtin_amdgcn_readlane(count, at);
       it.stride = __builtin_amdgcn_readlane(tiles, at);
       const int local = g - before - __builtin_amdgcn_readlane(incl - mine, at), b = __builtin_amdgcn_readlane(blocks, at);
-      it.index = local / it.stride;
+      // (divisions are done on the vector unit: back to scalar registers)
+      it.index = __builtin_amdgcn_readfirstlane(local / it.stride);
       it.tile = local - it.index * it.stride;
-      it.block0 = (int)((int64_t)b * it.index / it.count);
-      it.block1 = (int)((int64_t)b * (it.index + 1) / it.count);
+      it.block0 = __builtin_amdgcn_readfirstlane((int)((int64_t)b * it.index / it.count));
+      it.block1 = __builtin_amdgcn_readfirstlane((int)((int64_t)b * (it.index + 1) / it.count));
       return true;
     }
     before += __builtin_amdgcn_readlane(incl, 63);
@@ -278,6 +281,94 @@ __device__ __forceinline__ float* part_slot(const TreeParams& p, int64_t g, int 
   return p.parts + (g * p.n_kv_heads + kvh) * (int64_t)(BM * (D + 2));
 }
 
+// ---- results of a tile of BM rows, by all WAVES waves of its workgroup.  sum_at(r, c, M, L): four columns of row r from column c
+// on, added up over the waves that share the row, with their maximum and sum.  A row with a value that is not finite (an infinity
+// or a NaN among the values, which the matrix product spreads to rows that do not see it), or with scores beyond what the loop's
+// arithmetic is made for, is worked out again by itself.  Its q is read again for that, so nothing is written before: out may be
+// q.  lds: 2 * D floats a wave, free once every thread has its sums; bad_rows: BM / 32 words of zeros.
+constexpr float kLargestScore = 0x1p20f;
+template <typename T, int D, int BM, int KB, int WAVES, typename Sum>
+__device__ __forceinline__ void finish_tile(const TreeParams& p, const TreePiece& it, int piece, int kvh, int n_rows, float* lds,
+                                            unsigned* bad_rows, Sum sum_at) {
+  constexpr int kQuads = BM * D / 4, kTurns = (kQuads + 64 * WAVES - 1) / (64 * WAVES);
+  typedef T vec __attribute__((ext_vector_type(4)));
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = p.n_q_heads / p.n_kv_heads;
+  const unsigned row0 = (unsigned)it.tile * BM;
+  const bool whole = it.count == 1;
+  float* const slot = whole ? nullptr : part_slot<BM, D>(p, piece, kvh);
+  f32x4 x[kTurns];
+  f32x2 state[kTurns];
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    const int i = tid + t * 64 * WAVES, r = i / (D / 4), c0 = 4 * (i % (D / 4));
+    if (i >= kQuads || r >= n_rows) break;
+    float M, L;
+    f32x4 sum = sum_at(t, r, c0, M, L);
+    if (L == 0.f) sum = f32x4{0.f, 0.f, 0.f, 0.f};  // (no probability: whatever values the product brought in are not the row's)
+    bool bad = false;
+    float scale = 1.0f, none = 0.f;
+    if (whole) {
+      scale = L == 0.f ? 0.f : 1.0f / L;
+      if (L == 0.f) none = nothing_seen(p, it, (int)((row0 + r) / (unsigned)G));
+    }
+    state[t] = f32x2{M, L};
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      sum[v] = sum[v] * scale + none;
+      bad = bad || !(fabsf(sum[v]) < INFINITY);
+    }
+    x[t] = sum;
+    // (a sum that is NaN comes from a score that is: every value of the row is NaN either way; so is 0 / 0)
+    bad = (bad && L == L && L != 0.f) || (fabsf(M) > kLargestScore && M != -INFINITY);
+    if (bad) atomicOr(&bad_rows[r >> 5], 1u << (r & 31));
+  }
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < kTurns; ++t) {
+    const int i = tid + t * 64 * WAVES, r = i / (D / 4), c0 = 4 * (i % (D / 4));
+    if (i >= kQuads || r >= n_rows) break;
+    if ((bad_rows[r >> 5] >> (r & 31)) & 1) continue;
+    if (whole) {
+      const unsigned row = row0 + r, tok = row / (unsigned)G;
+      T* const op = (T*)p.out + ((int64_t)(it.cu + (int)tok) * p.n_q_heads + kvh * G + (int)(row - tok * G)) * D;
+      vec y;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) y[v] = (T)x[t][v];
+      *reinterpret_cast<vec*>(op + c0) = y;
+    } else {
+      *reinterpret_cast<f32x4*>(slot + r * D + c0) = x[t];
+      if (c0 == 0) {
+        slot[BM * D + r] = state[t][0];
+        slot[BM * D + BM + r] = state[t][1];
+      }
+    }
+  }
+  int turn = 0;
+  for (int word = 0; word < (BM + 31) / 32; ++word)
+    for (unsigned left = __builtin_amdgcn_readfirstlane(bad_rows[word]); left; left &= left - 1) {
+      if (turn++ % WAVES != wave) continue;
+      const int r = word * 32 + __builtin_ctz(left);
+      const unsigned row = row0 + r, tok = row / (unsigned)G;
+      const int h = kvh * G + (int)(row - tok * G);
+      float* const own = lds + wave * 2 * D;
+      float m, l;
+      row_by_lanes<T, D, KB, 64>(p, it, (int)tok, h, own, m, l);
+      if (whole) {
+        T* const op = (T*)p.out + ((int64_t)(it.cu + (int)tok) * p.n_q_heads + h) * D;
+        const float none = l == 0.f ? nothing_seen(p, it, (int)tok) : 0.f;
+        for (int c = lane; c < D; c += 64) op[c] = (T)(l == 0.f ? none : own[D + c] * (1.0f / l));
+      } else {
+        for (int c = lane; c < D; c += 64) slot[r * D + c] = own[D + c];
+        if (lane == 0) {
+          slot[BM * D + r] = m;
+          slot[BM * D + BM + r] = l;
+        }
+      }
+    }
+}
+
 // ---- the tiled kernel ----------------------------------------------------------------------------------------------
 template <typename T, int D, int RW>
 __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const TreeParams p) {
@@ -289,7 +380,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
   constexpr int kJoinBytes = W * R * kStride * 4;
   __shared__ __attribute__((aligned(16))) char lds[kVBytes > kJoinBytes ? kVBytes : kJoinBytes];
   __shared__ float wave_m[W][R], wave_l[W][R];
-  __shared__ unsigned bad_rows[RW];
+  __shared__ unsigned bad_rows[(BM + 31) / 32];
 
   const int Hkv = p.n_kv_heads;
   const int G = p.n_q_heads / Hkv;
@@ -306,7 +397,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
   const unsigned row0 = (unsigned)it.tile * BM;
   const int n_rows = (int)min((unsigned)BM, (unsigned)N * (unsigned)G - row0);
   const int prefix_blocks = P / R + (P % R != 0);
-  if (tid < RW) bad_rows[tid] = 0;
+  if (tid < (BM + 31) / 32) bad_rows[tid] = 0;
 
   const unsigned my_row = row0 + min(rw * R + n, n_rows - 1);
   const int tok = (int)(my_row / (unsigned)G);
@@ -458,18 +549,6 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
           for (int e = 0; e < 16; ++e) o[dt][e] *= a;
       }
       const float ref = m == -INFINITY ? 0.f : m;
-      // One multiplication and subtraction without a rounding between them: the rounding of `ref` itself is common to all keys
-      // and cancels, unless scores are so large that it is more than an exponent's range.
-      float to_log2 = cs;
-      if (__any(fabsf(ref) > 0x1p20f)) {
-        to_log2 = 1.0f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float y = x[e] * cs;
-          asm("" : "+v"(y));
-          x[e] = y;
-        }
-      }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // (here, so that V operands can be read beside the exponentials)
       __builtin_amdgcn_wave_barrier();
       // the probabilities as two bf16 values each, w = hi + lo with 16 bits in all: the leading bits, then those of what is left
@@ -480,7 +559,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
         float w[2], rest[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          w[k] = __builtin_amdgcn_exp2f(fmaf(x[e + k], to_log2, -ref));
+          w[k] = __builtin_amdgcn_exp2f(fmaf(x[e + k], cs, -ref));
           sum += w[k];
           rest[k] = w[k] - upper_part(w[k]);
         }
@@ -642,21 +721,12 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
   }
   __syncthreads();
 
-  // ---- results of the tile: a thread adds up four columns of a row at a time over the KW waves.  A row with a value that is not
-  // finite (an infinity or a NaN among the values, which the matrix product spreads to rows that do not see it) is worked out
-  // again by itself.  Its q is read again for that, so nothing is written before: out may be q.
-  constexpr int kQuads = BM * D / 4, kTurns = (kQuads + 64 * W - 1) / (64 * W);
-  typedef T vec __attribute__((ext_vector_type(4)));
   const float* const all = reinterpret_cast<const float*>(lds);
-  const bool whole = it.count == 1;
-  float* const slot = whole ? nullptr : part_slot<BM, D>(p, piece, kvh);
-  f32x4 x[kTurns];
-#pragma unroll
-  for (int t = 0; t < kTurns; ++t) {
-    const int i = tid + t * 64 * W, r = i / (D / 4), c0 = 4 * (i % (D / 4));
-    if (i >= kQuads || r >= n_rows) break;
+  finish_tile<T, D, BM, R, W>(p, it, piece, kvh, n_rows, reinterpret_cast<float*>(lds), bad_rows,
+                              [&](int, int r, int c0, float& M, float& L) {
     const int w0 = (r / R) * KW;
-    float L = 0.f, M = -INFINITY;
+    M = -INFINITY;
+    L = 0.f;
     f32x4 sum{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
@@ -664,76 +734,437 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
       M = fmaxf(M, wave_m[w0 + w][r % R]);
       sum += *reinterpret_cast<const f32x4*>(all + ((w0 + w) * R + r % R) * kStride + c0);
     }
-    if (L == 0.f) sum = f32x4{0.f, 0.f, 0.f, 0.f};  // (no probability: whatever values the product brought in are not the row's)
-    bool bad = false;
-    float scale = 1.0f, none = 0.f;
-    if (whole) {
-      scale = L == 0.f ? 0.f : 1.0f / L;
-      if (L == 0.f) none = nothing_seen(p, it, (int)((row0 + r) / (unsigned)G));
-    } else if (c0 == 0) {
-      slot[BM * D + r] = M;
-      slot[BM * D + BM + r] = L;
-    }
-#pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      sum[v] = sum[v] * scale + none;
-      bad = bad || !(fabsf(sum[v]) < INFINITY);
-    }
-    x[t] = sum;
-    // (a sum that is NaN comes from a score that is: every value of the row is NaN either way; so is 0 / 0)
-    if (bad && L == L && L != 0.f) atomicOr(&bad_rows[r / R], 1u << (r % R));
-  }
-  __syncthreads();
-#pragma unroll
-  for (int t = 0; t < kTurns; ++t) {
-    const int i = tid + t * 64 * W, r = i / (D / 4), c0 = 4 * (i % (D / 4));
-    if (i >= kQuads || r >= n_rows) break;
-    if ((bad_rows[r / R] >> (r % R)) & 1) continue;
-    if (whole) {
-      const unsigned row = row0 + r, tk = row / (unsigned)G;
-      T* const op = (T*)p.out + ((int64_t)(cu + (int)tk) * p.n_q_heads + kvh * G + (int)(row - tk * G)) * D;
-      vec y;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) y[v] = (T)x[t][v];
-      *reinterpret_cast<vec*>(op + c0) = y;
-    } else {
-      *reinterpret_cast<f32x4*>(slot + r * D + c0) = x[t];
-    }
-  }
-  int turn = 0;
-  for (int grp = 0; grp < RW; ++grp)
-    for (unsigned left = __builtin_amdgcn_readfirstlane(bad_rows[grp]); left; left &= left - 1) {
-      if (turn++ % W != wave) continue;
-      const int r = grp * R + __builtin_ctz(left);
-      const unsigned row = row0 + r, tk = row / (unsigned)G;
-      const int h = kvh * G + (int)(row - tk * G);
-      float* const own = reinterpret_cast<float*>(lds) + wave * 2 * D;
-      float rm, rl;
-      row_by_lanes<T, D, R, 64>(p, it, (int)tk, h, own, rm, rl);
-      if (whole) {
-        T* const op = (T*)p.out + ((int64_t)(cu + (int)tk) * p.n_q_heads + h) * D;
-        const float none = rl == 0.f ? nothing_seen(p, it, (int)tk) : 0.f;
-        for (int c = lane; c < D; c += 64) op[c] = (T)(rl == 0.f ? none : own[D + c] * (1.0f / rl));
-      } else {
-        for (int c = lane; c < D; c += 64) slot[r * D + c] = own[D + c];
-        if (lane == 0) {
-          slot[BM * D + r] = rm;
-          slot[BM * D + BM + r] = rl;
-        }
-      }
-    }
+    return sum;
+  });
 }
 
+// ---- wide tiles (bf16, more than 64 query rows that share their keys): four waves of 32 rows each, all on the same keys, so that
+// a tile of 64 keys is read from memory once for 128 rows, straight into LDS and two tiles ahead.  S(j+1) = K(j+1) Q^T runs beside
+// the exponentials of S(j), O += V(j)^T P(j) beside the first half of those of S(j+1): an instruction stream that gives the matrix
+// cores and the vector unit independent work.  The softmax reference is the maximum of the first tile a row sees and is raised only
+// where a row sum says that it has to be (a probability of 2^40): numerator and denominator carry the same factor, so nothing is
+// lost by a reference that is too low.
+constexpr int kWideKeys = 64;
+constexpr float kRaiseSum = 1.0995116e12f;  // 2^40
+
+// LDS layout of 64 rows of K or V such that the 16 rows a quarter-wave reads of K, and the 4 rows x 32 bytes that 16 lanes read of V
+// by the transposing read, lie in different banks.  One direct load writes 1 KiB, lane l to place 16 * l: which 16 bytes of which
+// row it fetches is what the layout chooses.
+template <int D>
+struct WideLds;
+template <>
+struct WideLds<128> {  // 1 KiB: four rows, chunk c of row r at place c ^ ((r & 3) << 2); 16 bytes between such groups
+  static constexpr int kGroup = 1024 + 16, kBytes = 16 * kGroup, kLoads = 4;
+  static __device__ __forceinline__ int row_of(int load, int wave, int lane) { return 16 * load + 4 * wave + (lane >> 4); }
+  static __device__ __forceinline__ int chunk_of(int, int lane) { return (lane & 15) ^ (((lane >> 4) & 3) << 2); }
+  static __device__ __forceinline__ int at(int load, int wave) { return (4 * load + wave) * kGroup; }
+  static __device__ __forceinline__ int place(int r, int c) { return (r >> 2) * kGroup + (r & 3) * 256 + ((c ^ ((r & 3) << 2)) << 4); }
+  static __device__ __forceinline__ int id_of(int load, int) { return load; }  // which of the tile's four 16-key groups
+};
+template <>
+struct WideLds<64> {  // 1 KiB: eight rows, chunk c of row r at place c ^ twist(r)
+  static constexpr int kBytes = 8 * 1024, kLoads = 2;
+  static __device__ __forceinline__ int twist(int r) { return (((r >> 1) & 3) << 1) | ((r >> 3) & 1); }
+  static __device__ __forceinline__ int row_of(int load, int wave, int lane) { return 32 * load + 8 * wave + (lane >> 3); }
+  static __device__ __forceinline__ int chunk_of(int row, int lane) { return (lane & 7) ^ twist(row); }
+  static __device__ __forceinline__ int at(int load, int wave) { return (4 * load + wave) * 1024; }
+  static __device__ __forceinline__ int place(int r, int c) { return (r >> 3) * 1024 + (r & 7) * 128 + ((c ^ twist(r)) << 4); }
+  static __device__ __forceinline__ int id_of(int load, int wave) { return 2 * load + (wave >> 1); }
+};
+
+#define SYMPH_TREE_GLDS16(src, dst)                                                              \
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),         \
+                                   (__attribute__((address_space(3))) void*)(dst), 16, 0, 0)
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
+  typedef __bf16 T;
+  typedef WideLds<D> Lds;
+  constexpr int BM = 128, KB = kWideKeys, NS = D / 16, NT = D / 32;
+  constexpr int kFrags = 4 * NT;  // operands of V a tile: (32-key half, 16-key step, 32-column tile)
+  // (arrays of their own, so that the compiler can tell which loads an LDS read has to wait for)
+  __shared__ __attribute__((aligned(16))) char K0[Lds::kBytes];
+  __shared__ __attribute__((aligned(16))) char K1[Lds::kBytes];
+  __shared__ __attribute__((aligned(16))) char V0[Lds::kBytes];
+  __shared__ __attribute__((aligned(16))) char V1[Lds::kBytes];
+  __shared__ float row_m[BM], row_l[BM];
+  __shared__ unsigned bad_rows[BM / 32];
+
+  const int Hkv = p.n_kv_heads;
+  const int G = p.n_q_heads / Hkv;
+  const int kvh = blockIdx.x % Hkv;
+  const int piece = blockIdx.x / Hkv;
+  TreePiece it;
+  if (!find_piece<BM, KB>(p, G, piece, it)) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31;  // query row of this lane within its wave's; also its row of the K operand
+  const int kg = lane >> 5;
+  const int cu = it.cu, P = it.P, N = it.N;
+  const unsigned row0 = (unsigned)it.tile * BM;
+  const int n_rows = (int)min((unsigned)BM, (unsigned)N * (unsigned)G - row0);
+  const bool works = wave * 32 < n_rows;  // (a wave without rows only moves its share of the tiles)
+  const int prefix_tiles = P / KB + (P % KB != 0), full_tiles = P / KB;
+  const int begin = it.block0, end = it.block1;
+  if (tid < BM / 32) bad_rows[tid] = 0;
+
+  const unsigned my_row = row0 + min(wave * 32 + n, n_rows - 1);
+  const int tok = (int)(my_row / (unsigned)G);
+  const uint32_t* const mask_row = p.mask + (int64_t)(cu + tok) * p.mask_words;
+  bf16x8 q[NS];
+  {
+    const T* const qp = (const T*)p.q + ((int64_t)(cu + tok) * p.n_q_heads + kvh * G + (int)(my_row - (unsigned)tok * G)) * D;
+#pragma unroll
+    for (int st = 0; st < NS; ++st) q[st] = *reinterpret_cast<const bf16x8*>(qp + 16 * st + 8 * kg);
+  }
+
+  // ---- memory -> LDS.  Block ids of a tile's four 16-key groups: asked for by lanes an iteration before they are needed, then
+  // moved to scalar registers (asking for the value at once would also wait for the tiles under way).
+  const bool has_table = p.table != nullptr && p.table_stride > 0;
+  const int32_t* const table_row = p.table + (int64_t)it.s * p.table_stride;
+  const unsigned row_bytes = (unsigned)(Hkv * D * (int)sizeof(T));
+  const char* const k_pool = reinterpret_cast<const char*>((const T*)p.k_layer + kvh * D);
+  const char* const v_pool = reinterpret_cast<const char*>((const T*)p.v_layer + kvh * D);
+  const char* const k_fresh = reinterpret_cast<const char*>((const T*)p.k_new + (int64_t)cu * Hkv * D + kvh * D);
+  const char* const v_fresh = reinterpret_cast<const char*>((const T*)p.v_new + (int64_t)cu * Hkv * D + kvh * D);
+  const int bs_mask = p.block_size - 1;
+  auto ask_ids = [&](int tile) {  // lane i: group i & 3 of tile + (i >> 2 & 1)
+    const int64_t key = (int64_t)(tile + ((lane >> 2) & 1)) * KB + 16 * (lane & 3);
+    const int64_t at = key >> p.bs_shift;
+    const int id = has_table ? table_row[(int)min(at, (int64_t)p.table_stride - 1)] : -1;
+    return at < p.table_stride ? id : -1;
+  };
+  int ids_k[Lds::kLoads], ids_v[Lds::kLoads], asked;  // of the groups that this wave's loads lie in
+  unsigned lane_off[2];  // (load i > 1 of a 128-wide head: the lane's place in the 16-key group is that of load 0)
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = Lds::row_of(D == 64 ? i : 0, wave, lane);
+    lane_off[i] = (unsigned)(row & 15) * row_bytes + (unsigned)Lds::chunk_of(row, lane) * 16u;
+  }
+  auto issue_tile = [&](const char* pool, const char* fresh, char* buf, int tile, const int (&ids)[Lds::kLoads]) {
+    unsigned id_max = (unsigned)ids[0];
+#pragma unroll
+    for (int i = 1; i < Lds::kLoads; ++i) id_max = max(id_max, (unsigned)ids[i]);
+    if (__builtin_expect(tile < full_tiles && id_max < (unsigned)p.n_blocks, 1)) {
+#pragma unroll
+      for (int i = 0; i < Lds::kLoads; ++i) {
+        const int g = Lds::id_of(i, wave);
+        // (scalar base and 32-bit lane offset, kept apart for the compiler: with 64-bit addresses per lane the issue of such a
+        // load waits for the matrix instructions of the SIMD's other wave)
+        const uint64_t at = (uint64_t)(unsigned)ids[i] * p.group_bytes + (uint64_t)((tile * KB + 16 * g) & bs_mask) * row_bytes;
+        const char* base = pool + at;
+        unsigned off = lane_off[D == 64 ? i : 0];
+        asm("" : "+s"(base), "+v"(off));
+        SYMPH_TREE_GLDS16(base + off, buf + Lds::at(i, wave));
+      }
+      asm volatile("; end of the scalar-base loads");  // keeps the last one from being merged with the other path's
+    } else {
+      // a tile at the prefix's end, of the tree, or with an id outside the cache: rows that do not exist come from a row of zeros.
+      // (Its pieces of addresses are worked out here, from a lane number the optimiser cannot see through: no registers for them
+      // in the loop.)
+      int l = lane;
+      asm volatile("" : "+v"(l));
+#pragma unroll
+      for (int i = 0; i < Lds::kLoads; ++i) {
+        const int row = Lds::row_of(i, wave, l);
+        const unsigned in_row = (unsigned)Lds::chunk_of(row, l) * 16u;
+        const unsigned id = (unsigned)ids[i];
+        const char* src = reinterpret_cast<const char*>(kNoRow) + in_row;
+        if (tile < prefix_tiles) {
+          const int64_t key = (int64_t)tile * KB + row;
+          if (key < P && (key >> p.bs_shift) < p.table_stride && id < (unsigned)p.n_blocks)
+            src = pool + (uint64_t)id * p.group_bytes + (uint64_t)((unsigned)key & bs_mask) * row_bytes + in_row;
+        } else {
+          const int j = (tile - prefix_tiles) * KB + row;
+          if (j < N) src = fresh + (uint64_t)j * row_bytes + in_row;
+        }
+        SYMPH_TREE_GLDS16(src, buf + Lds::at(i, wave));
+      }
+    }
+  };
+
+  // ---- LDS reads.  K: lane (n, kg) reads chunk 2 * st + kg of key row key_of_row(n) (+ 32 for the second half).  V: 16 lanes read
+  // 4 rows x 32 bytes and each gets one column, i.e. 4 consecutive keys of it.
+  const int krow = key_of_row(n);
+  int k_off[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) k_off[i] = Lds::place(krow, D == 128 ? 4 * i + kg : 2 * i + kg);
+  auto k_frag = [&](const char* buf, int st, int kb) {
+    if constexpr (D == 128)
+      return *reinterpret_cast<const bf16x8*>(buf + k_off[st >> 1] + 32 * (st & 1) + kb * 8 * WideLds<128>::kGroup);
+    else
+      return *reinterpret_cast<const bf16x8*>(buf + k_off[st] + kb * 4096);
+  };
+  const int i16 = lane & 15;
+  int v_off[4];  // 128: by column tile; 64: by column tile and half of the 8 keys
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int dt = D == 128 ? i : i >> 1, half = D == 128 ? 0 : i & 1;
+    const int row = 8 * kg + 4 * half + (i16 >> 2);
+    v_off[i] = Lds::place(row, 4 * dt + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) + 8 * (i16 & 1);
+  }
+  auto v_frag = [&](const char* buf, int g) {  // g = (kb * 2 + u) * NT + dt
+    const int dt = g % NT, step = g / NT;      // step: 16 keys
+    const char *a, *b;
+    if constexpr (D == 128) {
+      a = buf + v_off[dt] + step * 4 * WideLds<128>::kGroup;
+      b = a + WideLds<128>::kGroup;
+    } else {
+      a = buf + v_off[2 * dt] + step * 2048;
+      b = buf + v_off[2 * dt + 1] + step * 2048;
+    }
+    const s16x4 lo = lds_read_tr16(reinterpret_cast<const __bf16*>(a));
+    const s16x4 hi = lds_read_tr16(reinterpret_cast<const __bf16*>(b));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+
+  f32x16 o[NT];
+#pragma unroll
+  for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+  float m_ref = -INFINITY, l_run = 0.f;  // the reference in log2 units, this lane's share of the sum
+  const float cs = p.scale * 1.4426950408889634f;
+
+  auto scores = [&](const char* buf, f32x16 (&sc)[2]) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[kb][e] = 0.f;
+#pragma unroll
+    for (int st = 0; st < NS; ++st)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+        sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(buf, st, kb), q[st], sc[kb], 0, 0, 0);
+  };
+  // Keys that the lane's row does not see
+  auto hide = [&](f32x16 (&sc)[2], int tile) {
+    if (tile < full_tiles) return;
+    const int left = tile < prefix_tiles ? P - tile * KB : N - (tile - prefix_tiles) * KB;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const int here = left - 32 * kb;
+      uint32_t bits = here >= 32 ? ~0u : here > 0 ? (1u << here) - 1u : 0u;
+      if (tile >= prefix_tiles) {
+        const int w = 2 * (tile - prefix_tiles) + kb;
+        bits &= w < p.mask_words ? mask_row[w] : 0u;
+      }
+      bits >>= 8 * kg;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (!((bits >> (16 * (e >> 3) + (e & 7))) & 1)) sc[kb][e] = -INFINITY;
+    }
+  };
+  // The reference := max(reference, maximum of this tile); returns the factor for what has been accumulated
+  auto raise_reference = [&](const f32x16 (&sc)[2], float& ref) {
+    float mx = sc[0][0];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[kb][e]);
+    const float m_new = fmaxf(m_ref, max_across_halves(mx) * cs);
+    const float a = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - m_new);
+    m_ref = m_new;
+    ref = m_new == -INFINITY ? 0.f : m_new;
+    return a;
+  };
+  // Probabilities of a half of the tile as two bf16 values each, w = hi + lo with 16 bits in all; returns their sum
+  auto probabilities = [&](const f32x16& sc, float ref, bf16x8 (&hi)[2], bf16x8 (&lo)[2]) {
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      float w[2], rest[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        w[k] = __builtin_amdgcn_exp2f(fmaf(sc[e + k], cs, -ref));
+        sum[k] += w[k];
+        rest[k] = w[k] - upper_part(w[k]);
+      }
+      put_pair(hi[e >> 3], e & 7, w[0], w[1]);
+      put_pair(lo[e >> 3], e & 7, rest[0], rest[1]);
+    }
+    return sum[0] + sum[1];
+  };
+
+  f32x16 s_even[2], s_odd[2];  // scores of the even and of the odd tiles, counted from the first
+  bf16x8 hi[2][2], lo[2][2];   // P(j)
+  float ref = 0.f, sum_first = 0.f;
+  asked = ask_ids(begin);
+#pragma unroll
+  for (int i = 0; i < Lds::kLoads; ++i) {
+    ids_k[i] = __builtin_amdgcn_readlane(asked, Lds::id_of(i, wave));
+    ids_v[i] = __builtin_amdgcn_readlane(asked, 4 + Lds::id_of(i, wave));  // (of the second tile)
+  }
+  issue_tile(k_pool, k_fresh, K0, begin, ids_k);
+  issue_tile(v_pool, v_fresh, V0, begin, ids_k);
+  if (begin + 1 < end) issue_tile(k_pool, k_fresh, K1, begin + 1, ids_v);
+  // The first product needs K0 only: V0 and K1, issued after it, may still be on their way (loads return in order)
+  if (begin + 1 < end)
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * Lds::kLoads));
+  else
+    __builtin_amdgcn_s_waitcnt(0x0F70 | Lds::kLoads);
+  __syncthreads();
+  if (works) {
+    scores(K0, s_even);
+    hide(s_even, begin);
+    raise_reference(s_even, ref);
+    sum_first = probabilities(s_even[0], ref, hi[0], lo[0]);
+  }
+  asked = ask_ids(begin + 2);
+  auto arrived = [&]() {
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's loads into LDS have landed
+    __syncthreads();
+  };
+  arrived();
+
+  // P(j)'s second half and the end of its statistics; a row without a reference yet, or with one that is far too low, gets one
+  auto rest_of_tile = [&](const f32x16 (&sc)[2]) {
+    float sum = sum_first + probabilities(sc[1], ref, hi[1], lo[1]);
+    return sum;
+  };
+  auto settle = [&](const f32x16 (&sc)[2], float sum) {
+    if (__any(!(sum <= kRaiseSum) || m_ref == -INFINITY)) {
+      const float a = raise_reference(sc, ref);
+      l_run *= a;
+#pragma unroll
+      for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] *= a;
+      sum = probabilities(sc[0], ref, hi[0], lo[0]) + probabilities(sc[1], ref, hi[1], lo[1]);
+    }
+    l_run += sum;
+  };
+
+  auto iteration = [&](const int j, auto parity) {
+    constexpr int PAR = decltype(parity)::value;
+    char* const k_same = PAR ? K1 : K0;   // held K(j), free now: receives K(j+2)
+    char* const k_other = PAR ? K0 : K1;  // holds K(j+1)
+    char* const v_same = PAR ? V1 : V0;   // holds V(j)
+    char* const v_other = PAR ? V0 : V1;  // held V(j-1), free now: receives V(j+1)
+    f32x16(&s_cur)[2] = PAR ? s_odd : s_even;  // S(j)
+    f32x16(&s_nxt)[2] = PAR ? s_even : s_odd;  // receives S(j+1)
+#pragma unroll
+    for (int i = 0; i < Lds::kLoads; ++i) ids_k[i] = __builtin_amdgcn_readlane(asked, Lds::id_of(i, wave));  // of tile j+2
+    asked = ask_ids(j + 3);
+    issue_tile(v_pool, v_fresh, v_other, j + 1, ids_v);
+    if (j + 2 < end) issue_tile(k_pool, k_fresh, k_same, j + 2, ids_k);
+#pragma unroll
+    for (int i = 0; i < Lds::kLoads; ++i) ids_v[i] = ids_k[i];
+    if (works) {
+      scores(k_other, s_nxt);
+      float sum = rest_of_tile(s_cur);
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);  // K operands: six reads up front
+#pragma unroll
+      for (int g = 0; g < 2 * NS; ++g) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one matrix instruction of S(j+1)
+        if (g < 2 * NS - 6) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 5 * 8 / NS, 0);  // scale, sum, split
+        __builtin_amdgcn_sched_group_barrier(0x400, 8 / NS, 0);      // exponentials
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(hi[kb][u]), "+v"(lo[kb][u]));  // (computed here, not past the branch)
+      asm volatile("" : "+v"(sum));
+      settle(s_cur, sum);
+      hide(s_nxt, j + 1);
+      // O += V(j)^T P(j) beside the first half of P(j+1): in every slot the LDS reads of the operand some slots ahead, the two
+      // products of one operand and their share of the 16 exponentials
+      bf16x8 hi_first[2], lo_first[2];
+      bf16x8 frag[kFrags];
+      constexpr int kAhead = 4, kPer = 16 / kFrags;  // exponentials of a slot
+      float pe[16], sums[2] = {0.f, 0.f};
+#pragma unroll
+      for (int g = 0; g < kAhead; ++g) frag[g] = v_frag(v_same, g);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int g = 0; g < kFrags; ++g) {
+        if (g + kAhead < kFrags) frag[g + kAhead] = v_frag(v_same, g + kAhead);
+        const int step = g / NT;
+        o[g % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[g], hi[step >> 1][step & 1], o[g % NT], 0, 0, 0);
+#pragma unroll
+        for (int k = kPer * g; k < kPer * (g + 1); ++k) {
+          pe[k] = __builtin_amdgcn_exp2f(fmaf(s_nxt[0][k], cs, -ref));
+          asm volatile("" : "+v"(pe[k]));  // (in this slot, not next to its use)
+          sums[k & 1] += pe[k];
+        }
+        o[g % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[g], lo[step >> 1][step & 1], o[g % NT], 0, 0, 0);
+#pragma unroll
+        for (int k = kPer * g; k < kPer * (g + 1); ++k)
+          if (k & 1) {
+            put_pair(hi_first[k >> 3], (k & 7) - 1, pe[k - 1], pe[k]);
+            put_pair(lo_first[k >> 3], (k & 7) - 1, pe[k - 1] - upper_part(pe[k - 1]), pe[k] - upper_part(pe[k]));
+          }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      sum_first = sums[0] + sums[1];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        hi[0][u] = hi_first[u];
+        lo[0][u] = lo_first[u];
+        asm volatile("" : "+v"(hi[0][u]), "+v"(lo[0][u]));
+      }
+    }
+    arrived();
+  };
+  for (int j = begin; j + 1 < end; j += 2) {
+    iteration(j, std::integral_constant<int, 0>{});
+    if (j + 2 < end) iteration(j + 1, std::integral_constant<int, 1>{});
+  }
+  // The last tile has no successor
+  if (works) {
+    const bool odd = (end - 1 - begin) & 1;
+    if (odd) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) s_even[kb] = s_odd[kb];
+    }
+    const char* const v_last = odd ? V1 : V0;
+    settle(s_even, rest_of_tile(s_even));
+#pragma unroll
+    for (int g = 0; g < kFrags; ++g) {
+      const int step = g / NT;
+      const bf16x8 v = v_frag(v_last, g);
+      o[g % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, hi[step >> 1][step & 1], o[g % NT], 0, 0, 0);
+      o[g % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, lo[step >> 1][step & 1], o[g % NT], 0, 0, 0);
+    }
+  }
+  const float l = sum_across_halves(l_run);
+  if (lane < 32) {
+    row_m[wave * 32 + n] = m_ref;
+    row_l[wave * 32 + n] = l;
+  }
+  __syncthreads();  // the tile buffers are free: a wave's rows go through one of its own, 16-byte piece c of row r at c ^ r
+  constexpr int kPieces = D / 4;
+  auto rows_of = [&](int w) { return reinterpret_cast<float*>(w == 0 ? K0 : w == 1 ? K1 : w == 2 ? V0 : V1); };
+  if (works) {
+    float* const mine = rows_of(wave) + n * D;
+#pragma unroll
+    for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(mine + 4 * ((8 * dt + kg + 2 * i) ^ (n & (kPieces - 1)))) =
+            f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+  }
+  __syncthreads();
+  constexpr int kRowsPerTurn = 256 / kPieces;
+  finish_tile<T, D, BM, KB, 4>(p, it, piece, kvh, n_rows, reinterpret_cast<float*>(K0), bad_rows,
+                               [&](int t, int r, int c0, float& M, float& L) {
+    M = row_m[r];
+    L = row_l[r];
+    return *reinterpret_cast<const f32x4*>(rows_of(t * kRowsPerTurn / 32) + (r & 31) * D +
+                                           4 * ((c0 / 4) ^ (r & 31 & (kPieces - 1))));
+  });
+}
 // ---- joins the pieces of cut tiles: out = sum_c f_c O_c / sum_c f_c l_c, f_c = e^(m_c - max_c m_c).  Each of a tile's pieces
 // has a workgroup here too, which joins an equal share of the tile's rows, a wave per row.
-template <typename T, int D, int RW>
+template <typename T, int D, int BM, int KB>
 __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
-  constexpr int R = TreeTile<T>::R, BM = R * RW, LPR = D / 4, SUB = 64 / LPR;  // lanes per row, pieces side by side
+  constexpr int LPR = D / 4, SUB = 64 / LPR;  // lanes per row, pieces side by side
   const int Hkv = p.n_kv_heads;
   const int G = p.n_q_heads / Hkv;
   const int kvh = blockIdx.x % Hkv, piece = blockIdx.x / Hkv;
   TreePiece it;
-  if (!find_piece<BM, R>(p, G, piece, it) || it.count == 1) return;
+  if (!find_piece<BM, KB>(p, G, piece, it) || it.count == 1) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const unsigned row0 = (unsigned)it.tile * BM;
   const int n_rows = (int)min((unsigned)BM, (unsigned)it.N * (unsigned)G - row0);
@@ -787,15 +1218,23 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
 // ------------------------------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------------------------------
-constexpr int kTreePieces = 1024;  // workgroups that the key axis is cut for, all kv-heads together
-constexpr int kTreeMinBlocks = 16; // key blocks below which a tile is not cut
+constexpr int kTreePieces = 1024;   // workgroups that the key axis is cut for, all kv-heads together
+constexpr int kTreeMinKeys = 512;   // keys of a tile that are not cut further
 
 struct TreePlan {
-  int rw;              // waves side by side on the rows
+  bool wide;           // 128-row tiles through LDS
+  int rw;              // else: waves side by side on the rows
   int64_t pieces;      // per kv-head
+  int32_t c_min;       // key blocks
   bool cut;
   int64_t bytes;
 };
+
+// 16 consecutive keys lie in one block of the cache and a block fits 32 bits: rows can be addressed by groups
+static bool grouped_rows(const symph_kv_cache* c) {
+  return c->block_size >= 16 && (c->block_size & (c->block_size - 1)) == 0 &&
+         c->block_stride * (int64_t)elem_bytes_of(c->dtype) <= 0x7FFFFFFFLL;
+}
 
 // Everything that follows from host-side values alone; the workspace query and the call agree on it.
 static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions, int32_t n_q_heads, int32_t total,
@@ -803,11 +1242,13 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   const int R = c->dtype == SYMPH_BF16 ? 32 : 16;
   const int64_t G = n_q_heads / c->n_kv_heads;
   const int64_t rows = (int64_t)max_new * G;
+  pl.wide = c->dtype == SYMPH_BF16 && rows > 64 && grouped_rows(c);
   pl.rw = rows <= R ? 1 : rows <= 2 * R ? 2 : 4;
-  const int64_t BM = (int64_t)R * pl.rw;
+  const int64_t BM = pl.wide ? 128 : (int64_t)R * pl.rw, KB = pl.wide ? kWideKeys : R;
+  pl.c_min = (int32_t)(kTreeMinKeys / KB);
   const int64_t tiles = (int64_t)total * G / BM + n_sessions;  // at least as many as there are
-  const int64_t blocks = ceil_div64(max_prefix, R) + ceil_div64(max_new, R);
-  const int64_t per_tile = ceil_div64(blocks, kTreeMinBlocks);
+  const int64_t blocks = ceil_div64(max_prefix, KB) + ceil_div64(max_new, KB);
+  const int64_t per_tile = ceil_div64(blocks, pl.c_min);
   const int64_t target = ceil_div64(kTreePieces, c->n_kv_heads);
   const int64_t more = per_tile <= 1 ? 0 : (tiles > target ? target : (tiles * (per_tile - 1) < target ? tiles * (per_tile - 1) : target));
   pl.cut = more > 0;
@@ -818,8 +1259,15 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
 
 template <typename T, int D, int RW>
 static void launch_tree(const TreeParams& p, unsigned groups, hipStream_t stream) {
+  constexpr int R = TreeTile<T>::R;
   hipLaunchKernelGGL((tree_attn_kernel<T, D, RW>), dim3(groups), dim3(64 * kTreeWaves), 0, stream, p);
-  if (p.cut) hipLaunchKernelGGL((tree_join_kernel<T, D, RW>), dim3(groups), dim3(256), 0, stream, p);
+  if (p.cut) hipLaunchKernelGGL((tree_join_kernel<T, D, R * RW, R>), dim3(groups), dim3(256), 0, stream, p);
+}
+
+template <int D>
+static void launch_wide(const TreeParams& p, unsigned groups, hipStream_t stream) {
+  hipLaunchKernelGGL((tree_wide_kernel<D>), dim3(groups), dim3(256), 0, stream, p);
+  if (p.cut) hipLaunchKernelGGL((tree_join_kernel<__bf16, D, 128, kWideKeys>), dim3(groups), dim3(256), 0, stream, p);
 }
 
 template <typename T, int D>
@@ -828,6 +1276,12 @@ static int32_t launch_tree(TreeParams& p, const TreePlan& pl, bool wide, hipStre
     hipLaunchKernelGGL((tree_row_kernel<T, D>), dim3((unsigned)p.total * (unsigned)p.n_q_heads), dim3(64), 0, stream, p);
   } else {
     const unsigned groups = (unsigned)(pl.pieces * p.n_kv_heads);
+    if constexpr (sizeof(T) == 2) {
+      if (pl.wide) {
+        launch_wide<D>(p, groups, stream);
+        return hipGetLastError() == hipSuccess ? SYMPH_OK : SYMPH_ELAUNCH;
+      }
+    }
     if (pl.rw == 1)
       launch_tree<T, D, 1>(p, groups, stream);
     else if (pl.rw == 2)
@@ -902,9 +1356,9 @@ int32_t symph_tree_attn(const symph_kv_cache* cache, int32_t layer, const void* 
   p.total = total_new_tokens;
   p.scale = scale;
   const int64_t block_bytes = cache->block_stride * (int64_t)eb;
-  p.group_bytes = p.bs_shift >= 4 && block_bytes <= 0x7FFFFFFFLL ? (uint32_t)block_bytes : 0;
+  p.group_bytes = grouped_rows(cache) ? (uint32_t)block_bytes : 0;
   p.max_pieces = (int32_t)pl.pieces;
-  p.c_min = kTreeMinBlocks;
+  p.c_min = pl.c_min;
   p.cut = pl.cut;
   p.parts = (float*)d_workspace;
   const uintptr_t address_bits = (uintptr_t)p.k_layer | (uintptr_t)p.v_layer | (uintptr_t)d_q | (uintptr_t)d_k_new |
