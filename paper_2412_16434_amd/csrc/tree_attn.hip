@@ -67,6 +67,13 @@ __device__ __forceinline__ float score_scale(float scale) {
   return sizeof(T) == 2 ? scale * 1.4426950408889634f : scale;
 }
 
+// A score, or minus infinity where bit `at` of `seen` is clear: two bit operations (written as a choice it became a branch per
+// score, 26 000 lines of them).
+__device__ __forceinline__ float score_if(uint32_t seen, int at, float x) {
+  const unsigned keep = (unsigned)((int)(seen << (31 - at)) >> 31);
+  return __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, x) & keep) | (0xFF800000u & ~keep));
+}
+
 // ---- which piece of which tile a workgroup has --------------------------------------------------------------------
 struct TreePiece {
   int s, cu, P, N;
@@ -533,7 +540,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
         const uint32_t bits = seen_of(blk) >> (8 * kg);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (!((bits >> (16 * (e >> 3) + (e & 7))) & 1)) x[e] = -INFINITY;
+          x[e] = score_if(bits, 16 * (e >> 3) + (e & 7), x[e]);
       }
       float mx = x[0];
 #pragma unroll
@@ -671,7 +678,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
         const uint32_t bits = seen_of(blk) >> (4 * kg);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (!((bits >> e) & 1)) x[e] = -INFINITY;
+          x[e] = score_if(bits, e, x[e]);
       }
       float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
       mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -782,6 +789,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   typedef WideLds<D> Lds;
   constexpr int BM = 128, KB = kWideKeys, NS = D / 16, NT = D / 32;
   constexpr int kFrags = 4 * NT;  // operands of V a tile: (32-key half, 16-key step, 32-column tile)
+  constexpr int kAhead = 4;       // operands read from LDS ahead of their use
   // (arrays of their own, so that the compiler can tell which loads an LDS read has to wait for)
   __shared__ __attribute__((aligned(16))) char K0[Lds::kBytes];
   __shared__ __attribute__((aligned(16))) char K1[Lds::kBytes];
@@ -851,7 +859,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
         const int g = Lds::id_of(i, wave);
         // (scalar base and 32-bit lane offset, kept apart for the compiler: with 64-bit addresses per lane the issue of such a
         // load waits for the matrix instructions of the SIMD's other wave)
-        const uint64_t at = (uint64_t)(unsigned)ids[i] * p.group_bytes + (uint64_t)((tile * KB + 16 * g) & bs_mask) * row_bytes;
+        const uint64_t at = (uint64_t)(unsigned)ids[i] * p.group_bytes + (unsigned)((tile * KB + 16 * g) & bs_mask) * row_bytes;
         const char* base = pool + at;
         unsigned off = lane_off[D == 64 ? i : 0];
         asm("" : "+s"(base), "+v"(off));
@@ -952,7 +960,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
       bits >>= 8 * kg;
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        if (!((bits >> (16 * (e >> 3) + (e & 7))) & 1)) sc[kb][e] = -INFINITY;
+        sc[kb][e] = score_if(bits, 16 * (e >> 3) + (e & 7), sc[kb][e]);
     }
   };
   // The reference := max(reference, maximum of this tile); returns the factor for what has been accumulated
@@ -1051,20 +1059,41 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
 #pragma unroll
     for (int i = 0; i < Lds::kLoads; ++i) ids_v[i] = ids_k[i];
     if (works) {
-      scores(k_other, s_nxt);
-      float sum = rest_of_tile(s_cur);
-      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);  // K operands: six reads up front
+      // In explicit slots, between which nothing moves (the compiler's own order reads an operand right before its use and puts
+      // the exponentials behind the products): the LDS read of the operand four slots ahead, one matrix instruction of S(j+1),
+      // its share of the 16 exponentials of P(j)'s second half.
+      float sums_a[2] = {0.f, 0.f};
+      {
+        constexpr int kPer = 16 / (2 * NS);
+        bf16x8 frag[2 * NS];
+        float pe[16];
 #pragma unroll
-      for (int g = 0; g < 2 * NS; ++g) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // one matrix instruction of S(j+1)
-        if (g < 2 * NS - 6) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, 5 * 8 / NS, 0);  // scale, sum, split
-        __builtin_amdgcn_sched_group_barrier(0x400, 8 / NS, 0);      // exponentials
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s_nxt[kb][e] = 0.f;
+#pragma unroll
+        for (int g = 0; g < kAhead; ++g) frag[g] = k_frag(k_other, g >> 1, g & 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = 0; g < 2 * NS; ++g) {
+          if (g + kAhead < 2 * NS) frag[g + kAhead] = k_frag(k_other, (g + kAhead) >> 1, (g + kAhead) & 1);
+          s_nxt[g & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[g], q[g >> 1], s_nxt[g & 1], 0, 0, 0);
+#pragma unroll
+          for (int k = kPer * g; k < kPer * (g + 1); ++k) {
+            pe[k] = __builtin_amdgcn_exp2f(fmaf(s_cur[1][k], cs, -ref));
+            asm volatile("" : "+v"(pe[k]));  // (in this slot, not next to its use)
+            sums_a[k & 1] += pe[k];
+            if (k & 1) {
+              put_pair(hi[1][k >> 3], (k & 7) - 1, pe[k - 1], pe[k]);
+              put_pair(lo[1][k >> 3], (k & 7) - 1, pe[k - 1] - upper_part(pe[k - 1]), pe[k] - upper_part(pe[k]));
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(hi[1][u]), "+v"(lo[1][u]));  // (computed here, not past the branch)
       }
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(hi[kb][u]), "+v"(lo[kb][u]));  // (computed here, not past the branch)
+      float sum = sum_first + sums_a[0] + sums_a[1];
       asm volatile("" : "+v"(sum));
       settle(s_cur, sum);
       hide(s_nxt, j + 1);
@@ -1072,7 +1101,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
       // products of one operand and their share of the 16 exponentials
       bf16x8 hi_first[2], lo_first[2];
       bf16x8 frag[kFrags];
-      constexpr int kAhead = 4, kPer = 16 / kFrags;  // exponentials of a slot
+      constexpr int kPer = 16 / kFrags;  // exponentials of a slot
       float pe[16], sums[2] = {0.f, 0.f};
 #pragma unroll
       for (int g = 0; g < kAhead; ++g) frag[g] = v_frag(v_same, g);
