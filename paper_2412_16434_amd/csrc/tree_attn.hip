@@ -39,18 +39,6 @@ struct TreeParams {
   float* parts;
 };
 
-template <typename T>
-struct TreeTile;
-template <>
-struct TreeTile<__bf16> {
-  static constexpr int R = 32;  // query rows of a wave, and keys of a block
-};
-template <>
-struct TreeTile<float> {
-  static constexpr int R = 16;
-};
-constexpr int kTreeWaves = 8;
-
 static __device__ __attribute__((aligned(256))) const unsigned kNoRow[128] = {};  // a head's row of zeros
 
 __device__ __forceinline__ float widen(float x) { return x; }
@@ -246,7 +234,7 @@ __device__ __forceinline__ void row_by_lanes(const TreeParams& p, const TreePiec
 // Addresses that the tiled kernel cannot load 16 bytes wide from: a wave per (token, head), all keys.
 template <typename T, int D>
 __global__ __launch_bounds__(64) void tree_row_kernel(const TreeParams p) {
-  constexpr int KB = TreeTile<T>::R;
+  constexpr int KB = 32;  // (any: all keys are this wave's)
   __shared__ float lds[2 * D];
   const int lane = threadIdx.x;
   const int tok_all = (int)(blockIdx.x / (unsigned)p.n_q_heads), h = (int)(blockIdx.x % (unsigned)p.n_q_heads);
@@ -376,16 +364,344 @@ __device__ __forceinline__ void finish_tile(const TreeParams& p, const TreePiece
     }
 }
 
-// ---- the tiled kernel ----------------------------------------------------------------------------------------------
-template <typename T, int D, int RW>
-__global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const TreeParams p) {
-  constexpr bool kBf16 = sizeof(T) == 2;
-  constexpr int R = TreeTile<T>::R, BM = R * RW, W = kTreeWaves, KW = W / RW;
-  constexpr int kVRow = D * 2 + 64;  // bytes between V rows in LDS (bf16): the transposing read then has no conflicts
-  constexpr int kVBytes = kBf16 ? W * 32 * kVRow : 0;
+// LDS layout of rows of K or V such that the 16 rows a quarter-wave reads of K, and the 4 rows x 32 bytes that 16 lanes read of V by
+// the transposing read, lie in different banks.  One direct load writes 1 KiB, lane l to place 16 * l: which 16 bytes of which row
+// it fetches is what the layout chooses.  Two uses: a tile of 64 keys loaded by the four waves of a workgroup, and one of 8 KB
+// loaded by a single wave (stream_*).
+template <int D>
+struct TileLds;
+template <>
+struct TileLds<128> {  // 1 KiB: four rows, chunk c of row r at place c ^ ((r & 3) << 2); 16 bytes between such groups
+  static constexpr int kGroupRows = 4, kGroup = 1024 + 16, kBytes = 16 * kGroup, kLoads = 4;
+  static constexpr int kStreamKeys = 32, kStreamBytes = 8 * kGroup;
+  static __device__ __forceinline__ int row_of(int load, int wave, int lane) { return 16 * load + 4 * wave + (lane >> 4); }
+  static __device__ __forceinline__ int chunk_of(int, int lane) { return (lane & 15) ^ (((lane >> 4) & 3) << 2); }
+  static __device__ __forceinline__ int at(int load, int wave) { return (4 * load + wave) * kGroup; }
+  static __device__ __forceinline__ int id_of(int load, int) { return load; }  // which of the tile's four 16-key groups
+  static __device__ __forceinline__ int stream_row(int load, int lane) { return 4 * load + (lane >> 4); }
+  static __device__ __forceinline__ int place(int r, int c) { return (r >> 2) * kGroup + (r & 3) * 256 + ((c ^ ((r & 3) << 2)) << 4); }
+  // Operand of K for 16 columns `st` of the 32-key half `kb`; k_off[i]: place of the lane's chunk in columns 32 i ..
+  static __device__ __forceinline__ bf16x8 k_frag(const char* buf, const int (&k_off)[4], int st, int kb) {
+    return *reinterpret_cast<const bf16x8*>(buf + k_off[st >> 1] + 32 * (st & 1) + kb * 8 * kGroup);
+  }
+  // Operand of V for 16 keys g / 4 and 32 columns g % 4; v_off[i]: place for columns 32 i ..
+  static __device__ __forceinline__ bf16x8 v_frag(const char* buf, const int (&v_off)[4], int g) {
+    const char* const a = buf + v_off[g & 3] + (g >> 2) * 4 * kGroup;
+    const s16x4 lo = lds_read_tr16(reinterpret_cast<const __bf16*>(a));
+    const s16x4 hi = lds_read_tr16(reinterpret_cast<const __bf16*>(a + kGroup));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+template <>
+struct TileLds<64> {  // 1 KiB: eight rows, chunk c of row r at place c ^ twist(r)
+  static constexpr int kGroupRows = 8, kGroup = 1024, kBytes = 8 * kGroup, kLoads = 2;
+  static constexpr int kStreamKeys = 64, kStreamBytes = 8 * kGroup;
+  static __device__ __forceinline__ int twist(int r) { return (((r >> 1) & 3) << 1) | ((r >> 3) & 1); }
+  static __device__ __forceinline__ int row_of(int load, int wave, int lane) { return 32 * load + 8 * wave + (lane >> 3); }
+  static __device__ __forceinline__ int chunk_of(int row, int lane) { return (lane & 7) ^ twist(row); }
+  static __device__ __forceinline__ int at(int load, int wave) { return (4 * load + wave) * kGroup; }
+  static __device__ __forceinline__ int id_of(int load, int wave) { return 2 * load + (wave >> 1); }
+  static __device__ __forceinline__ int stream_row(int load, int lane) { return 8 * load + (lane >> 3); }
+  static __device__ __forceinline__ int place(int r, int c) { return (r >> 3) * kGroup + (r & 7) * 128 + ((c ^ twist(r)) << 4); }
+  static __device__ __forceinline__ bf16x8 k_frag(const char* buf, const int (&k_off)[4], int st, int kb) {
+    return *reinterpret_cast<const bf16x8*>(buf + k_off[st] + kb * 4 * kGroup);
+  }
+  // v_off[2 i + h]: place for columns 32 i .. and half h of the lane's 8 keys
+  static __device__ __forceinline__ bf16x8 v_frag(const char* buf, const int (&v_off)[4], int g) {
+    const s16x4 lo = lds_read_tr16(reinterpret_cast<const __bf16*>(buf + v_off[2 * (g & 1)] + (g >> 1) * 2 * kGroup));
+    const s16x4 hi = lds_read_tr16(reinterpret_cast<const __bf16*>(buf + v_off[2 * (g & 1) + 1] + (g >> 1) * 2 * kGroup));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+#define SYMPH_TREE_GLDS16(src, dst)                                                              \
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),         \
+                                   (__attribute__((address_space(3))) void*)(dst), 16, 0, 0)
+
+// The keys of 32 that a row sees, a bit each: `left` of them exist; word < 0: keys of the prefix, else that word of the row's mask.
+__device__ __forceinline__ uint32_t seen_keys(const TreeParams& p, const uint32_t* mask_row, int left, int word) {
+  uint32_t bits = left >= 32 ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
+  if (word >= 0) bits &= word < p.mask_words ? mask_row[word] : 0u;
+  return bits;
+}
+
+// Probabilities of 32 keys, 2^(x * cs - ref), as two bf16 values each, w = hi + lo with 16 bits in all: the leading 8 bits, then
+// those of what is left.  Returns the lane's sum of them.
+__device__ __forceinline__ float probabilities(const f32x16& x, float cs, float ref, bf16x8 (&hi)[2], bf16x8 (&lo)[2]) {
+  float sum[2] = {0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < 16; e += 2) {
+    float w[2], rest[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      w[k] = __builtin_amdgcn_exp2f(fmaf(x[e + k], cs, -ref));
+      sum[k] += w[k];
+      rest[k] = w[k] - upper_part(w[k]);
+    }
+    put_pair(hi[e >> 3], e & 7, w[0], w[1]);
+    put_pair(lo[e >> 3], e & 7, rest[0], rest[1]);
+  }
+  return sum[0] + sum[1];
+}
+
+// ---- narrow tiles (bf16): W waves, RW side by side on the rows, W / RW on the keys.  Up to 64 rows a read of 16 KB of K and V takes
+// longer than all arithmetic on it, so a wave is a stream of its own: tiles of 16 KB through two LDS buffers that no other wave
+// touches, no barrier.  The K buffer is filled again as soon as the scores are done, the V buffer as soon as the values are: one
+// of the two is always under way.  Loads return in order, so "all but the last eight" is exactly the older of the two.
+template <int D, int RW, int W>
+__global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams p) {
+  typedef __bf16 T;
+  typedef TileLds<D> Lds;
+  constexpr int BM = 32 * RW, KW = W / RW, KT = Lds::kStreamKeys, NB = KT / 32, NS = D / 16, NT = D / 32;
+  __shared__ __attribute__((aligned(16))) char k_lds[W][Lds::kStreamBytes];
+  __shared__ __attribute__((aligned(16))) char v_lds[W][Lds::kStreamBytes];
+  __shared__ float wave_m[W][32], wave_l[W][32];
+  __shared__ unsigned bad_rows[RW];
+
+  const int Hkv = p.n_kv_heads;
+  const int G = p.n_q_heads / Hkv;
+  const int kvh = blockIdx.x % Hkv;
+  const int piece = blockIdx.x / Hkv;
+  TreePiece it;
+  if (!find_piece<BM, KT>(p, G, piece, it)) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = wave % RW, kw = wave / RW;
+  const int n = lane & 31;  // query row of this lane within its wave's; also its row of the K operand
+  const int kg = lane >> 5;
+  const int cu = it.cu, P = it.P, N = it.N;
+  const unsigned row0 = (unsigned)it.tile * BM;
+  const int n_rows = (int)min((unsigned)BM, (unsigned)N * (unsigned)G - row0);
+  const int prefix_tiles = P / KT + (P % KT != 0), full_tiles = P / KT;
+  if (tid < RW) bad_rows[tid] = 0;
+
+  const unsigned my_row = row0 + min(rw * 32 + n, n_rows - 1);
+  const int tok = (int)(my_row / (unsigned)G);
+  const uint32_t* const mask_row = p.mask + (int64_t)(cu + tok) * p.mask_words;
+  bf16x8 q[NS];
+  {
+    const T* const qp = (const T*)p.q + ((int64_t)(cu + tok) * p.n_q_heads + kvh * G + (int)(my_row - (unsigned)tok * G)) * D;
+#pragma unroll
+    for (int st = 0; st < NS; ++st) q[st] = *reinterpret_cast<const bf16x8*>(qp + 16 * st + 8 * kg);
+  }
+
+  // ---- memory -> LDS.  Block ids one per lane (lane i: key i of the tile), asked for two tiles ahead.
+  const int32_t* const table_row = p.table + (int64_t)it.s * p.table_stride;
+  auto block_of = [&](int key) { return p.bs_shift >= 0 ? key >> p.bs_shift : key / p.block_size; };
+  const int begin = it.block0 + kw;
+  const int end = rw * 32 < n_rows ? it.block1 : it.block0;  // (waves without a row have no tiles)
+  auto ask_ids = [&](int tile) {
+    const int key = tile * KT + (lane & (KT - 1));
+    if (tile >= min(prefix_tiles, end) || key >= P) return -1;
+    const int j = block_of(key);
+    return j < p.table_stride ? table_row[j] : -1;
+  };
+  const unsigned row_bytes = (unsigned)(Hkv * D * (int)sizeof(T));
+  const char* const k_pool = reinterpret_cast<const char*>((const T*)p.k_layer + kvh * D);
+  const char* const v_pool = reinterpret_cast<const char*>((const T*)p.v_layer + kvh * D);
+  const char* const k_fresh = reinterpret_cast<const char*>((const T*)p.k_new + (int64_t)cu * Hkv * D + kvh * D);
+  const char* const v_fresh = reinterpret_cast<const char*>((const T*)p.v_new + (int64_t)cu * Hkv * D + kvh * D);
+  constexpr int kSplit = D == 64 ? 2 : 1;  // loads of a 16-key group's rows differ in the lane's place by this many kinds
+  unsigned lane_off[kSplit];
+#pragma unroll
+  for (int i = 0; i < kSplit; ++i) {
+    const int row = Lds::stream_row(i, lane);
+    lane_off[i] = (unsigned)(row & 15) * row_bytes + (unsigned)Lds::chunk_of(row, lane) * 16u;
+  }
+  // A tile that lies whole in the prefix, its 16-key groups in a block of the cache each.  A scalar base and a lane's 32-bit offset,
+  // kept apart for the compiler (see tree_wide_kernel).  No branch: rows of an id outside the cache come from the row of zeros.
+  auto issue_whole = [&](const char* pool, char* buf, int tile, int ids) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int g = i * Lds::kGroupRows / 16, rest = i * Lds::kGroupRows % 16;
+      const unsigned id = (unsigned)__builtin_amdgcn_readlane(ids, 16 * g);
+      const uint64_t at = (uint64_t)id * p.group_bytes +
+                          (unsigned)(((tile * KT + 16 * g) & (p.block_size - 1)) + (D == 128 ? rest : 0)) * row_bytes;
+      const bool known = id < (unsigned)p.n_blocks;
+      const char* base = known ? pool + at : reinterpret_cast<const char*>(kNoRow);
+      unsigned off = known ? lane_off[D == 128 ? 0 : i & 1] : (unsigned)(lane % (D / 8)) * 16u;
+      asm("" : "+s"(base), "+v"(off));
+      SYMPH_TREE_GLDS16(base + off, buf + i * Lds::kGroup);
+    }
+  };
+  // Any other: at the prefix's end, in the tree, small or odd blocks.  Rows that do not exist are zeros.
+  auto issue_rows = [&](const char* pool, const char* fresh, char* buf, int tile, int ids) {
+    int l = lane;
+    asm volatile("" : "+v"(l));  // (its pieces of addresses are worked out here: no registers for them in the loop)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = Lds::stream_row(i, l);
+      const unsigned in_row = (unsigned)Lds::chunk_of(row, l) * 16u;
+      const int id = __shfl(ids, row);
+      const char* src = reinterpret_cast<const char*>(kNoRow) + in_row;
+      if (tile < prefix_tiles) {
+        const int key = tile * KT + row;
+        if (key < P && (unsigned)id < (unsigned)p.n_blocks)
+          src = pool + (int64_t)id * p.block_stride * (int64_t)sizeof(T) +
+                (uint64_t)(unsigned)(key - block_of(key) * p.block_size) * row_bytes + in_row;
+      } else {
+        const int j = (tile - prefix_tiles) * KT + row;
+        if (j < N) src = fresh + (uint64_t)j * row_bytes + in_row;
+      }
+      SYMPH_TREE_GLDS16(src, buf + i * Lds::kGroup);
+    }
+  };
+
+  // ---- LDS reads, as in tree_wide_kernel
+  const int krow = key_of_row(n);
+  int k_off[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) k_off[i] = Lds::place(krow, D == 128 ? 4 * i + kg : 2 * i + kg);
+  const int i16 = lane & 15;
+  int v_off[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int dt = D == 128 ? i : i >> 1, half = D == 128 ? 0 : i & 1;
+    const int row = 8 * kg + 4 * half + (i16 >> 2);
+    v_off[i] = Lds::place(row, 4 * dt + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) + 8 * (i16 & 1);
+  }
+  char* const k_buf = k_lds[wave];
+  char* const v_buf = v_lds[wave];
+
+  f32x16 o[NT];
+#pragma unroll
+  for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+  float m = -INFINITY, l = 0.f;  // in log2 units
+  const float cs = score_scale<T>(p.scale);
+
+  int ids = ask_ids(begin), ids_next = ask_ids(begin + KW);
+  // Three copies of the loop's body, by what comes after the tile: one that lies whole in the prefix, any other, none.  (With the
+  // next tile's loads under a condition the compiler takes K for the youngest load under way, and waits for V too.)
+  enum { kWhole, kRows, kNone };
+  auto use_tile = [&](const int tile, auto next) {
+    constexpr int kNext = decltype(next)::value;
+    __builtin_amdgcn_s_waitcnt(0x0F70 | 8);  // vmcnt(8): K has landed, V may be on its way
+    asm volatile("" ::: "memory");
+    f32x16 x[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[b][e] = 0.f;
+#pragma unroll
+    for (int st = 0; st < NS; ++st)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Lds::k_frag(k_buf, k_off, st, b), q[st], x[b], 0, 0, 0);
+    asm volatile("" ::: "memory");
+    if constexpr (kNext != kNone) {
+      ids = ids_next;
+      ids_next = ask_ids(tile + 2 * KW);
+    }
+    if constexpr (kNext == kWhole) issue_whole(k_pool, k_buf, tile + KW, ids);
+    if constexpr (kNext == kRows) issue_rows(k_pool, k_fresh, k_buf, tile + KW, ids);
+    if (kNext != kWhole && tile >= full_tiles) {
+      const int left = tile < prefix_tiles ? P - tile * KT : N - (tile - prefix_tiles) * KT;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const uint32_t seen = seen_keys(p, mask_row, left - 32 * b, tile < prefix_tiles ? -1 : (tile - prefix_tiles) * NB + b) >> (8 * kg);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[b][e] = score_if(seen, 16 * (e >> 3) + (e & 7), x[b][e]);
+      }
+    }
+    float mx = x[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[b][e]);
+    const float m_new = fmaxf(m, max_across_halves(mx) * cs);
+    if (__any(m_new > m)) {
+      const float a = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= a;
+#pragma unroll
+      for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] *= a;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    bf16x8 hi[NB][2], lo[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) l += probabilities(x[b], cs, ref, hi[b], lo[b]);
+    if constexpr (kNext != kNone)
+      __builtin_amdgcn_s_waitcnt(0x0F70 | 8);  // V has landed, the next K may be on its way
+    else
+      __builtin_amdgcn_s_waitcnt(0x0F70);
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int g = 0; g < 2 * NB * NT; ++g) {
+      const int step = g / NT;
+      const bf16x8 v = Lds::v_frag(v_buf, v_off, g);
+      o[g % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, hi[step >> 1][step & 1], o[g % NT], 0, 0, 0);
+      o[g % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, lo[step >> 1][step & 1], o[g % NT], 0, 0, 0);
+    }
+    asm volatile("" ::: "memory");
+    if constexpr (kNext == kWhole) issue_whole(v_pool, v_buf, tile + KW, ids);
+    if constexpr (kNext == kRows) issue_rows(v_pool, v_fresh, v_buf, tile + KW, ids);
+  };
+  if (begin < end) {
+    const int whole_end = p.group_bytes != 0 ? min(end, full_tiles) : begin;
+    if (begin < whole_end) {
+      issue_whole(k_pool, k_buf, begin, ids);
+      issue_whole(v_pool, v_buf, begin, ids);
+    } else {
+      issue_rows(k_pool, k_fresh, k_buf, begin, ids);
+      issue_rows(v_pool, v_fresh, v_buf, begin, ids);
+    }
+    int tile = begin;
+    for (; tile + KW < whole_end; tile += KW) use_tile(tile, std::integral_constant<int, kWhole>{});
+    for (; tile + KW < end; tile += KW) use_tile(tile, std::integral_constant<int, kRows>{});
+    use_tile(tile, std::integral_constant<int, kNone>{});
+  }
+
+  // ---- the KW waves of a row group: maximum, factors, and their rows through the wave's own buffers (16 rows in each, 16-byte
+  // piece c of row r at c ^ r)
+  const float l_row = sum_across_halves(l);
+  if (lane < 32) wave_m[wave][n] = m;
+  __syncthreads();
+  float M = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < KW; ++w) M = fmaxf(M, wave_m[w * RW + rw][n]);
+  const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+  if (lane < 32) wave_l[wave][n] = m == -INFINITY ? l_row : l_row * f;  // (no maximum: 0, or NaN scores)
+  constexpr int kPieces = D / 4;
+  auto row_at = [&](int w, int r) { return reinterpret_cast<float*>(r < 16 ? k_lds[w] : v_lds[w]) + (r & 15) * D; };
+  if (rw * 32 < n_rows) {
+    float* const mine = row_at(wave, n);
+#pragma unroll
+    for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(mine + 4 * ((8 * dt + kg + 2 * i) ^ (n & (kPieces - 1)))) =
+            f32x4{o[dt][4 * i] * f, o[dt][4 * i + 1] * f, o[dt][4 * i + 2] * f, o[dt][4 * i + 3] * f};
+  }
+  __syncthreads();
+  finish_tile<T, D, BM, KT, W>(p, it, piece, kvh, n_rows, reinterpret_cast<float*>(k_lds), bad_rows,
+                               [&](int, int r, int c0, float& Mr, float& L) {
+    const int g = r >> 5, i = r & 31;
+    Mr = -INFINITY;
+    L = 0.f;
+    f32x4 sum{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < KW; ++w) {
+      Mr = fmaxf(Mr, wave_m[w * RW + g][i]);
+      L += wave_l[w * RW + g][i];
+      sum += *reinterpret_cast<const f32x4*>(row_at(w * RW + g, i) + 4 * ((c0 / 4) ^ (i & (kPieces - 1))));
+    }
+    return sum;
+  });
+}
+
+// ---- fp32: eight waves, RW side by side on rows (16 each), 8 / RW on the keys (blocks of 16); the fp32 matrix instruction
+// throughout.  K and V go from memory into operand registers (V's operand has one value per lane: no transposing).
+constexpr int kFp32Rows = 16;
+template <int D, int RW>
+__global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
+  typedef float T;
+  constexpr int R = kFp32Rows, BM = R * RW, W = 8, KW = W / RW;
   constexpr int kStride = D + 4;  // floats between rows of the results
-  constexpr int kJoinBytes = W * R * kStride * 4;
-  __shared__ __attribute__((aligned(16))) char lds[kVBytes > kJoinBytes ? kVBytes : kJoinBytes];
+  __shared__ __attribute__((aligned(16))) char lds[W * R * kStride * 4];
   __shared__ float wave_m[W][R], wave_l[W][R];
   __shared__ unsigned bad_rows[(BM + 31) / 32];
 
@@ -432,14 +748,9 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
   };
   // The keys of a block that the lane's row sees, a bit each
   auto seen_of = [&](int blk) -> uint32_t {
-    constexpr uint32_t kAll = R == 32 ? ~0u : 0xFFFFu;
-    const int left = blk < prefix_blocks ? P - blk * R : N - (blk - prefix_blocks) * R;
-    uint32_t bits = left >= R ? kAll : (1u << left) - 1u;
-    if (blk >= prefix_blocks) {
-      const int at = (blk - prefix_blocks) * R;
-      bits &= (at >> 5) < p.mask_words ? mask_row[at >> 5] >> (at & 31) : 0u;
-    }
-    return bits;
+    if (blk < prefix_blocks) return seen_keys(p, mask_row, P - blk * R, -1);
+    const int at = (blk - prefix_blocks) * R;
+    return seen_keys(p, mask_row, N - (at & ~31), at >> 5) >> (at & 31);
   };
   // Blocks that lie whole in the prefix, their 16-key groups in a block of the cache each: a group's rows start at a scalar
   // address and a lane adds a constant.
@@ -452,7 +763,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
   };
   auto load_vec = [](const void* at) { return *(const u32x4 __attribute__((address_space(1)))*)(uintptr_t)at; };
   auto load16 = [&](const char* base, unsigned lane_off) {
-    if constexpr (kBf16 || D == 128) asm("" : "+s"(base), "+v"(lane_off));
+    if constexpr (D == 128) asm("" : "+s"(base), "+v"(lane_off));
     return load_vec(base + lane_off);
   };
   const char* const k_head = (const char*)((const T*)p.k_layer + kvh * D);
@@ -476,255 +787,132 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
     return f;
   };
 
-  if constexpr (kBf16) {
-    constexpr int NS = D / 16;            // contraction steps of the first product
-    constexpr int NT = D / 32;            // 32-column tiles of the output
-    constexpr int LPR = D / 8, RPI = 64 / LPR, NV = 32 / RPI;  // lanes per V row, rows per load, loads
-    char* const v_lds = lds + wave * 32 * kVRow;
-    bf16x8 q[NS];
+  constexpr int NS = D / 16;  // 16-byte loads of a row per lane
+  constexpr int NH = D / 64;  // groups of 64 output columns
+  f32x4 q[NS];
 #pragma unroll
-    for (int st = 0; st < NS; ++st) q[st] = *reinterpret_cast<const bf16x8*>(qp + 16 * st + 8 * kg);
-    const int krow = key_of_row(n);
-    const int vlane_row = lane / LPR, vlane_col = (lane % LPR) * 16;
-    bf16x8 kr[NS];
-    u32x4 vr[NV];
-    const unsigned k_off = (krow & 15) * row_bytes + 16 * kg;
-    unsigned v_off_mem[NV / 2];
+  for (int j = 0; j < NS; ++j) q[j] = *reinterpret_cast<const f32x4*>(qp + 16 * j + 4 * kg);
+  f32x4 kr[NS], vr[4][NH];
+  const unsigned k_off = n * row_bytes + 16 * kg, v_off_mem = 4 * kg * row_bytes + 16 * n;
+  auto load_block = [&](int blk, int id) {
+    const int id0 = group_id(id, 0);
+    if (grouped && blk < prefix_blocks && (blk + 1) * 16 <= P && in_cache(id0)) {
+      const uint64_t off = group_off(blk * 16, id0);
 #pragma unroll
-    for (int i = 0; i < NV / 2; ++i) v_off_mem[i] = (unsigned)(i * RPI + vlane_row) * row_bytes + vlane_col;
-    auto load_block = [&](int blk, int id) {
-      const int id0 = group_id(id, 0), id1 = group_id(id, 1);
-      if (grouped && blk < prefix_blocks && (blk + 1) * 32 <= P && in_cache(id0) && in_cache(id1)) {
-        const uint64_t off0 = group_off(blk * 32, id0), off1 = group_off(blk * 32 + 16, id1);
-        const char* const k_row = k_head + (krow < 16 ? off0 : off1) + k_off;
+      for (int j = 0; j < NS; ++j) kr[j] = __builtin_bit_cast(f32x4, load16(k_head + off + 64 * j, k_off));
+      const char* const v_rows = v_head + off;
 #pragma unroll
-        for (int st = 0; st < NS; ++st) kr[st] = __builtin_bit_cast(bf16x8, load_vec(k_row + 32 * st));
-        const char* const v0 = v_head + off0;
-        const char* const v1 = v_head + off1;
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) vr[i] = load16(i < NV / 2 ? v0 : v1, v_off_mem[i % (NV / 2)]);
-        return;
-      }
-      const T* const k_row = row_of(p.k_layer, p.k_new, blk, krow, __shfl(id, krow)) + 8 * kg;
-#pragma unroll
-      for (int st = 0; st < NS; ++st) kr[st] = __builtin_bit_cast(bf16x8, load_vec(k_row + 16 * st));
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int r = i * RPI + vlane_row;
-        const T* const v_row = row_of(p.v_layer, p.v_new, blk, r, __shfl(id, r));
-        vr[i] = load_vec(reinterpret_cast<const char*>(v_row) + vlane_col);
-      }
-    };
-    const int i16 = lane & 15;
-    const int v_off = (8 * kg + (i16 >> 2)) * kVRow + 32 * ((lane >> 4) & 1) + 8 * (i16 & 3);
-    f32x16 o[NT];
-#pragma unroll
-    for (int dt = 0; dt < NT; ++dt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
-    int id_next = first < last ? fetch_id(first) : -1;
-    if (first < last) load_block(first, id_next);
-    id_next = fetch_id(first + KW);
-    for (int blk = first; blk < last; blk += KW) {
-      f32x16 x;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = 0.f;
-#pragma unroll
-      for (int st = 0; st < NS; ++st) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[st], q[st], x, 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        *reinterpret_cast<u32x4*>(v_lds + (i * RPI + vlane_row) * kVRow + vlane_col) = vr[i];
-      if (blk + KW < last) load_block(blk + KW, id_next);
-      id_next = fetch_id(blk + 2 * KW);
-      if (blk >= prefix_blocks || (blk + 1) * 32 > P) {
-        const uint32_t bits = seen_of(blk) >> (8 * kg);
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          x[e] = score_if(bits, 16 * (e >> 3) + (e & 7), x[e]);
-      }
-      float mx = x[0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
-      const float m_new = fmaxf(m, max_across_halves(mx) * cs);
-      if (__any(m_new > m)) {
-        const float a = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
-        m = m_new;
-        l *= a;
-#pragma unroll
-        for (int dt = 0; dt < NT; ++dt)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[dt][e] *= a;
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // (here, so that V operands can be read beside the exponentials)
-      __builtin_amdgcn_wave_barrier();
-      // the probabilities as two bf16 values each, w = hi + lo with 16 bits in all: the leading bits, then those of what is left
-      bf16x8 hi[2], lo[2];
-      float sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; e += 2) {
-        float w[2], rest[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          w[k] = __builtin_amdgcn_exp2f(fmaf(x[e + k], cs, -ref));
-          sum += w[k];
-          rest[k] = w[k] - upper_part(w[k]);
-        }
-        put_pair(hi[e >> 3], e & 7, w[0], w[1]);
-        put_pair(lo[e >> 3], e & 7, rest[0], rest[1]);
-      }
-      l += sum;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int dt = 0; dt < NT; ++dt) {
-          const char* vp = v_lds + v_off + 16 * u * kVRow + 64 * dt;
-          const s16x4 a0 = lds_read_tr16(reinterpret_cast<const __bf16*>(vp));
-          const s16x4 a1 = lds_read_tr16(reinterpret_cast<const __bf16*>(vp + 4 * kVRow));
-          const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
-          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, hi[u], o[dt], 0, 0, 0);
-          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, lo[u], o[dt], 0, 0, 0);
-        }
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      __builtin_amdgcn_wave_barrier();  // the tile has been read before the next one is written
+        for (int h = 0; h < NH; ++h)
+          vr[e][h] = __builtin_bit_cast(f32x4, load16(v_rows + e * row_bytes + 256 * h, v_off_mem));
+      return;
     }
-    const float f = share_state(sum_across_halves(l));
-    if (rw * R < n_rows) {
+    const T* const k_row = row_of(p.k_layer, p.k_new, blk, n, id) + 4 * kg;
 #pragma unroll
-      for (int dt = 0; dt < NT; ++dt)
+    for (int j = 0; j < NS; ++j) kr[j] = __builtin_bit_cast(f32x4, load_vec(k_row + 16 * j));
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f32x4*>(mine + n * kStride + 32 * dt + 4 * kg + 8 * i) =
-              f32x4{o[dt][4 * i] * f, o[dt][4 * i + 1] * f, o[dt][4 * i + 2] * f, o[dt][4 * i + 3] * f};
+    for (int e = 0; e < 4; ++e) {  // key 4 * kg + e: values 64 * h + 4 * n .. + 3 of its row
+      const T* const v_row = row_of(p.v_layer, p.v_new, blk, 4 * kg + e, __shfl(id, 4 * kg + e)) + 4 * n;
+#pragma unroll
+      for (int h = 0; h < NH; ++h) vr[e][h] = __builtin_bit_cast(f32x4, load_vec(v_row + 64 * h));
     }
-  } else {
-    constexpr int NS = D / 16;  // 16-byte loads of a row per lane
-    constexpr int NH = D / 64;  // groups of 64 output columns
-    f32x4 q[NS];
+  };
+  // o[h][c][e]: column 64 * h + 16 * kg + 4 * e + c of row n.  A sum over thousands of keys in one chain loses bits: kRun blocks
+  // are added up by themselves (o_run, l_run) before they join the rest.
+  constexpr int kRun = 8;
+  f32x4 o[NH][4], o_run[NH][4];
 #pragma unroll
-    for (int j = 0; j < NS; ++j) q[j] = *reinterpret_cast<const f32x4*>(qp + 16 * j + 4 * kg);
-    f32x4 kr[NS], vr[4][NH];
-    const unsigned k_off = n * row_bytes + 16 * kg, v_off_mem = 4 * kg * row_bytes + 16 * n;
-    auto load_block = [&](int blk, int id) {
-      const int id0 = group_id(id, 0);
-      if (grouped && blk < prefix_blocks && (blk + 1) * 16 <= P && in_cache(id0)) {
-        const uint64_t off = group_off(blk * 16, id0);
+  for (int h = 0; h < NH; ++h)
 #pragma unroll
-        for (int j = 0; j < NS; ++j) kr[j] = __builtin_bit_cast(f32x4, load16(k_head + off + 64 * j, k_off));
-        const char* const v_rows = v_head + off;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int h = 0; h < NH; ++h)
-            vr[e][h] = __builtin_bit_cast(f32x4, load16(v_rows + e * row_bytes + 256 * h, v_off_mem));
-        return;
-      }
-      const T* const k_row = row_of(p.k_layer, p.k_new, blk, n, id) + 4 * kg;
-#pragma unroll
-      for (int j = 0; j < NS; ++j) kr[j] = __builtin_bit_cast(f32x4, load_vec(k_row + 16 * j));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {  // key 4 * kg + e: values 64 * h + 4 * n .. + 3 of its row
-        const T* const v_row = row_of(p.v_layer, p.v_new, blk, 4 * kg + e, __shfl(id, 4 * kg + e)) + 4 * n;
-#pragma unroll
-        for (int h = 0; h < NH; ++h) vr[e][h] = __builtin_bit_cast(f32x4, load_vec(v_row + 64 * h));
-      }
-    };
-    // o[h][c][e]: column 64 * h + 16 * kg + 4 * e + c of row n.  A sum over thousands of keys in one chain loses bits: kRun blocks
-    // are added up by themselves (o_run, l_run) before they join the rest.
-    constexpr int kRun = 8;
-    f32x4 o[NH][4], o_run[NH][4];
+    for (int c = 0; c < 4; ++c) o[h][c] = o_run[h][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float l_run = 0.f;
+  auto join_run = [&]() {
+    l += l_run;
+    l_run = 0.f;
 #pragma unroll
     for (int h = 0; h < NH; ++h)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) o[h][c] = o_run[h][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float l_run = 0.f;
-    auto join_run = [&]() {
-      l += l_run;
-      l_run = 0.f;
+      for (int c = 0; c < 4; ++c) {
+        o[h][c] += o_run[h][c];
+        o_run[h][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+  };
+  int run = 0;
+  int id_next = first < last ? fetch_id(first) : -1;
+  if (first < last) load_block(first, id_next);
+  id_next = fetch_id(first + KW);
+  for (int blk = first; blk < last; blk += KW) {
+    f32x4 sc[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NS; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j][e], q[j][e], sc[e], 0, 0, 0);
+    f32x4 v[4][NH];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int h = 0; h < NH; ++h) v[e][h] = vr[e][h];
+    if (blk + KW < last) load_block(blk + KW, id_next);
+    id_next = fetch_id(blk + 2 * KW);
+    float x[4];  // key 4 * kg + e
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = cs * ((sc[0][e] + sc[1][e]) + (sc[2][e] + sc[3][e]));
+      asm("" : "+v"(x[e]));  // (rounded before the maximum is taken off, so that the largest score's exponent is 0 at any size)
+    }
+    if (blk >= prefix_blocks || (blk + 1) * 16 > P) {
+      const uint32_t bits = seen_of(blk) >> (4 * kg);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        x[e] = score_if(bits, e, x[e]);
+    }
+    float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float m_new = fmaxf(m, mx);
+    if (__any(m_new > m)) {
+      const float a = m == -INFINITY ? 0.f : expf(m - m_new);
+      m = m_new;
+      l *= a;
+      l_run *= a;
 #pragma unroll
       for (int h = 0; h < NH; ++h)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          o[h][c] += o_run[h][c];
-          o_run[h][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+          o[h][c] *= a;
+          o_run[h][c] *= a;
         }
-    };
-    int run = 0;
-    int id_next = first < last ? fetch_id(first) : -1;
-    if (first < last) load_block(first, id_next);
-    id_next = fetch_id(first + KW);
-    for (int blk = first; blk < last; blk += KW) {
-      f32x4 sc[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < NS; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j][e], q[j][e], sc[e], 0, 0, 0);
-      f32x4 v[4][NH];
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int h = 0; h < NH; ++h) v[e][h] = vr[e][h];
-      if (blk + KW < last) load_block(blk + KW, id_next);
-      id_next = fetch_id(blk + 2 * KW);
-      float x[4];  // key 4 * kg + e
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] = cs * ((sc[0][e] + sc[1][e]) + (sc[2][e] + sc[3][e]));
-        asm("" : "+v"(x[e]));  // (rounded before the maximum is taken off, so that the largest score's exponent is 0 at any size)
-      }
-      if (blk >= prefix_blocks || (blk + 1) * 16 > P) {
-        const uint32_t bits = seen_of(blk) >> (4 * kg);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          x[e] = score_if(bits, e, x[e]);
-      }
-      float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float m_new = fmaxf(m, mx);
-      if (__any(m_new > m)) {
-        const float a = m == -INFINITY ? 0.f : expf(m - m_new);
-        m = m_new;
-        l *= a;
-        l_run *= a;
-#pragma unroll
-        for (int h = 0; h < NH; ++h)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            o[h][c] *= a;
-            o_run[h][c] *= a;
-          }
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float w = expf(x[e] - ref);
-        l_run += w;
-#pragma unroll
-        for (int h = 0; h < NH; ++h)
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            o_run[h][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][h][c], w, o_run[h][c], 0, 0, 0);
-      }
-      if (++run == kRun) {
-        join_run();
-        run = 0;
-      }
     }
-    join_run();
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    const float f = share_state(l);
-    if (rw * R < n_rows) {
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float w = expf(x[e] - ref);
+      l_run += w;
 #pragma unroll
       for (int h = 0; h < NH; ++h)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<f32x4*>(mine + n * kStride + 64 * h + 16 * kg + 4 * e) =
-              f32x4{o[h][0][e] * f, o[h][1][e] * f, o[h][2][e] * f, o[h][3][e] * f};
+        for (int c = 0; c < 4; ++c)
+          o_run[h][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][h][c], w, o_run[h][c], 0, 0, 0);
     }
+    if (++run == kRun) {
+      join_run();
+      run = 0;
+    }
+  }
+  join_run();
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  const float f = share_state(l);
+  if (rw * R < n_rows) {
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4*>(mine + n * kStride + 64 * h + 16 * kg + 4 * e) =
+            f32x4{o[h][0][e] * f, o[h][1][e] * f, o[h][2][e] * f, o[h][3][e] * f};
   }
   __syncthreads();
 
@@ -754,39 +942,10 @@ __global__ __launch_bounds__(64 * kTreeWaves, 2) void tree_attn_kernel(const Tre
 constexpr int kWideKeys = 64;
 constexpr float kRaiseSum = 1.0995116e12f;  // 2^40
 
-// LDS layout of 64 rows of K or V such that the 16 rows a quarter-wave reads of K, and the 4 rows x 32 bytes that 16 lanes read of V
-// by the transposing read, lie in different banks.  One direct load writes 1 KiB, lane l to place 16 * l: which 16 bytes of which
-// row it fetches is what the layout chooses.
-template <int D>
-struct WideLds;
-template <>
-struct WideLds<128> {  // 1 KiB: four rows, chunk c of row r at place c ^ ((r & 3) << 2); 16 bytes between such groups
-  static constexpr int kGroup = 1024 + 16, kBytes = 16 * kGroup, kLoads = 4;
-  static __device__ __forceinline__ int row_of(int load, int wave, int lane) { return 16 * load + 4 * wave + (lane >> 4); }
-  static __device__ __forceinline__ int chunk_of(int, int lane) { return (lane & 15) ^ (((lane >> 4) & 3) << 2); }
-  static __device__ __forceinline__ int at(int load, int wave) { return (4 * load + wave) * kGroup; }
-  static __device__ __forceinline__ int place(int r, int c) { return (r >> 2) * kGroup + (r & 3) * 256 + ((c ^ ((r & 3) << 2)) << 4); }
-  static __device__ __forceinline__ int id_of(int load, int) { return load; }  // which of the tile's four 16-key groups
-};
-template <>
-struct WideLds<64> {  // 1 KiB: eight rows, chunk c of row r at place c ^ twist(r)
-  static constexpr int kBytes = 8 * 1024, kLoads = 2;
-  static __device__ __forceinline__ int twist(int r) { return (((r >> 1) & 3) << 1) | ((r >> 3) & 1); }
-  static __device__ __forceinline__ int row_of(int load, int wave, int lane) { return 32 * load + 8 * wave + (lane >> 3); }
-  static __device__ __forceinline__ int chunk_of(int row, int lane) { return (lane & 7) ^ twist(row); }
-  static __device__ __forceinline__ int at(int load, int wave) { return (4 * load + wave) * 1024; }
-  static __device__ __forceinline__ int place(int r, int c) { return (r >> 3) * 1024 + (r & 7) * 128 + ((c ^ twist(r)) << 4); }
-  static __device__ __forceinline__ int id_of(int load, int wave) { return 2 * load + (wave >> 1); }
-};
-
-#define SYMPH_TREE_GLDS16(src, dst)                                                              \
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),         \
-                                   (__attribute__((address_space(3))) void*)(dst), 16, 0, 0)
-
 template <int D>
 __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   typedef __bf16 T;
-  typedef WideLds<D> Lds;
+  typedef TileLds<D> Lds;
   constexpr int BM = 128, KB = kWideKeys, NS = D / 16, NT = D / 32;
   constexpr int kFrags = 4 * NT;  // operands of V a tile: (32-key half, 16-key step, 32-column tile)
   constexpr int kAhead = 4;       // operands read from LDS ahead of their use
@@ -897,12 +1056,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   int k_off[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) k_off[i] = Lds::place(krow, D == 128 ? 4 * i + kg : 2 * i + kg);
-  auto k_frag = [&](const char* buf, int st, int kb) {
-    if constexpr (D == 128)
-      return *reinterpret_cast<const bf16x8*>(buf + k_off[st >> 1] + 32 * (st & 1) + kb * 8 * WideLds<128>::kGroup);
-    else
-      return *reinterpret_cast<const bf16x8*>(buf + k_off[st] + kb * 4096);
-  };
+  auto k_frag = [&](const char* buf, int st, int kb) { return Lds::k_frag(buf, k_off, st, kb); };
   const int i16 = lane & 15;
   int v_off[4];  // 128: by column tile; 64: by column tile and half of the 8 keys
 #pragma unroll
@@ -911,20 +1065,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
     const int row = 8 * kg + 4 * half + (i16 >> 2);
     v_off[i] = Lds::place(row, 4 * dt + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) + 8 * (i16 & 1);
   }
-  auto v_frag = [&](const char* buf, int g) {  // g = (kb * 2 + u) * NT + dt
-    const int dt = g % NT, step = g / NT;      // step: 16 keys
-    const char *a, *b;
-    if constexpr (D == 128) {
-      a = buf + v_off[dt] + step * 4 * WideLds<128>::kGroup;
-      b = a + WideLds<128>::kGroup;
-    } else {
-      a = buf + v_off[2 * dt] + step * 2048;
-      b = buf + v_off[2 * dt + 1] + step * 2048;
-    }
-    const s16x4 lo = lds_read_tr16(reinterpret_cast<const __bf16*>(a));
-    const s16x4 hi = lds_read_tr16(reinterpret_cast<const __bf16*>(b));
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-  };
+  auto v_frag = [&](const char* buf, int g) { return Lds::v_frag(buf, v_off, g); };
 
   f32x16 o[NT];
 #pragma unroll
@@ -951,16 +1092,10 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
     const int left = tile < prefix_tiles ? P - tile * KB : N - (tile - prefix_tiles) * KB;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      const int here = left - 32 * kb;
-      uint32_t bits = here >= 32 ? ~0u : here > 0 ? (1u << here) - 1u : 0u;
-      if (tile >= prefix_tiles) {
-        const int w = 2 * (tile - prefix_tiles) + kb;
-        bits &= w < p.mask_words ? mask_row[w] : 0u;
-      }
-      bits >>= 8 * kg;
+      const uint32_t bits =
+          seen_keys(p, mask_row, left - 32 * kb, tile < prefix_tiles ? -1 : 2 * (tile - prefix_tiles) + kb) >> (8 * kg);
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        sc[kb][e] = score_if(bits, 16 * (e >> 3) + (e & 7), sc[kb][e]);
+      for (int e = 0; e < 16; ++e) sc[kb][e] = score_if(bits, 16 * (e >> 3) + (e & 7), sc[kb][e]);
     }
   };
   // The reference := max(reference, maximum of this tile); returns the factor for what has been accumulated
@@ -976,24 +1111,6 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
     ref = m_new == -INFINITY ? 0.f : m_new;
     return a;
   };
-  // Probabilities of a half of the tile as two bf16 values each, w = hi + lo with 16 bits in all; returns their sum
-  auto probabilities = [&](const f32x16& sc, float ref, bf16x8 (&hi)[2], bf16x8 (&lo)[2]) {
-    float sum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int e = 0; e < 16; e += 2) {
-      float w[2], rest[2];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        w[k] = __builtin_amdgcn_exp2f(fmaf(sc[e + k], cs, -ref));
-        sum[k] += w[k];
-        rest[k] = w[k] - upper_part(w[k]);
-      }
-      put_pair(hi[e >> 3], e & 7, w[0], w[1]);
-      put_pair(lo[e >> 3], e & 7, rest[0], rest[1]);
-    }
-    return sum[0] + sum[1];
-  };
-
   f32x16 s_even[2], s_odd[2];  // scores of the even and of the odd tiles, counted from the first
   bf16x8 hi[2][2], lo[2][2];   // P(j)
   float ref = 0.f, sum_first = 0.f;
@@ -1016,7 +1133,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
     scores(K0, s_even);
     hide(s_even, begin);
     raise_reference(s_even, ref);
-    sum_first = probabilities(s_even[0], ref, hi[0], lo[0]);
+    sum_first = probabilities(s_even[0], cs, ref, hi[0], lo[0]);
   }
   asked = ask_ids(begin + 2);
   auto arrived = [&]() {
@@ -1027,7 +1144,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
 
   // P(j)'s second half and the end of its statistics; a row without a reference yet, or with one that is far too low, gets one
   auto rest_of_tile = [&](const f32x16 (&sc)[2]) {
-    float sum = sum_first + probabilities(sc[1], ref, hi[1], lo[1]);
+    float sum = sum_first + probabilities(sc[1], cs, ref, hi[1], lo[1]);
     return sum;
   };
   auto settle = [&](const f32x16 (&sc)[2], float sum) {
@@ -1038,7 +1155,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
       for (int dt = 0; dt < NT; ++dt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[dt][e] *= a;
-      sum = probabilities(sc[0], ref, hi[0], lo[0]) + probabilities(sc[1], ref, hi[1], lo[1]);
+      sum = probabilities(sc[0], cs, ref, hi[0], lo[0]) + probabilities(sc[1], cs, ref, hi[1], lo[1]);
     }
     l_run += sum;
   };
@@ -1249,6 +1366,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kTreePieces = 1024;   // workgroups that the key axis is cut for, all kv-heads together
 constexpr int kTreeMinKeys = 512;   // keys of a tile that are not cut further
+constexpr int kStreamWaves = 8;
 
 struct TreePlan {
   bool wide;           // 128-row tiles through LDS
@@ -1273,7 +1391,7 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   const int64_t rows = (int64_t)max_new * G;
   pl.wide = c->dtype == SYMPH_BF16 && rows > 64 && grouped_rows(c);
   pl.rw = rows <= R ? 1 : rows <= 2 * R ? 2 : 4;
-  const int64_t BM = pl.wide ? 128 : (int64_t)R * pl.rw, KB = pl.wide ? kWideKeys : R;
+  const int64_t BM = pl.wide ? 128 : (int64_t)R * pl.rw, KB = pl.wide || (R == 32 && c->head_dim == 64) ? 64 : R;
   pl.c_min = (int32_t)(kTreeMinKeys / KB);
   const int64_t tiles = (int64_t)total * G / BM + n_sessions;  // at least as many as there are
   const int64_t blocks = ceil_div64(max_prefix, KB) + ceil_div64(max_new, KB);
@@ -1288,9 +1406,14 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
 
 template <typename T, int D, int RW>
 static void launch_tree(const TreeParams& p, unsigned groups, hipStream_t stream) {
-  constexpr int R = TreeTile<T>::R;
-  hipLaunchKernelGGL((tree_attn_kernel<T, D, RW>), dim3(groups), dim3(64 * kTreeWaves), 0, stream, p);
-  if (p.cut) hipLaunchKernelGGL((tree_join_kernel<T, D, R * RW, R>), dim3(groups), dim3(256), 0, stream, p);
+  if constexpr (sizeof(T) == 2) {
+    hipLaunchKernelGGL((tree_stream_kernel<D, RW, kStreamWaves>), dim3(groups), dim3(64 * kStreamWaves), 0, stream, p);
+    if (p.cut)
+      hipLaunchKernelGGL((tree_join_kernel<T, D, 32 * RW, TileLds<D>::kStreamKeys>), dim3(groups), dim3(256), 0, stream, p);
+  } else {
+    hipLaunchKernelGGL((tree_fp32_kernel<D, RW>), dim3(groups), dim3(512), 0, stream, p);
+    if (p.cut) hipLaunchKernelGGL((tree_join_kernel<T, D, kFp32Rows * RW, kFp32Rows>), dim3(groups), dim3(256), 0, stream, p);
+  }
 }
 
 template <int D>
