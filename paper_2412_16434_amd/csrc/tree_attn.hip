@@ -12,6 +12,7 @@
 //     the low bits in its last block, the caller's mask in the blocks of the tree, which start at the tree's first token.
 #include "attn_lanes.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace symph {
@@ -33,8 +34,8 @@ struct TreeParams {
   int32_t table_stride, n_sessions, total;
   float scale;
   uint32_t group_bytes;  // bytes between blocks where 16 consecutive keys lie in one block and a block fits 32 bits; else 0
-  int32_t max_pieces;    // per kv-head: what the grid and the workspace have room for
-  int32_t c_min;         // key blocks of a tile that are not cut further
+  int32_t max_pieces;    // of tiles (per kv-head) or ranges: what the grid and the workspace have room for
+  int32_t c_min;         // key blocks of a tile that are not cut further, of a range at least
   int32_t cut;           // 0: one piece per tile
   float* parts;
 };
@@ -138,6 +139,112 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
     before += __builtin_amdgcn_readlane(incl, 63);
   }
   return false;
+}
+
+// ---- the other way to cut: all tiles' key blocks laid end to end, in session order, and cut into equal ranges, one per workgroup,
+// whatever tiles they run through.  Nothing is left over at the end of a launch (pieces of tiles, a third more of them than the
+// chip takes at once, made 64 short drafts take 246 us instead of @@); what it costs is that tiles of one session are read at
+// different times, so it is for batches whose sessions have one tile.
+struct TreeRanges {
+  int64_t total, per;  // blocks; of a range
+  int count, longer;   // ranges; the first `longer` of them have one block more
+  __device__ __forceinline__ int64_t begin(int r) const { return per * r + min(r, longer); }
+  __device__ __forceinline__ int holding(int64_t x) const {
+    const int64_t head = longer * (per + 1);
+    const int64_t a = x < head ? x : x - head, b = x < head ? per + 1 : per;
+    const int q = (a | b) >> 31 ? (int)(a / b) : (int)((unsigned)a / (unsigned)b);
+    return __builtin_amdgcn_readfirstlane(x < head ? q : longer + q);
+  }
+};
+
+struct SessionLane {  // what a lane knows of its session
+  int cu, P, N, tiles, blocks;
+  // (a lane's share of a 64-lane sum of 32 bits; a session of more has more than 10^9 keys times tiles)
+  __device__ __forceinline__ int work() const { return (int)min((int64_t)tiles * blocks, (int64_t)0x7FFFFFFF / 64); }
+};
+
+template <int BM, int KB>
+__device__ __forceinline__ TreeRanges cut_ranges(const TreeParams& p, int G, SessionLane& mine) {
+  const int lane = threadIdx.x & 63;
+  tree_session<BM, KB>(p, G, lane, mine.cu, mine.P, mine.N, mine.tiles, mine.blocks);
+  TreeRanges rg;
+  rg.total = __builtin_amdgcn_readlane(wave_inclusive_scan(mine.work()), 63);
+  for (int i0 = 64; i0 < p.n_sessions; i0 += 64) {
+    SessionLane other;
+    tree_session<BM, KB>(p, G, i0 + lane, other.cu, other.P, other.N, other.tiles, other.blocks);
+    rg.total += __builtin_amdgcn_readlane(wave_inclusive_scan(other.work()), 63);
+  }
+  const int64_t most = rg.total >> 31 ? rg.total / p.c_min : (unsigned)rg.total / (unsigned)p.c_min;
+  rg.count = __builtin_amdgcn_readfirstlane((int)max(min(most, (int64_t)p.max_pieces), (int64_t)1));
+  rg.per = rg.total >> 31 ? rg.total / rg.count : (unsigned)rg.total / (unsigned)rg.count;
+  rg.per = (int64_t)__builtin_amdgcn_readfirstlane((int)(rg.per >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)rg.per);
+  rg.longer = (int)(rg.total - rg.per * rg.count);
+  return rg;
+}
+
+// The tile that block x lies in, all of its blocks; `start`: its first.  mine: the lane's of the first 64 sessions.
+template <int BM, int KB>
+__device__ __forceinline__ bool find_tile(const TreeParams& p, int G, const SessionLane& mine, int64_t x, TreePiece& it,
+                                          int64_t& start) {
+  const int lane = threadIdx.x & 63;
+  SessionLane here = mine;
+  int64_t before = 0;
+  for (int i0 = 0; i0 < p.n_sessions; i0 += 64) {
+    if (i0 > 0) tree_session<BM, KB>(p, G, i0 + lane, here.cu, here.P, here.N, here.tiles, here.blocks);
+    const int work = here.work(), incl = wave_inclusive_scan(work);
+    const uint64_t holds = __ballot(before + incl > x);
+    if (holds) {
+      const int at = __builtin_ctzll(holds);
+      it.s = i0 + at;
+      it.cu = __builtin_amdgcn_readlane(here.cu, at);
+      it.P = __builtin_amdgcn_readlane(here.P, at);
+      it.N = __builtin_amdgcn_readlane(here.N, at);
+      it.block0 = 0;
+      it.block1 = __builtin_amdgcn_readlane(here.blocks, at);
+      const int64_t first = before + __builtin_amdgcn_readlane(incl - work, at);
+      it.tile = __builtin_amdgcn_readfirstlane((int)(x - first) / it.block1);
+      start = first + (int64_t)it.tile * it.block1;
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
+// Results of a cut tile's part in range r: the first place of the range's two if the part starts with the range, else the second.
+__device__ __forceinline__ int64_t range_place(const TreeRanges& rg, int r, int64_t tile_start) {
+  return 2 * (int64_t)r + (tile_start > rg.begin(r));
+}
+
+// Runs `segment(it, place)` for every part of a tile that lies in range r; it.count: 1 if that is all of it, place: else where its
+// results go.  Without a cut: for tile r.
+template <int BM, int KB, typename Segment>
+__device__ __forceinline__ void for_segments(const TreeParams& p, int G, int r, Segment segment) {
+  SessionLane mine;
+  TreeRanges rg;
+  TreePiece it;
+  int64_t x = 0, end = 1, start = 0;
+  if (p.cut) {
+    rg = cut_ranges<BM, KB>(p, G, mine);
+    if (r >= rg.count) return;
+    x = rg.begin(r);
+    end = rg.begin(r + 1);
+  }
+  while (x < end) {
+    if (!p.cut) {
+      if (!find_piece<BM, KB>(p, G, r, it)) return;
+      x = end;
+    } else {
+      if (!find_tile<BM, KB>(p, G, mine, x, it, start)) return;
+      const int64_t tile_end = start + it.block1, stop = min(tile_end, end);
+      it.block0 = (int)(x - start);
+      it.block1 = (int)(stop - start);
+      it.index = 0;
+      it.count = it.block0 == 0 && stop == tile_end ? 1 : 2;
+      x = stop;
+    }
+    segment(it, p.cut ? range_place(rg, r, start) : 0);
+  }
 }
 
 // What a row without any probability gets: zero if it sees no key, NaN if all its scores are minus infinity (0 / 0).
@@ -276,45 +383,49 @@ __device__ __forceinline__ float* part_slot(const TreeParams& p, int64_t g, int 
   return p.parts + (g * p.n_kv_heads + kvh) * (int64_t)(BM * (D + 2));
 }
 
-// ---- results of a tile of BM rows, by all WAVES waves of its workgroup.  sum_at(r, c, M, L): four columns of row r from column c
-// on, added up over the waves that share the row, with their maximum and sum.  A row with a value that is not finite (an infinity
-// or a NaN among the values, which the matrix product spreads to rows that do not see it), or with scores beyond what the loop's
-// arithmetic is made for, is worked out again by itself.  Its q is read again for that, so nothing is written before: out may be
-// q.  lds: 2 * D floats a wave, free once every thread has its sums; bad_rows: BM / 32 words of zeros.
+// ---- results of a tile of BM rows by all WAVES waves of the workgroup.  slot: where the results of a tile that is cut go.  sum_at(t, r, c, M, L):
+// four columns of row r from column c on, added up over the waves that share the row, with their maximum
+// and sum; t: turn of the thread.  A row with a value that is not finite (an infinity or a NaN among the values, which the matrix
+// product spreads to rows that do not see it), or with scores beyond what the loop's arithmetic is made for, is worked out again
+// by itself, from its q: it is not written before (out may be q).  lds: 2 * D floats a wave, which may be where sum_at reads;
+// bad_rows: a bit per row, zeros.
 constexpr float kLargestScore = 0x1p20f;
 template <typename T, int D, int BM, int KB, int WAVES, typename Sum>
-__device__ __forceinline__ void finish_tile(const TreeParams& p, const TreePiece& it, int piece, int kvh, int n_rows, float* lds,
+__device__ __forceinline__ void finish_tile(const TreeParams& p, const TreePiece& it, float* slot, int kvh, int n_rows, float* lds,
                                             unsigned* bad_rows, Sum sum_at) {
   constexpr int kQuads = BM * D / 4, kTurns = (kQuads + 64 * WAVES - 1) / (64 * WAVES);
   typedef T vec __attribute__((ext_vector_type(4)));
-  const int tid = threadIdx.x, lane = tid & 63;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));  // (a number that the optimiser cannot see through: no addresses for what follows held in loops before)
+  const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = p.n_q_heads / p.n_kv_heads;
   const unsigned row0 = (unsigned)it.tile * BM;
   const bool whole = it.count == 1;
-  float* const slot = whole ? nullptr : part_slot<BM, D>(p, piece, kvh);
-  f32x4 x[kTurns];
-  f32x2 state[kTurns];
+  // A value of the thread's turn: final for a whole tile
+  auto value_of = [&](int t, int r, int c0, float& M, float& L) {
+    f32x4 sum = sum_at(t, r, c0, M, L);
+    if (L == 0.f) sum = f32x4{0.f, 0.f, 0.f, 0.f};  // (no probability: whatever values the product brought in are not the row's)
+    if (whole) {
+      if (L == 0.f) {
+        const float none = nothing_seen(p, it, (int)((row0 + r) / (unsigned)G));
+        sum = f32x4{none, none, none, none};
+      } else {
+        sum *= 1.0f / L;
+      }
+    }
+    return sum;
+  };
+  // (twice: the values are read from LDS again rather than kept, up to 96 registers)
 #pragma unroll
   for (int t = 0; t < kTurns; ++t) {
     const int i = tid + t * 64 * WAVES, r = i / (D / 4), c0 = 4 * (i % (D / 4));
-    if (i >= kQuads || r >= n_rows) break;
+    if (i >= kQuads || r >= n_rows) continue;
     float M, L;
-    f32x4 sum = sum_at(t, r, c0, M, L);
-    if (L == 0.f) sum = f32x4{0.f, 0.f, 0.f, 0.f};  // (no probability: whatever values the product brought in are not the row's)
+    const f32x4 x = value_of(t, r, c0, M, L);
     bool bad = false;
-    float scale = 1.0f, none = 0.f;
-    if (whole) {
-      scale = L == 0.f ? 0.f : 1.0f / L;
-      if (L == 0.f) none = nothing_seen(p, it, (int)((row0 + r) / (unsigned)G));
-    }
-    state[t] = f32x2{M, L};
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      sum[v] = sum[v] * scale + none;
-      bad = bad || !(fabsf(sum[v]) < INFINITY);
-    }
-    x[t] = sum;
+    for (int v = 0; v < 4; ++v) bad = bad || !(fabsf(x[v]) < INFINITY);
     // (a sum that is NaN comes from a score that is: every value of the row is NaN either way; so is 0 / 0)
     bad = (bad && L == L && L != 0.f) || (fabsf(M) > kLargestScore && M != -INFINITY);
     if (bad) atomicOr(&bad_rows[r >> 5], 1u << (r & 31));
@@ -323,23 +434,29 @@ __device__ __forceinline__ void finish_tile(const TreeParams& p, const TreePiece
 #pragma unroll
   for (int t = 0; t < kTurns; ++t) {
     const int i = tid + t * 64 * WAVES, r = i / (D / 4), c0 = 4 * (i % (D / 4));
-    if (i >= kQuads || r >= n_rows) break;
-    if ((bad_rows[r >> 5] >> (r & 31)) & 1) continue;
+    if (i >= kQuads || r >= n_rows || ((bad_rows[r >> 5] >> (r & 31)) & 1)) continue;
+    float M, L;
+    const f32x4 x = value_of(t, r, c0, M, L);
     if (whole) {
       const unsigned row = row0 + r, tok = row / (unsigned)G;
       T* const op = (T*)p.out + ((int64_t)(it.cu + (int)tok) * p.n_q_heads + kvh * G + (int)(row - tok * G)) * D;
       vec y;
 #pragma unroll
-      for (int v = 0; v < 4; ++v) y[v] = (T)x[t][v];
+      for (int v = 0; v < 4; ++v) y[v] = (T)x[v];
       *reinterpret_cast<vec*>(op + c0) = y;
     } else {
-      *reinterpret_cast<f32x4*>(slot + r * D + c0) = x[t];
+      *reinterpret_cast<f32x4*>(slot + r * D + c0) = x;
       if (c0 == 0) {
-        slot[BM * D + r] = state[t][0];
-        slot[BM * D + BM + r] = state[t][1];
+        slot[BM * D + r] = M;
+        slot[BM * D + BM + r] = L;
       }
     }
   }
+  unsigned any = 0;
+#pragma unroll
+  for (int word = 0; word < (BM + 31) / 32; ++word) any |= bad_rows[word];
+  if (__builtin_amdgcn_readfirstlane(any) == 0) return;
+  __syncthreads();  // (lds has been read for the last time)
   int turn = 0;
   for (int word = 0; word < (BM + 31) / 32; ++word)
     for (unsigned left = __builtin_amdgcn_readfirstlane(bad_rows[word]); left; left &= left - 1) {
@@ -414,9 +531,10 @@ struct TileLds<64> {  // 1 KiB: eight rows, chunk c of row r at place c ^ twist(
   }
 };
 
-#define SYMPH_TREE_GLDS16(src, dst)                                                              \
+// 16 bytes a lane from memory straight into LDS; POLICY 2: non-temporal, for rows that are read once
+#define SYMPH_TREE_GLDS16(src, dst, POLICY)                                                      \
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),         \
-                                   (__attribute__((address_space(3))) void*)(dst), 16, 0, 0)
+                                   (__attribute__((address_space(3))) void*)(dst), 16, 0, POLICY)
 
 // The keys of 32 that a row sees, a bit each: `left` of them exist; word < 0: keys of the prefix, else that word of the row's mask.
 __device__ __forceinline__ uint32_t seen_keys(const TreeParams& p, const uint32_t* mask_row, int left, int word) {
@@ -461,14 +579,12 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
   const int Hkv = p.n_kv_heads;
   const int G = p.n_q_heads / Hkv;
   const int kvh = blockIdx.x % Hkv;
-  const int piece = blockIdx.x / Hkv;
-  TreePiece it;
-  if (!find_piece<BM, KT>(p, G, piece, it)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kw = wave / RW;
   const int n = lane & 31;  // query row of this lane within its wave's; also its row of the K operand
   const int kg = lane >> 5;
+  for_segments<BM, KT>(p, G, blockIdx.x / Hkv, [&](const TreePiece& it, const int64_t place) {
   const int cu = it.cu, P = it.P, N = it.N;
   const unsigned row0 = (unsigned)it.tile * BM;
   const int n_rows = (int)min((unsigned)BM, (unsigned)N * (unsigned)G - row0);
@@ -521,7 +637,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
       const char* base = known ? pool + at : reinterpret_cast<const char*>(kNoRow);
       unsigned off = known ? lane_off[D == 128 ? 0 : i & 1] : (unsigned)(lane % (D / 8)) * 16u;
       asm("" : "+s"(base), "+v"(off));
-      SYMPH_TREE_GLDS16(base + off, buf + i * Lds::kGroup);
+      SYMPH_TREE_GLDS16(base + off, buf + i * Lds::kGroup, RW == 1 ? 2 : 0);
     }
   };
   // Any other: at the prefix's end, in the tree, small or odd blocks.  Rows that do not exist are zeros.
@@ -543,7 +659,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
         const int j = (tile - prefix_tiles) * KT + row;
         if (j < N) src = fresh + (uint64_t)j * row_bytes + in_row;
       }
-      SYMPH_TREE_GLDS16(src, buf + i * Lds::kGroup);
+      SYMPH_TREE_GLDS16(src, buf + i * Lds::kGroup, RW == 1 ? 2 : 0);
     }
   };
 
@@ -677,19 +793,21 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
             f32x4{o[dt][4 * i] * f, o[dt][4 * i + 1] * f, o[dt][4 * i + 2] * f, o[dt][4 * i + 3] * f};
   }
   __syncthreads();
-  finish_tile<T, D, BM, KT, W>(p, it, piece, kvh, n_rows, reinterpret_cast<float*>(k_lds), bad_rows,
+  finish_tile<T, D, BM, KT, W>(p, it, part_slot<BM, D>(p, place, kvh), kvh, n_rows, reinterpret_cast<float*>(k_lds), bad_rows,
                                [&](int, int r, int c0, float& Mr, float& L) {
-    const int g = r >> 5, i = r & 31;
+    const int first = r >> 5, i = r & 31;  // the first of the row's waves
     Mr = -INFINITY;
     L = 0.f;
     f32x4 sum{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
-      Mr = fmaxf(Mr, wave_m[w * RW + g][i]);
-      L += wave_l[w * RW + g][i];
-      sum += *reinterpret_cast<const f32x4*>(row_at(w * RW + g, i) + 4 * ((c0 / 4) ^ (i & (kPieces - 1))));
+      Mr = fmaxf(Mr, wave_m[first + w * RW][i]);
+      L += wave_l[first + w * RW][i];
+      sum += *reinterpret_cast<const f32x4*>(row_at(first + w * RW, i) + 4 * ((c0 / 4) ^ (i & (kPieces - 1))));
     }
     return sum;
+  });
+  __syncthreads();  // (the buffers and flags of this segment are used again)
   });
 }
 
@@ -708,14 +826,12 @@ __global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
   const int Hkv = p.n_kv_heads;
   const int G = p.n_q_heads / Hkv;
   const int kvh = blockIdx.x % Hkv;
-  const int piece = blockIdx.x / Hkv;
-  TreePiece it;
-  if (!find_piece<BM, R>(p, G, piece, it)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kw = wave / RW;
   const int n = lane & (R - 1);  // query row of this lane within its wave's; also its row of the K operand
   const int kg = lane / R;       // its share of the contraction index: half (bf16) or quarter (fp32) of the wave
+  for_segments<BM, R>(p, G, blockIdx.x / Hkv, [&](const TreePiece& it, const int64_t place) {
   const int cu = it.cu, P = it.P, N = it.N;
   const unsigned row0 = (unsigned)it.tile * BM;
   const int n_rows = (int)min((unsigned)BM, (unsigned)N * (unsigned)G - row0);
@@ -917,7 +1033,7 @@ __global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
   __syncthreads();
 
   const float* const all = reinterpret_cast<const float*>(lds);
-  finish_tile<T, D, BM, R, W>(p, it, piece, kvh, n_rows, reinterpret_cast<float*>(lds), bad_rows,
+  finish_tile<T, D, BM, R, W>(p, it, part_slot<BM, D>(p, place, kvh), kvh, n_rows, reinterpret_cast<float*>(lds), bad_rows,
                               [&](int, int r, int c0, float& M, float& L) {
     const int w0 = (r / R) * KW;
     M = -INFINITY;
@@ -930,6 +1046,8 @@ __global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
       sum += *reinterpret_cast<const f32x4*>(all + ((w0 + w) * R + r % R) * kStride + c0);
     }
     return sum;
+  });
+  __syncthreads();  // (the buffer and flags of this segment are used again)
   });
 }
 
@@ -1022,7 +1140,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
         const char* base = pool + at;
         unsigned off = lane_off[D == 64 ? i : 0];
         asm("" : "+s"(base), "+v"(off));
-        SYMPH_TREE_GLDS16(base + off, buf + Lds::at(i, wave));
+        SYMPH_TREE_GLDS16(base + off, buf + Lds::at(i, wave), 0);
       }
       asm volatile("; end of the scalar-base loads");  // keeps the last one from being merged with the other path's
     } else {
@@ -1045,7 +1163,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
           const int j = (tile - prefix_tiles) * KB + row;
           if (j < N) src = fresh + (uint64_t)j * row_bytes + in_row;
         }
-        SYMPH_TREE_GLDS16(src, buf + Lds::at(i, wave));
+        SYMPH_TREE_GLDS16(src, buf + Lds::at(i, wave), 0);
       }
     }
   };
@@ -1293,7 +1411,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   }
   __syncthreads();
   constexpr int kRowsPerTurn = 256 / kPieces;
-  finish_tile<T, D, BM, KB, 4>(p, it, piece, kvh, n_rows, reinterpret_cast<float*>(K0), bad_rows,
+  finish_tile<T, D, BM, KB, 4>(p, it, part_slot<BM, D>(p, piece, kvh), kvh, n_rows, reinterpret_cast<float*>(K0), bad_rows,
                                [&](int t, int r, int c0, float& M, float& L) {
     M = row_m[r];
     L = row_l[r];
@@ -1301,64 +1419,121 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
                                            4 * ((c0 / 4) ^ (r & 31 & (kPieces - 1))));
   });
 }
-// ---- joins the pieces of cut tiles: out = sum_c f_c O_c / sum_c f_c l_c, f_c = e^(m_c - max_c m_c).  Each of a tile's pieces
-// has a workgroup here too, which joins an equal share of the tile's rows, a wave per row.
-template <typename T, int D, int BM, int KB>
-__global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
-  constexpr int LPR = D / 4, SUB = 64 / LPR;  // lanes per row, pieces side by side
-  const int Hkv = p.n_kv_heads;
-  const int G = p.n_q_heads / Hkv;
-  const int kvh = blockIdx.x % Hkv, piece = blockIdx.x / Hkv;
-  TreePiece it;
-  if (!find_piece<BM, KB>(p, G, piece, it) || it.count == 1) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// ---- joins the pieces of cut tiles: out = sum_c f_c O_c / sum_c f_c l_c, f_c = e^(m_c - max_c m_c).  Each of a tile's pieces has
+// a workgroup here too, which joins an equal share of the tile's rows.  A join is nothing but trips to memory: D / 4 lanes take a
+// row's columns of eight pieces at a time, and where there are fewer rows than such groups of lanes, several share a row.
+template <typename T, int D, int BM, typename Slot>
+__device__ __forceinline__ void join_rows(const TreeParams& p, const TreePiece& it, int kvh, Slot slot_of) {
+  constexpr int kLanes = D / 4, kSubs = 256 / kLanes, kAtOnce = 8;
+  __shared__ f32x4 part_o[kSubs][kLanes];
+  __shared__ float part_m[kSubs], part_l[kSubs];
+  const int tid = threadIdx.x, sub = tid / kLanes, c0 = 4 * (tid % kLanes);
+  const int G = p.n_q_heads / p.n_kv_heads;
   const unsigned row0 = (unsigned)it.tile * BM;
   const int n_rows = (int)min((unsigned)BM, (unsigned)it.N * (unsigned)G - row0);
   const int r0 = (int)((int64_t)n_rows * it.index / it.count), r1 = (int)((int64_t)n_rows * (it.index + 1) / it.count);
-  const int64_t first = piece - (int64_t)it.index * it.stride;
-  const int sub = lane / LPR, c0 = 4 * (lane % LPR);
-  for (int r = r0 + wave; r < r1; r += 4) {
+  int at_once = 1;  // rows
+  while (at_once < kSubs && at_once < r1 - r0) at_once *= 2;
+  const int share = sub / at_once, shares = kSubs / at_once;
+  for (int rb = r0; rb < r1; rb += at_once) {
+    const int r = rb + sub % at_once;
     float M = -INFINITY, L = 0.f;
-    for (int c = lane; c < it.count; c += 64) M = fmaxf(M, part_slot<BM, D>(p, first + (int64_t)c * it.stride, kvh)[BM * D + r]);
+    f32x4 o{0.f, 0.f, 0.f, 0.f};
+    if (r < r1) {
+      for (int c = share; c < it.count; c += kAtOnce * shares) {
+        f32x4 oc[kAtOnce];
+        float mc[kAtOnce], lc[kAtOnce];
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    f32x4 sum{0.f, 0.f, 0.f, 0.f};
-    for (int b = 0; b < it.count; b += 64) {
-      const int c = b + lane;
-      float f = 0.f;
-      if (c < it.count) {
-        const float* const slot = part_slot<BM, D>(p, first + (int64_t)c * it.stride, kvh);
-        const float m = slot[BM * D + r], l = slot[BM * D + BM + r];
-        f = m == -INFINITY ? (l == l ? 0.f : 1.f) : exp_of<T>(m - M);
-        L += l * f;
-      }
-      const int here = min(64, it.count - b);
-      for (int k = 0; k < here; k += SUB) {
-        const int at = k + sub;
-        const float fc = __shfl(f, min(at, 63));
-        if (at < here) {
-          const float* const slot = part_slot<BM, D>(p, first + (int64_t)(b + at) * it.stride, kvh);
-          sum += *reinterpret_cast<const f32x4*>(slot + r * D + c0) * fc;
+        for (int k = 0; k < kAtOnce; ++k) {  // (past the last piece: it again, without weight)
+          const float* const slot = slot_of(min(c + k * shares, it.count - 1));
+          oc[k] = *reinterpret_cast<const f32x4*>(slot + r * D + c0);
+          mc[k] = slot[BM * D + r];
+          lc[k] = slot[BM * D + BM + r];
+        }
+        float m_new = M;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) m_new = fmaxf(m_new, mc[k]);
+        const float a = M == -INFINITY ? 0.f : exp_of<T>(M - m_new);
+        M = m_new;
+        L = L == L ? L * a : L;
+        o *= a;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          // (a piece without a maximum has no key that the row sees, or scores that are NaN: then so is its sum)
+          const float f = c + k * shares >= it.count ? 0.f : mc[k] == -INFINITY ? (lc[k] == lc[k] ? 0.f : 1.f) : exp_of<T>(mc[k] - M);
+          if (f != 0.f) {
+            L += lc[k] * f;
+            o += oc[k] * f;
+          }
         }
       }
     }
+    if (shares > 1) {
+      if (r < r1) {
+        part_o[sub][tid % kLanes] = o;
+        part_m[sub] = M;
+        part_l[sub] = L;
+      }
+      __syncthreads();
+      if (share == 0 && r < r1) {
+        float top = M;
+        for (int k = 1; k < shares; ++k) top = fmaxf(top, part_m[sub + k * at_once]);
+        float f = M == -INFINITY ? (L == L ? 0.f : 1.f) : exp_of<T>(M - top);
+        L *= f;
+        o *= f;
+        for (int k = 1; k < shares; ++k) {
+          const float mk = part_m[sub + k * at_once], lk = part_l[sub + k * at_once];
+          f = mk == -INFINITY ? (lk == lk ? 0.f : 1.f) : exp_of<T>(mk - top);
+          L += lk * f;
+          o += part_o[sub + k * at_once][tid % kLanes] * f;
+        }
+      }
+      __syncthreads();
+    }
+    if (share == 0 && r < r1) {
+      const unsigned row = row0 + r, tok = row / (unsigned)G;
+      const float none = L == 0.f ? nothing_seen(p, it, (int)tok) : 0.f;
+      typedef T vec __attribute__((ext_vector_type(4)));
+      vec y;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) L += __shfl_xor(L, o);
-#pragma unroll
-    for (int o = 32; o >= LPR; o >>= 1)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) sum[v] += __shfl_xor(sum[v], o);
-    const unsigned row = row0 + r, tok = row / (unsigned)G;
-    const float none = L == 0.f ? nothing_seen(p, it, (int)tok) : 0.f;
-    typedef T vec __attribute__((ext_vector_type(4)));
-    vec y;
-#pragma unroll
-    for (int v = 0; v < 4; ++v) y[v] = (T)(L == 0.f ? none : sum[v] * (1.0f / L));
-    if (sub == 0) {
+      for (int v = 0; v < 4; ++v) y[v] = (T)(L == 0.f ? none : o[v] * (1.0f / L));
       T* const op = (T*)p.out + ((int64_t)(it.cu + (int)tok) * p.n_q_heads + kvh * G + (int)(row - tok * G)) * D;
       *reinterpret_cast<vec*>(op + c0) = y;
     }
   }
+}
+
+template <typename T, int D, int BM, int KB>
+__global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
+  const int Hkv = p.n_kv_heads;
+  const int kvh = blockIdx.x % Hkv, piece = blockIdx.x / Hkv;
+  TreePiece it;
+  if (!find_piece<BM, KB>(p, p.n_q_heads / Hkv, piece, it) || it.count == 1) return;
+  const int64_t first = piece - (int64_t)it.index * it.stride;
+  join_rows<T, D, BM>(p, it, kvh, [&](int c) { return part_slot<BM, D>(p, first + (int64_t)c * it.stride, kvh); });
+}
+
+// The same for ranges: a workgroup for each of the two places of a range
+template <typename T, int D, int BM, int KB>
+__global__ __launch_bounds__(256) void tree_join_ranges_kernel(const TreeParams p) {
+  const int Hkv = p.n_kv_heads, G = p.n_q_heads / Hkv;
+  const int kvh = blockIdx.x % Hkv, r = blockIdx.x / Hkv >> 1, second = blockIdx.x / Hkv & 1;
+  SessionLane mine;
+  const TreeRanges rg = cut_ranges<BM, KB>(p, G, mine);
+  if (r >= rg.count || rg.total == 0) return;
+  TreePiece it;
+  int64_t start;
+  if (!find_tile<BM, KB>(p, G, mine, second ? rg.begin(r + 1) - 1 : rg.begin(r), it, start)) return;
+  if (second && start <= rg.begin(r)) return;  // (it starts with the range or before: the first place's)
+  const int first = rg.holding(start);
+  it.index = r - first;
+  it.count = rg.holding(start + it.block1 - 1) - first + 1;
+  if (it.count == 1) return;
+  // (the second and later pieces of a tile start with their ranges)
+  const float* const own = part_slot<BM, D>(p, range_place(rg, first, start), kvh);
+  const float* const later = part_slot<BM, D>(p, 2 * (int64_t)first, kvh);
+  const int64_t stride = 2 * (int64_t)Hkv * (BM * (D + 2));
+  join_rows<T, D, BM>(p, it, kvh, [&](int c) { return c == 0 ? own : later + c * stride; });
 }
 
 // ------------------------------------------------------------------------------------------------------------
@@ -1366,6 +1541,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kTreePieces = 1024;   // workgroups that the key axis is cut for, all kv-heads together
 constexpr int kTreeMinKeys = 512;   // keys of a tile that are not cut further
+constexpr int kRanges = 256;          // the same for ranges: workgroups that are on the chip at once
 constexpr int kStreamWaves = 8;
 
 struct TreePlan {
@@ -1396,28 +1572,34 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   const int64_t tiles = (int64_t)total * G / BM + n_sessions;  // at least as many as there are
   const int64_t blocks = ceil_div64(max_prefix, KB) + ceil_div64(max_new, KB);
   const int64_t per_tile = ceil_div64(blocks, pl.c_min);
-  const int64_t target = ceil_div64(kTreePieces, c->n_kv_heads);
-  const int64_t more = per_tile <= 1 ? 0 : (tiles > target ? target : (tiles * (per_tile - 1) < target ? tiles * (per_tile - 1) : target));
-  pl.cut = more > 0;
-  pl.pieces = tiles + more;
-  pl.bytes = pl.cut ? pl.pieces * c->n_kv_heads * BM * (c->head_dim + 2) * 4 : 0;
-  return pl.pieces * c->n_kv_heads <= 0x7FFFFFFFLL;
+  const int64_t target = ceil_div64(pl.wide ? kTreePieces : kRanges, c->n_kv_heads);
+  if (pl.wide) {
+    const int64_t more = per_tile <= 1 ? 0 : tiles >= target ? target : std::min(tiles * (per_tile - 1), target);
+    pl.cut = more > 0;
+    pl.pieces = tiles + more;
+  } else {
+    pl.cut = per_tile > 1;
+    pl.pieces = pl.cut ? std::min(tiles * per_tile, target) : tiles;
+  }
+  pl.bytes = pl.cut ? (pl.wide ? 1 : 2) * pl.pieces * c->n_kv_heads * BM * (c->head_dim + 2) * 4 : 0;
+  return 2 * pl.pieces * c->n_kv_heads <= 0x7FFFFFFFLL;
 }
 
 template <typename T, int D, int RW>
-static void launch_tree(const TreeParams& p, unsigned groups, hipStream_t stream) {
+static void launch_tree(const TreeParams& p, int64_t pieces, hipStream_t stream) {
+  const dim3 grid((unsigned)(pieces * p.n_kv_heads)), join((unsigned)(2 * pieces * p.n_kv_heads));
   if constexpr (sizeof(T) == 2) {
-    hipLaunchKernelGGL((tree_stream_kernel<D, RW, kStreamWaves>), dim3(groups), dim3(64 * kStreamWaves), 0, stream, p);
-    if (p.cut)
-      hipLaunchKernelGGL((tree_join_kernel<T, D, 32 * RW, TileLds<D>::kStreamKeys>), dim3(groups), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((tree_stream_kernel<D, RW, kStreamWaves>), grid, dim3(64 * kStreamWaves), 0, stream, p);
+    if (p.cut) hipLaunchKernelGGL((tree_join_ranges_kernel<T, D, 32 * RW, TileLds<D>::kStreamKeys>), join, dim3(256), 0, stream, p);
   } else {
-    hipLaunchKernelGGL((tree_fp32_kernel<D, RW>), dim3(groups), dim3(512), 0, stream, p);
-    if (p.cut) hipLaunchKernelGGL((tree_join_kernel<T, D, kFp32Rows * RW, kFp32Rows>), dim3(groups), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((tree_fp32_kernel<D, RW>), grid, dim3(512), 0, stream, p);
+    if (p.cut) hipLaunchKernelGGL((tree_join_ranges_kernel<T, D, kFp32Rows * RW, kFp32Rows>), join, dim3(256), 0, stream, p);
   }
 }
 
 template <int D>
-static void launch_wide(const TreeParams& p, unsigned groups, hipStream_t stream) {
+static void launch_wide(const TreeParams& p, int64_t pieces, hipStream_t stream) {
+  const unsigned groups = (unsigned)(pieces * p.n_kv_heads);
   hipLaunchKernelGGL((tree_wide_kernel<D>), dim3(groups), dim3(256), 0, stream, p);
   if (p.cut) hipLaunchKernelGGL((tree_join_kernel<__bf16, D, 128, kWideKeys>), dim3(groups), dim3(256), 0, stream, p);
 }
@@ -1427,19 +1609,17 @@ static int32_t launch_tree(TreeParams& p, const TreePlan& pl, bool wide, hipStre
   if (!wide) {
     hipLaunchKernelGGL((tree_row_kernel<T, D>), dim3((unsigned)p.total * (unsigned)p.n_q_heads), dim3(64), 0, stream, p);
   } else {
-    const unsigned groups = (unsigned)(pl.pieces * p.n_kv_heads);
     if constexpr (sizeof(T) == 2) {
-      if (pl.wide) {
-        launch_wide<D>(p, groups, stream);
-        return hipGetLastError() == hipSuccess ? SYMPH_OK : SYMPH_ELAUNCH;
-      }
+      if (pl.wide) launch_wide<D>(p, pl.pieces, stream);
     }
-    if (pl.rw == 1)
-      launch_tree<T, D, 1>(p, groups, stream);
-    else if (pl.rw == 2)
-      launch_tree<T, D, 2>(p, groups, stream);
-    else
-      launch_tree<T, D, 4>(p, groups, stream);
+    if (!pl.wide) {
+      if (pl.rw == 1)
+        launch_tree<T, D, 1>(p, pl.pieces, stream);
+      else if (pl.rw == 2)
+        launch_tree<T, D, 2>(p, pl.pieces, stream);
+      else
+        launch_tree<T, D, 4>(p, pl.pieces, stream);
+    }
   }
   return hipGetLastError() == hipSuccess ? SYMPH_OK : SYMPH_ELAUNCH;
 }
