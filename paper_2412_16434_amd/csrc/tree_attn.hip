@@ -531,7 +531,14 @@ struct TileLds<64> {  // 1 KiB: eight rows, chunk c of row r at place c ^ twist(
   }
 };
 
-// 16 bytes a lane from memory straight into LDS; POLICY 2: non-temporal, for rows that are read once
+// 16 bytes a lane from memory straight into LDS, from a scalar base and a lane's 32-bit offset; POLICY 2: non-temporal, for rows
+// that are read once.  As a buffer load: beside a flat one under way (a pointer per lane, SYMPH_TREE_GLDS16) the compiler waits for
+// every LDS read with "none may be left", because flat loads may use LDS, and the reads ahead of their use were ahead of nothing.
+template <int POLICY>
+__device__ __forceinline__ void load_lds16(const char* base, unsigned off, char* dst) {
+  const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, 0xFFFFFFFFu, 0x00027000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)dst, 16, off, 0, 0, POLICY);
+}
 #define SYMPH_TREE_GLDS16(src, dst, POLICY)                                                      \
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),         \
                                    (__attribute__((address_space(3))) void*)(dst), 16, 0, POLICY)
@@ -566,7 +573,7 @@ __device__ __forceinline__ float probabilities(const f32x16& x, float cs, float 
 // longer than all arithmetic on it, so a wave is a stream of its own: tiles of 16 KB through two LDS buffers that no other wave
 // touches, no barrier.  The K buffer is filled again as soon as the scores are done, the V buffer as soon as the values are: one
 // of the two is always under way.  Loads return in order, so "all but the last eight" is exactly the older of the two.
-template <int D, int RW, int W>
+template <int D, int RW, int W, bool GROUPED>
 __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams p) {
   typedef __bf16 T;
   typedef TileLds<D> Lds;
@@ -624,8 +631,9 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
     const int row = Lds::stream_row(i, lane);
     lane_off[i] = (unsigned)(row & 15) * row_bytes + (unsigned)Lds::chunk_of(row, lane) * 16u;
   }
-  // A tile that lies whole in the prefix, its 16-key groups in a block of the cache each.  A scalar base and a lane's 32-bit offset,
-  // kept apart for the compiler (see tree_wide_kernel).  No branch: rows of an id outside the cache come from the row of zeros.
+  constexpr int kPolicy = RW == 1 ? 2 : 0;  // (one wave reads them, or RW)
+  // A tile that lies whole in the prefix, its 16-key groups in a block of the cache each.  Rows of an id outside the cache come
+  // from the row of zeros.
   auto issue_whole = [&](const char* pool, char* buf, int tile, int ids) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -634,32 +642,54 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
       const uint64_t at = (uint64_t)id * p.group_bytes +
                           (unsigned)(((tile * KT + 16 * g) & (p.block_size - 1)) + (D == 128 ? rest : 0)) * row_bytes;
       const bool known = id < (unsigned)p.n_blocks;
-      const char* base = known ? pool + at : reinterpret_cast<const char*>(kNoRow);
-      unsigned off = known ? lane_off[D == 128 ? 0 : i & 1] : (unsigned)(lane % (D / 8)) * 16u;
-      asm("" : "+s"(base), "+v"(off));
-      SYMPH_TREE_GLDS16(base + off, buf + i * Lds::kGroup, RW == 1 ? 2 : 0);
+      load_lds16<kPolicy>(known ? pool + at : reinterpret_cast<const char*>(kNoRow),
+                          known ? lane_off[D == 128 ? 0 : i & 1] : (unsigned)(lane % (D / 8)) * 16u, buf + i * Lds::kGroup);
     }
   };
-  // Any other: at the prefix's end, in the tree, small or odd blocks.  Rows that do not exist are zeros.
+  // Any other tile
   auto issue_rows = [&](const char* pool, const char* fresh, char* buf, int tile, int ids) {
     int l = lane;
     asm volatile("" : "+v"(l));  // (its pieces of addresses are worked out here: no registers for them in the loop)
+    if constexpr (GROUPED) {
+      // the prefix's last, or one of the tree: in place of rows that do not exist the last one that does (no row sees them)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row = Lds::stream_row(i, l);
-      const unsigned in_row = (unsigned)Lds::chunk_of(row, l) * 16u;
-      const int id = __shfl(ids, row);
-      const char* src = reinterpret_cast<const char*>(kNoRow) + in_row;
-      if (tile < prefix_tiles) {
-        const int key = tile * KT + row;
-        if (key < P && (unsigned)id < (unsigned)p.n_blocks)
-          src = pool + (int64_t)id * p.block_stride * (int64_t)sizeof(T) +
-                (uint64_t)(unsigned)(key - block_of(key) * p.block_size) * row_bytes + in_row;
-      } else {
-        const int j = (tile - prefix_tiles) * KT + row;
-        if (j < N) src = fresh + (uint64_t)j * row_bytes + in_row;
+      for (int i = 0; i < 8; ++i) {
+        const int row = Lds::stream_row(i, l), g = i * Lds::kGroupRows / 16;
+        const unsigned id = (unsigned)__builtin_amdgcn_readlane(ids, 16 * g);
+        const char* base = reinterpret_cast<const char*>(kNoRow);
+        unsigned off = (unsigned)Lds::chunk_of(row, l) * 16u;
+        if (tile < prefix_tiles) {
+          const int first = tile * KT + 16 * g;
+          if (first < P && id < (unsigned)p.n_blocks) {
+            base = pool + ((uint64_t)id * p.group_bytes + (unsigned)(first & (p.block_size - 1)) * row_bytes);
+            off += (unsigned)min(row & 15, P - 1 - first) * row_bytes;
+          }
+        } else {
+          const int first = (tile - prefix_tiles) * KT;
+          base = fresh + (uint64_t)first * row_bytes;
+          off += (unsigned)min(row, N - 1 - first) * row_bytes;
+        }
+        load_lds16<kPolicy>(base, off, buf + i * Lds::kGroup);
       }
-      SYMPH_TREE_GLDS16(src, buf + i * Lds::kGroup, RW == 1 ? 2 : 0);
+    } else {
+      // small or odd blocks: an address per lane; rows that do not exist are zeros
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = Lds::stream_row(i, l);
+        const unsigned in_row = (unsigned)Lds::chunk_of(row, l) * 16u;
+        const int id = __shfl(ids, row);
+        const char* src = reinterpret_cast<const char*>(kNoRow) + in_row;
+        if (tile < prefix_tiles) {
+          const int key = tile * KT + row;
+          if (key < P && (unsigned)id < (unsigned)p.n_blocks)
+            src = pool + (int64_t)id * p.block_stride * (int64_t)sizeof(T) +
+                  (uint64_t)(unsigned)(key - block_of(key) * p.block_size) * row_bytes + in_row;
+        } else {
+          const int j = (tile - prefix_tiles) * KT + row;
+          if (j < N) src = fresh + (uint64_t)j * row_bytes + in_row;
+        }
+        SYMPH_TREE_GLDS16(src, buf + i * Lds::kGroup, kPolicy);
+      }
     }
   };
 
@@ -757,8 +787,8 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
     if constexpr (kNext == kRows) issue_rows(v_pool, v_fresh, v_buf, tile + KW, ids);
   };
   if (begin < end) {
-    const int whole_end = p.group_bytes != 0 ? min(end, full_tiles) : begin;
-    if (begin < whole_end) {
+    const int whole_end = GROUPED ? min(end, full_tiles) : begin;
+    if (GROUPED && begin < whole_end) {
       issue_whole(k_pool, k_buf, begin, ids);
       issue_whole(v_pool, v_buf, begin, ids);
     } else {
@@ -766,7 +796,9 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
       issue_rows(v_pool, v_fresh, v_buf, begin, ids);
     }
     int tile = begin;
-    for (; tile + KW < whole_end; tile += KW) use_tile(tile, std::integral_constant<int, kWhole>{});
+    if constexpr (GROUPED) {
+      for (; tile + KW < whole_end; tile += KW) use_tile(tile, std::integral_constant<int, kWhole>{});
+    }
     for (; tile + KW < end; tile += KW) use_tile(tile, std::integral_constant<int, kRows>{});
     use_tile(tile, std::integral_constant<int, kNone>{});
   }
@@ -1127,43 +1159,39 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
     lane_off[i] = (unsigned)(row & 15) * row_bytes + (unsigned)Lds::chunk_of(row, lane) * 16u;
   }
   auto issue_tile = [&](const char* pool, const char* fresh, char* buf, int tile, const int (&ids)[Lds::kLoads]) {
-    unsigned id_max = (unsigned)ids[0];
-#pragma unroll
-    for (int i = 1; i < Lds::kLoads; ++i) id_max = max(id_max, (unsigned)ids[i]);
-    if (__builtin_expect(tile < full_tiles && id_max < (unsigned)p.n_blocks, 1)) {
+    if (__builtin_expect(tile < full_tiles, 1)) {
 #pragma unroll
       for (int i = 0; i < Lds::kLoads; ++i) {
-        const int g = Lds::id_of(i, wave);
-        // (scalar base and 32-bit lane offset, kept apart for the compiler: with 64-bit addresses per lane the issue of such a
-        // load waits for the matrix instructions of the SIMD's other wave)
-        const uint64_t at = (uint64_t)(unsigned)ids[i] * p.group_bytes + (unsigned)((tile * KB + 16 * g) & bs_mask) * row_bytes;
-        const char* base = pool + at;
-        unsigned off = lane_off[D == 64 ? i : 0];
-        asm("" : "+s"(base), "+v"(off));
-        SYMPH_TREE_GLDS16(base + off, buf + Lds::at(i, wave), 0);
+        const unsigned id = (unsigned)ids[i];
+        const bool known = id < (unsigned)p.n_blocks;  // (else rows of zeros)
+        const uint64_t at = (uint64_t)id * p.group_bytes +
+                            (unsigned)((tile * KB + 16 * Lds::id_of(i, wave)) & bs_mask) * row_bytes;
+        load_lds16<0>(known ? pool + at : reinterpret_cast<const char*>(kNoRow),
+                      known ? lane_off[D == 64 ? i : 0] : (unsigned)(lane % (D / 8)) * 16u, buf + Lds::at(i, wave));
       }
-      asm volatile("; end of the scalar-base loads");  // keeps the last one from being merged with the other path's
     } else {
-      // a tile at the prefix's end, of the tree, or with an id outside the cache: rows that do not exist come from a row of zeros.
-      // (Its pieces of addresses are worked out here, from a lane number the optimiser cannot see through: no registers for them
-      // in the loop.)
+      // the prefix's last tile, or one of the tree: in place of rows that do not exist the last one that does (no row sees them)
       int l = lane;
-      asm volatile("" : "+v"(l));
+      asm volatile("" : "+v"(l));  // (its pieces of addresses are worked out here: no registers for them in the loop)
 #pragma unroll
       for (int i = 0; i < Lds::kLoads; ++i) {
         const int row = Lds::row_of(i, wave, l);
         const unsigned in_row = (unsigned)Lds::chunk_of(row, l) * 16u;
-        const unsigned id = (unsigned)ids[i];
-        const char* src = reinterpret_cast<const char*>(kNoRow) + in_row;
+        const char* base = reinterpret_cast<const char*>(kNoRow);
+        unsigned off = in_row;
         if (tile < prefix_tiles) {
-          const int64_t key = (int64_t)tile * KB + row;
-          if (key < P && (key >> p.bs_shift) < p.table_stride && id < (unsigned)p.n_blocks)
-            src = pool + (uint64_t)id * p.group_bytes + (uint64_t)((unsigned)key & bs_mask) * row_bytes + in_row;
+          const int first = tile * KB + 16 * Lds::id_of(i, wave);
+          const unsigned id = (unsigned)ids[i];
+          if (first < P && id < (unsigned)p.n_blocks) {
+            base = pool + ((uint64_t)id * p.group_bytes + (unsigned)(first & bs_mask) * row_bytes);
+            off += (unsigned)min(row & 15, P - 1 - first) * row_bytes;
+          }
         } else {
-          const int j = (tile - prefix_tiles) * KB + row;
-          if (j < N) src = fresh + (uint64_t)j * row_bytes + in_row;
+          const int first = (tile - prefix_tiles) * KB;
+          base = fresh + (uint64_t)first * row_bytes;
+          off += (unsigned)min(row, N - 1 - first) * row_bytes;
         }
-        SYMPH_TREE_GLDS16(src, buf + Lds::at(i, wave), 0);
+        load_lds16<0>(base, off, buf + Lds::at(i, wave));
       }
     }
   };
@@ -1589,7 +1617,10 @@ template <typename T, int D, int RW>
 static void launch_tree(const TreeParams& p, int64_t pieces, hipStream_t stream) {
   const dim3 grid((unsigned)(pieces * p.n_kv_heads)), join((unsigned)(2 * pieces * p.n_kv_heads));
   if constexpr (sizeof(T) == 2) {
-    hipLaunchKernelGGL((tree_stream_kernel<D, RW, kStreamWaves>), grid, dim3(64 * kStreamWaves), 0, stream, p);
+    if (p.group_bytes == 0)
+      hipLaunchKernelGGL((tree_stream_kernel<D, RW, kStreamWaves, false>), grid, dim3(64 * kStreamWaves), 0, stream, p);
+    else if constexpr (RW <= 2)  // (more rows: wide tiles)
+      hipLaunchKernelGGL((tree_stream_kernel<D, RW, kStreamWaves, true>), grid, dim3(64 * kStreamWaves), 0, stream, p);
     if (p.cut) hipLaunchKernelGGL((tree_join_ranges_kernel<T, D, 32 * RW, TileLds<D>::kStreamKeys>), join, dim3(256), 0, stream, p);
   } else {
     hipLaunchKernelGGL((tree_fp32_kernel<D, RW>), grid, dim3(512), 0, stream, p);
