@@ -84,6 +84,11 @@ __device__ __forceinline__ void tree_session(const TreeParams& p, int G, int i, 
   blocks = P / KB + (P % KB != 0) + (N + KB - 1) / KB;
 }
 
+// A session's key blocks times tiles, as a lane's share of a 64-lane sum of 32 bits.  (The host refuses calls whose bounds allow a
+// session more than that: 10^9 keys.)
+constexpr int kMostWork = 0x7FFFFFFF / 64;
+__device__ __forceinline__ int share_of_work(int tiles, int blocks) { return (int)min((int64_t)tiles * blocks, (int64_t)kMostWork); }
+
 // Piece `g` of the batch.  A tile of b key blocks is cut into ceil(b / c) near-equal pieces, c being the smallest length for
 // which the batch's pieces fit; the tiles of a session have their pieces of the same keys beside each other.  Every wave works
 // this out by itself, a session per lane: no scheduling launch, no barrier.
@@ -94,25 +99,17 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
   int c = 0x7FFFFFFF;
   tree_session<BM, KB>(p, G, lane, cu, P, N, tiles, blocks);
   if (p.cut) {
-    int64_t work = (int64_t)tiles * blocks;
-    int n_tiles = tiles;
-    for (int i = 64 + lane; i < p.n_sessions; i += 64) {
+    int64_t work = __builtin_amdgcn_readlane(wave_inclusive_scan(share_of_work(tiles, blocks)), 63);
+    int n_tiles = __builtin_amdgcn_readlane(wave_inclusive_scan(tiles), 63);
+    for (int i0 = 64; i0 < p.n_sessions; i0 += 64) {
       int a, b, d, t, k;
-      tree_session<BM, KB>(p, G, i, a, b, d, t, k);
-      work += (int64_t)t * k;
-      n_tiles += t;
+      tree_session<BM, KB>(p, G, i0 + lane, a, b, d, t, k);
+      work += __builtin_amdgcn_readlane(wave_inclusive_scan(share_of_work(t, k)), 63);
+      n_tiles += __builtin_amdgcn_readlane(wave_inclusive_scan(t), 63);
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-      work += __shfl_xor((long long)work, o);
-      n_tiles += __shfl_xor(n_tiles, o);
-    }
-    const int64_t room = p.max_pieces - n_tiles;
-    if (room > 0) {
-      const int64_t even =  // (a 32-bit division where that is enough: a quarter of the instructions)
-          work + room <= 0x7FFFFFFFLL ? ((unsigned)work + (unsigned)room - 1) / (unsigned)room : (work + room - 1) / room;
-      c = (int)min(max(even, (int64_t)p.c_min), (int64_t)0x7FFFFFFF);
-    }
+    const int room = p.max_pieces - n_tiles;
+    if (room > 0 && work <= 0x7FFFFFFF)
+      c = max(__builtin_amdgcn_readfirstlane((int)(((unsigned)work + (unsigned)room - 1) / (unsigned)room)), p.c_min);
   }
   int before = 0;
   for (int i0 = 0; i0 < p.n_sessions; i0 += 64) {
@@ -132,8 +129,9 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
       // (divisions are done on the vector unit: back to scalar registers)
       it.index = __builtin_amdgcn_readfirstlane(local / it.stride);
       it.tile = local - it.index * it.stride;
-      it.block0 = __builtin_amdgcn_readfirstlane((int)((int64_t)b * it.index / it.count));
-      it.block1 = __builtin_amdgcn_readfirstlane((int)((int64_t)b * (it.index + 1) / it.count));
+      const int each = __builtin_amdgcn_readfirstlane(b / it.count), longer = b - each * it.count;
+      it.block0 = each * it.index + min(it.index, longer);
+      it.block1 = it.block0 + each + (it.index < longer);
       return true;
     }
     before += __builtin_amdgcn_readlane(incl, 63);
@@ -159,8 +157,7 @@ struct TreeRanges {
 
 struct SessionLane {  // what a lane knows of its session
   int cu, P, N, tiles, blocks;
-  // (a lane's share of a 64-lane sum of 32 bits; a session of more has more than 10^9 keys times tiles)
-  __device__ __forceinline__ int work() const { return (int)min((int64_t)tiles * blocks, (int64_t)0x7FFFFFFF / 64); }
+  __device__ __forceinline__ int work() const { return share_of_work(tiles, blocks); }
 };
 
 template <int BM, int KB>
@@ -256,6 +253,11 @@ __device__ __forceinline__ float nothing_seen(const TreeParams& p, const TreePie
   return sees ? NAN : 0.f;
 }
 
+// A row worked out by itself has its probabilities, and with them its sums, 2^24 times smaller than its maximum says: products with
+// the largest values a type has then add up without an overflow.
+template <typename T>
+constexpr float kHeadroom = sizeof(T) == 2 ? 24.0f : 16.635532f;  // log2, or the natural logarithm, of 2^24
+
 // ---- one row by one wave, lanes over the keys of blocks block0 .. block1 - 1, fp32 on the vector unit.  Keys that the row does
 // not see are not read.  The result (unnormalised, relative to the maximum m) is left in lds[D .. 2 D - 1]; lds: 2 * D floats of
 // the wave's own.  CH columns at a time, the scores worked out again for each.
@@ -306,7 +308,7 @@ __device__ __forceinline__ void row_by_lanes(const TreeParams& p, const TreePiec
       const float m_new = fmaxf(m, x);
       const float ref = m_new == -INFINITY ? 0.f : m_new;
       const float alpha = exp_of<T>(m - ref);
-      const float w = exp_of<T>(x - ref);
+      const float w = exp_of<T>(x - ref - kHeadroom<T>);
       l = l * alpha + w;
       if (vp) {
 #pragma unroll
@@ -331,7 +333,7 @@ __device__ __forceinline__ void row_by_lanes(const TreeParams& p, const TreePiec
       for (int o = 32; o >= 1; o >>= 1) a += __shfl_xor(a, o);
       if (lane == 0) lds[D + c0 + c] = a;  // (a store by lane c each would keep CH lane masks in scalar registers)
     }
-    m_row = M;
+    m_row = M == -INFINITY ? M : M + kHeadroom<T>;
     l_row = lt;
   }
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -1092,6 +1094,12 @@ __global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
 constexpr int kWideKeys = 64;
 constexpr float kRaiseSum = 1.0995116e12f;  // 2^40
 
+// A wide tile's piece in the workspace: the registers of its 256 threads, then (m, l) of each
+template <int D>
+__device__ __forceinline__ float* wide_slot(const TreeParams& p, int64_t piece, int kvh) {
+  return p.parts + (piece * p.n_kv_heads + kvh) * (int64_t)(128 * D + 512);
+}
+
 template <int D>
 __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   typedef __bf16 T;
@@ -1104,8 +1112,6 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   __shared__ __attribute__((aligned(16))) char K1[Lds::kBytes];
   __shared__ __attribute__((aligned(16))) char V0[Lds::kBytes];
   __shared__ __attribute__((aligned(16))) char V1[Lds::kBytes];
-  __shared__ float row_m[BM], row_l[BM];
-  __shared__ unsigned bad_rows[BM / 32];
 
   const int Hkv = p.n_kv_heads;
   const int G = p.n_q_heads / Hkv;
@@ -1123,7 +1129,6 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   const bool works = wave * 32 < n_rows;  // (a wave without rows only moves its share of the tiles)
   const int prefix_tiles = P / KB + (P % KB != 0), full_tiles = P / KB;
   const int begin = it.block0, end = it.block1;
-  if (tid < BM / 32) bad_rows[tid] = 0;
 
   const unsigned my_row = row0 + min(wave * 32 + n, n_rows - 1);
   const int tok = (int)(my_row / (unsigned)G);
@@ -1420,35 +1425,103 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
       o[g % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, lo[step >> 1][step & 1], o[g % NT], 0, 0, 0);
     }
   }
+  // ---- results, from the registers they are in: a lane has columns 32 dt + 8 i + 4 kg .. + 3 of its row at o[dt][4 i ..].  A row
+  // with a value that is not finite, or with scores beyond what the loop's arithmetic is made for, is worked out again by itself
+  // (see finish_tile), from its q, which `out` may be: it is not written here.
   const float l = sum_across_halves(l_run);
-  if (lane < 32) {
-    row_m[wave * 32 + n] = m_ref;
-    row_l[wave * 32 + n] = l;
-  }
-  __syncthreads();  // the tile buffers are free: a wave's rows go through one of its own, 16-byte piece c of row r at c ^ r
-  constexpr int kPieces = D / 4;
-  auto rows_of = [&](int w) { return reinterpret_cast<float*>(w == 0 ? K0 : w == 1 ? K1 : w == 2 ? V0 : V1); };
+  const bool whole = it.count == 1;
+  float* const slot = whole ? nullptr : wide_slot<D>(p, piece, kvh);
+  unsigned again = 0;
   if (works) {
-    float* const mine = rows_of(wave) + n * D;
+    float not_finite = 0.f;  // 0 times every value: 0, or NaN
 #pragma unroll
     for (int dt = 0; dt < NT; ++dt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4*>(mine + 4 * ((8 * dt + kg + 2 * i) ^ (n & (kPieces - 1)))) =
-            f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+      for (int e = 0; e < 16; ++e) not_finite = fmaf(o[dt][e], 0.f, not_finite);
+    not_finite = sum_across_halves(not_finite);
+    const bool bad = (not_finite != 0.f && l == l && l != 0.f) || (fabsf(m_ref) > kLargestScore && m_ref != -INFINITY);
+    const bool exists = wave * 32 + n < n_rows;
+    again = (unsigned)__ballot(bad && exists);
+    float scale = 1.0f, none = 0.f;
+    if (whole) {
+      scale = l == 0.f ? 0.f : 1.0f / l;
+      if (l == 0.f) none = nothing_seen(p, it, tok);
+    }
+    // (a row without any probability: whatever values the product brought in are not its own)
+    if (whole) {
+      if (exists && !bad) {
+        typedef T vec __attribute__((ext_vector_type(4)));
+        T* const op =
+            (T*)p.out + ((int64_t)(cu + tok) * p.n_q_heads + kvh * G + (int)(my_row - (unsigned)tok * G)) * D + 4 * kg;
+#pragma unroll
+        for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            vec y;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) y[v] = (T)(l == 0.f ? none : o[dt][4 * i + v] * scale);
+            *reinterpret_cast<vec*>(op + 32 * dt + 8 * i) = y;
+          }
+      }
+    } else {
+      // as the registers are, 16 bytes per lane: whole lines, nothing to arrange
+#pragma unroll
+      for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f32x4 x{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+          if (l == 0.f) x = f32x4{0.f, 0.f, 0.f, 0.f};
+          *reinterpret_cast<f32x4*>(slot + ((dt * 4 + i) * 256 + tid) * 4) = x;
+        }
+      *reinterpret_cast<f32x2*>(slot + BM * D + 2 * tid) = f32x2{m_ref, l};
+    }
   }
-  __syncthreads();
-  constexpr int kRowsPerTurn = 256 / kPieces;
-  finish_tile<T, D, BM, KB, 4>(p, it, part_slot<BM, D>(p, piece, kvh), kvh, n_rows, reinterpret_cast<float*>(K0), bad_rows,
-                               [&](int t, int r, int c0, float& M, float& L) {
-    M = row_m[r];
-    L = row_l[r];
-    return *reinterpret_cast<const f32x4*>(rows_of(t * kRowsPerTurn / 32) + (r & 31) * D +
-                                           4 * ((c0 / 4) ^ (r & 31 & (kPieces - 1))));
-  });
+  if (!__syncthreads_or((int)again)) return;  // (also: the tile buffers are free, and written results have a place in line)
+  float* const own = reinterpret_cast<float*>(wave == 0 ? K0 : wave == 1 ? K1 : wave == 2 ? V0 : V1);
+  for (unsigned left = __builtin_amdgcn_readfirstlane(again); left; left &= left - 1) {
+    const int r = __builtin_ctz(left);
+    const unsigned row = row0 + wave * 32 + r, tk = row / (unsigned)G;
+    const int h = kvh * G + (int)(row - tk * G);
+    float m, lr;
+    row_by_lanes<T, D, KB, 64>(p, it, (int)tk, h, own, m, lr);
+    if (whole) {
+      T* const op = (T*)p.out + ((int64_t)(cu + (int)tk) * p.n_q_heads + h) * D;
+      const float none = lr == 0.f ? nothing_seen(p, it, (int)tk) : 0.f;
+      for (int c = lane; c < D; c += 64) op[c] = (T)(lr == 0.f ? none : own[D + c] * (1.0f / lr));
+    } else {
+      for (int c = lane; c < D; c += 64)
+        slot[(c / 8 * 256 + wave * 64 + 32 * (c / 4 & 1) + r) * 4 + (c & 3)] = own[D + c];
+      if (lane < 2) *reinterpret_cast<f32x2*>(slot + BM * D + 2 * (wave * 64 + 32 * lane + r)) = f32x2{m, lr};
+    }
+  }
 }
-// ---- joins the pieces of cut tiles: out = sum_c f_c O_c / sum_c f_c l_c, f_c = e^(m_c - max_c m_c).  Each of a tile's pieces has
-// a workgroup here too, which joins an equal share of the tile's rows.  A join is nothing but trips to memory: D / 4 lanes take a
+
+// ---- joins the pieces of cut tiles: out = sum_c f_c O_c / sum_c f_c l_c, f_c = e^(m_c - max_c m_c).
+
+// AT_ONCE pieces, of which the first `left` count, into a running maximum, sum and row
+template <typename T, int AT_ONCE>
+__device__ __forceinline__ void add_pieces(float& M, float& L, f32x4& o, const f32x4 (&oc)[AT_ONCE], const f32x2 (&ml)[AT_ONCE],
+                                           int left) {
+  float m_new = M;
+#pragma unroll
+  for (int k = 0; k < AT_ONCE; ++k) m_new = fmaxf(m_new, ml[k][0]);
+  const float a = M == -INFINITY ? 0.f : exp_of<T>(M - m_new);
+  M = m_new;
+  L = L == L ? L * a : L;
+  o *= a;
+#pragma unroll
+  for (int k = 0; k < AT_ONCE; ++k) {
+    const float m = ml[k][0], l = ml[k][1];
+    // (a piece without a maximum has no key that the row sees, or scores that are NaN: then so is its sum)
+    const float f = k >= left ? 0.f : m == -INFINITY ? (l == l ? 0.f : 1.f) : exp_of<T>(m - M);
+    if (f != 0.f) {
+      L += l * f;
+      o += oc[k] * f;
+    }
+  }
+}
+
+// Each of a tile's pieces has a workgroup here too, which joins an equal share of the tile's rows.  A join is nothing but trips to memory: D / 4 lanes take a
 // row's columns of eight pieces at a time, and where there are fewer rows than such groups of lanes, several share a row.
 template <typename T, int D, int BM, typename Slot>
 __device__ __forceinline__ void join_rows(const TreeParams& p, const TreePiece& it, int kvh, Slot slot_of) {
@@ -1470,30 +1543,14 @@ __device__ __forceinline__ void join_rows(const TreeParams& p, const TreePiece& 
     if (r < r1) {
       for (int c = share; c < it.count; c += kAtOnce * shares) {
         f32x4 oc[kAtOnce];
-        float mc[kAtOnce], lc[kAtOnce];
+        f32x2 ml[kAtOnce];
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {  // (past the last piece: it again, without weight)
           const float* const slot = slot_of(min(c + k * shares, it.count - 1));
           oc[k] = *reinterpret_cast<const f32x4*>(slot + r * D + c0);
-          mc[k] = slot[BM * D + r];
-          lc[k] = slot[BM * D + BM + r];
+          ml[k] = f32x2{slot[BM * D + r], slot[BM * D + BM + r]};
         }
-        float m_new = M;
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) m_new = fmaxf(m_new, mc[k]);
-        const float a = M == -INFINITY ? 0.f : exp_of<T>(M - m_new);
-        M = m_new;
-        L = L == L ? L * a : L;
-        o *= a;
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
-          // (a piece without a maximum has no key that the row sees, or scores that are NaN: then so is its sum)
-          const float f = c + k * shares >= it.count ? 0.f : mc[k] == -INFINITY ? (lc[k] == lc[k] ? 0.f : 1.f) : exp_of<T>(mc[k] - M);
-          if (f != 0.f) {
-            L += lc[k] * f;
-            o += oc[k] * f;
-          }
-        }
+        add_pieces<T, kAtOnce>(M, L, o, oc, ml, (it.count - c + shares - 1) / shares);
       }
     }
     if (shares > 1) {
@@ -1531,14 +1588,45 @@ __device__ __forceinline__ void join_rows(const TreeParams& p, const TreePiece& 
   }
 }
 
-template <typename T, int D, int BM, int KB>
-__global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
-  const int Hkv = p.n_kv_heads;
+// Wide tiles: a workgroup of the tile's pieces takes its share of the 16-byte vectors of a thread, thread by thread as they were
+// written.
+template <int D>
+__global__ __launch_bounds__(256) void tree_join_wide_kernel(const TreeParams p) {
+  typedef __bf16 T;
+  typedef T vec __attribute__((ext_vector_type(4)));
+  constexpr int BM = 128, kVecs = D / 8, kAtOnce = 8;
+  const int Hkv = p.n_kv_heads, G = p.n_q_heads / Hkv;
   const int kvh = blockIdx.x % Hkv, piece = blockIdx.x / Hkv;
   TreePiece it;
-  if (!find_piece<BM, KB>(p, p.n_q_heads / Hkv, piece, it) || it.count == 1) return;
-  const int64_t first = piece - (int64_t)it.index * it.stride;
-  join_rows<T, D, BM>(p, it, kvh, [&](int c) { return part_slot<BM, D>(p, first + (int64_t)c * it.stride, kvh); });
+  if (!find_piece<BM, kWideKeys>(p, G, piece, it) || it.count == 1 || it.index >= kVecs) return;
+  const int tid = threadIdx.x, r = (tid >> 6) * 32 + (tid & 31);
+  const unsigned row0 = (unsigned)it.tile * BM;
+  const int n_rows = (int)min((unsigned)BM, (unsigned)it.N * (unsigned)G - row0);
+  if (r >= n_rows) return;
+  const float* const first = wide_slot<D>(p, piece - (int64_t)it.index * it.stride, kvh);
+  const int64_t stride = (int64_t)it.stride * Hkv * (128 * D + 512);
+  const unsigned row = row0 + r, tok = row / (unsigned)G;
+  T* const op = (T*)p.out + ((int64_t)(it.cu + (int)tok) * p.n_q_heads + kvh * G + (int)(row - tok * G)) * D + 4 * (tid >> 5 & 1);
+  for (int v = it.index; v < kVecs; v += it.count) {
+    float M = -INFINITY, L = 0.f;
+    f32x4 o{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < it.count; c += kAtOnce) {
+      f32x4 oc[kAtOnce];
+      f32x2 ml[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {  // (past the last piece: it again, without weight)
+        const float* const slot = first + min(c + k, it.count - 1) * stride;
+        oc[k] = *reinterpret_cast<const f32x4*>(slot + (v * 256 + tid) * 4);
+        ml[k] = *reinterpret_cast<const f32x2*>(slot + BM * D + 2 * tid);
+      }
+      add_pieces<T, kAtOnce>(M, L, o, oc, ml, it.count - c);
+    }
+    const float none = L == 0.f ? nothing_seen(p, it, (int)tok) : 0.f;
+    vec y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (T)(L == 0.f ? none : o[e] * (1.0f / L));
+    *reinterpret_cast<vec*>(op + 8 * v) = y;
+  }
 }
 
 // The same for ranges: a workgroup for each of the two places of a range
@@ -1609,7 +1697,9 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
     pl.cut = per_tile > 1;
     pl.pieces = pl.cut ? std::min(tiles * per_tile, target) : tiles;
   }
-  pl.bytes = pl.cut ? (pl.wide ? 1 : 2) * pl.pieces * c->n_kv_heads * BM * (c->head_dim + 2) * 4 : 0;
+  pl.bytes = !pl.cut ? 0 : pl.wide ? pl.pieces * c->n_kv_heads * (128 * c->head_dim + 512) * 4
+                                   : 2 * pl.pieces * c->n_kv_heads * BM * (c->head_dim + 2) * 4;
+  if (tiles * blocks > kMostWork) return false;
   return 2 * pl.pieces * c->n_kv_heads <= 0x7FFFFFFFLL;
 }
 
@@ -1632,7 +1722,7 @@ template <int D>
 static void launch_wide(const TreeParams& p, int64_t pieces, hipStream_t stream) {
   const unsigned groups = (unsigned)(pieces * p.n_kv_heads);
   hipLaunchKernelGGL((tree_wide_kernel<D>), dim3(groups), dim3(256), 0, stream, p);
-  if (p.cut) hipLaunchKernelGGL((tree_join_kernel<__bf16, D, 128, kWideKeys>), dim3(groups), dim3(256), 0, stream, p);
+  if (p.cut) hipLaunchKernelGGL((tree_join_wide_kernel<D>), dim3(groups), dim3(256), 0, stream, p);
 }
 
 template <typename T, int D>
