@@ -37,6 +37,7 @@ struct TreeParams {
   int32_t max_pieces;    // of tiles (per kv-head) or ranges: what the grid and the workspace have room for
   int32_t c_min;         // key blocks of a tile that are not cut further, of a range at least
   int32_t cut;           // 0: one piece per tile
+  int32_t slots;         // workgroups per kv-head that are on the chip at once
   float* parts;
 };
 
@@ -89,8 +90,10 @@ __device__ __forceinline__ void tree_session(const TreeParams& p, int G, int i, 
 constexpr int kMostWork = 0x7FFFFFFF / 64;
 __device__ __forceinline__ int share_of_work(int tiles, int blocks) { return (int)min((int64_t)tiles * blocks, (int64_t)kMostWork); }
 
-// Piece `g` of the batch.  A tile of b key blocks is cut into ceil(b / c) near-equal pieces, c being the smallest length for
-// which the batch's pieces fit; the tiles of a session have their pieces of the same keys beside each other.  Every wave works
+constexpr int kPieceCost = 8;  // start, end and join of a piece of a wide tile, in blocks of 64 keys
+
+// Piece `g` of the batch.  A tile of b key blocks is cut into ceil(b / c) near-equal pieces, of a length c that depends on the whole
+// batch; the tiles of a session have their pieces of the same keys beside each other.  Every wave works
 // this out by itself, a session per lane: no scheduling launch, no barrier.
 template <int BM, int KB>
 __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, TreePiece& it) {
@@ -107,9 +110,30 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
       work += __builtin_amdgcn_readlane(wave_inclusive_scan(share_of_work(t, k)), 63);
       n_tiles += __builtin_amdgcn_readlane(wave_inclusive_scan(t), 63);
     }
-    const int room = p.max_pieces - n_tiles;
-    if (room > 0 && work <= 0x7FFFFFFF)
-      c = max(__builtin_amdgcn_readfirstlane((int)(((unsigned)work + (unsigned)room - 1) / (unsigned)room)), p.c_min);
+    // Workgroups run in rounds of p.slots per kv-head.  For 1 .. 4 rounds: the length that fills them, half a piece per tile being
+    // lost to its last one, and what it takes, rounds times (a piece's blocks and what it costs beside them); the pieces are counted
+    // where a lane has all sessions, else bounded.
+    if (n_tiles < p.max_pieces && work <= 0x7FFFFFFF) {
+      const int least = __builtin_amdgcn_readfirstlane((int)(((unsigned)work + (unsigned)(p.max_pieces - n_tiles) - 1) /
+                                                             (unsigned)(p.max_pieces - n_tiles)));
+      int best = 0x7FFFFFFF;
+#pragma unroll 1
+      for (int rounds = 1; rounds <= 4; ++rounds) {
+        const int room = p.slots * rounds - n_tiles / 2;
+        if (room <= 0) continue;
+        const int len = max(max(__builtin_amdgcn_readfirstlane((int)(((unsigned)work + (unsigned)room - 1) / (unsigned)room)), least),
+                            p.c_min);
+        int pieces = tiles * ((blocks + len - 1) / len);
+        pieces = p.n_sessions <= 64 ? __builtin_amdgcn_readlane(wave_inclusive_scan(pieces), 63) : p.slots * rounds;
+        const int takes = (pieces + p.slots - 1) / p.slots * (len + kPieceCost);
+        if (takes < best) {
+          best = takes;
+          c = len;
+        }
+        if (len <= p.c_min) break;
+      }
+      c = __builtin_amdgcn_readfirstlane(c);
+    }
   }
   int before = 0;
   for (int i0 = 0; i0 < p.n_sessions; i0 += 64) {
@@ -1655,9 +1679,9 @@ __global__ __launch_bounds__(256) void tree_join_ranges_kernel(const TreeParams 
 // ------------------------------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------------------------------
-constexpr int kTreePieces = 1024;   // workgroups that the key axis is cut for, all kv-heads together
-constexpr int kTreeMinKeys = 512;   // keys of a tile that are not cut further
-constexpr int kRanges = 256;          // the same for ranges: workgroups that are on the chip at once
+constexpr int kWideSlots = 512;  // workgroups of wide tiles that are on the chip at once: two per compute unit
+constexpr int kWidePieces = 1024; // and that the key axis is cut for at most, all kv-heads together
+constexpr int kRanges = 256;     // the same for ranges: one workgroup per compute unit
 constexpr int kStreamWaves = 8;
 
 struct TreePlan {
@@ -1684,11 +1708,14 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   pl.wide = c->dtype == SYMPH_BF16 && rows > 64 && grouped_rows(c);
   pl.rw = rows <= R ? 1 : rows <= 2 * R ? 2 : 4;
   const int64_t BM = pl.wide ? 128 : (int64_t)R * pl.rw, KB = pl.wide || (R == 32 && c->head_dim == 64) ? 64 : R;
-  pl.c_min = (int32_t)(kTreeMinKeys / KB);
   const int64_t tiles = (int64_t)total * G / BM + n_sessions;  // at least as many as there are
   const int64_t blocks = ceil_div64(max_prefix, KB) + ceil_div64(max_new, KB);
-  const int64_t per_tile = ceil_div64(blocks, pl.c_min);
-  const int64_t target = ceil_div64(pl.wide ? kTreePieces : kRanges, c->n_kv_heads);
+  // A second launch that joins pieces takes 4 to 5 us, as long as a workgroup does for `uncut` blocks; where it is worth that, pieces
+  // are as short as pays: a wide tile's 64 keys are 1.4 us of its 6, a workgroup of streams is full with a block per wave.
+  const int64_t uncut = pl.wide ? 5 : R == 16 ? (c->head_dim == 64 ? 20 : 12) : c->head_dim == 64 ? 12 : 20;
+  pl.c_min = pl.wide ? 2 : R == 16 ? 4 : 4;
+  const int64_t per_tile = blocks <= uncut ? 1 : ceil_div64(blocks, pl.c_min);
+  const int64_t target = ceil_div64(pl.wide ? kWidePieces : kRanges, c->n_kv_heads);
   if (pl.wide) {
     const int64_t more = per_tile <= 1 ? 0 : tiles >= target ? target : std::min(tiles * (per_tile - 1), target);
     pl.cut = more > 0;
@@ -1813,6 +1840,7 @@ int32_t symph_tree_attn(const symph_kv_cache* cache, int32_t layer, const void* 
   p.max_pieces = (int32_t)pl.pieces;
   p.c_min = pl.c_min;
   p.cut = pl.cut;
+  p.slots = (int32_t)std::max<int64_t>(kWideSlots / cache->n_kv_heads, 1);
   p.parts = (float*)d_workspace;
   const uintptr_t address_bits = (uintptr_t)p.k_layer | (uintptr_t)p.v_layer | (uintptr_t)d_q | (uintptr_t)d_k_new |
                                  (uintptr_t)d_v_new | (uintptr_t)d_out | (uintptr_t)block_bytes;
