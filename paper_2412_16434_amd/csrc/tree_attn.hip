@@ -38,6 +38,7 @@ struct TreeParams {
   int32_t c_min;         // key blocks of a tile that are not cut further, of a range at least
   int32_t cut;           // 0: one piece per tile
   int32_t slots;         // workgroups per kv-head that are on the chip at once
+  int32_t group, group_shift, heads_shift;  // query heads of a kv-head; log2 of it and of n_kv_heads, or -1
   float* parts;
 };
 
@@ -90,6 +91,15 @@ __device__ __forceinline__ void tree_session(const TreeParams& p, int G, int i, 
 constexpr int kMostWork = 0x7FFFFFFF / 64;
 __device__ __forceinline__ int share_of_work(int tiles, int blocks) { return (int)min((int64_t)tiles * blocks, (int64_t)kMostWork); }
 
+// (Divisions are forty instructions, and a call of one session is short: shifts where there is a power of two.)
+__device__ __forceinline__ int token_of(const TreeParams& p, unsigned row) {
+  return (int)(p.group_shift >= 0 ? row >> p.group_shift : row / (unsigned)p.group);
+}
+__device__ __forceinline__ void split_block(const TreeParams& p, unsigned block, int& kvh, int& rest) {
+  rest = (int)(p.heads_shift >= 0 ? block >> p.heads_shift : block / (unsigned)p.n_kv_heads);
+  kvh = (int)block - rest * p.n_kv_heads;
+}
+
 constexpr int kPieceCost = 8;  // start, end and join of a piece of a wide tile, in blocks of 64 keys
 
 // Piece `g` of the batch.  A tile of b key blocks is cut into ceil(b / c) near-equal pieces, of a length c that depends on the whole
@@ -100,10 +110,18 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
   const int lane = threadIdx.x & 63;
   int cu, P, N, tiles, blocks;
   int c = 0x7FFFFFFF;
-  tree_session<BM, KB>(p, G, lane, cu, P, N, tiles, blocks);
+  const bool single = p.n_sessions == 1;  // (then every lane has it: nothing to add up or to search)
+  tree_session<BM, KB>(p, G, single ? 0 : lane, cu, P, N, tiles, blocks);
   if (p.cut) {
-    int64_t work = __builtin_amdgcn_readlane(wave_inclusive_scan(share_of_work(tiles, blocks)), 63);
-    int n_tiles = __builtin_amdgcn_readlane(wave_inclusive_scan(tiles), 63);
+    int64_t work = share_of_work(tiles, blocks);
+    int n_tiles = tiles;
+    if (!single) {
+      work = __builtin_amdgcn_readlane(wave_inclusive_scan((int)work), 63);
+      n_tiles = __builtin_amdgcn_readlane(wave_inclusive_scan(tiles), 63);
+    } else {
+      work = __builtin_amdgcn_readfirstlane((int)work);
+      n_tiles = __builtin_amdgcn_readfirstlane(n_tiles);
+    }
     for (int i0 = 64; i0 < p.n_sessions; i0 += 64) {
       int a, b, d, t, k;
       tree_session<BM, KB>(p, G, i0 + lane, a, b, d, t, k);
@@ -124,7 +142,9 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
         const int len = max(max(__builtin_amdgcn_readfirstlane((int)(((unsigned)work + (unsigned)room - 1) / (unsigned)room)), least),
                             p.c_min);
         int pieces = tiles * ((blocks + len - 1) / len);
-        pieces = p.n_sessions <= 64 ? __builtin_amdgcn_readlane(wave_inclusive_scan(pieces), 63) : p.slots * rounds;
+        pieces = single ? __builtin_amdgcn_readfirstlane(pieces)
+                 : p.n_sessions <= 64 ? __builtin_amdgcn_readlane(wave_inclusive_scan(pieces), 63)
+                                      : p.slots * rounds;
         const int takes = (pieces + p.slots - 1) / p.slots * (len + kPieceCost);
         if (takes < best) {
           best = takes;
@@ -138,8 +158,8 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
   int before = 0;
   for (int i0 = 0; i0 < p.n_sessions; i0 += 64) {
     if (i0 > 0) tree_session<BM, KB>(p, G, i0 + lane, cu, P, N, tiles, blocks);
-    const int count = blocks / c + (blocks % c != 0), mine = tiles * count;
-    const int incl = wave_inclusive_scan(mine);
+    const int count = c == 0x7FFFFFFF ? blocks != 0 : (blocks + c - 1) / c, mine = tiles * count;
+    const int incl = single ? mine : wave_inclusive_scan(mine);
     const uint64_t holds = __ballot(before + incl > g);
     if (holds) {
       const int at = __builtin_ctzll(holds);
@@ -151,9 +171,9 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
       it.stride = __builtin_amdgcn_readlane(tiles, at);
       const int local = g - before - __builtin_amdgcn_readlane(incl - mine, at), b = __builtin_amdgcn_readlane(blocks, at);
       // (divisions are done on the vector unit: back to scalar registers)
-      it.index = __builtin_amdgcn_readfirstlane(local / it.stride);
+      it.index = it.stride == 1 ? local : __builtin_amdgcn_readfirstlane(local / it.stride);
       it.tile = local - it.index * it.stride;
-      const int each = __builtin_amdgcn_readfirstlane(b / it.count), longer = b - each * it.count;
+      const int each = it.count == 1 ? b : __builtin_amdgcn_readfirstlane(b / it.count), longer = b - each * it.count;
       it.block0 = each * it.index + min(it.index, longer);
       it.block1 = it.block0 + each + (it.index < longer);
       return true;
@@ -187,9 +207,10 @@ struct SessionLane {  // what a lane knows of its session
 template <int BM, int KB>
 __device__ __forceinline__ TreeRanges cut_ranges(const TreeParams& p, int G, SessionLane& mine) {
   const int lane = threadIdx.x & 63;
-  tree_session<BM, KB>(p, G, lane, mine.cu, mine.P, mine.N, mine.tiles, mine.blocks);
+  const bool single = p.n_sessions == 1;  // (then every lane has it)
+  tree_session<BM, KB>(p, G, single ? 0 : lane, mine.cu, mine.P, mine.N, mine.tiles, mine.blocks);
   TreeRanges rg;
-  rg.total = __builtin_amdgcn_readlane(wave_inclusive_scan(mine.work()), 63);
+  rg.total = single ? __builtin_amdgcn_readfirstlane(mine.work()) : __builtin_amdgcn_readlane(wave_inclusive_scan(mine.work()), 63);
   for (int i0 = 64; i0 < p.n_sessions; i0 += 64) {
     SessionLane other;
     tree_session<BM, KB>(p, G, i0 + lane, other.cu, other.P, other.N, other.tiles, other.blocks);
@@ -212,7 +233,7 @@ __device__ __forceinline__ bool find_tile(const TreeParams& p, int G, const Sess
   int64_t before = 0;
   for (int i0 = 0; i0 < p.n_sessions; i0 += 64) {
     if (i0 > 0) tree_session<BM, KB>(p, G, i0 + lane, here.cu, here.P, here.N, here.tiles, here.blocks);
-    const int work = here.work(), incl = wave_inclusive_scan(work);
+    const int work = here.work(), incl = p.n_sessions == 1 ? work : wave_inclusive_scan(work);
     const uint64_t holds = __ballot(before + incl > x);
     if (holds) {
       const int at = __builtin_ctzll(holds);
@@ -223,7 +244,7 @@ __device__ __forceinline__ bool find_tile(const TreeParams& p, int G, const Sess
       it.block0 = 0;
       it.block1 = __builtin_amdgcn_readlane(here.blocks, at);
       const int64_t first = before + __builtin_amdgcn_readlane(incl - work, at);
-      it.tile = __builtin_amdgcn_readfirstlane((int)(x - first) / it.block1);
+      it.tile = x - first < it.block1 ? 0 : __builtin_amdgcn_readfirstlane((int)(x - first) / it.block1);
       start = first + (int64_t)it.tile * it.block1;
       return true;
     }
@@ -289,7 +310,7 @@ template <typename T, int D, int KB, int CH>
 __device__ __forceinline__ void row_by_lanes(const TreeParams& p, const TreePiece& it, int tok, int h, float* lds, float& m_row,
                                              float& l_row) {
   const int lane = threadIdx.x & 63;
-  const int g = h / (p.n_q_heads / p.n_kv_heads);
+  const int g = token_of(p, (unsigned)h);  // (the kv-head: the same quotient)
   const int prefix_blocks = it.P / KB + (it.P % KB != 0);
   const T* const q = (const T*)p.q + ((int64_t)(it.cu + tok) * p.n_q_heads + h) * D;
   for (int c = lane; c < D; c += 64) lds[c] = widen(q[c]);
@@ -425,7 +446,7 @@ __device__ __forceinline__ void finish_tile(const TreeParams& p, const TreePiece
   asm volatile("" : "+v"(tid));  // (a number that the optimiser cannot see through: no addresses for what follows held in loops before)
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int G = p.n_q_heads / p.n_kv_heads;
+  const int G = p.group;
   const unsigned row0 = (unsigned)it.tile * BM;
   const bool whole = it.count == 1;
   // A value of the thread's turn: final for a whole tile
@@ -434,7 +455,7 @@ __device__ __forceinline__ void finish_tile(const TreeParams& p, const TreePiece
     if (L == 0.f) sum = f32x4{0.f, 0.f, 0.f, 0.f};  // (no probability: whatever values the product brought in are not the row's)
     if (whole) {
       if (L == 0.f) {
-        const float none = nothing_seen(p, it, (int)((row0 + r) / (unsigned)G));
+        const float none = nothing_seen(p, it, token_of(p, row0 + r));
         sum = f32x4{none, none, none, none};
       } else {
         sum *= 1.0f / L;
@@ -464,7 +485,7 @@ __device__ __forceinline__ void finish_tile(const TreeParams& p, const TreePiece
     float M, L;
     const f32x4 x = value_of(t, r, c0, M, L);
     if (whole) {
-      const unsigned row = row0 + r, tok = row / (unsigned)G;
+      const unsigned row = row0 + r, tok = (unsigned)token_of(p, row);
       T* const op = (T*)p.out + ((int64_t)(it.cu + (int)tok) * p.n_q_heads + kvh * G + (int)(row - tok * G)) * D;
       vec y;
 #pragma unroll
@@ -488,7 +509,7 @@ __device__ __forceinline__ void finish_tile(const TreeParams& p, const TreePiece
     for (unsigned left = __builtin_amdgcn_readfirstlane(bad_rows[word]); left; left &= left - 1) {
       if (turn++ % WAVES != wave) continue;
       const int r = word * 32 + __builtin_ctz(left);
-      const unsigned row = row0 + r, tok = row / (unsigned)G;
+      const unsigned row = row0 + r, tok = (unsigned)token_of(p, row);
       const int h = kvh * G + (int)(row - tok * G);
       float* const own = lds + wave * 2 * D;
       float m, l;
@@ -610,14 +631,15 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
   __shared__ unsigned bad_rows[RW];
 
   const int Hkv = p.n_kv_heads;
-  const int G = p.n_q_heads / Hkv;
-  const int kvh = blockIdx.x % Hkv;
+  const int G = p.group;
+  int kvh, range;
+  split_block(p, blockIdx.x, kvh, range);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kw = wave / RW;
   const int n = lane & 31;  // query row of this lane within its wave's; also its row of the K operand
   const int kg = lane >> 5;
-  for_segments<BM, KT>(p, G, blockIdx.x / Hkv, [&](const TreePiece& it, const int64_t place) {
+  for_segments<BM, KT>(p, G, range, [&](const TreePiece& it, const int64_t place) {
   const int cu = it.cu, P = it.P, N = it.N;
   const unsigned row0 = (unsigned)it.tile * BM;
   const int n_rows = (int)min((unsigned)BM, (unsigned)N * (unsigned)G - row0);
@@ -625,7 +647,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
   if (tid < RW) bad_rows[tid] = 0;
 
   const unsigned my_row = row0 + min(rw * 32 + n, n_rows - 1);
-  const int tok = (int)(my_row / (unsigned)G);
+  const int tok = token_of(p, my_row);
   const uint32_t* const mask_row = p.mask + (int64_t)(cu + tok) * p.mask_words;
   bf16x8 q[NS];
   {
@@ -882,14 +904,15 @@ __global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
   __shared__ unsigned bad_rows[(BM + 31) / 32];
 
   const int Hkv = p.n_kv_heads;
-  const int G = p.n_q_heads / Hkv;
-  const int kvh = blockIdx.x % Hkv;
+  const int G = p.group;
+  int kvh, range;
+  split_block(p, blockIdx.x, kvh, range);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kw = wave / RW;
   const int n = lane & (R - 1);  // query row of this lane within its wave's; also its row of the K operand
   const int kg = lane / R;       // its share of the contraction index: half (bf16) or quarter (fp32) of the wave
-  for_segments<BM, R>(p, G, blockIdx.x / Hkv, [&](const TreePiece& it, const int64_t place) {
+  for_segments<BM, R>(p, G, range, [&](const TreePiece& it, const int64_t place) {
   const int cu = it.cu, P = it.P, N = it.N;
   const unsigned row0 = (unsigned)it.tile * BM;
   const int n_rows = (int)min((unsigned)BM, (unsigned)N * (unsigned)G - row0);
@@ -897,7 +920,7 @@ __global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
   if (tid < (BM + 31) / 32) bad_rows[tid] = 0;
 
   const unsigned my_row = row0 + min(rw * R + n, n_rows - 1);
-  const int tok = (int)(my_row / (unsigned)G);
+  const int tok = token_of(p, my_row);
   const T* const qp = (const T*)p.q + ((int64_t)(cu + tok) * p.n_q_heads + kvh * G + (int)(my_row - (unsigned)tok * G)) * D;
   const uint32_t* const mask_row = p.mask + (int64_t)(cu + tok) * p.mask_words;
 
@@ -1138,9 +1161,9 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   __shared__ __attribute__((aligned(16))) char V1[Lds::kBytes];
 
   const int Hkv = p.n_kv_heads;
-  const int G = p.n_q_heads / Hkv;
-  const int kvh = blockIdx.x % Hkv;
-  const int piece = blockIdx.x / Hkv;
+  const int G = p.group;
+  int kvh, piece;
+  split_block(p, blockIdx.x, kvh, piece);
   TreePiece it;
   if (!find_piece<BM, KB>(p, G, piece, it)) return;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -1155,7 +1178,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   const int begin = it.block0, end = it.block1;
 
   const unsigned my_row = row0 + min(wave * 32 + n, n_rows - 1);
-  const int tok = (int)(my_row / (unsigned)G);
+  const int tok = token_of(p, my_row);
   const uint32_t* const mask_row = p.mask + (int64_t)(cu + tok) * p.mask_words;
   bf16x8 q[NS];
   {
@@ -1504,7 +1527,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   float* const own = reinterpret_cast<float*>(wave == 0 ? K0 : wave == 1 ? K1 : wave == 2 ? V0 : V1);
   for (unsigned left = __builtin_amdgcn_readfirstlane(again); left; left &= left - 1) {
     const int r = __builtin_ctz(left);
-    const unsigned row = row0 + wave * 32 + r, tk = row / (unsigned)G;
+    const unsigned row = row0 + wave * 32 + r, tk = (unsigned)token_of(p, row);
     const int h = kvh * G + (int)(row - tk * G);
     float m, lr;
     row_by_lanes<T, D, KB, 64>(p, it, (int)tk, h, own, m, lr);
@@ -1553,7 +1576,7 @@ __device__ __forceinline__ void join_rows(const TreeParams& p, const TreePiece& 
   __shared__ f32x4 part_o[kSubs][kLanes];
   __shared__ float part_m[kSubs], part_l[kSubs];
   const int tid = threadIdx.x, sub = tid / kLanes, c0 = 4 * (tid % kLanes);
-  const int G = p.n_q_heads / p.n_kv_heads;
+  const int G = p.group;
   const unsigned row0 = (unsigned)it.tile * BM;
   const int n_rows = (int)min((unsigned)BM, (unsigned)it.N * (unsigned)G - row0);
   const int r0 = (int)((int64_t)n_rows * it.index / it.count), r1 = (int)((int64_t)n_rows * (it.index + 1) / it.count);
@@ -1600,7 +1623,7 @@ __device__ __forceinline__ void join_rows(const TreeParams& p, const TreePiece& 
       __syncthreads();
     }
     if (share == 0 && r < r1) {
-      const unsigned row = row0 + r, tok = row / (unsigned)G;
+      const unsigned row = row0 + r, tok = (unsigned)token_of(p, row);
       const float none = L == 0.f ? nothing_seen(p, it, (int)tok) : 0.f;
       typedef T vec __attribute__((ext_vector_type(4)));
       vec y;
@@ -1619,8 +1642,9 @@ __global__ __launch_bounds__(256) void tree_join_wide_kernel(const TreeParams p)
   typedef __bf16 T;
   typedef T vec __attribute__((ext_vector_type(4)));
   constexpr int BM = 128, kVecs = D / 8, kAtOnce = 8;
-  const int Hkv = p.n_kv_heads, G = p.n_q_heads / Hkv;
-  const int kvh = blockIdx.x % Hkv, piece = blockIdx.x / Hkv;
+  const int Hkv = p.n_kv_heads, G = p.group;
+  int kvh, piece;
+  split_block(p, blockIdx.x, kvh, piece);
   TreePiece it;
   if (!find_piece<BM, kWideKeys>(p, G, piece, it) || it.count == 1 || it.index >= kVecs) return;
   const int tid = threadIdx.x, r = (tid >> 6) * 32 + (tid & 31);
@@ -1629,7 +1653,7 @@ __global__ __launch_bounds__(256) void tree_join_wide_kernel(const TreeParams p)
   if (r >= n_rows) return;
   const float* const first = wide_slot<D>(p, piece - (int64_t)it.index * it.stride, kvh);
   const int64_t stride = (int64_t)it.stride * Hkv * (128 * D + 512);
-  const unsigned row = row0 + r, tok = row / (unsigned)G;
+  const unsigned row = row0 + r, tok = (unsigned)token_of(p, row);
   T* const op = (T*)p.out + ((int64_t)(it.cu + (int)tok) * p.n_q_heads + kvh * G + (int)(row - tok * G)) * D + 4 * (tid >> 5 & 1);
   for (int v = it.index; v < kVecs; v += it.count) {
     float M = -INFINITY, L = 0.f;
@@ -1656,8 +1680,10 @@ __global__ __launch_bounds__(256) void tree_join_wide_kernel(const TreeParams p)
 // The same for ranges: a workgroup for each of the two places of a range
 template <typename T, int D, int BM, int KB>
 __global__ __launch_bounds__(256) void tree_join_ranges_kernel(const TreeParams p) {
-  const int Hkv = p.n_kv_heads, G = p.n_q_heads / Hkv;
-  const int kvh = blockIdx.x % Hkv, r = blockIdx.x / Hkv >> 1, second = blockIdx.x / Hkv & 1;
+  const int Hkv = p.n_kv_heads, G = p.group;
+  int kvh, place;
+  split_block(p, blockIdx.x, kvh, place);
+  const int r = place >> 1, second = place & 1;
   SessionLane mine;
   const TreeRanges rg = cut_ranges<BM, KB>(p, G, mine);
   if (r >= rg.count || rg.total == 0) return;
@@ -1840,6 +1866,10 @@ int32_t symph_tree_attn(const symph_kv_cache* cache, int32_t layer, const void* 
   p.max_pieces = (int32_t)pl.pieces;
   p.c_min = pl.c_min;
   p.cut = pl.cut;
+  p.group = n_q_heads / cache->n_kv_heads;
+  const auto log2_or_neg = [](int32_t v) { return (v & (v - 1)) == 0 ? __builtin_ctz((unsigned)v) : -1; };
+  p.group_shift = log2_or_neg(p.group);
+  p.heads_shift = log2_or_neg(cache->n_kv_heads);
   p.slots = (int32_t)std::max<int64_t>(kWideSlots / cache->n_kv_heads, 1);
   p.parts = (float*)d_workspace;
   const uintptr_t address_bits = (uintptr_t)p.k_layer | (uintptr_t)p.v_layer | (uintptr_t)d_q | (uintptr_t)d_k_new |
