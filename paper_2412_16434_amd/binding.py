@@ -442,6 +442,24 @@ def _attn_args(cache: KVCache, layer, q, k_new, v_new, out, cu_new_lens, prefix_
 
 
 _attn_call = None
+_draft_calls = None  # the compiled marshalling's module, or False: the general path makes the drafted step's calls
+
+
+def _load_draft_calls():
+    """The same for the operators of a drafted step (they share the module: what it needs of torch is bound once)."""
+    global _draft_calls
+    compiled = _attn_call or _load_attn_call()
+    if compiled is not _attn_call:  # (no library)
+        return False
+    _draft_calls = False
+    module = getattr(compiled, "__self__", None)
+    if hasattr(module, "bind_draft"):
+        lib = load_library()
+        module.bind_draft(*(C.cast(f, C.c_void_p).value for f in (
+            lib.symph_build_tables, lib.symph_tree_mask, lib.symph_tree_attn, lib.symph_tree_accept, lib.symph_kv_commit)),
+            _torch().int64)
+        _draft_calls = module
+    return _draft_calls
 
 
 def _load_attn_call():
@@ -517,6 +535,13 @@ def build_tables(prefix_lens, new_lens, block_table, free_blocks, block_size: in
     """Block table entries for ``new_lens`` more tokens of every session, taken from ``free_blocks`` in session order, and
     what is asked for of: prefix sums (``cu_new_lens`` int32, ``token_offsets`` int64), the slot of every new token in a
     layer's pool (``slot_map`` int64, -1: none), ``positions`` and the entries of the free list used up so far."""
+    calls = stream is None and (_load_draft_calls() if _draft_calls is None else _draft_calls)
+    if calls:
+        status = calls.tables(prefix_lens, new_lens, block_table, free_blocks, block_size, n_blocks, total_new_tokens,
+                              cu_new_lens, token_offsets, slot_map, positions, blocks_taken, held_blocks, held_after,
+                              free_begin)
+        if status is not None:
+            return _check(status, "symph_build_tables")
     torch = _torch()
     i32, i64 = torch.int32, torch.int64
     n, t = prefix_lens.shape[0], int(total_new_tokens)
@@ -543,6 +568,11 @@ def _mask_words(mask, rows: int, name: str):
 def tree_mask(parents, cu_new_lens, max_new_len: int, mask, prefix_lens=None, positions=None, stream=None) -> None:
     """mask[T][words] (int64, 64 bits a word) <- bit j of row i: node j is node i or an ancestor of it.  ``parents`` holds
     indices within the session (anything outside 0 .. i-1: a root); ``positions`` <- prefix length + number of ancestors."""
+    calls = stream is None and (_load_draft_calls() if _draft_calls is None else _draft_calls)
+    if calls:
+        status = calls.mask(parents, cu_new_lens, max_new_len, mask, prefix_lens, positions)
+        if status is not None:
+            return _check(status, "symph_tree_mask")
     i32 = _torch().int32
     n, t = cu_new_lens.shape[0] - 1, parents.shape[0]
     mp, words = _mask_words(mask, t, "mask")
@@ -566,6 +596,12 @@ def tree_attn(cache: KVCache, layer: int, q, k_new, v_new, out, tree_mask, cu_ne
               max_new_len: int, max_prefix_len: int, scale: float, workspace=None, stream=None) -> None:
     """out[T][H_q][d] <- attention of drafted tokens over [cached prefix ; the drafted tokens whose bit is set in
     ``tree_mask`` (int64 [T][words])] for one layer.  A row that sees nothing is zero."""
+    calls = stream is None and type(cache) is KVCache and (_load_draft_calls() if _draft_calls is None else _draft_calls)
+    if calls:
+        status = calls.tree(cache.k_pool, cache.v_pool, layer, q, k_new, v_new, out, cu_new_lens, prefix_lens, block_table,
+                            max_new_len, max_prefix_len, scale, workspace, tree_mask)
+        if status is not None:
+            return _check(status, "symph_tree_attn")
     st = cache.struct()
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     args = _attn_args(cache, layer, q, k_new, v_new, out, cu_new_lens, prefix_lens, block_table, max_new_len,
@@ -585,6 +621,12 @@ def tree_accept(draft_tokens, parents, target_tokens, cu_new_lens, prefix_lens, 
                 new_prefix_lens=None, stream=None) -> None:
     """The path of every session's tree that agrees with ``target_tokens`` (the model's token behind each node): ``rows`` <-
     rows of the accepted nodes from entry cu[s] on, then -1; ``n_accepted``, ``next_tokens`` and the new lengths per session."""
+    calls = stream is None and (_load_draft_calls() if _draft_calls is None else _draft_calls)
+    if calls:
+        status = calls.accept(draft_tokens, parents, target_tokens, cu_new_lens, prefix_lens, rows, n_accepted, next_tokens,
+                              new_prefix_lens)
+        if status is not None:
+            return _check(status, "symph_tree_accept")
     i32 = _torch().int32
     n, t = cu_new_lens.shape[0] - 1, draft_tokens.shape[0]
     _check(load_library().symph_tree_accept(
@@ -598,6 +640,11 @@ def tree_accept(draft_tokens, parents, target_tokens, cu_new_lens, prefix_lens, 
 def kv_commit(cache: KVCache, k_new, v_new, rows, slot_map, stream=None) -> None:
     """Row ``rows[t]`` of ``k_new`` / ``v_new`` [L][n_rows][H_kv][d] into slot ``slot_map[t]`` of every layer, for every t where
     both are valid (>= 0 and in range)."""
+    calls = stream is None and type(cache) is KVCache and (_load_draft_calls() if _draft_calls is None else _draft_calls)
+    if calls:
+        status = calls.commit(cache.k_pool, cache.v_pool, k_new, v_new, rows, slot_map)
+        if status is not None:
+            return _check(status, "symph_kv_commit")
     st = cache.struct()
     k = cache.k_pool
     if k_new.dim() != 4 or v_new.shape != k_new.shape or (k_new.shape[0], *k_new.shape[2:]) != (k.shape[0], *k.shape[3:]):
