@@ -32,7 +32,7 @@ constexpr int kTabThreads = 256, kTabSess = 4;             // sessions a thread 
 constexpr int kTabChunk = kTabThreads * kTabSess;
 constexpr int kTabStep = kTabThreads * 2;  // tokens of a workgroup whose threads have one pair each
 constexpr int kTabPairs = 4;               // pairs of a thread in calls of many tokens,
-constexpr int64_t kTabMany = 1 << 20;      // that is
+constexpr int64_t kTabMany = 3 << 18;      // that is
 
 // Sums over the lanes up to this one.  The terms are below 2^37, so the low 24 bits and the rest add up in 32 bits each.
 __device__ __forceinline__ int64_t wave_scan64(int64_t v) {
@@ -47,7 +47,8 @@ __device__ __forceinline__ int32_t clamp32(int64_t v) { return (int32_t)min(max(
 // A thread has PAIRS pairs of consecutive tokens, kTabStep apart: a pair is one 16-byte store of slots, and the pairs' searches
 // and loads wait together.  What bounds it: the chain of lengths, sums, search, free list and store, 5 us with nothing beside
 // it (64 sessions, 2200 tokens); 256 arriving sessions of 2.3 million tokens, 28 MB, take 12 us with four pairs a thread, 14
-// with two or eight, 20 with one; below some hundred thousand tokens one pair fills more of the chip.
+// with two or eight, 20 with one.  One pair fills more of the chip: half a million tokens in 6.5 us against 7.4, a million in
+// 10.5 against 8.7, even at three quarters.
 template <int PAIRS>
 __global__ __launch_bounds__(kTabThreads) void build_tables_kernel(const TablesParams p) {
   __shared__ int32_t first_tok[kTabChunk + 1];  // relative to the run's first token (what does not fit is far from it)
