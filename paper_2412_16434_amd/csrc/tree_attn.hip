@@ -33,7 +33,8 @@ struct TreeParams {
   const int32_t* table;
   int32_t table_stride, n_sessions, total;
   float scale;
-  uint32_t group_bytes;  // bytes between blocks where 16 consecutive keys lie in one block and a block fits 32 bits; else 0
+  uint32_t group_bytes;  // bytes between blocks where the rows of a load lie in one block and a block fits 32 bits; else 0
+  uint32_t bs_magic, bs_more;  // key / block_size = key * bs_magic >> 32 >> bs_more for keys below 2^31
   int32_t max_pieces;    // of tiles (per kv-head) or ranges: what the grid and the workspace have room for
   int32_t c_min;         // key blocks of a tile that are not cut further, of a range at least
   int32_t cut;           // 0: one piece per tile
@@ -541,7 +542,6 @@ struct TileLds<128> {  // 1 KiB: four rows, chunk c of row r at place c ^ ((r & 
   static __device__ __forceinline__ int row_of(int load, int wave, int lane) { return 16 * load + 4 * wave + (lane >> 4); }
   static __device__ __forceinline__ int chunk_of(int, int lane) { return (lane & 15) ^ (((lane >> 4) & 3) << 2); }
   static __device__ __forceinline__ int at(int load, int wave) { return (4 * load + wave) * kGroup; }
-  static __device__ __forceinline__ int id_of(int load, int) { return load; }  // which of the tile's four 16-key groups
   static __device__ __forceinline__ int stream_row(int load, int lane) { return 4 * load + (lane >> 4); }
   static __device__ __forceinline__ int place(int r, int c) { return (r >> 2) * kGroup + (r & 3) * 256 + ((c ^ ((r & 3) << 2)) << 4); }
   // Operand of K for 16 columns `st` of the 32-key half `kb`; k_off[i]: place of the lane's chunk in columns 32 i ..
@@ -564,7 +564,6 @@ struct TileLds<64> {  // 1 KiB: eight rows, chunk c of row r at place c ^ twist(
   static __device__ __forceinline__ int row_of(int load, int wave, int lane) { return 32 * load + 8 * wave + (lane >> 3); }
   static __device__ __forceinline__ int chunk_of(int row, int lane) { return (lane & 7) ^ twist(row); }
   static __device__ __forceinline__ int at(int load, int wave) { return (4 * load + wave) * kGroup; }
-  static __device__ __forceinline__ int id_of(int load, int wave) { return 2 * load + (wave >> 1); }
   static __device__ __forceinline__ int stream_row(int load, int lane) { return 8 * load + (lane >> 3); }
   static __device__ __forceinline__ int place(int r, int c) { return (r >> 3) * kGroup + (r & 7) * 128 + ((c ^ twist(r)) << 4); }
   static __device__ __forceinline__ bf16x8 k_frag(const char* buf, const int (&k_off)[4], int st, int kb) {
@@ -589,6 +588,17 @@ __device__ __forceinline__ void load_lds16(const char* base, unsigned off, char*
 #define SYMPH_TREE_GLDS16(src, dst, POLICY)                                                      \
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),         \
                                    (__attribute__((address_space(3))) void*)(dst), 16, 0, POLICY)
+
+// Where the rows of a load are in a pool, given the load's first key, its place in the block table (from table_place) and the id
+// found there; negative: nowhere.  A load has four or eight consecutive keys, which lie in one block of the cache.
+__device__ __forceinline__ unsigned table_place(const TreeParams& p, unsigned key) { return __umulhi(key, p.bs_magic) >> p.bs_more; }
+__device__ __forceinline__ int64_t rows_at(const TreeParams& p, unsigned key, unsigned at, int id, unsigned row_bytes) {
+  const uint64_t off = (uint64_t)(unsigned)id * p.group_bytes + (key - at * (unsigned)p.block_size) * row_bytes;
+  return (unsigned)id < (unsigned)p.n_blocks && at < (unsigned)p.table_stride ? (int64_t)off : -1;
+}
+__device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
+  return (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, lane);
+}
 
 // The keys of 32 that a row sees, a bit each: `left` of them exist; word < 0: keys of the prefix, else that word of the row's mask.
 __device__ __forceinline__ uint32_t seen_keys(const TreeParams& p, const uint32_t* mask_row, int left, int word) {
@@ -656,15 +666,17 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
     for (int st = 0; st < NS; ++st) q[st] = *reinterpret_cast<const bf16x8*>(qp + 16 * st + 8 * kg);
   }
 
-  // ---- memory -> LDS.  Block ids one per lane (lane i: key i of the tile), asked for two tiles ahead.
+  // ---- memory -> LDS.  Block ids one per lane, asked for two tiles ahead: lane i has key i of the tile, or the first key of load
+  // i & 7 where a load's rows lie in one block.
   const int32_t* const table_row = p.table + (int64_t)it.s * p.table_stride;
   auto block_of = [&](int key) { return p.bs_shift >= 0 ? key >> p.bs_shift : key / p.block_size; };
   const int begin = it.block0 + kw;
   const int end = rw * 32 < n_rows ? it.block1 : it.block0;  // (waves without a row have no tiles)
+  auto my_key = [&](int tile) { return tile * KT + (GROUPED ? (lane & 7) * Lds::kGroupRows : lane & (KT - 1)); };
   auto ask_ids = [&](int tile) {
-    const int key = tile * KT + (lane & (KT - 1));
+    const int key = my_key(tile);
     if (tile >= min(prefix_tiles, end) || key >= P) return -1;
-    const int j = block_of(key);
+    const int j = GROUPED ? (int)table_place(p, (unsigned)key) : block_of(key);
     return j < p.table_stride ? table_row[j] : -1;
   };
   const unsigned row_bytes = (unsigned)(Hkv * D * (int)sizeof(T));
@@ -672,45 +684,45 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
   const char* const v_pool = reinterpret_cast<const char*>((const T*)p.v_layer + kvh * D);
   const char* const k_fresh = reinterpret_cast<const char*>((const T*)p.k_new + (int64_t)cu * Hkv * D + kvh * D);
   const char* const v_fresh = reinterpret_cast<const char*>((const T*)p.v_new + (int64_t)cu * Hkv * D + kvh * D);
-  constexpr int kSplit = D == 64 ? 2 : 1;  // loads of a 16-key group's rows differ in the lane's place by this many kinds
+  auto find_rows = [&](int tile, int ids) -> int64_t {
+    if constexpr (!GROUPED) return 0;
+    const unsigned key = (unsigned)my_key(tile);
+    return rows_at(p, key, table_place(p, key), ids, row_bytes);
+  };
+  constexpr int kSplit = D == 64 ? 2 : 1;  // loads differ in the lane's 16 bytes by this many kinds
   unsigned lane_off[kSplit];
 #pragma unroll
   for (int i = 0; i < kSplit; ++i) {
     const int row = Lds::stream_row(i, lane);
-    lane_off[i] = (unsigned)(row & 15) * row_bytes + (unsigned)Lds::chunk_of(row, lane) * 16u;
+    lane_off[i] = (unsigned)(row % Lds::kGroupRows) * row_bytes + (unsigned)Lds::chunk_of(row, lane) * 16u;
   }
   constexpr int kPolicy = RW == 1 ? 2 : 0;  // (one wave reads them, or RW)
-  // A tile that lies whole in the prefix, its 16-key groups in a block of the cache each.  Rows of an id outside the cache come
-  // from the row of zeros.
-  auto issue_whole = [&](const char* pool, char* buf, int tile, int ids) {
+  // A tile that lies whole in the prefix.  Rows of an id outside the cache come from the row of zeros.
+  auto issue_whole = [&](const char* pool, char* buf, int64_t rows) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int g = i * Lds::kGroupRows / 16, rest = i * Lds::kGroupRows % 16;
-      const unsigned id = (unsigned)__builtin_amdgcn_readlane(ids, 16 * g);
-      const uint64_t at = (uint64_t)id * p.group_bytes +
-                          (unsigned)(((tile * KT + 16 * g) & (p.block_size - 1)) + (D == 128 ? rest : 0)) * row_bytes;
-      const bool known = id < (unsigned)p.n_blocks;
-      load_lds16<kPolicy>(known ? pool + at : reinterpret_cast<const char*>(kNoRow),
-                          known ? lane_off[D == 128 ? 0 : i & 1] : (unsigned)(lane % (D / 8)) * 16u, buf + i * Lds::kGroup);
+      const int64_t at = lane_value(rows, i);
+      load_lds16<kPolicy>(at >= 0 ? pool + at : reinterpret_cast<const char*>(kNoRow),
+                          at >= 0 ? lane_off[D == 128 ? 0 : i & 1] : (unsigned)(lane % (D / 8)) * 16u, buf + i * Lds::kGroup);
     }
   };
   // Any other tile
-  auto issue_rows = [&](const char* pool, const char* fresh, char* buf, int tile, int ids) {
+  auto issue_rows = [&](const char* pool, const char* fresh, char* buf, int tile, int ids, int64_t rows) {
     int l = lane;
     asm volatile("" : "+v"(l));  // (its pieces of addresses are worked out here: no registers for them in the loop)
     if constexpr (GROUPED) {
       // the prefix's last, or one of the tree: in place of rows that do not exist the last one that does (no row sees them)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int row = Lds::stream_row(i, l), g = i * Lds::kGroupRows / 16;
-        const unsigned id = (unsigned)__builtin_amdgcn_readlane(ids, 16 * g);
+        const int row = Lds::stream_row(i, l);
         const char* base = reinterpret_cast<const char*>(kNoRow);
         unsigned off = (unsigned)Lds::chunk_of(row, l) * 16u;
         if (tile < prefix_tiles) {
-          const int first = tile * KT + 16 * g;
-          if (first < P && id < (unsigned)p.n_blocks) {
-            base = pool + ((uint64_t)id * p.group_bytes + (unsigned)(first & (p.block_size - 1)) * row_bytes);
-            off += (unsigned)min(row & 15, P - 1 - first) * row_bytes;
+          const int first = tile * KT + i * Lds::kGroupRows;
+          const int64_t at = lane_value(rows, i);
+          if (first < P && at >= 0) {
+            base = pool + at;
+            off += (unsigned)min(row % Lds::kGroupRows, P - 1 - first) * row_bytes;
           }
         } else {
           const int first = (tile - prefix_tiles) * KT;
@@ -766,6 +778,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
   const float cs = score_scale<T>(p.scale);
 
   int ids = ask_ids(begin), ids_next = ask_ids(begin + KW);
+  int64_t rows = find_rows(begin, ids);
   // Three copies of the loop's body, by what comes after the tile: one that lies whole in the prefix, any other, none.  (With the
   // next tile's loads under a condition the compiler takes K for the youngest load under way, and waits for V too.)
   enum { kWhole, kRows, kNone };
@@ -786,10 +799,11 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
     asm volatile("" ::: "memory");
     if constexpr (kNext != kNone) {
       ids = ids_next;
+      rows = find_rows(tile + KW, ids);
       ids_next = ask_ids(tile + 2 * KW);
     }
-    if constexpr (kNext == kWhole) issue_whole(k_pool, k_buf, tile + KW, ids);
-    if constexpr (kNext == kRows) issue_rows(k_pool, k_fresh, k_buf, tile + KW, ids);
+    if constexpr (kNext == kWhole) issue_whole(k_pool, k_buf, rows);
+    if constexpr (kNext == kRows) issue_rows(k_pool, k_fresh, k_buf, tile + KW, ids, rows);
     if (kNext != kWhole && tile >= full_tiles) {
       const int left = tile < prefix_tiles ? P - tile * KT : N - (tile - prefix_tiles) * KT;
 #pragma unroll
@@ -831,17 +845,17 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
       o[g % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, lo[step >> 1][step & 1], o[g % NT], 0, 0, 0);
     }
     asm volatile("" ::: "memory");
-    if constexpr (kNext == kWhole) issue_whole(v_pool, v_buf, tile + KW, ids);
-    if constexpr (kNext == kRows) issue_rows(v_pool, v_fresh, v_buf, tile + KW, ids);
+    if constexpr (kNext == kWhole) issue_whole(v_pool, v_buf, rows);
+    if constexpr (kNext == kRows) issue_rows(v_pool, v_fresh, v_buf, tile + KW, ids, rows);
   };
   if (begin < end) {
     const int whole_end = GROUPED ? min(end, full_tiles) : begin;
     if (GROUPED && begin < whole_end) {
-      issue_whole(k_pool, k_buf, begin, ids);
-      issue_whole(v_pool, v_buf, begin, ids);
+      issue_whole(k_pool, k_buf, rows);
+      issue_whole(v_pool, v_buf, rows);
     } else {
-      issue_rows(k_pool, k_fresh, k_buf, begin, ids);
-      issue_rows(v_pool, v_fresh, v_buf, begin, ids);
+      issue_rows(k_pool, k_fresh, k_buf, begin, ids, rows);
+      issue_rows(v_pool, v_fresh, v_buf, begin, ids, rows);
     }
     int tile = begin;
     if constexpr (GROUPED) {
@@ -1187,8 +1201,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
     for (int st = 0; st < NS; ++st) q[st] = *reinterpret_cast<const bf16x8*>(qp + 16 * st + 8 * kg);
   }
 
-  // ---- memory -> LDS.  Block ids of a tile's four 16-key groups: asked for by lanes an iteration before they are needed, then
-  // moved to scalar registers (asking for the value at once would also wait for the tiles under way).
+  // ---- memory -> LDS.  Block ids of the wave's loads: asked for by lanes an iteration before they are needed, then made addresses
+  // and moved to scalar registers (asking for the value at once would also wait for the tiles under way).
   const bool has_table = p.table != nullptr && p.table_stride > 0;
   const int32_t* const table_row = p.table + (int64_t)it.s * p.table_stride;
   const unsigned row_bytes = (unsigned)(Hkv * D * (int)sizeof(T));
@@ -1196,47 +1210,44 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   const char* const v_pool = reinterpret_cast<const char*>((const T*)p.v_layer + kvh * D);
   const char* const k_fresh = reinterpret_cast<const char*>((const T*)p.k_new + (int64_t)cu * Hkv * D + kvh * D);
   const char* const v_fresh = reinterpret_cast<const char*>((const T*)p.v_new + (int64_t)cu * Hkv * D + kvh * D);
-  const int bs_mask = p.block_size - 1;
-  auto ask_ids = [&](int tile) {  // lane i: group i & 3 of tile + (i >> 2 & 1)
-    const int64_t key = (int64_t)(tile + ((lane >> 2) & 1)) * KB + 16 * (lane & 3);
-    const int64_t at = key >> p.bs_shift;
-    const int id = has_table ? table_row[(int)min(at, (int64_t)p.table_stride - 1)] : -1;
-    return at < p.table_stride ? id : -1;
+  constexpr int kLoads = Lds::kLoads;
+  auto my_key = [&](int tile) {  // of lane i: the first of load i % kLoads, of tile or the one behind it
+    return (unsigned)(tile + lane / kLoads % 2) * KB + (unsigned)Lds::row_of(lane % kLoads, wave, 0);
   };
-  int ids_k[Lds::kLoads], ids_v[Lds::kLoads], asked;  // of the groups that this wave's loads lie in
-  unsigned lane_off[2];  // (load i > 1 of a 128-wide head: the lane's place in the 16-key group is that of load 0)
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int row = Lds::row_of(D == 64 ? i : 0, wave, lane);
-    lane_off[i] = (unsigned)(row & 15) * row_bytes + (unsigned)Lds::chunk_of(row, lane) * 16u;
-  }
-  auto issue_tile = [&](const char* pool, const char* fresh, char* buf, int tile, const int (&ids)[Lds::kLoads]) {
+  auto ask_ids = [&](int tile) {
+    const unsigned at = table_place(p, my_key(tile));
+    return has_table ? table_row[(int)min(at, (unsigned)p.table_stride - 1)] : -1;
+  };
+  auto find_rows = [&](int tile, int ids) {
+    const unsigned key = my_key(tile);
+    return rows_at(p, key, table_place(p, key), ids, row_bytes);
+  };
+  int64_t rows_k[kLoads], rows_v[kLoads];  // of this wave's loads
+  int asked;
+  const unsigned lane_off = (unsigned)(lane / (D / 8)) * row_bytes + (unsigned)Lds::chunk_of(Lds::row_of(0, wave, lane), lane) * 16u;
+  auto issue_tile = [&](const char* pool, const char* fresh, char* buf, int tile, const int64_t (&rows)[kLoads]) {
     if (__builtin_expect(tile < full_tiles, 1)) {
 #pragma unroll
-      for (int i = 0; i < Lds::kLoads; ++i) {
-        const unsigned id = (unsigned)ids[i];
-        const bool known = id < (unsigned)p.n_blocks;  // (else rows of zeros)
-        const uint64_t at = (uint64_t)id * p.group_bytes +
-                            (unsigned)((tile * KB + 16 * Lds::id_of(i, wave)) & bs_mask) * row_bytes;
-        load_lds16<0>(known ? pool + at : reinterpret_cast<const char*>(kNoRow),
-                      known ? lane_off[D == 64 ? i : 0] : (unsigned)(lane % (D / 8)) * 16u, buf + Lds::at(i, wave));
+      for (int i = 0; i < kLoads; ++i) {
+        const bool known = rows[i] >= 0;  // (else rows of zeros)
+        load_lds16<0>(known ? pool + rows[i] : reinterpret_cast<const char*>(kNoRow),
+                      known ? lane_off : (unsigned)(lane % (D / 8)) * 16u, buf + Lds::at(i, wave));
       }
     } else {
       // the prefix's last tile, or one of the tree: in place of rows that do not exist the last one that does (no row sees them)
       int l = lane;
       asm volatile("" : "+v"(l));  // (its pieces of addresses are worked out here: no registers for them in the loop)
 #pragma unroll
-      for (int i = 0; i < Lds::kLoads; ++i) {
-        const int row = Lds::row_of(i, wave, l);
+      for (int i = 0; i < kLoads; ++i) {
+        const int row = Lds::row_of(i, wave, l), first_row = Lds::row_of(i, wave, 0);
         const unsigned in_row = (unsigned)Lds::chunk_of(row, l) * 16u;
         const char* base = reinterpret_cast<const char*>(kNoRow);
         unsigned off = in_row;
         if (tile < prefix_tiles) {
-          const int first = tile * KB + 16 * Lds::id_of(i, wave);
-          const unsigned id = (unsigned)ids[i];
-          if (first < P && id < (unsigned)p.n_blocks) {
-            base = pool + ((uint64_t)id * p.group_bytes + (unsigned)(first & bs_mask) * row_bytes);
-            off += (unsigned)min(row & 15, P - 1 - first) * row_bytes;
+          const int first = tile * KB + first_row;
+          if (first < P && rows[i] >= 0) {
+            base = pool + rows[i];
+            off += (unsigned)min(row - first_row, P - 1 - first) * row_bytes;
           }
         } else {
           const int first = (tile - prefix_tiles) * KB;
@@ -1313,14 +1324,17 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   bf16x8 hi[2][2], lo[2][2];   // P(j)
   float ref = 0.f, sum_first = 0.f;
   asked = ask_ids(begin);
+  {
+    const int64_t found = find_rows(begin, asked);
 #pragma unroll
-  for (int i = 0; i < Lds::kLoads; ++i) {
-    ids_k[i] = __builtin_amdgcn_readlane(asked, Lds::id_of(i, wave));
-    ids_v[i] = __builtin_amdgcn_readlane(asked, 4 + Lds::id_of(i, wave));  // (of the second tile)
+    for (int i = 0; i < kLoads; ++i) {
+      rows_k[i] = lane_value(found, i);
+      rows_v[i] = lane_value(found, kLoads + i);  // (of the second tile)
+    }
   }
-  issue_tile(k_pool, k_fresh, K0, begin, ids_k);
-  issue_tile(v_pool, v_fresh, V0, begin, ids_k);
-  if (begin + 1 < end) issue_tile(k_pool, k_fresh, K1, begin + 1, ids_v);
+  issue_tile(k_pool, k_fresh, K0, begin, rows_k);
+  issue_tile(v_pool, v_fresh, V0, begin, rows_k);
+  if (begin + 1 < end) issue_tile(k_pool, k_fresh, K1, begin + 1, rows_v);
   // The first product needs K0 only: V0 and K1, issued after it, may still be on their way (loads return in order)
   if (begin + 1 < end)
     __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * Lds::kLoads));
@@ -1366,13 +1380,16 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
     char* const v_other = PAR ? V0 : V1;  // held V(j-1), free now: receives V(j+1)
     f32x16(&s_cur)[2] = PAR ? s_odd : s_even;  // S(j)
     f32x16(&s_nxt)[2] = PAR ? s_even : s_odd;  // receives S(j+1)
+    {
+      const int64_t found = find_rows(j + 2, asked);
 #pragma unroll
-    for (int i = 0; i < Lds::kLoads; ++i) ids_k[i] = __builtin_amdgcn_readlane(asked, Lds::id_of(i, wave));  // of tile j+2
+      for (int i = 0; i < kLoads; ++i) rows_k[i] = lane_value(found, i);
+    }
     asked = ask_ids(j + 3);
-    issue_tile(v_pool, v_fresh, v_other, j + 1, ids_v);
-    if (j + 2 < end) issue_tile(k_pool, k_fresh, k_same, j + 2, ids_k);
+    issue_tile(v_pool, v_fresh, v_other, j + 1, rows_v);
+    if (j + 2 < end) issue_tile(k_pool, k_fresh, k_same, j + 2, rows_k);
 #pragma unroll
-    for (int i = 0; i < Lds::kLoads; ++i) ids_v[i] = ids_k[i];
+    for (int i = 0; i < kLoads; ++i) rows_v[i] = rows_k[i];
     if (works) {
       // In explicit slots, between which nothing moves (the compiler's own order reads an operand right before its use and puts
       // the exponentials behind the products): the LDS read of the operand four slots ahead, one matrix instruction of S(j+1),
@@ -1719,10 +1736,11 @@ struct TreePlan {
   int64_t bytes;
 };
 
-// 16 consecutive keys lie in one block of the cache and a block fits 32 bits: rows can be addressed by groups
+// The rows of a load lie in one block of the cache and a block fits 32 bits: rows can be addressed by groups
 static bool grouped_rows(const symph_kv_cache* c) {
-  return c->block_size >= 16 && (c->block_size & (c->block_size - 1)) == 0 &&
-         c->block_stride * (int64_t)elem_bytes_of(c->dtype) <= 0x7FFFFFFFLL;
+  if (c->block_stride * (int64_t)elem_bytes_of(c->dtype) > 0x7FFFFFFFLL) return false;
+  if (c->dtype == SYMPH_BF16) return c->block_size % (c->head_dim == 128 ? TileLds<128>::kGroupRows : TileLds<64>::kGroupRows) == 0;
+  return c->block_size >= kFp32Rows && (c->block_size & (c->block_size - 1)) == 0;
 }
 
 // Everything that follows from host-side values alone; the workspace query and the call agree on it.
@@ -1863,6 +1881,11 @@ int32_t symph_tree_attn(const symph_kv_cache* cache, int32_t layer, const void* 
   p.scale = scale;
   const int64_t block_bytes = cache->block_stride * (int64_t)eb;
   p.group_bytes = grouped_rows(cache) ? (uint32_t)block_bytes : 0;
+  // With 2^l >= block_size > 2^(l - 1): the factor 2^(31 + l) / block_size, rounded up, is off by less than 2^-31 of itself
+  int l = 1;
+  while (((int64_t)1 << l) < p.block_size) ++l;
+  p.bs_magic = (uint32_t)(((uint64_t)1 << (31 + l)) / (uint64_t)p.block_size + 1);
+  p.bs_more = (uint32_t)(l - 1);
   p.max_pieces = (int32_t)pl.pieces;
   p.c_min = pl.c_min;
   p.cut = pl.cut;

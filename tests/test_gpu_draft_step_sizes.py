@@ -7,7 +7,7 @@ import torch
 import draft_ref as R
 import paper_2412_16434_amd as S
 from gpu_util import DEV
-from test_gpu_draft_step import check_mask, check_tables, cumulated, dev, random_parents
+from test_gpu_draft_step import Draft, check_mask, check_tables, cumulated, dev, random_parents
 
 pytestmark = pytest.mark.gpu
 
@@ -99,3 +99,18 @@ def test_commit_of_rows_of_every_width(hkv, d, accepted):
     torch.cuda.synchronize()
     for p, w in zip(pools, want):
         assert torch.equal(p.view_as(w), w)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bs", [2, 4, 8, 12, 20, 24, 40, 56, 1000])
+@pytest.mark.parametrize("prefix,new", [([0, 3, 700], [33, 20, 64]), ([1990], [40]), ([65, 1000], [3, 8])])
+def test_attention_over_blocks_of_every_size(d, bs, prefix, new):
+    Draft(prefix, new, "bf16", d, bs=bs, hkv=2, g=4, seed=31).check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bs", [8, 24])
+def test_block_ids_outside_the_cache_under_wide_tiles(d, bs):
+    draft = Draft([300, 45], [40, 36], "bf16", d, bs=bs, seed=32)
+    draft.table[0, 2], draft.table[0, 7], draft.table[1, 0] = -5, 1 << 30, draft.k_pool.shape[0]
+    draft.check()
