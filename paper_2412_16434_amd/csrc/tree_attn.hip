@@ -21,7 +21,7 @@ struct TreeParams {
   const void* k_layer;
   const void* v_layer;
   int64_t block_stride;  // elements
-  int32_t n_blocks, block_size, bs_shift, n_kv_heads, n_q_heads;  // bs_shift: log2(block_size) or -1
+  int32_t n_blocks, block_size, n_kv_heads, n_q_heads;
   const void* q;
   const void* k_new;
   const void* v_new;
@@ -34,7 +34,7 @@ struct TreeParams {
   int32_t table_stride, n_sessions, total;
   float scale;
   uint32_t group_bytes;  // bytes between blocks where the rows of a load lie in one block and a block fits 32 bits; else 0
-  uint32_t bs_magic, bs_more;  // key / block_size = key * bs_magic >> 32 >> bs_more for keys below 2^31
+  uint32_t bs_magic, bs_more;  // key / block_size = key * bs_magic >> 32 >> bs_more for keys below 2^31, block_size > 1
   int32_t max_pieces;    // of tiles (per kv-head) or ranges: what the grid and the workspace have room for
   int32_t c_min;         // key blocks of a tile that are not cut further, of a range at least
   int32_t cut;           // 0: one piece per tile
@@ -589,9 +589,13 @@ __device__ __forceinline__ void load_lds16(const char* base, unsigned off, char*
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),         \
                                    (__attribute__((address_space(3))) void*)(dst), 16, 0, POLICY)
 
+// Where a key's block is in the table (a division would be forty instructions)
+__device__ __forceinline__ unsigned table_place(const TreeParams& p, unsigned key) { return __umulhi(key, p.bs_magic) >> p.bs_more; }
+__device__ __forceinline__ int block_of_key(const TreeParams& p, int key) {
+  return p.block_size == 1 ? key : (int)table_place(p, (unsigned)key);
+}
 // Where the rows of a load are in a pool, given the load's first key, its place in the block table (from table_place) and the id
 // found there; negative: nowhere.  A load has four or eight consecutive keys, which lie in one block of the cache.
-__device__ __forceinline__ unsigned table_place(const TreeParams& p, unsigned key) { return __umulhi(key, p.bs_magic) >> p.bs_more; }
 __device__ __forceinline__ int64_t rows_at(const TreeParams& p, unsigned key, unsigned at, int id, unsigned row_bytes) {
   const uint64_t off = (uint64_t)(unsigned)id * p.group_bytes + (key - at * (unsigned)p.block_size) * row_bytes;
   return (unsigned)id < (unsigned)p.n_blocks && at < (unsigned)p.table_stride ? (int64_t)off : -1;
@@ -669,7 +673,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
   // ---- memory -> LDS.  Block ids one per lane, asked for two tiles ahead: lane i has key i of the tile, or the first key of load
   // i & 7 where a load's rows lie in one block.
   const int32_t* const table_row = p.table + (int64_t)it.s * p.table_stride;
-  auto block_of = [&](int key) { return p.bs_shift >= 0 ? key >> p.bs_shift : key / p.block_size; };
+  auto block_of = [&](int key) { return block_of_key(p, key); };
   const int begin = it.block0 + kw;
   const int end = rw * 32 < n_rows ? it.block1 : it.block0;  // (waves without a row have no tiles)
   auto my_key = [&](int tile) { return tile * KT + (GROUPED ? (lane & 7) * Lds::kGroupRows : lane & (KT - 1)); };
@@ -938,7 +942,7 @@ __global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
   const T* const qp = (const T*)p.q + ((int64_t)(cu + tok) * p.n_q_heads + kvh * G + (int)(my_row - (unsigned)tok * G)) * D;
   const uint32_t* const mask_row = p.mask + (int64_t)(cu + tok) * p.mask_words;
 
-  auto block_of = [&](int key) { return p.bs_shift >= 0 ? key >> p.bs_shift : key / p.block_size; };
+  auto block_of = [&](int key) { return block_of_key(p, key); };
   const int32_t* const table_row = p.table + (int64_t)it.s * p.table_stride;
   // Block ids one per lane (lane i: key i of the block), passed between lanes
   auto fetch_id = [&](int blk) {
@@ -963,15 +967,7 @@ __global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
     const int at = (blk - prefix_blocks) * R;
     return seen_keys(p, mask_row, N - (at & ~31), at >> 5) >> (at & 31);
   };
-  // Blocks that lie whole in the prefix, their 16-key groups in a block of the cache each: a group's rows start at a scalar
-  // address and a lane adds a constant.
-  const bool grouped = p.group_bytes != 0;
-  auto group_id = [&](int id, int g) { return __builtin_amdgcn_readlane(id, 16 * g); };
-  auto in_cache = [&](int id) { return (unsigned)id < (unsigned)p.n_blocks; };
   const unsigned row_bytes = (unsigned)(Hkv * D * (int)sizeof(T));
-  auto group_off = [&](int key, int id) {
-    return (uint64_t)(unsigned)id * p.group_bytes + (unsigned)(key & (p.block_size - 1)) * row_bytes;
-  };
   auto load_vec = [](const void* at) { return *(const u32x4 __attribute__((address_space(1)))*)(uintptr_t)at; };
   auto load16 = [&](const char* base, unsigned lane_off) {
     if constexpr (D == 128) asm("" : "+s"(base), "+v"(lane_off));
@@ -979,6 +975,8 @@ __global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
   };
   const char* const k_head = (const char*)((const T*)p.k_layer + kvh * D);
   const char* const v_head = (const char*)((const T*)p.v_layer + kvh * D);
+  const char* const k_fresh = (const char*)((const T*)p.k_new + (int64_t)cu * Hkv * D + kvh * D);
+  const char* const v_fresh = (const char*)((const T*)p.v_new + (int64_t)cu * Hkv * D + kvh * D);
 
   const int first = it.block0 + kw;
   const int last = rw * R < n_rows ? it.block1 : it.block0;  // (waves without a row have no blocks)
@@ -1006,17 +1004,54 @@ __global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
   f32x4 kr[NS], vr[4][NH];
   const unsigned k_off = n * row_bytes + 16 * kg, v_off_mem = 4 * kg * row_bytes + 16 * n;
   auto load_block = [&](int blk, int id) {
-    const int id0 = group_id(id, 0);
-    if (grouped && blk < prefix_blocks && (blk + 1) * 16 <= P && in_cache(id0)) {
-      const uint64_t off = group_off(blk * 16, id0);
+    if (p.group_bytes != 0 || blk >= prefix_blocks) {
+      // The rows of eight keys each follow each other: from a scalar address and a lane's constant where the sixteen do, else from
+      // two.  In place of rows that do not exist the last one that does (no row sees them), rows of zeros where there is no block.
+      const char *k_at[2], *v_at[2];
+      unsigned step[2] = {row_bytes, row_bytes};
+      int last;
+      bool whole = true;
+      if (blk >= prefix_blocks) {
+        const int j = (blk - prefix_blocks) * 16;
+        last = N - 1 - j;
+        k_at[0] = k_fresh + (uint64_t)j * row_bytes;
+        v_at[0] = v_fresh + (uint64_t)j * row_bytes;
+        k_at[1] = k_at[0] + 8 * row_bytes;
+        v_at[1] = v_at[0] + 8 * row_bytes;
+      } else {
+        last = P - 1 - blk * 16;
+        int64_t at[2];
 #pragma unroll
-      for (int j = 0; j < NS; ++j) kr[j] = __builtin_bit_cast(f32x4, load16(k_head + off + 64 * j, k_off));
-      const char* const v_rows = v_head + off;
+        for (int i = 0; i < 2; ++i) {
+          const unsigned key = (unsigned)(blk * 16 + 8 * i);
+          at[i] = rows_at(p, key, table_place(p, key), __builtin_amdgcn_readlane(id, 8 * i), row_bytes);
+          k_at[i] = at[i] < 0 ? (const char*)kNoRow : k_head + at[i];
+          v_at[i] = at[i] < 0 ? (const char*)kNoRow : v_head + at[i];
+          if (at[i] < 0) step[i] = 0;
+        }
+        whole = at[0] >= 0 && at[1] == at[0] + 8 * (int64_t)row_bytes;
+      }
+      if (whole && last >= 15) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+        for (int j = 0; j < NS; ++j) kr[j] = __builtin_bit_cast(f32x4, load16(k_at[0] + 64 * j, k_off));
 #pragma unroll
-        for (int h = 0; h < NH; ++h)
-          vr[e][h] = __builtin_bit_cast(f32x4, load16(v_rows + e * row_bytes + 256 * h, v_off_mem));
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int h = 0; h < NH; ++h)
+            vr[e][h] = __builtin_bit_cast(f32x4, load16(v_at[0] + e * row_bytes + 256 * h, v_off_mem));
+        return;
+      }
+      const int kr_row = min(n, last);
+      const char* const k_row = (kr_row & 8 ? k_at[1] : k_at[0]) + (kr_row & 7) * (kr_row & 8 ? step[1] : step[0]) + 16 * kg;
+#pragma unroll
+      for (int j = 0; j < NS; ++j) kr[j] = __builtin_bit_cast(f32x4, load_vec(k_row + 64 * j));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = min(4 * kg + e, last);
+        const char* const v_row = (row & 8 ? v_at[1] : v_at[0]) + (row & 7) * (row & 8 ? step[1] : step[0]) + 16 * n;
+#pragma unroll
+        for (int h = 0; h < NH; ++h) vr[e][h] = __builtin_bit_cast(f32x4, load_vec(v_row + 256 * h));
+      }
       return;
     }
     const T* const k_row = row_of(p.k_layer, p.k_new, blk, n, id) + 4 * kg;
@@ -1729,6 +1764,7 @@ constexpr int kStreamWaves = 8;
 
 struct TreePlan {
   bool wide;           // 128-row tiles through LDS
+  int waves;           // streams: of a workgroup
   int rw;              // else: waves side by side on the rows
   int64_t pieces;      // per kv-head
   int32_t c_min;       // key blocks
@@ -1739,8 +1775,7 @@ struct TreePlan {
 // The rows of a load lie in one block of the cache and a block fits 32 bits: rows can be addressed by groups
 static bool grouped_rows(const symph_kv_cache* c) {
   if (c->block_stride * (int64_t)elem_bytes_of(c->dtype) > 0x7FFFFFFFLL) return false;
-  if (c->dtype == SYMPH_BF16) return c->block_size % (c->head_dim == 128 ? TileLds<128>::kGroupRows : TileLds<64>::kGroupRows) == 0;
-  return c->block_size >= kFp32Rows && (c->block_size & (c->block_size - 1)) == 0;
+  return c->block_size % (c->dtype == SYMPH_BF16 && c->head_dim == 128 ? TileLds<128>::kGroupRows : 8) == 0;
 }
 
 // Everything that follows from host-side values alone; the workspace query and the call agree on it.
@@ -1758,7 +1793,22 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   // are as short as pays: a wide tile's 64 keys are 1.4 us of its 6, a workgroup of streams is full with a block per wave.
   const int64_t uncut = pl.wide ? 5 : R == 16 ? (c->head_dim == 64 ? 20 : 12) : c->head_dim == 64 ? 12 : 20;
   pl.c_min = pl.wide ? 2 : R == 16 ? 4 : 4;
-  const int64_t per_tile = blocks <= uncut ? 1 : ceil_div64(blocks, pl.c_min);
+  // Streams: eight waves fill a compute unit, fewer let it take more workgroups, for sessions that keep few waves busy.  A round of
+  // workgroups takes some 6 us and 2.5 for every block of a wave, and a cut batch of many sessions some 40 us beside its bytes
+  // (parts of several tiles per workgroup, their results, the join).
+  pl.waves = kStreamWaves;
+  bool brief = false;
+  if (!pl.wide && R == 32 && pl.rw <= 2 && grouped_rows(c)) {
+    const int64_t all = (int64_t)n_sessions * c->n_kv_heads;  // (a session is one tile)
+    int64_t best = INT64_MAX;
+    for (int w = kStreamWaves; w >= 2; w /= 2) {
+      const int64_t takes = ceil_div64(all, kRanges * kStreamWaves / w) * (12 + 5 * ceil_div64(blocks, w / pl.rw));
+      if (takes < best) best = takes, pl.waves = w;
+    }
+    brief = all >= kRanges / 2 && best <= 80;
+    if (blocks > uncut && !brief) pl.waves = kStreamWaves;
+  }
+  const int64_t per_tile = blocks <= uncut || brief ? 1 : ceil_div64(blocks, pl.c_min);
   const int64_t target = ceil_div64(pl.wide ? kWidePieces : kRanges, c->n_kv_heads);
   if (pl.wide) {
     const int64_t more = per_tile <= 1 ? 0 : tiles >= target ? target : std::min(tiles * (per_tile - 1), target);
@@ -1775,13 +1825,19 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
 }
 
 template <typename T, int D, int RW>
-static void launch_tree(const TreeParams& p, int64_t pieces, hipStream_t stream) {
+static void launch_tree(const TreeParams& p, int64_t pieces, int waves, hipStream_t stream) {
   const dim3 grid((unsigned)(pieces * p.n_kv_heads)), join((unsigned)(2 * pieces * p.n_kv_heads));
   if constexpr (sizeof(T) == 2) {
     if (p.group_bytes == 0)
       hipLaunchKernelGGL((tree_stream_kernel<D, RW, kStreamWaves, false>), grid, dim3(64 * kStreamWaves), 0, stream, p);
-    else if constexpr (RW <= 2)  // (more rows: wide tiles)
-      hipLaunchKernelGGL((tree_stream_kernel<D, RW, kStreamWaves, true>), grid, dim3(64 * kStreamWaves), 0, stream, p);
+    else if constexpr (RW <= 2) {  // (more rows: wide tiles)
+      if (waves == 2)
+        hipLaunchKernelGGL((tree_stream_kernel<D, RW, 2, true>), grid, dim3(128), 0, stream, p);
+      else if (waves == 4)
+        hipLaunchKernelGGL((tree_stream_kernel<D, RW, 4, true>), grid, dim3(256), 0, stream, p);
+      else
+        hipLaunchKernelGGL((tree_stream_kernel<D, RW, kStreamWaves, true>), grid, dim3(64 * kStreamWaves), 0, stream, p);
+    }
     if (p.cut) hipLaunchKernelGGL((tree_join_ranges_kernel<T, D, 32 * RW, TileLds<D>::kStreamKeys>), join, dim3(256), 0, stream, p);
   } else {
     hipLaunchKernelGGL((tree_fp32_kernel<D, RW>), grid, dim3(512), 0, stream, p);
@@ -1806,11 +1862,11 @@ static int32_t launch_tree(TreeParams& p, const TreePlan& pl, bool wide, hipStre
     }
     if (!pl.wide) {
       if (pl.rw == 1)
-        launch_tree<T, D, 1>(p, pl.pieces, stream);
+        launch_tree<T, D, 1>(p, pl.pieces, pl.waves, stream);
       else if (pl.rw == 2)
-        launch_tree<T, D, 2>(p, pl.pieces, stream);
+        launch_tree<T, D, 2>(p, pl.pieces, pl.waves, stream);
       else
-        launch_tree<T, D, 4>(p, pl.pieces, stream);
+        launch_tree<T, D, 4>(p, pl.pieces, pl.waves, stream);
     }
   }
   return hipGetLastError() == hipSuccess ? SYMPH_OK : SYMPH_ELAUNCH;
@@ -1863,7 +1919,6 @@ int32_t symph_tree_attn(const symph_kv_cache* cache, int32_t layer, const void* 
   p.block_stride = cache->block_stride;
   p.n_blocks = cache->n_blocks;
   p.block_size = cache->block_size;
-  p.bs_shift = (cache->block_size & (cache->block_size - 1)) == 0 ? __builtin_ctz((unsigned)cache->block_size) : -1;
   p.n_kv_heads = cache->n_kv_heads;
   p.n_q_heads = n_q_heads;
   p.q = d_q;

@@ -114,3 +114,29 @@ def test_block_ids_outside_the_cache_under_wide_tiles(d, bs):
     draft = Draft([300, 45], [40, 36], "bf16", d, bs=bs, seed=32)
     draft.table[0, 2], draft.table[0, 7], draft.table[1, 0] = -5, 1 << 30, draft.k_pool.shape[0]
     draft.check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bs", [2, 8, 12, 16, 24, 40])
+@pytest.mark.parametrize("prefix,new", [([0, 3, 700], [33, 20, 64]), ([1990], [40]), ([65, 8, 128, 136], [3, 16, 1, 17])])
+def test_fp32_attention_over_blocks_of_every_size(d, bs, prefix, new):
+    Draft(prefix, new, "fp32", d, bs=bs, hkv=2, g=3, tree="bits", seed=33).check()
+
+
+@pytest.mark.parametrize("bs", [8, 24, 16])
+def test_fp32_block_ids_outside_the_cache(bs):
+    draft = Draft([300, 45], [6, 6], "fp32", 128, bs=bs, seed=34)
+    draft.table[0, 2], draft.table[0, 7], draft.table[1, 0] = -5, 1 << 30, draft.k_pool.shape[0]
+    draft.check()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("fp32", 64)])
+@pytest.mark.parametrize("bs", [16, 8])
+@pytest.mark.parametrize("hkv,g,new_hi", [(4, 1, 5), (2, 4, 16), (1, 7, 9)])
+def test_many_sessions_with_hardly_a_cache(dtype, d, bs, hkv, g, new_hi):
+    rng = np.random.default_rng(bs + hkv)
+    prefix, new = rng.integers(0, 40, 140), rng.integers(0, new_hi + 1, 140)
+    prefix[7], new[7] = 200, new_hi
+    draft = Draft(prefix, new, dtype, d, bs=bs, hkv=hkv, g=g, tree="bits", seed=35)
+    draft.check()
+    draft.check(max_prefix=1)
