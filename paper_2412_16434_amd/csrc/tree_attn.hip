@@ -1208,6 +1208,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   __shared__ __attribute__((aligned(16))) char K1[Lds::kBytes];
   __shared__ __attribute__((aligned(16))) char V0[Lds::kBytes];
   __shared__ __attribute__((aligned(16))) char V1[Lds::kBytes];
+  __shared__ float again_lds[4][2 * D];
 
   const int Hkv = p.n_kv_heads;
   const int G = p.group;
@@ -1575,8 +1576,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
       *reinterpret_cast<f32x2*>(slot + BM * D + 2 * tid) = f32x2{m_ref, l};
     }
   }
-  if (!__syncthreads_or((int)again)) return;  // (also: the tile buffers are free, and written results have a place in line)
-  float* const own = reinterpret_cast<float*>(wave == 0 ? K0 : wave == 1 ? K1 : wave == 2 ? V0 : V1);
+  // (no barrier: other waves' stores are not waited for, their rows and the tile buffers not touched)
+  float* const own = again_lds[wave];
   for (unsigned left = __builtin_amdgcn_readfirstlane(again); left; left &= left - 1) {
     const int r = __builtin_ctz(left);
     const unsigned row = row0 + wave * 32 + r, tk = (unsigned)token_of(p, row);
