@@ -611,6 +611,27 @@ __device__ __forceinline__ uint32_t seen_keys(const TreeParams& p, const uint32_
   return bits;
 }
 
+// Blocks of KEYS of the tree's keys up to the last that a row of the tile sees: with parents before children a tile has no use for
+// what comes after its last token.  (A wave looks at all rows of the tile, eight words of each at a time.)
+template <int KEYS>
+__device__ __forceinline__ int tree_blocks_seen(const TreeParams& p, int cu, int N, unsigned row0, int n_rows) {
+  const int lane = threadIdx.x & 63;
+  const int from = token_of(p, row0), to = token_of(p, row0 + (unsigned)n_rows - 1);
+#pragma unroll 1
+  for (int w1 = min((N + 31) >> 5, p.mask_words); w1 > 0; w1 -= 8) {
+    uint32_t seen[8] = {};
+    for (int t = from + lane; t <= to; t += 64) {
+      const uint32_t* const row = p.mask + (int64_t)(cu + t) * p.mask_words;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) seen[k] |= row[max(w1 - 1 - k, 0)];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (__any(seen[k] != 0)) return (max(w1 - 1 - k, 0) * 32 + 31) / KEYS + 1;
+  }
+  return 0;
+}
+
 // Probabilities of 32 keys, 2^(x * cs - ref), as two bf16 values each, w = hi + lo with 16 bits in all: the leading 8 bits, then
 // those of what is left.  Returns the lane's sum of them.
 __device__ __forceinline__ float probabilities(const f32x16& x, float cs, float ref, bf16x8 (&hi)[2], bf16x8 (&lo)[2]) {
@@ -912,10 +933,10 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
 // ---- fp32: eight waves, RW side by side on rows (16 each), 8 / RW on the keys (blocks of 16); the fp32 matrix instruction
 // throughout.  K and V go from memory into operand registers (V's operand has one value per lane: no transposing).
 constexpr int kFp32Rows = 16;
-template <int D, int RW>
-__global__ __launch_bounds__(512, 2) void tree_fp32_kernel(const TreeParams p) {
+template <int D, int RW, int W>
+__global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p) {
   typedef float T;
-  constexpr int R = kFp32Rows, BM = R * RW, W = 8, KW = W / RW;
+  constexpr int R = kFp32Rows, BM = R * RW, KW = W / RW;
   constexpr int kStride = D + 4;  // floats between rows of the results
   __shared__ __attribute__((aligned(16))) char lds[W * R * kStride * 4];
   __shared__ float wave_m[W][R], wave_l[W][R];
@@ -1225,7 +1246,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   const int n_rows = (int)min((unsigned)BM, (unsigned)N * (unsigned)G - row0);
   const bool works = wave * 32 < n_rows;  // (a wave without rows only moves its share of the tiles)
   const int prefix_tiles = P / KB + (P % KB != 0), full_tiles = P / KB;
-  const int begin = it.block0, end = it.block1;
+  const int begin = it.block0;
+  int end = it.block1;
 
   const unsigned my_row = row0 + min(wave * 32 + n, n_rows - 1);
   const int tok = token_of(p, my_row);
@@ -1360,6 +1382,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   bf16x8 hi[2][2], lo[2][2];   // P(j)
   float ref = 0.f, sum_first = 0.f;
   asked = ask_ids(begin);
+  if (N > KB)  // (at least one tile: its rows are told that they saw nothing)
+    end = min(end, max(prefix_tiles + tree_blocks_seen<KB>(p, cu, N, row0, n_rows), begin + 1));
   {
     const int64_t found = find_rows(begin, asked);
 #pragma unroll
@@ -1794,22 +1818,25 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   // are as short as pays: a wide tile's 64 keys are 1.4 us of its 6, a workgroup of streams is full with a block per wave.
   const int64_t uncut = pl.wide ? 5 : R == 16 ? (c->head_dim == 64 ? 20 : 12) : c->head_dim == 64 ? 12 : 20;
   pl.c_min = pl.wide ? 2 : R == 16 ? 4 : 4;
-  // Streams: eight waves fill a compute unit, fewer let it take more workgroups, for sessions that keep few waves busy.  A round of
-  // workgroups takes some 6 us and 2.5 for every block of a wave, and a cut batch of many sessions some 40 us beside its bytes
+  // Else eight waves fill a compute unit, fewer let it take more workgroups, for tiles that keep few waves busy or are many.  A round
+  // of workgroups takes some 6 us and 2.5 for every block of a wave, and a cut batch of many sessions some 40 us beside its bytes
   // (parts of several tiles per workgroup, their results, the join).
   pl.waves = kStreamWaves;
   bool brief = false;
-  if (!pl.wide && R == 32 && pl.rw <= 2 && grouped_rows(c)) {
-    const int64_t all = (int64_t)n_sessions * c->n_kv_heads;  // (a session is one tile)
+  if (!pl.wide && (R == 16 || grouped_rows(c))) {
+    const int64_t all = (pl.rw <= 2 ? n_sessions : tiles) * c->n_kv_heads;  // (few rows: a session is one tile)
     int64_t best = INT64_MAX;
-    for (int w = kStreamWaves; w >= 2; w /= 2) {
+    for (int w = kStreamWaves; w >= std::max(2, pl.rw); w /= 2) {
       const int64_t takes = ceil_div64(all, kRanges * kStreamWaves / w) * (12 + 5 * ceil_div64(blocks, w / pl.rw));
       if (takes < best) best = takes, pl.waves = w;
     }
     brief = all >= kRanges / 2 && best <= 80;
     if (blocks > uncut && !brief) pl.waves = kStreamWaves;
   }
-  const int64_t per_tile = blocks <= uncut || brief ? 1 : ceil_div64(blocks, pl.c_min);
+  // Wide tiles that fill the chip as they are, and are not long: a tail costs less than pieces do (their search, results and join;
+  // 144 sessions of 38 tokens and up to 400 keys 93 us against 117).
+  const bool many = pl.wide && (int64_t)total * G / BM * c->n_kv_heads >= kWideSlots / 2 && blocks <= 48;
+  const int64_t per_tile = blocks <= uncut || brief || many ? 1 : ceil_div64(blocks, pl.c_min);
   const int64_t target = ceil_div64(pl.wide ? kWidePieces : kRanges, c->n_kv_heads);
   if (pl.wide) {
     const int64_t more = per_tile <= 1 ? 0 : tiles >= target ? target : std::min(tiles * (per_tile - 1), target);
@@ -1841,7 +1868,11 @@ static void launch_tree(const TreeParams& p, int64_t pieces, int waves, hipStrea
     }
     if (p.cut) hipLaunchKernelGGL((tree_join_ranges_kernel<T, D, 32 * RW, TileLds<D>::kStreamKeys>), join, dim3(256), 0, stream, p);
   } else {
-    hipLaunchKernelGGL((tree_fp32_kernel<D, RW>), grid, dim3(512), 0, stream, p);
+    if constexpr (RW <= 2) {
+      if (waves == 2) hipLaunchKernelGGL((tree_fp32_kernel<D, RW, 2>), grid, dim3(128), 0, stream, p);
+    }
+    if (waves == 4) hipLaunchKernelGGL((tree_fp32_kernel<D, RW, 4>), grid, dim3(256), 0, stream, p);
+    if (waves == kStreamWaves) hipLaunchKernelGGL((tree_fp32_kernel<D, RW, kStreamWaves>), grid, dim3(64 * kStreamWaves), 0, stream, p);
     if (p.cut) hipLaunchKernelGGL((tree_join_ranges_kernel<T, D, kFp32Rows * RW, kFp32Rows>), join, dim3(256), 0, stream, p);
   }
 }

@@ -140,3 +140,19 @@ def test_many_sessions_with_hardly_a_cache(dtype, d, bs, hkv, g, new_hi):
     draft = Draft(prefix, new, dtype, d, bs=bs, hkv=hkv, g=g, tree="bits", seed=35)
     draft.check()
     draft.check(max_prefix=1)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("fp32", 64)])
+@pytest.mark.parametrize("tree", ["tree", "bits", "none"])
+def test_wide_trees_whose_tiles_see_only_their_beginning(dtype, d, tree):
+    """Tiles of rows far apart in a large tree; rows that see nothing of it, with and without a cache."""
+    Draft([0, 70], [200, 131], dtype, d, hkv=1, g=4, tree=tree, seed=36).check()
+    Draft([0], [256], dtype, d, hkv=2, g=1, tree=tree, seed=37).check()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("fp32", 64)])
+def test_many_tiles_are_not_cut(dtype, d):
+    rng = np.random.default_rng(38)
+    prefix, new = rng.integers(0, 500, 70), rng.integers(20, 34, 70)
+    prefix[3], new[5] = 0, 0
+    Draft(prefix, new, dtype, d, hkv=4, g=4, tree="bits", seed=38).check()
