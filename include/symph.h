@@ -412,7 +412,9 @@ int32_t symph_tree_mask(const int32_t* d_parents, const int32_t* d_cu_new_lens, 
  * NULL where that is 0); nothing has to be cleared.
  * Arithmetic: fp32 sums and softmax state.  bf16: products on the matrix cores, probabilities as two bf16 values whose sum
  * keeps 16 bits of each, output rounded to nearest even.  fp32 throughout for fp32.
- * Supported: head_dim 64 or 128, n_q_heads a multiple of n_kv_heads, any block size.
+ * Supported: head_dim 64 or 128, n_q_heads a multiple of n_kv_heads, any block size (multiples of 8 are read the quick way; of 4
+ * too in bf16 with 128-wide heads), addresses on 16 bytes likewise.  Calls whose bounds allow a session more than 3 * 10^7 key
+ * blocks times row tiles (10^9 keys under one tile) are refused: SYMPH_EUNSUPPORTED, a negative size below.
  */
 int32_t symph_tree_attn(const symph_kv_cache* cache, int32_t layer, const void* d_q, const void* d_k_new,
                         const void* d_v_new, void* d_out, const uint64_t* d_tree_mask, int32_t mask_words,

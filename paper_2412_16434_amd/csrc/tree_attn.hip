@@ -1,15 +1,21 @@
 // tree_attn: drafted tokens against [paged cached prefix ; the drafted tokens themselves under a bit mask].
+//   x_j = scale q.k_j over the keys j that the row sees, p = softmax(x), out = sum_j p_j v_j; zero for a row that sees nothing.
 //
-// The N drafted tokens of a session and the G query heads of a kv-head are N * G query rows that read the same keys; a tile
-// is up to 32 * RW of them (bf16; 16 * RW in fp32).  One workgroup of eight waves has one tile, one kv-head and one range of
-// keys: RW waves side by side on the rows, 8 / RW on the keys, each with a softmax of its own, joined through LDS at the end.
-// Trees are small and prefixes long, so the key axis is cut (a piece per workgroup) until the chip is full; the pieces of a
-// tile leave (maximum, sum, unnormalised rows) in the workspace and a second launch joins them.
+// The N drafted tokens of a session and the G query heads of a kv-head are N * G query rows that read the same keys.  Three
+// kernels, by how many rows there are and of what type; in each a workgroup has one kv-head and a tile of rows:
+//   wide    bf16, more than 64 rows: tiles of 128 rows, keys through LDS, bound by the matrix cores
+//   stream  bf16, up to 64 rows: every wave reads keys of its own, bound by memory
+//   fp32    tiles of 16 to 64 rows on the fp32 matrix instruction
+// and a wave per row where addresses are not on 16 bytes.  What they share:
 //   * Scores are computed transposed, S^T = K Q^T: a query per lane, so the softmax state is a scalar of the lane, and the
 //     probabilities a lane holds are the operand of O^T += V^T P^T as they are.
-//   * K goes from memory into operand registers; V through LDS (bf16: the transposing read) or registers (fp32).
+//   * Statistics and sums are fp32.  Probabilities go into the bf16 products as two values, 16 bits in all: rounded to the 8 bits of
+//     one they would be as far off as the values of a flat softmax over a few hundred keys cancel.  It costs the wide kernel half
+//     again as many products (14 % of its time).
 //   * Every key block has one 32-bit word per query row that says which of its keys the row sees: all ones inside the prefix,
 //     the low bits in its last block, the caller's mask in the blocks of the tree, which start at the tree's first token.
+//   * Trees are small and prefixes long: where the tiles do not fill the chip the key axis is cut, the parts leave (maximum, sum,
+//     unnormalised rows) in the workspace and a second launch joins them.  Every workgroup works out its part from the lengths.
 #include "attn_lanes.h"
 
 #include <algorithm>
@@ -186,7 +192,7 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
 
 // ---- the other way to cut: all tiles' key blocks laid end to end, in session order, and cut into equal ranges, one per workgroup,
 // whatever tiles they run through.  Nothing is left over at the end of a launch (pieces of tiles, a third more of them than the
-// chip takes at once, made 64 short drafts take 246 us instead of @@); what it costs is that tiles of one session are read at
+// chip takes at once, made 64 short drafts take 246 us instead of 211); what it costs is that tiles of one session are read at
 // different times, so it is for batches whose sessions have one tile.
 struct TreeRanges {
   int64_t total, per;  // blocks; of a range
@@ -655,6 +661,9 @@ __device__ __forceinline__ float probabilities(const f32x16& x, float cs, float 
 // longer than all arithmetic on it, so a wave is a stream of its own: tiles of 16 KB through two LDS buffers that no other wave
 // touches, no barrier.  The K buffer is filled again as soon as the scores are done, the V buffer as soon as the values are: one
 // of the two is always under way.  Loads return in order, so "all but the last eight" is exactly the older of the two.
+// Bound by memory: 64 sessions with drafts of 2 to 8 tokens and 512 to 8192 cached ones (G 4, 1.13 GB) take 209 us, 5.4 TB/s of the
+// 6.5 that a copy reaches; the rest is what a workgroup does around its keys, some 15 us, and 25 more where sessions are ragged.
+// Four waves in twice as many workgroups take as long, two or one are slower, and so is a barrier per tile.
 template <int D, int RW, int W, bool GROUPED>
 __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams p) {
   typedef __bf16 T;
@@ -930,8 +939,13 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
   });
 }
 
-// ---- fp32: eight waves, RW side by side on rows (16 each), 8 / RW on the keys (blocks of 16); the fp32 matrix instruction
+// ---- fp32: W waves, RW side by side on rows (16 each), W / RW on the keys (blocks of 16); the fp32 matrix instruction
 // throughout.  K and V go from memory into operand registers (V's operand has one value per lane: no transposing).
+// Few rows: bound by memory (41 sessions of 16064 to 31443 keys and up to 3 tokens, 1 GB: 190 us, 5.2 TB/s) or, small, by its trips
+// to it: 8 tokens behind 256 take 10.7 us, 5.5 of them three blocks of a wave, 2 in front of the first.  Many rows: by the first
+// cache, which every wave reads K and V from for itself (16 KB per 64 products of 128-wide heads): a third to a half of the matrix
+// cores' rate.  Two blocks on their way instead of one were slower for small calls (12.2 against 10.7 us), and so were lines of the
+// second and third asked for with the first (11.1): a longer program.
 constexpr int kFp32Rows = 16;
 template <int D, int RW, int W>
 __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p) {
@@ -1208,6 +1222,11 @@ __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p
 // cores and the vector unit independent work.  The softmax reference is the maximum of the first tile a row sees and is raised only
 // where a row sum says that it has to be (a probability of 2^40): numerator and denominator carry the same factor, so nothing is
 // lost by a reference that is too low.
+// Bound by the matrix cores: a tile of 64 keys takes a workgroup 3500 clocks alone and 3900 beside the other one of its compute unit,
+// 79 % of them products, at a clock that falls to 1.4 to 1.8 GHz under them.  32 sessions with trees of 24 to 64 tokens over 2048
+// to 16384 keys (G 4: 1.31 GB, 243 GF): 485 us, 500 TF, or 750 with the products of the probabilities' second halves; 64 tokens over
+// 32768 keys (G 8) 113 us.  A small call is made of trips to memory: 26 tokens over 3001 keys 20 us, 2.2 to find the piece, 2.5 for
+// ids and first tiles, 1.6 a tile, 1.9 at the end, 6 for the join.
 constexpr int kWideKeys = 64;
 constexpr float kRaiseSum = 1.0995116e12f;  // 2^40
 
@@ -1817,7 +1836,7 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   // A second launch that joins pieces takes 4 to 5 us, as long as a workgroup does for `uncut` blocks; where it is worth that, pieces
   // are as short as pays: a wide tile's 64 keys are 1.4 us of its 6, a workgroup of streams is full with a block per wave.
   const int64_t uncut = pl.wide ? 5 : R == 16 ? (c->head_dim == 64 ? 20 : 12) : c->head_dim == 64 ? 12 : 20;
-  pl.c_min = pl.wide ? 2 : R == 16 ? 4 : 4;
+  pl.c_min = pl.wide ? 2 : 4;
   // Else eight waves fill a compute unit, fewer let it take more workgroups, for tiles that keep few waves busy or are many.  A round
   // of workgroups takes some 6 us and 2.5 for every block of a wave, and a cut batch of many sessions some 40 us beside its bytes
   // (parts of several tiles per workgroup, their results, the join).
@@ -1848,7 +1867,7 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   }
   pl.bytes = !pl.cut ? 0 : pl.wide ? pl.pieces * c->n_kv_heads * (128 * c->head_dim + 512) * 4
                                    : 2 * pl.pieces * c->n_kv_heads * BM * (c->head_dim + 2) * 4;
-  if (tiles * blocks > kMostWork) return false;
+  if (ceil_div64(rows, BM) * blocks > kMostWork) return false;
   return 2 * pl.pieces * c->n_kv_heads <= 0x7FFFFFFFLL;
 }
 
