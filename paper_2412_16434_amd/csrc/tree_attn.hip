@@ -610,11 +610,14 @@ __device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
   return (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, lane);
 }
 
-// The keys of 32 that a row sees, a bit each: `left` of them exist; word < 0: keys of the prefix, else that word of the row's mask.
-__device__ __forceinline__ uint32_t seen_keys(const TreeParams& p, const uint32_t* mask_row, int left, int word) {
-  uint32_t bits = left >= 32 ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
-  if (word >= 0) bits &= word < p.mask_words ? mask_row[word] : 0u;
-  return bits;
+// The keys of 32 that a row sees, a bit each: `left` of them exist, `word`: the row's mask (all ones in the prefix).  The words of a
+// block are asked for before the loads of the block: asked for when they are needed they would be the youngest load under way, and
+// waiting for them waiting for all.
+__device__ __forceinline__ uint32_t seen_keys(int left, uint32_t word) {
+  return word & (left >= 32 ? ~0u : left > 0 ? (1u << left) - 1u : 0u);
+}
+__device__ __forceinline__ uint32_t mask_word(const TreeParams& p, const uint32_t* mask_row, int word) {
+  return word < 0 ? ~0u : word < p.mask_words ? mask_row[word] : 0u;
 }
 
 // Blocks of KEYS of the tree's keys up to the last that a row of the tile sees: with parents before children a tile has no use for
@@ -812,6 +815,12 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
   const float cs = score_scale<T>(p.scale);
 
   int ids = ask_ids(begin), ids_next = ask_ids(begin + KW);
+  uint32_t words[NB] = {};  // of the mask, for the tile at hand
+  auto ask_words = [&](int tile) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) words[b] = mask_word(p, mask_row, tile < prefix_tiles ? -1 : (tile - prefix_tiles) * NB + b);
+  };
+  if (begin < end) ask_words(begin);
   int64_t rows = find_rows(begin, ids);
   // Three copies of the loop's body, by what comes after the tile: one that lies whole in the prefix, any other, none.  (With the
   // next tile's loads under a condition the compiler takes K for the youngest load under way, and waits for V too.)
@@ -831,20 +840,24 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
       for (int b = 0; b < NB; ++b)
         x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Lds::k_frag(k_buf, k_off, st, b), q[st], x[b], 0, 0, 0);
     asm volatile("" ::: "memory");
+    uint32_t seen[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) seen[b] = words[b];
     if constexpr (kNext != kNone) {
       ids = ids_next;
       rows = find_rows(tile + KW, ids);
       ids_next = ask_ids(tile + 2 * KW);
     }
+    if constexpr (kNext == kRows) ask_words(tile + KW);
     if constexpr (kNext == kWhole) issue_whole(k_pool, k_buf, rows);
     if constexpr (kNext == kRows) issue_rows(k_pool, k_fresh, k_buf, tile + KW, ids, rows);
     if (kNext != kWhole && tile >= full_tiles) {
       const int left = tile < prefix_tiles ? P - tile * KT : N - (tile - prefix_tiles) * KT;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const uint32_t seen = seen_keys(p, mask_row, left - 32 * b, tile < prefix_tiles ? -1 : (tile - prefix_tiles) * NB + b) >> (8 * kg);
+        const uint32_t bits = seen_keys(left - 32 * b, seen[b]) >> (8 * kg);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[b][e] = score_if(seen, 16 * (e >> 3) + (e & 7), x[b][e]);
+        for (int e = 0; e < 16; ++e) x[b][e] = score_if(bits, 16 * (e >> 3) + (e & 7), x[b][e]);
       }
     }
     float mx = x[0][0];
@@ -996,11 +1009,12 @@ __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p
     const int j = (blk - prefix_blocks) * R + r;
     return j < N ? (const T*)fresh + ((int64_t)(cu + j) * Hkv + kvh) * D : (const T*)kNoRow;
   };
-  // The keys of a block that the lane's row sees, a bit each
-  auto seen_of = [&](int blk) -> uint32_t {
-    if (blk < prefix_blocks) return seen_keys(p, mask_row, P - blk * R, -1);
+  // The word of the mask for a block, and the keys of the block that the lane's row sees, a bit each
+  auto ask_word = [&](int blk) { return mask_word(p, mask_row, blk < prefix_blocks ? -1 : ((blk - prefix_blocks) * R) >> 5); };
+  auto seen_of = [&](int blk, uint32_t word) -> uint32_t {
+    if (blk < prefix_blocks) return seen_keys(P - blk * R, word);
     const int at = (blk - prefix_blocks) * R;
-    return seen_keys(p, mask_row, N - (at & ~31), at >> 5) >> (at & 31);
+    return seen_keys(N - (at & ~31), word) >> (at & 31);
   };
   const unsigned row_bytes = (unsigned)(Hkv * D * (int)sizeof(T));
   auto load_vec = [](const void* at) { return *(const u32x4 __attribute__((address_space(1)))*)(uintptr_t)at; };
@@ -1121,8 +1135,10 @@ __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p
   };
   int run = 0;
   int id_next = first < last ? fetch_id(first) : -1;
-  if (first < last) load_block(first, id_next);
+  uint32_t word = first < last ? ask_word(first) : 0u;
+  const int id_first = id_next;
   id_next = fetch_id(first + KW);
+  if (first < last) load_block(first, id_first);
   for (int blk = first; blk < last; blk += KW) {
     f32x4 sc[4];
 #pragma unroll
@@ -1136,8 +1152,13 @@ __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int h = 0; h < NH; ++h) v[e][h] = vr[e][h];
-    if (blk + KW < last) load_block(blk + KW, id_next);
+    const uint32_t my_word = word;
+    const int id = id_next;
     id_next = fetch_id(blk + 2 * KW);
+    if (blk + KW < last) {
+      word = ask_word(blk + KW);
+      load_block(blk + KW, id);
+    }
     float x[4];  // key 4 * kg + e
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -1145,7 +1166,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p
       asm("" : "+v"(x[e]));  // (rounded before the maximum is taken off, so that the largest score's exponent is 0 at any size)
     }
     if (blk >= prefix_blocks || (blk + 1) * 16 > P) {
-      const uint32_t bits = seen_of(blk) >> (4 * kg);
+      const uint32_t bits = seen_of(blk, my_word) >> (4 * kg);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         x[e] = score_if(bits, e, x[e]);
@@ -1372,14 +1393,18 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
       for (int kb = 0; kb < 2; ++kb)
         sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(buf, st, kb), q[st], sc[kb], 0, 0, 0);
   };
-  // Keys that the lane's row does not see
-  auto hide = [&](f32x16 (&sc)[2], int tile) {
+  // Keys that the lane's row does not see, given the mask's words of the tile
+  auto ask_words = [&](int tile, uint32_t (&words)[2]) {
+    if (tile < full_tiles) return;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) words[kb] = mask_word(p, mask_row, tile < prefix_tiles ? -1 : 2 * (tile - prefix_tiles) + kb);
+  };
+  auto hide = [&](f32x16 (&sc)[2], int tile, const uint32_t (&words)[2]) {
     if (tile < full_tiles) return;
     const int left = tile < prefix_tiles ? P - tile * KB : N - (tile - prefix_tiles) * KB;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      const uint32_t bits =
-          seen_keys(p, mask_row, left - 32 * kb, tile < prefix_tiles ? -1 : 2 * (tile - prefix_tiles) + kb) >> (8 * kg);
+      const uint32_t bits = seen_keys(left - 32 * kb, words[kb]) >> (8 * kg);
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[kb][e] = score_if(bits, 16 * (e >> 3) + (e & 7), sc[kb][e]);
     }
@@ -1411,6 +1436,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
       rows_v[i] = lane_value(found, kLoads + i);  // (of the second tile)
     }
   }
+  uint32_t words_first[2] = {};
+  ask_words(begin, words_first);
   issue_tile(k_pool, k_fresh, K0, begin, rows_k);
   issue_tile(v_pool, v_fresh, V0, begin, rows_k);
   if (begin + 1 < end) issue_tile(k_pool, k_fresh, K1, begin + 1, rows_v);
@@ -1422,7 +1449,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   __syncthreads();
   if (works) {
     scores(K0, s_even);
-    hide(s_even, begin);
+    hide(s_even, begin, words_first);
     raise_reference(s_even, ref);
     sum_first = probabilities(s_even[0], cs, ref, hi[0], lo[0]);
   }
@@ -1465,6 +1492,8 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
       for (int i = 0; i < kLoads; ++i) rows_k[i] = lane_value(found, i);
     }
     asked = ask_ids(j + 3);
+    uint32_t words[2] = {};
+    ask_words(j + 1, words);
     issue_tile(v_pool, v_fresh, v_other, j + 1, rows_v);
     if (j + 2 < end) issue_tile(k_pool, k_fresh, k_same, j + 2, rows_k);
 #pragma unroll
@@ -1507,7 +1536,7 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
       float sum = sum_first + sums_a[0] + sums_a[1];
       asm volatile("" : "+v"(sum));
       settle(s_cur, sum);
-      hide(s_nxt, j + 1);
+      hide(s_nxt, j + 1, words);
       // O += V(j)^T P(j) beside the first half of P(j+1): in every slot the LDS reads of the operand some slots ahead, the two
       // products of one operand and their share of the 16 exponentials
       bf16x8 hi_first[2], lo_first[2];
