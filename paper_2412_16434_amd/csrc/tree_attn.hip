@@ -297,7 +297,8 @@ __device__ __forceinline__ void for_segments(const TreeParams& p, int G, int r, 
 }
 
 // What a row without any probability gets: zero if it sees no key, NaN if all its scores are minus infinity (0 / 0).
-__device__ __forceinline__ float nothing_seen(const TreeParams& p, const TreePiece& it, int tok) {
+template <typename Piece>
+__device__ __forceinline__ float nothing_seen(const TreeParams& p, const Piece& it, int tok) {
   bool sees = it.P > 0;
   const uint32_t* row = p.mask + (int64_t)(it.cu + tok) * p.mask_words;
   for (int w = 0; w < p.mask_words && w * 32 < it.N && !sees; ++w)
@@ -1251,10 +1252,16 @@ __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p
 constexpr int kWideKeys = 64;
 constexpr float kRaiseSum = 1.0995116e12f;  // 2^40
 
-// A wide tile's piece in the workspace: the registers of its 256 threads, then (m, l) of each
+// A wide tile's piece in the workspace: the registers of its 256 threads, then (m, l) of each, then which piece of what it is (the
+// join reads that instead of working it out again: 1.5 us)
+struct WideNote {
+  int32_t cu, P, N, tile, index, count, stride, reserved;  // count 0: no piece
+};
+template <int D>
+constexpr int kWideSlot = 128 * D + 512 + (int)(sizeof(WideNote) / 4);
 template <int D>
 __device__ __forceinline__ float* wide_slot(const TreeParams& p, int64_t piece, int kvh) {
-  return p.parts + (piece * p.n_kv_heads + kvh) * (int64_t)(128 * D + 512);
+  return p.parts + (piece * p.n_kv_heads + kvh) * (int64_t)kWideSlot<D>;
 }
 
 template <int D>
@@ -1276,7 +1283,11 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
   int kvh, piece;
   split_block(p, blockIdx.x, kvh, piece);
   TreePiece it;
-  if (!find_piece<BM, KB>(p, G, piece, it)) return;
+  const bool found = find_piece<BM, KB>(p, G, piece, it);
+  if (p.cut && threadIdx.x == 0)
+    *reinterpret_cast<WideNote*>(wide_slot<D>(p, piece, kvh) + 128 * D + 512) =
+        found ? WideNote{it.cu, it.P, it.N, it.tile, it.index, it.count, it.stride, 0} : WideNote{};
+  if (!found) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31;  // query row of this lane within its wave's; also its row of the K operand
@@ -1760,7 +1771,7 @@ __device__ __forceinline__ void join_rows(const TreeParams& p, const TreePiece& 
   }
 }
 
-// Wide tiles: a workgroup of the tile's pieces takes its share of the 16-byte vectors of a thread, thread by thread as they were
+// Wide tiles: the workgroups of the tile's pieces take their shares of the 16-byte vectors of a thread, thread by thread as they were
 // written.
 template <int D>
 __global__ __launch_bounds__(256) void tree_join_wide_kernel(const TreeParams p) {
@@ -1770,17 +1781,18 @@ __global__ __launch_bounds__(256) void tree_join_wide_kernel(const TreeParams p)
   const int Hkv = p.n_kv_heads, G = p.group;
   int kvh, piece;
   split_block(p, blockIdx.x, kvh, piece);
-  TreePiece it;
-  if (!find_piece<BM, kWideKeys>(p, G, piece, it) || it.count == 1 || it.index >= kVecs) return;
+  const WideNote it = *reinterpret_cast<const WideNote*>(wide_slot<D>(p, piece, kvh) + 128 * D + 512);
+  const int mine = it.index + it.count * (int)blockIdx.y;
+  if (it.count <= 1 || mine >= kVecs) return;
   const int tid = threadIdx.x, r = (tid >> 6) * 32 + (tid & 31);
   const unsigned row0 = (unsigned)it.tile * BM;
   const int n_rows = (int)min((unsigned)BM, (unsigned)it.N * (unsigned)G - row0);
   if (r >= n_rows) return;
   const float* const first = wide_slot<D>(p, piece - (int64_t)it.index * it.stride, kvh);
-  const int64_t stride = (int64_t)it.stride * Hkv * (128 * D + 512);
+  const int64_t stride = (int64_t)it.stride * Hkv * kWideSlot<D>;
   const unsigned row = row0 + r, tok = (unsigned)token_of(p, row);
   T* const op = (T*)p.out + ((int64_t)(it.cu + (int)tok) * p.n_q_heads + kvh * G + (int)(row - tok * G)) * D + 4 * (tid >> 5 & 1);
-  for (int v = it.index; v < kVecs; v += it.count) {
+  for (int v = mine; v < kVecs; v += it.count * (int)gridDim.y) {
     float M = -INFINITY, L = 0.f;
     f32x4 o{0.f, 0.f, 0.f, 0.f};
     for (int c = 0; c < it.count; c += kAtOnce) {
@@ -1834,10 +1846,12 @@ constexpr int kWideSlots = 512;  // workgroups of wide tiles that are on the chi
 constexpr int kWidePieces = 1024; // and that the key axis is cut for at most, all kv-heads together
 constexpr int kRanges = 256;     // the same for ranges: one workgroup per compute unit
 constexpr int kStreamWaves = 8;
+constexpr int kJoinParts = 16;   // parts of a tile's join, as far as it does not have as many pieces
 
 struct TreePlan {
   bool wide;           // 128-row tiles through LDS
   int waves;           // streams: of a workgroup
+  unsigned join_parts; // workgroups that join what one has produced
   int rw;              // else: waves side by side on the rows
   int64_t pieces;      // per kv-head
   int32_t c_min;       // key blocks
@@ -1890,11 +1904,12 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
     const int64_t more = per_tile <= 1 ? 0 : tiles >= target ? target : std::min(tiles * (per_tile - 1), target);
     pl.cut = more > 0;
     pl.pieces = tiles + more;
+    pl.join_parts = (unsigned)std::clamp<int64_t>(kJoinParts * tiles / pl.pieces, 1, 4);
   } else {
     pl.cut = per_tile > 1;
     pl.pieces = pl.cut ? std::min(tiles * per_tile, target) : tiles;
   }
-  pl.bytes = !pl.cut ? 0 : pl.wide ? pl.pieces * c->n_kv_heads * (128 * c->head_dim + 512) * 4
+  pl.bytes = !pl.cut ? 0 : pl.wide ? pl.pieces * c->n_kv_heads * (c->head_dim == 128 ? kWideSlot<128> : kWideSlot<64>) * 4
                                    : 2 * pl.pieces * c->n_kv_heads * BM * (c->head_dim + 2) * 4;
   if (ceil_div64(rows, BM) * blocks > kMostWork) return false;
   return 2 * pl.pieces * c->n_kv_heads <= 0x7FFFFFFFLL;
@@ -1926,10 +1941,11 @@ static void launch_tree(const TreeParams& p, int64_t pieces, int waves, hipStrea
 }
 
 template <int D>
-static void launch_wide(const TreeParams& p, int64_t pieces, hipStream_t stream) {
+static void launch_wide(const TreeParams& p, int64_t pieces, unsigned parts, hipStream_t stream) {
   const unsigned groups = (unsigned)(pieces * p.n_kv_heads);
   hipLaunchKernelGGL((tree_wide_kernel<D>), dim3(groups), dim3(256), 0, stream, p);
-  if (p.cut) hipLaunchKernelGGL((tree_join_wide_kernel<D>), dim3(groups), dim3(256), 0, stream, p);
+  // (tiles of few pieces: their workgroups would take several vectors one after another)
+  if (p.cut) hipLaunchKernelGGL((tree_join_wide_kernel<D>), dim3(groups, parts), dim3(256), 0, stream, p);
 }
 
 template <typename T, int D>
@@ -1938,7 +1954,7 @@ static int32_t launch_tree(TreeParams& p, const TreePlan& pl, bool wide, hipStre
     hipLaunchKernelGGL((tree_row_kernel<T, D>), dim3((unsigned)p.total * (unsigned)p.n_q_heads), dim3(64), 0, stream, p);
   } else {
     if constexpr (sizeof(T) == 2) {
-      if (pl.wide) launch_wide<D>(p, pl.pieces, stream);
+      if (pl.wide) launch_wide<D>(p, pl.pieces, pl.join_parts, stream);
     }
     if (!pl.wide) {
       if (pl.rw == 1)

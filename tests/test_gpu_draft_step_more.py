@@ -141,3 +141,13 @@ def test_a_session_before_any_token_and_an_empty_batch():
     S.tree_accept(empty, empty, empty, cu, empty, empty, empty, empty)
     S.kv_commit(cache, kv[None], kv[None], empty, torch.zeros(0, dtype=torch.int64, device=DEV))
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("fp32", 64)])
+@pytest.mark.parametrize("sessions,g,long", [(64, 2, 0), (65, 2, 900), (256, 1, 0), (257, 4, 0), (300, 1, 1500), (600, 2, 0), (257, 16, 700)])
+def test_numbers_of_sessions_around_a_waves_shares(dtype, d, sessions, g, long):
+    """A lane has one session, or four, or four of every 256: empty ones at the edges, tiles of several sessions in a range."""
+    rng = np.random.default_rng(sessions)
+    prefix, new = rng.integers(0, 40, sessions), rng.integers(0, 6, sessions)
+    new[[0, 63, sessions - 1]], prefix[sessions // 2], new[sessions // 2] = [0, 0, 4], max(long, 50), 5
+    Draft(prefix, new, dtype, d, hkv=1, g=g, tree="bits", seed=61).check()
