@@ -44,6 +44,7 @@ struct TreeParams {
   int32_t max_pieces;    // of tiles (per kv-head) or ranges: what the grid and the workspace have room for
   int32_t c_min;         // key blocks of a tile that are not cut further, of a range at least
   int32_t cut;           // 0: one piece per tile
+  int32_t aligned;       // narrow tiles: cut into pieces, not ranges
   int32_t slots;         // workgroups per kv-head that are on the chip at once
   int32_t group, group_shift, heads_shift;  // query heads of a kv-head; log2 of it and of n_kv_heads, or -1
   float* parts;
@@ -144,7 +145,7 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
       int best = 0x7FFFFFFF;
 #pragma unroll 1
       for (int rounds = 1; rounds <= 4; ++rounds) {
-        const int room = p.slots * rounds - n_tiles / 2;
+        const int room = p.slots * rounds - (p.aligned ? n_tiles : n_tiles / 2);
         if (room <= 0) continue;
         const int len = max(max(__builtin_amdgcn_readfirstlane((int)(((unsigned)work + (unsigned)room - 1) / (unsigned)room)), least),
                             p.c_min);
@@ -193,7 +194,8 @@ __device__ __forceinline__ bool find_piece(const TreeParams& p, int G, int g, Tr
 // ---- the other way to cut: all tiles' key blocks laid end to end, in session order, and cut into equal ranges, one per workgroup,
 // whatever tiles they run through.  Nothing is left over at the end of a launch (pieces of tiles, a third more of them than the
 // chip takes at once, made 64 short drafts take 246 us instead of 211); what it costs is that tiles of one session are read at
-// different times, so it is for batches whose sessions have one tile.
+// different times, so it is for sessions of one tile, and for batches where pieces that end with their tiles would be too unlike
+// (see the host's choice).
 struct TreeRanges {
   int64_t total, per;  // blocks; of a range
   int count, longer;   // ranges; the first `longer` of them have one block more
@@ -265,34 +267,71 @@ __device__ __forceinline__ int64_t range_place(const TreeRanges& rg, int r, int6
   return 2 * (int64_t)r + (tile_start > rg.begin(r));
 }
 
+// A part of a narrow tile in the workspace: its rows, m and l of each, and which part of what it is, for the join (which would
+// otherwise work that out again, for 2 us)
+struct PartNote {
+  int32_t cu, P, N, tile, index, count, own, step;  // count 0: no part.  The tile's first is at place `own`, part c at (own & ~1) + c * step
+};
+template <int BM, int D>
+constexpr int kPartSlot = BM * (D + 2) + (int)(sizeof(PartNote) / 4);
+template <int BM, int D>
+__device__ __forceinline__ float* part_slot(const TreeParams& p, int64_t place, int kvh) {
+  return p.parts + (place * p.n_kv_heads + kvh) * (int64_t)kPartSlot<BM, D>;
+}
+template <int BM, int D>
+__device__ __forceinline__ PartNote* part_note(const TreeParams& p, int64_t place, int kvh) {
+  return reinterpret_cast<PartNote*>(part_slot<BM, D>(p, place, kvh) + BM * (D + 2));
+}
+
 // Runs `segment(it, place)` for every part of a tile that lies in range r; it.count: 1 if that is all of it, place: else where its
 // results go.  Without a cut: for tile r.
-template <int BM, int KB, typename Segment>
-__device__ __forceinline__ void for_segments(const TreeParams& p, int G, int r, Segment segment) {
+template <int BM, int KB, int D, bool PIECES, typename Segment>
+__device__ __forceinline__ void for_segments(const TreeParams& p, int G, int kvh, int r, Segment segment) {
   SessionLane mine;
   TreeRanges rg;
   TreePiece it;
   int64_t x = 0, end = 1, start = 0;
   if (p.cut) {
-    rg = cut_ranges<BM, KB>(p, G, mine);
-    if (r >= rg.count) return;
-    x = rg.begin(r);
-    end = rg.begin(r + 1);
+    if (threadIdx.x < 2) *part_note<BM, D>(p, 2 * (int64_t)r + threadIdx.x, kvh) = PartNote{};
+    if (!PIECES || !p.aligned) {
+      rg = cut_ranges<BM, KB>(p, G, mine);
+      if (r >= rg.count) return;
+      x = rg.begin(r);
+      end = rg.begin(r + 1);
+    }
   }
   while (x < end) {
-    if (!p.cut) {
+    int64_t place = 0;
+    if (!p.cut || (PIECES && p.aligned)) {
       if (!find_piece<BM, KB>(p, G, r, it)) return;
       x = end;
+      place = 2 * (int64_t)r;
+      if (PIECES && p.cut && threadIdx.x == 0)
+        *part_note<BM, D>(p, place, kvh) =
+            PartNote{it.cu, it.P, it.N, it.tile, it.index, it.count, 2 * (r - it.index * it.stride), 2 * it.stride};
     } else {
       if (!find_tile<BM, KB>(p, G, mine, x, it, start)) return;
       const int64_t tile_end = start + it.block1, stop = min(tile_end, end);
       it.block0 = (int)(x - start);
       it.block1 = (int)(stop - start);
       it.index = 0;
-      it.count = it.block0 == 0 && stop == tile_end ? 1 : 2;
+      it.count = 1;
+      if (it.block0 > 0 || stop < tile_end) {
+        const int first = rg.holding(start);
+        it.index = r - first;
+        it.count = rg.holding(tile_end - 1) - first + 1;
+        place = range_place(rg, r, start);
+        if (threadIdx.x == (place & 1))  // (the thread that has cleared it)
+          *part_note<BM, D>(p, place, kvh) =
+              PartNote{it.cu, it.P, it.N, it.tile, it.index, it.count, (int)range_place(rg, first, start), 2};
+      }
       x = stop;
     }
-    segment(it, p.cut ? range_place(rg, r, start) : 0);
+    if constexpr (PIECES) {
+      for (int* v : {&it.s, &it.cu, &it.P, &it.N, &it.tile, &it.count, &it.block0, &it.block1})
+        *v = __builtin_amdgcn_readfirstlane(*v);  // (the compiler has them in vector registers)
+    }
+    segment(it, place);
   }
 }
 
@@ -431,11 +470,6 @@ __device__ __forceinline__ void put_pair(bf16x8& v, int at, float x, float y) {
   u32x4 words = __builtin_bit_cast(u32x4, v);
   words[at >> 1] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, y), __builtin_bit_cast(unsigned, x), 0x07060302u);
   v = __builtin_bit_cast(bf16x8, words);
-}
-
-template <int BM, int D>
-__device__ __forceinline__ float* part_slot(const TreeParams& p, int64_t g, int kvh) {
-  return p.parts + (g * p.n_kv_heads + kvh) * (int64_t)(BM * (D + 2));
 }
 
 // ---- results of a tile of BM rows by all WAVES waves of the workgroup.  slot: where the results of a tile that is cut go.  sum_at(t, r, c, M, L):
@@ -687,7 +721,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
   const int rw = wave % RW, kw = wave / RW;
   const int n = lane & 31;  // query row of this lane within its wave's; also its row of the K operand
   const int kg = lane >> 5;
-  for_segments<BM, KT>(p, G, range, [&](const TreePiece& it, const int64_t place) {
+  for_segments<BM, KT, D, true>(p, G, kvh, range, [&](const TreePiece& it, const int64_t place) {
   const int cu = it.cu, P = it.P, N = it.N;
   const unsigned row0 = (unsigned)it.tile * BM;
   const int n_rows = (int)min((unsigned)BM, (unsigned)N * (unsigned)G - row0);
@@ -979,7 +1013,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p
   const int rw = wave % RW, kw = wave / RW;
   const int n = lane & (R - 1);  // query row of this lane within its wave's; also its row of the K operand
   const int kg = lane / R;       // its share of the contraction index: half (bf16) or quarter (fp32) of the wave
-  for_segments<BM, R>(p, G, range, [&](const TreePiece& it, const int64_t place) {
+  for_segments<BM, R, D, false>(p, G, kvh, range, [&](const TreePiece& it, const int64_t place) {
   const int cu = it.cu, P = it.P, N = it.N;
   const unsigned row0 = (unsigned)it.tile * BM;
   const int n_rows = (int)min((unsigned)BM, (unsigned)N * (unsigned)G - row0);
@@ -1246,9 +1280,9 @@ __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p
 // lost by a reference that is too low.
 // Bound by the matrix cores: a tile of 64 keys takes a workgroup 3500 clocks alone and 3900 beside the other one of its compute unit,
 // 79 % of them products, at a clock that falls to 1.4 to 1.8 GHz under them.  32 sessions with trees of 24 to 64 tokens over 2048
-// to 16384 keys (G 4: 1.31 GB, 243 GF): 485 us, 500 TF, or 750 with the products of the probabilities' second halves; 64 tokens over
-// 32768 keys (G 8) 113 us.  A small call is made of trips to memory: 26 tokens over 3001 keys 20 us, 2.2 to find the piece, 2.5 for
-// ids and first tiles, 1.6 a tile, 1.9 at the end, 6 for the join.
+// to 16384 keys (G 4: 1.31 GB, 243 GF): 475 us, 510 TF, or 770 with the products of the probabilities' second halves; 64 tokens over
+// 32768 keys (G 8) 112 us.  A small call is made of trips to memory: 26 tokens over 3001 keys 18.7 us, 2.2 to find the piece, 2.5 for
+// ids and first tiles, 1.6 a tile, 1.9 at the end, 4.7 for the join.
 constexpr int kWideKeys = 64;
 constexpr float kRaiseSum = 1.0995116e12f;  // 2^40
 
@@ -1707,7 +1741,7 @@ __device__ __forceinline__ void add_pieces(float& M, float& L, f32x4& o, const f
 // Each of a tile's pieces has a workgroup here too, which joins an equal share of the tile's rows.  A join is nothing but trips to memory: D / 4 lanes take a
 // row's columns of eight pieces at a time, and where there are fewer rows than such groups of lanes, several share a row.
 template <typename T, int D, int BM, typename Slot>
-__device__ __forceinline__ void join_rows(const TreeParams& p, const TreePiece& it, int kvh, Slot slot_of) {
+__device__ __forceinline__ void join_rows(const TreeParams& p, const PartNote& it, int kvh, Slot slot_of) {
   constexpr int kLanes = D / 4, kSubs = 256 / kLanes, kAtOnce = 8;
   __shared__ f32x4 part_o[kSubs][kLanes];
   __shared__ float part_m[kSubs], part_l[kSubs];
@@ -1815,27 +1849,16 @@ __global__ __launch_bounds__(256) void tree_join_wide_kernel(const TreeParams p)
 }
 
 // The same for ranges: a workgroup for each of the two places of a range
-template <typename T, int D, int BM, int KB>
+template <typename T, int D, int BM>
 __global__ __launch_bounds__(256) void tree_join_ranges_kernel(const TreeParams p) {
-  const int Hkv = p.n_kv_heads, G = p.group;
   int kvh, place;
   split_block(p, blockIdx.x, kvh, place);
-  const int r = place >> 1, second = place & 1;
-  SessionLane mine;
-  const TreeRanges rg = cut_ranges<BM, KB>(p, G, mine);
-  if (r >= rg.count || rg.total == 0) return;
-  TreePiece it;
-  int64_t start;
-  if (!find_tile<BM, KB>(p, G, mine, second ? rg.begin(r + 1) - 1 : rg.begin(r), it, start)) return;
-  if (second && start <= rg.begin(r)) return;  // (it starts with the range or before: the first place's)
-  const int first = rg.holding(start);
-  it.index = r - first;
-  it.count = rg.holding(start + it.block1 - 1) - first + 1;
-  if (it.count == 1) return;
-  // (the second and later pieces of a tile start with their ranges)
-  const float* const own = part_slot<BM, D>(p, range_place(rg, first, start), kvh);
-  const float* const later = part_slot<BM, D>(p, 2 * (int64_t)first, kvh);
-  const int64_t stride = 2 * (int64_t)Hkv * (BM * (D + 2));
+  const PartNote it = *part_note<BM, D>(p, place, kvh);
+  if (it.count <= 1) return;
+  // (the second and later parts of a tile start with their ranges, in the first of their two places)
+  const float* const own = part_slot<BM, D>(p, it.own, kvh);
+  const float* const later = part_slot<BM, D>(p, it.own & ~1, kvh);
+  const int64_t stride = it.step * (int64_t)p.n_kv_heads * kPartSlot<BM, D>;
   join_rows<T, D, BM>(p, it, kvh, [&](int c) { return c == 0 ? own : later + c * stride; });
 }
 
@@ -1854,6 +1877,7 @@ struct TreePlan {
   unsigned join_parts; // workgroups that join what one has produced
   int rw;              // else: waves side by side on the rows
   int64_t pieces;      // per kv-head
+  bool aligned;        // narrow tiles in pieces
   int32_t c_min;       // key blocks
   bool cut;
   int64_t bytes;
@@ -1871,6 +1895,7 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   const int R = c->dtype == SYMPH_BF16 ? 32 : 16;
   const int64_t G = n_q_heads / c->n_kv_heads;
   const int64_t rows = (int64_t)max_new * G;
+  pl.aligned = false;
   pl.wide = c->dtype == SYMPH_BF16 && rows > 64 && grouped_rows(c);
   pl.rw = rows <= R ? 1 : rows <= 2 * R ? 2 : 4;
   const int64_t BM = pl.wide ? 128 : (int64_t)R * pl.rw, KB = pl.wide || (R == 32 && c->head_dim == 64) ? 64 : R;
@@ -1908,9 +1933,15 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   } else {
     pl.cut = per_tile > 1;
     pl.pieces = pl.cut ? std::min(tiles * per_tile, target) : tiles;
+    // A range that runs into another session costs some 8 us more, a piece that ends with its tile leaves workgroups unlike: half a
+    // piece of a tile's share of 5 us for every block of a wave.  (Nine sessions of up to 940 keys 20.3 -> 14.6 us, eight of up to
+    // 4000 37 -> 33; 113 of up to 20 000 would take 210 against 170.  One session's ranges are its pieces.)
+    const int64_t count = pl.rw <= 2 ? n_sessions : tiles;
+    pl.aligned = pl.cut && R == 32 && n_sessions > 1 && 2 * count <= pl.pieces &&
+                 count * count * blocks <= 2 * kStreamWaves * pl.pieces * pl.pieces;
   }
   pl.bytes = !pl.cut ? 0 : pl.wide ? pl.pieces * c->n_kv_heads * (c->head_dim == 128 ? kWideSlot<128> : kWideSlot<64>) * 4
-                                   : 2 * pl.pieces * c->n_kv_heads * BM * (c->head_dim + 2) * 4;
+                                   : 2 * pl.pieces * c->n_kv_heads * (BM * (c->head_dim + 2) * 4 + (int64_t)sizeof(PartNote));
   if (ceil_div64(rows, BM) * blocks > kMostWork) return false;
   return 2 * pl.pieces * c->n_kv_heads <= 0x7FFFFFFFLL;
 }
@@ -1929,14 +1960,14 @@ static void launch_tree(const TreeParams& p, int64_t pieces, int waves, hipStrea
       else
         hipLaunchKernelGGL((tree_stream_kernel<D, RW, kStreamWaves, true>), grid, dim3(64 * kStreamWaves), 0, stream, p);
     }
-    if (p.cut) hipLaunchKernelGGL((tree_join_ranges_kernel<T, D, 32 * RW, TileLds<D>::kStreamKeys>), join, dim3(256), 0, stream, p);
+    if (p.cut) hipLaunchKernelGGL((tree_join_ranges_kernel<T, D, 32 * RW>), join, dim3(256), 0, stream, p);
   } else {
     if constexpr (RW <= 2) {
       if (waves == 2) hipLaunchKernelGGL((tree_fp32_kernel<D, RW, 2>), grid, dim3(128), 0, stream, p);
     }
     if (waves == 4) hipLaunchKernelGGL((tree_fp32_kernel<D, RW, 4>), grid, dim3(256), 0, stream, p);
     if (waves == kStreamWaves) hipLaunchKernelGGL((tree_fp32_kernel<D, RW, kStreamWaves>), grid, dim3(64 * kStreamWaves), 0, stream, p);
-    if (p.cut) hipLaunchKernelGGL((tree_join_ranges_kernel<T, D, kFp32Rows * RW, kFp32Rows>), join, dim3(256), 0, stream, p);
+    if (p.cut) hipLaunchKernelGGL((tree_join_ranges_kernel<T, D, kFp32Rows * RW>), join, dim3(256), 0, stream, p);
   }
 }
 
@@ -2044,7 +2075,8 @@ int32_t symph_tree_attn(const symph_kv_cache* cache, int32_t layer, const void* 
   const auto log2_or_neg = [](int32_t v) { return (v & (v - 1)) == 0 ? __builtin_ctz((unsigned)v) : -1; };
   p.group_shift = log2_or_neg(p.group);
   p.heads_shift = log2_or_neg(cache->n_kv_heads);
-  p.slots = (int32_t)std::max<int64_t>(kWideSlots / cache->n_kv_heads, 1);
+  p.aligned = pl.aligned;
+  p.slots = (int32_t)std::max<int64_t>((pl.wide ? kWideSlots : kRanges) / cache->n_kv_heads, 1);
   p.parts = (float*)d_workspace;
   const uintptr_t address_bits = (uintptr_t)p.k_layer | (uintptr_t)p.v_layer | (uintptr_t)d_q | (uintptr_t)d_k_new |
                                  (uintptr_t)d_v_new | (uintptr_t)d_out | (uintptr_t)block_bytes;
