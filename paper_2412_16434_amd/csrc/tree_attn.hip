@@ -1907,7 +1907,9 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   pl.c_min = pl.wide ? 2 : 4;
   // Else eight waves fill a compute unit, fewer let it take more workgroups, for tiles that keep few waves busy or are many.  A round
   // of workgroups takes some 6 us and 2.5 for every block of a wave, and a cut batch of many sessions some 40 us beside its bytes
-  // (parts of several tiles per workgroup, their results, the join).
+  // (parts of several tiles per workgroup, their results, the join).  So it stays whole where the rounds take less than that, or the
+  // tiles are so many that a long one at the end is a small part (249 sessions of up to 887 keys 160 -> 119 us, 191 fp32 trees of
+  // 247 tokens 1430 -> 1200).
   pl.waves = kStreamWaves;
   bool brief = false;
   if (!pl.wide && (R == 16 || grouped_rows(c))) {
@@ -1917,7 +1919,7 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
       const int64_t takes = ceil_div64(all, kRanges * kStreamWaves / w) * (12 + 5 * ceil_div64(blocks, w / pl.rw));
       if (takes < best) best = takes, pl.waves = w;
     }
-    brief = all >= kRanges / 2 && best <= 80;
+    brief = (all >= kRanges / 2 && best <= 80) || (all >= 2 * kRanges && blocks * kRanges <= R / 2 * all);
     if (blocks > uncut && !brief) pl.waves = kStreamWaves;
   }
   // Wide tiles that fill the chip as they are, and are not long: a tail costs less than pieces do (their search, results and join;
