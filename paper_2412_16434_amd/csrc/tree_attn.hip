@@ -630,6 +630,15 @@ __device__ __forceinline__ void load_lds16(const char* base, unsigned off, char*
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),         \
                                    (__attribute__((address_space(3))) void*)(dst), 16, 0, POLICY)
 
+// Behind the LDS reads of a buffer and in front of the loads that fill it again, where no barrier is between them: every read has
+// returned.  (Program order is not enough: reads and loads into LDS are two queues, and what orders them for other memory, a use of
+// the value read, the compiler may move behind the loads.)
+__device__ __forceinline__ void lds_reads_returned() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  asm volatile("" ::: "memory");
+}
+
 // Where a key's block is in the table (a division would be forty instructions)
 __device__ __forceinline__ unsigned table_place(const TreeParams& p, unsigned key) { return __umulhi(key, p.bs_magic) >> p.bs_more; }
 __device__ __forceinline__ int block_of_key(const TreeParams& p, int key) {
@@ -884,6 +893,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
       ids_next = ask_ids(tile + 2 * KW);
     }
     if constexpr (kNext == kRows) ask_words(tile + KW);
+    if constexpr (kNext != kNone) lds_reads_returned();
     if constexpr (kNext == kWhole) issue_whole(k_pool, k_buf, rows);
     if constexpr (kNext == kRows) issue_rows(k_pool, k_fresh, k_buf, tile + KW, ids, rows);
     if (kNext != kWhole && tile >= full_tiles) {
@@ -926,7 +936,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
       o[g % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, hi[step >> 1][step & 1], o[g % NT], 0, 0, 0);
       o[g % NT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, lo[step >> 1][step & 1], o[g % NT], 0, 0, 0);
     }
-    asm volatile("" ::: "memory");
+    if constexpr (kNext != kNone) lds_reads_returned();
     if constexpr (kNext == kWhole) issue_whole(v_pool, v_buf, rows);
     if constexpr (kNext == kRows) issue_rows(v_pool, v_fresh, v_buf, tile + KW, ids, rows);
   };
