@@ -1954,8 +1954,10 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
     // A range that runs into another session costs some 8 us more, a piece that ends with its tile leaves workgroups unlike: half a
     // piece of a tile's share of 5 us for every block of a wave.  (Nine sessions of up to 940 keys 20.3 -> 14.6 us, eight of up to
     // 4000 37 -> 33; 113 of up to 20 000 would take 210 against 170.  One session's ranges are its pieces.)
+    // Ranges cover whatever there is; of pieces every tile takes one at least, so there have to be as many as tiles of any lengths,
+    // not of those that max_new says.  (Where a session is one tile that is so: then tiles <= 2 * count.)
     const int64_t count = pl.rw <= 2 ? n_sessions : tiles;
-    pl.aligned = pl.cut && R == 32 && n_sessions > 1 && 2 * count <= pl.pieces &&
+    pl.aligned = pl.cut && R == 32 && n_sessions > 1 && tiles <= pl.pieces && 2 * count <= pl.pieces &&
                  count * count * blocks <= 2 * kStreamWaves * pl.pieces * pl.pieces;
   }
   pl.bytes = !pl.cut ? 0 : pl.wide ? pl.pieces * c->n_kv_heads * (c->head_dim == 128 ? kWideSlot<128> : kWideSlot<64>) * 4
