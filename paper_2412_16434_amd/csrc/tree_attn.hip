@@ -1724,8 +1724,12 @@ __global__ __launch_bounds__(256, 2) void tree_wide_kernel(const TreeParams p) {
 }
 
 // ---- joins the pieces of cut tiles: out = sum_c f_c O_c / sum_c f_c l_c, f_c = e^(m_c - max_c m_c).
+// The O_c are finite each, but as large as the type takes where the values are, so that the sum of a few would overflow: they are
+// added up 2^12 times smaller, which is more than a tile has pieces (1025 at most).  A power of two changes no bit of the quotient,
+// but where f_c is below 2^-114: there the product with it has fewer bits than a float, as f_c itself has from 2^-126 on.
+constexpr float kJoinShrink = 0x1p-12f, kJoinGrow = 0x1p12f;
 
-// AT_ONCE pieces, of which the first `left` count, into a running maximum, sum and row
+// AT_ONCE pieces, of which the first `left` count, into a running maximum, sum and row (kJoinShrink of it)
 template <typename T, int AT_ONCE>
 __device__ __forceinline__ void add_pieces(float& M, float& L, f32x4& o, const f32x4 (&oc)[AT_ONCE], const f32x2 (&ml)[AT_ONCE],
                                            int left) {
@@ -1743,7 +1747,7 @@ __device__ __forceinline__ void add_pieces(float& M, float& L, f32x4& o, const f
     const float f = k >= left ? 0.f : m == -INFINITY ? (l == l ? 0.f : 1.f) : exp_of<T>(m - M);
     if (f != 0.f) {
       L += l * f;
-      o += oc[k] * f;
+      o += oc[k] * (kJoinShrink * f);
     }
   }
 }
@@ -1809,7 +1813,7 @@ __device__ __forceinline__ void join_rows(const TreeParams& p, const PartNote& i
       typedef T vec __attribute__((ext_vector_type(4)));
       vec y;
 #pragma unroll
-      for (int v = 0; v < 4; ++v) y[v] = (T)(L == 0.f ? none : o[v] * (1.0f / L));
+      for (int v = 0; v < 4; ++v) y[v] = (T)(L == 0.f ? none : o[v] * (kJoinGrow / L));
       T* const op = (T*)p.out + ((int64_t)(it.cu + (int)tok) * p.n_q_heads + kvh * G + (int)(row - tok * G)) * D;
       *reinterpret_cast<vec*>(op + c0) = y;
     }
@@ -1854,7 +1858,7 @@ __global__ __launch_bounds__(256) void tree_join_wide_kernel(const TreeParams p)
     const float none = L == 0.f ? nothing_seen(p, it, (int)tok) : 0.f;
     vec y;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (T)(L == 0.f ? none : o[e] * (1.0f / L));
+    for (int e = 0; e < 4; ++e) y[e] = (T)(L == 0.f ? none : o[e] * (kJoinGrow / L));
     *reinterpret_cast<vec*>(op + 8 * v) = y;
   }
 }
