@@ -85,7 +85,7 @@ class Server:
         self.free = torch.randperm(self.n_blocks, generator=torch.Generator().manual_seed(1)).int().to(DEV)
         # (two of each: a call reads one and writes the other)
         self.used, self.held = [self.i32(1), self.i32(1)], [self.i32(n_sessions), self.i32(n_sessions)]
-        self.lens, self.longest = self.i32(n_sessions), 0  # cached tokens, and the most of a session as the host knows it
+        self.lens, self.host_lens = self.i32(n_sessions), [0] * n_sessions  # cached tokens, and the host's copy
         self.workspace = None
 
     @staticmethod
@@ -121,13 +121,13 @@ class Server:
         target, k_new, v_new = m.forward(tokens, positions, attend)
         S.kv_commit(self.cache, k_new, v_new, torch.arange(total, dtype=torch.int32, device=DEV), slots)
         self.lens = torch.tensor(lens, dtype=torch.int32).to(DEV)
-        self.longest = far
+        self.host_lens = lens
         return target[cu[1:].long() - 1].tolist()
 
     def step(self, trees):
         """One step; ``trees``: per session (tokens, parents), the first node being the session's last token, which is not
         cached yet.  Returns per session the indices of its accepted nodes and the token behind them."""
-        m, n = self.model, len(trees)
+        m, n, longest = self.model, len(trees), max(self.host_lens)
         sizes = [len(t) for t, _ in trees]
         total, most = sum(sizes), max(sizes)
         draft = torch.tensor([t for tokens, _ in trees for t in tokens], dtype=torch.int32).to(DEV)
@@ -137,13 +137,13 @@ class Server:
         positions = self.i32(total)
         S.tree_mask(parents, cu, most, mask, prefix_lens=self.lens, positions=positions)
 
-        size = S.tree_attn_workspace_bytes(self.cache, n, m.hq, total, most, self.longest)
+        size = S.tree_attn_workspace_bytes(self.cache, n, m.hq, total, most, longest)
         if size and (self.workspace is None or self.workspace.numel() < size):
             self.workspace = torch.empty(size, dtype=torch.uint8, device=DEV)
 
         def attend(layer, q, k, v):
             out = torch.empty_like(q)
-            S.tree_attn(self.cache, layer, q, k, v, out, mask, cu, self.lens, self.table, most, self.longest, m.d ** -0.5,
+            S.tree_attn(self.cache, layer, q, k, v, out, mask, cu, self.lens, self.table, most, longest, m.d ** -0.5,
                         self.workspace)
             return out
         target, k_new, v_new = m.forward(draft, positions, attend)
@@ -153,7 +153,7 @@ class Server:
         S.kv_commit(self.cache, k_new, v_new, rows, slots)
         self.lens = lens
         cu_h, rows_h, count_h, following_h = (x.tolist() for x in (cu, rows, count, following))
-        self.longest += max(count_h)
+        self.host_lens = [a + b for a, b in zip(self.host_lens, count_h)]
         return [[r - cu_h[s] for r in rows_h[cu_h[s]:cu_h[s] + count_h[s]]] for s in range(n)], following_h
 
 
@@ -188,7 +188,7 @@ def generate(model, prompts, n_tokens, branches=4, depth=7, block_size=16):
     history = [list(p) + [t] for p, t in zip(prompts, server.prompts(prompts))]
     steps = 0
     while min(len(h) - len(p) for h, p in zip(history, prompts)) < n_tokens:
-        # (a session that is done goes on with trees of one node until all are)
+        # (a session that is done goes on with no tree until all are)
         trees = []
         for h, p in zip(history, prompts):
             left = n_tokens - (len(h) - len(p))
