@@ -378,7 +378,8 @@ int32_t symph_debug_check_tables(const symph_kv_cache* cache, const int32_t* d_b
  * The last six may be NULL each, d_held_blocks and d_free_begin too; an output must not be the input it belongs to
  * (d_held_after and d_held_blocks, d_blocks_taken and d_free_begin).  With P_s = 0 this is the table of an arriving session
  * (symph_kv_unpack), with N_s = its drafted tokens that of a step.  total_new_tokens = sum of N (host copy) sizes the grid:
- * tokens past it get neither slot nor block; entries past the true sum are -1.  Lengths below 0 count as 0.
+ * tokens past it get neither slot nor block; entries past the true sum are -1.  Lengths below 0 count as 0.  Totals past 3.4 * 10^10
+ * (more threads than a grid takes) are refused: SYMPH_EUNSUPPORTED.
  */
 int32_t symph_build_tables(const int32_t* d_prefix_lens, const int32_t* d_new_lens, const int32_t* d_held_blocks,
                            int32_t n_sessions, int32_t* d_block_table, int32_t table_stride, const int32_t* d_free_blocks,

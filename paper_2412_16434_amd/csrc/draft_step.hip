@@ -33,6 +33,7 @@ constexpr int kTabChunk = kTabThreads * kTabSess;
 constexpr int kTabStep = kTabThreads * 2;  // tokens of a workgroup whose threads have one pair each
 constexpr int kTabPairs = 4;               // pairs of a thread in calls of many tokens,
 constexpr int64_t kTabMany = 3 << 18;      // that is
+constexpr int64_t kTabMost = (int64_t)(0xFFFFFFFFu / kTabThreads - 1) * kTabStep * kTabPairs;  // (a grid has less than 2^32 threads)
 
 // Sums over the lanes up to this one.  The terms are below 2^37, so the low 24 bits and the rest add up in 32 bits each.
 __device__ __forceinline__ int64_t wave_scan64(int64_t v) {
@@ -437,6 +438,7 @@ int32_t symph_build_tables(const int32_t* d_prefix_lens, const int32_t* d_new_le
   if (n_free > 0 && !d_free_blocks) return SYMPH_EINVAL;
   if (d_cu_new_lens && total_new_tokens > 0x7FFFFFFFLL) return SYMPH_EINVAL;
   if ((d_held_after && d_held_after == d_held_blocks) || (d_blocks_taken && d_blocks_taken == d_free_begin)) return SYMPH_EINVAL;
+  if (total_new_tokens > kTabMost) return SYMPH_EUNSUPPORTED;
   TablesParams p;
   p.prefix_lens = d_prefix_lens;
   p.new_lens = d_new_lens;
@@ -459,7 +461,6 @@ int32_t symph_build_tables(const int32_t* d_prefix_lens, const int32_t* d_new_le
   p.n_blocks = n_blocks;
   const bool many = total_new_tokens >= kTabMany;
   const int64_t groups = ceil_div64(total_new_tokens, kTabStep * (many ? kTabPairs : 1)) + 1;
-  if (groups > 0x7FFFFFFFLL) return SYMPH_EUNSUPPORTED;
   if (many)
     hipLaunchKernelGGL(build_tables_kernel<kTabPairs>, dim3((unsigned)groups), dim3(kTabThreads), 0, (hipStream_t)stream, p);
   else
