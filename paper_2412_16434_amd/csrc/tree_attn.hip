@@ -1044,15 +1044,11 @@ __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p
     const int j = block_of(key);
     return j < p.table_stride ? table_row[j] : -1;
   };
-  // Row r of key block blk
-  auto row_of = [&](const void* pool, const void* fresh, int blk, int r, int id) {
-    if (blk < prefix_blocks) {
-      const int key = blk * R + r;
-      if (key >= P || id < 0 || id >= p.n_blocks) return (const T*)kNoRow;
-      return (const T*)pool + (int64_t)id * p.block_stride + ((int64_t)(key - block_of(key) * p.block_size) * Hkv + kvh) * D;
-    }
-    const int j = (blk - prefix_blocks) * R + r;
-    return j < N ? (const T*)fresh + ((int64_t)(cu + j) * Hkv + kvh) * D : (const T*)kNoRow;
+  // Row r of the prefix's key block blk
+  auto row_of = [&](const void* pool, int blk, int r, int id) {
+    const int key = blk * R + r;
+    if (key >= P || id < 0 || id >= p.n_blocks) return (const T*)kNoRow;
+    return (const T*)pool + (int64_t)id * p.block_stride + ((int64_t)(key - block_of(key) * p.block_size) * Hkv + kvh) * D;
   };
   // The word of the mask for a block, and the keys of the block that the lane's row sees, a bit each
   auto ask_word = [&](int blk) { return mask_word(p, mask_row, blk < prefix_blocks ? -1 : ((blk - prefix_blocks) * R) >> 5); };
@@ -1148,12 +1144,12 @@ __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p
       }
       return;
     }
-    const T* const k_row = row_of(p.k_layer, p.k_new, blk, n, id) + 4 * kg;
+    const T* const k_row = row_of(p.k_layer, blk, n, id) + 4 * kg;
 #pragma unroll
     for (int j = 0; j < NS; ++j) kr[j] = __builtin_bit_cast(f32x4, load_vec(k_row + 16 * j));
 #pragma unroll
     for (int e = 0; e < 4; ++e) {  // key 4 * kg + e: values 64 * h + 4 * n .. + 3 of its row
-      const T* const v_row = row_of(p.v_layer, p.v_new, blk, 4 * kg + e, __shfl(id, 4 * kg + e)) + 4 * n;
+      const T* const v_row = row_of(p.v_layer, blk, 4 * kg + e, __shfl(id, 4 * kg + e)) + 4 * n;
 #pragma unroll
       for (int h = 0; h < NH; ++h) vr[e][h] = __builtin_bit_cast(f32x4, load_vec(v_row + 64 * h));
     }
