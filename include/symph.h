@@ -392,7 +392,7 @@ int32_t symph_build_tables(const int32_t* d_prefix_lens, const int32_t* d_new_le
  * where node j of the session is node i itself or an ancestor of it.  d_parents int32 [total_new_tokens]: index of the parent
  * within the session; any value outside 0 .. i-1 makes node i a root.  d_positions (int32 [total_new_tokens], may be NULL)
  * becomes P_s + number of ancestors (P_s from d_prefix_lens, 0 where that is NULL).
- * max_new_len >= max N_s; at most 64 * mask_words and SYMPH_TREE_MAX_NODES.  Rows of nodes past max_new_len are not written.
+ * max_new_len >= max N_s; at most total_new_tokens, 64 * mask_words and SYMPH_TREE_MAX_NODES.  Rows of nodes past it are not written.
  */
 #define SYMPH_TREE_MAX_NODES 4096
 int32_t symph_tree_mask(const int32_t* d_parents, const int32_t* d_cu_new_lens, const int32_t* d_prefix_lens,
@@ -415,7 +415,8 @@ int32_t symph_tree_mask(const int32_t* d_parents, const int32_t* d_cu_new_lens, 
  * keeps 16 bits of each, output rounded to nearest even.  fp32 throughout for fp32.
  * Supported: head_dim 64 or 128, n_q_heads a multiple of n_kv_heads, any block size (multiples of 8 are read the quick way; of 4
  * too in bf16 with 128-wide heads), addresses on 16 bytes likewise.  Calls whose bounds allow a session more than 3 * 10^7 key
- * blocks times row tiles (10^9 keys under one tile) are refused: SYMPH_EUNSUPPORTED, a negative size below.
+ * blocks times row tiles (10^9 keys under one tile) are refused: SYMPH_EUNSUPPORTED, a negative size below; of such a session
+ * behind bounds that do not say so, rows may stay unwritten.
  */
 int32_t symph_tree_attn(const symph_kv_cache* cache, int32_t layer, const void* d_q, const void* d_k_new,
                         const void* d_v_new, void* d_out, const uint64_t* d_tree_mask, int32_t mask_words,

@@ -223,8 +223,8 @@ constexpr int kMaskPitch = kMaskTile + 1;  // (odd: lanes that write the same wo
 // doubling between lanes; the ancestor with the lowest index leads out of the chunk through its parent (a parent comes
 // before its children).  What a row has in earlier chunks is then found by one walk over chunks, not over ancestors.
 // A row's words go to memory through LDS, so that a wave writes whole lines.  What bounds it: two trips to memory, the rounds
-// and the walk, one after another; 64 trees of up to 64 nodes 3 us, 48 of up to 1001 6 us (3.4 MB of masks).  Twice as many
-// threads (fewer chunks looked at twice) took 6.9 against 6.5, half as many 8.2.
+// and the walk, one after another: 3 us for 64 trees of up to 64 nodes, 6.7 for 48 of up to 1001 (3.4 MB of masks).  A call
+// of the latter among others takes 6.5, with twice as many threads (fewer chunks looked at twice) 6.9, with half as many 8.2.
 __global__ __launch_bounds__(256) void tree_mask_kernel(const TreeMaskParams p) {
   extern __shared__ __attribute__((aligned(16))) char tree_lds[];
   const int cap = (p.max_new + 63) & ~63;
@@ -309,7 +309,7 @@ struct AcceptParams {
 
 // A wave per session, 64 nodes at a time.  Which nodes agree with their parent's target token is known at once; the walk then
 // only asks the lanes: the lowest one whose parent is the present node.  Children come after their parents, so one pass is
-// enough.  Bound by its trips to memory: 2 us for one tree, 2.6 for 64.
+// enough.  Bound by its trips to memory: 2 us for one tree, 2.3 to 3.7 for 64.
 __global__ __launch_bounds__(256) void tree_accept_kernel(const AcceptParams p) {
   const int lane = threadIdx.x & 63;
   const int s = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));

@@ -706,9 +706,11 @@ __device__ __forceinline__ float probabilities(const f32x16& x, float cs, float 
 
 // ---- narrow tiles (bf16): W waves, RW side by side on the rows, W / RW on the keys.  Up to 64 rows a read of 16 KB of K and V takes
 // longer than all arithmetic on it, so a wave is a stream of its own: tiles of 16 KB through two LDS buffers that no other wave
-// touches, no barrier.  The K buffer is filled again as soon as the scores are done, the V buffer as soon as the values are: one
-// of the two is always under way.  Loads return in order, so "all but the last eight" is exactly the older of the two.
-// Bound by memory: 64 sessions with drafts of 2 to 8 tokens and 512 to 8192 cached ones (G 4, 1.13 GB) take 209 us, 5.4 TB/s of the
+// touches, no barrier.  The K buffer is filled again as soon as the scores are done, the V buffer as soon as the values are.  Loads
+// return in order, so "all but the last eight" is exactly the older of the two, which is all that the program waits for; as built the
+// compiler adds a wait for all loads in front of a buffer's reads, since it does not tell the two buffers apart, and what keeps memory
+// busy meanwhile is the other waves.
+// Bound by memory: 64 sessions with drafts of 2 to 8 tokens and 512 to 8192 cached ones (G 4, 1.13 GB) take 206 us, 5.5 TB/s of the
 // 6.5 that a copy reaches; the rest is what a workgroup does around its keys, some 15 us, and 25 more where sessions are ragged.
 // Four waves in twice as many workgroups take as long, two or one are slower, and so is a barrier per tile.
 template <int D, int RW, int W, bool GROUPED>
@@ -866,8 +868,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
   };
   if (begin < end) ask_words(begin);
   int64_t rows = find_rows(begin, ids);
-  // Three copies of the loop's body, by what comes after the tile: one that lies whole in the prefix, any other, none.  (With the
-  // next tile's loads under a condition the compiler takes K for the youngest load under way, and waits for V too.)
+  // Three copies of the loop's body, by what comes after the tile: one that lies whole in the prefix, any other, none.
   enum { kWhole, kRows, kNone };
   auto use_tile = [&](const int tile, auto next) {
     constexpr int kNext = decltype(next)::value;
@@ -1000,7 +1001,7 @@ __global__ __launch_bounds__(64 * W, 2) void tree_stream_kernel(const TreeParams
 // ---- fp32: W waves, RW side by side on rows (16 each), W / RW on the keys (blocks of 16); the fp32 matrix instruction
 // throughout.  K and V go from memory into operand registers (V's operand has one value per lane: no transposing).
 // Few rows: bound by memory (41 sessions of 16064 to 31443 keys and up to 3 tokens, 1 GB: 190 us, 5.2 TB/s) or, small, by its trips
-// to it: 8 tokens behind 256 take 10.3 us, 5.2 of them three blocks of a wave, 2 in front of the first.  Many rows: by the first
+// to it: 8 tokens behind 256 take 10.2 us, 5.2 of them three blocks of a wave, 2 in front of the first.  Many rows: by the first
 // cache, which every wave reads K and V from for itself (16 KB per 64 products of 128-wide heads): a third to a half of the matrix
 // cores' rate.  Two blocks on their way instead of one were slower for small calls (12.2 against 10.7 us), and so were lines of the
 // second and third asked for with the first (11.1): a longer program.
@@ -1284,11 +1285,10 @@ __global__ __launch_bounds__(64 * W, 2) void tree_fp32_kernel(const TreeParams p
 // cores and the vector unit independent work.  The softmax reference is the maximum of the first tile a row sees and is raised only
 // where a row sum says that it has to be (a probability of 2^40): numerator and denominator carry the same factor, so nothing is
 // lost by a reference that is too low.
-// Bound by the matrix cores: a tile of 64 keys takes a workgroup 3500 clocks alone and 3900 beside the other one of its compute unit,
-// 79 % of them products, at a clock that falls to 1.4 to 1.8 GHz under them.  32 sessions with trees of 24 to 64 tokens over 2048
-// to 16384 keys (G 4: 1.31 GB, 243 GF): 475 us, 510 TF, or 770 with the products of the probabilities' second halves; 64 tokens over
-// 32768 keys (G 8) 112 us.  A small call is made of trips to memory: 26 tokens over 3001 keys 18.7 us, 2.2 to find the piece, 2.5 for
-// ids and first tiles, 1.6 a tile, 1.9 at the end, 4.7 for the join.
+// Bound by the matrix cores, busy 52 to 56 % of the time (tiles whose last waves have no rows, starts and ends of pieces).  32 sessions
+// with trees of 24 to 64 tokens over 2048 to 16384 keys (G 4: 1.31 GB, 243 GF): 475 us, 512 TF, or 770 with the products of the
+// probabilities' second halves; 64 tokens over 32768 keys (G 8) 112 us.  A small call is made of trips to memory: 26 tokens over 3001
+// keys 18.1 us, 2.2 to find the piece, 2.5 for ids and first tiles, 1.6 a tile, 1.9 at the end, 4.6 for the join.
 constexpr int kWideKeys = 64;
 constexpr float kRaiseSum = 1.0995116e12f;  // 2^40
 
@@ -1817,7 +1817,7 @@ __device__ __forceinline__ void join_rows(const TreeParams& p, const PartNote& i
 }
 
 // Wide tiles: the workgroups of the tile's pieces take their shares of the 16-byte vectors of a thread, thread by thread as they were
-// written.  32 wide trees (1640 pieces of 64 KB) take 24 us, one user's 24 pieces 4.7.
+// written.  32 wide trees (1640 pieces of 64 KB) take 23 to 25 us, one user's 24 pieces 4.6.
 template <int D>
 __global__ __launch_bounds__(256) void tree_join_wide_kernel(const TreeParams p) {
   typedef __bf16 T;
@@ -1877,8 +1877,8 @@ __global__ __launch_bounds__(256) void tree_join_ranges_kernel(const TreeParams 
 // host side
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kWideSlots = 512;    // workgroups of wide tiles that are on the chip at once: two per compute unit
-// and that the key axis is cut for at most, all kv-heads together: two rounds level out what sessions differ by (32 wide trees 482 us,
-// 489 with one round)
+// and that the key axis is cut for at most, all kv-heads together: two rounds level out what sessions differ by (32 wide trees take
+// 1.5 % longer with one)
 constexpr int kWidePieces = 1024;
 constexpr int kRanges = 256;       // the same for ranges: one workgroup per compute unit (twice as many of half the waves: equal)
 constexpr int kStreamWaves = 8;
