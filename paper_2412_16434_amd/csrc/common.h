@@ -21,6 +21,9 @@ inline int elem_bytes_of(int32_t dtype) { return dtype == SYMPH_BF16 ? 2 : (dtyp
 
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Whether a grid takes so many workgroups along an axis: it has less than 2^32 threads there.
+inline bool grid_takes(int64_t groups, int64_t threads) { return groups <= 0xFFFFFFFFLL / threads; }
+
 // Host-side checks every entry point shares. Returns SYMPH_OK or the status to hand back.
 int32_t validate_cache(const symph_kv_cache* c);
 

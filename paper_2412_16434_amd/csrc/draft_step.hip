@@ -487,6 +487,7 @@ int32_t symph_tree_mask(const int32_t* d_parents, const int32_t* d_cu_new_lens, 
   p.max_new = max_new_len;
   p.words = mask_words;
   const unsigned threads = max_new_len <= 64 ? 64 : 256;
+  if (!grid_takes(n_sessions, threads)) return SYMPH_EUNSUPPORTED;
   const unsigned lds = (unsigned)((max_new_len + 63) & ~63) * 10 + threads * kMaskPitch * 8;
   hipLaunchKernelGGL(tree_mask_kernel, dim3((unsigned)n_sessions, (max_new_len + threads - 1) / threads), dim3(threads), lds,
                      (hipStream_t)stream, p);
@@ -501,6 +502,8 @@ int32_t symph_tree_accept(const int32_t* d_draft_tokens, const int32_t* d_parent
   if (n_sessions == 0) return SYMPH_OK;
   if (!d_cu_new_lens || !d_n_accepted || !d_next_tokens || (d_new_prefix_lens && !d_prefix_lens)) return SYMPH_EINVAL;
   if (total_new_tokens > 0 && (!d_draft_tokens || !d_parents || !d_target_tokens || !d_rows)) return SYMPH_EINVAL;
+  const int64_t groups = ceil_div64(n_sessions, 4);
+  if (!grid_takes(groups, 256)) return SYMPH_EUNSUPPORTED;
   AcceptParams p;
   p.draft = d_draft_tokens;
   p.parents = d_parents;
@@ -513,7 +516,7 @@ int32_t symph_tree_accept(const int32_t* d_draft_tokens, const int32_t* d_parent
   p.new_prefix_lens = d_new_prefix_lens;
   p.n_sessions = n_sessions;
   p.total = total_new_tokens;
-  hipLaunchKernelGGL(tree_accept_kernel, dim3((unsigned)((n_sessions + 3) / 4)), dim3(256), 0, (hipStream_t)stream, p);
+  hipLaunchKernelGGL(tree_accept_kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)stream, p);
   return hipGetLastError() == hipSuccess ? SYMPH_OK : SYMPH_ELAUNCH;
 }
 
@@ -526,7 +529,8 @@ int32_t symph_kv_commit(const symph_kv_cache* cache, const void* d_k_new, const 
   if (!d_k_new || !d_v_new || !d_rows || !d_slot_map) return SYMPH_EINVAL;
   const int eb = elem_bytes_of(cache->dtype);
   const int64_t row_bytes = (int64_t)cache->n_kv_heads * cache->head_dim * eb;
-  if (row_bytes > 0x7FFFFFFF || cache->n_layers > 65535) return SYMPH_EUNSUPPORTED;
+  const int64_t groups = ceil_div64(n_entries, 64);
+  if (row_bytes > 0x7FFFFFFF || cache->n_layers > 65535 || !grid_takes(groups, 256)) return SYMPH_EUNSUPPORTED;
   CommitParams p;
   p.k_base = (char*)cache->k_base;
   p.v_base = (char*)cache->v_base;
@@ -548,7 +552,7 @@ int32_t symph_kv_commit(const symph_kv_cache* cache, const void* d_k_new, const 
   p.n_blocks = cache->n_blocks;
   p.n_rows = n_rows;
   p.n_entries = n_entries;
-  const dim3 grid((unsigned)(((int64_t)n_entries + 63) / 64), (unsigned)cache->n_layers);
+  const dim3 grid((unsigned)groups, (unsigned)cache->n_layers);
   if (vec == 16)
     hipLaunchKernelGGL(kv_commit_kernel<u32x4>, grid, dim3(256), 0, (hipStream_t)stream, p);
   else

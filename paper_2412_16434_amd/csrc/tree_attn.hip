@@ -1963,7 +1963,8 @@ static bool plan_tree(TreePlan& pl, const symph_kv_cache* c, int32_t n_sessions,
   pl.bytes = !pl.cut ? 0 : pl.wide ? pl.pieces * c->n_kv_heads * (c->head_dim == 128 ? kWideSlot<128> : kWideSlot<64>) * 4
                                    : 2 * pl.pieces * c->n_kv_heads * (BM * (c->head_dim + 2) * 4 + (int64_t)sizeof(PartNote));
   if (ceil_div64(rows, BM) * blocks > kMostWork) return false;
-  return 2 * pl.pieces * c->n_kv_heads <= 0x7FFFFFFFLL;
+  return grid_takes(pl.pieces * c->n_kv_heads, pl.wide ? 256 : 64 * pl.waves) &&
+         (!pl.cut || pl.wide || grid_takes(2 * pl.pieces * c->n_kv_heads, 256));  // (the join of ranges)
 }
 
 template <typename T, int D, int RW>
@@ -2101,6 +2102,7 @@ int32_t symph_tree_attn(const symph_kv_cache* cache, int32_t layer, const void* 
   const uintptr_t address_bits = (uintptr_t)p.k_layer | (uintptr_t)p.v_layer | (uintptr_t)d_q | (uintptr_t)d_k_new |
                                  (uintptr_t)d_v_new | (uintptr_t)d_out | (uintptr_t)block_bytes;
   const bool wide = (address_bits & 15) == 0;
+  if (!wide && !grid_takes((int64_t)total_new_tokens * n_q_heads, 64)) return SYMPH_EUNSUPPORTED;
   if (pl.bytes > 0 && (!d_workspace || workspace_bytes < pl.bytes)) return SYMPH_EWORKSPACE;
   if (pl.bytes > 0 && ((uintptr_t)d_workspace & 15) != 0) return SYMPH_EUNSUPPORTED;
   if (cache->dtype == SYMPH_BF16)
