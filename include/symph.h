@@ -358,7 +358,8 @@ int32_t symph_debug_check_tables(const symph_kv_cache* cache, const int32_t* d_b
  *   symph_tree_accept    the accepted path, the next root
  *   symph_kv_commit      its K,V rows, all layers, into the cache
  * after which the lengths that symph_tree_accept wrote are the next step's prefix lengths.  Calls that would need 2^32 threads or
- * more (2^24 sessions, 2^30 entries, 2^26 rows of attention away from 16-byte addresses) are refused: SYMPH_EUNSUPPORTED.
+ * more (2^24 trees past 64 nodes, 2^30 entries to commit, 2^26 rows of attention away from 16-byte addresses) are refused:
+ * SYMPH_EUNSUPPORTED.
  */
 
 /*
