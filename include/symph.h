@@ -457,6 +457,119 @@ int32_t symph_tree_accept(const int32_t* d_draft_tokens, const int32_t* d_parent
 int32_t symph_kv_commit(const symph_kv_cache* cache, const void* d_k_new, const void* d_v_new, int32_t n_rows,
                         const int32_t* d_rows, const int64_t* d_slot_map, int32_t n_entries, void* stream);
 
+/*
+ * Beam search over the paged cache.  Every row of the block table is a beam: one of the continuations of its session that are still
+ * pursued.  Beams of a session share the blocks of the tokens that they have in common; d_refs int32 [n_blocks] holds, for every
+ * block of the pool, how many rows hold it (0: free).  A step, behind the model's logits for every beam's last token, is
+ *   symph_beam_select     the best continuations of every session: token, score and the beam it continues
+ *   symph_kv_fork         table rows for them, reference counts, copies to make of blocks that are not full
+ *   symph_kv_copy_blocks  those copies, all layers
+ *   symph_kv_free         the free list for the next step (and rows of sessions that are done)
+ *   symph_build_tables, symph_kv_append and the attention calls for the next token, a beam being a session of theirs.
+ * A prompt in one row becomes several beams by a fork whose parents name the row several times.  symph_kv_compact says which blocks
+ * move so that the end of a pool becomes free.  Contract on blocks: only full blocks are shared (what these calls keep); a row that
+ * holds blocks behind those in use (symph_build_tables' d_held_blocks) holds them alone.
+ * symph_kv_fork, symph_kv_free and symph_kv_compact write new tables and counts and leave the ones they read as they were, so a step
+ * that found too few free blocks is undone by dropping its outputs.  They do no work in memory but in what they are given; results
+ * are the same from call to call.  A row's blocks are the first H entries of its table row: ceil(len / block_size), or its entry of
+ * d_held_blocks (may be NULL) where that is more, table_stride at most.  Lengths below 0 count as 0; table entries outside
+ * [0, n_blocks) are carried over and hold nothing.
+ */
+
+/*
+ * The best continuations of every session.  Session s has beams d_cu_rows[s] .. d_cu_rows[s+1]-1 (rows of d_logits
+ * [n_rows][row_stride], of `dtype` (symph_dtype), `vocab` of row_stride values each) and wants W_s = d_cu_next[s+1] - d_cu_next[s]
+ * continuations.  A candidate is a token t behind a beam r; with x = d_logits and d_scores fp32 [n_rows] it has
+ *   score(r, t) = d_scores[r] + x[r][t] - log sum_u exp x[r][u].
+ * Candidates are ordered by score, then by the lower beam, then by the lower token.  Written at entries cu_next[s] + k, for the
+ * session's k-th candidate that does not end (t != end_token; a negative end_token: none ends):
+ *   d_parents int32: its beam r, as symph_kv_fork takes it;  d_tokens int32: t;  d_next_scores fp32: its score;
+ * -1, -1 and -infinity where there are fewer, and from max_next on.  Written per beam, where d_end_scores (fp32 [n_rows]) is not NULL:
+ * score(r, end_token) where that is among the first W_s (at most max_next) of ALL candidates of the session, else -infinity.
+ * No candidates: tokens with a logit of -infinity or NaN (they add nothing to the sum), beams whose score is not finite (an ended
+ * beam's is -infinity; their logits are not read).  A logit of +infinity counts as the largest fp32 number.
+ * max_next >= max W_s, at most SYMPH_BEAM_MAX; total_next: entries of the outputs.  row_stride in elements, any address of the type.
+ * Entries behind the last session's, and rows behind its beams, are left as they were.  d_next_scores must not be d_scores.
+ * d_workspace: at least symph_beam_select_workspace_bytes(...) bytes, 256-byte aligned; nothing has to be cleared.
+ * Arithmetic: exponentials in fp32, their sums, the logarithm and the scores in 64 bits, so that nearly equal scores of different
+ * beams keep their order to about 1e-8; scores are rounded to fp32 once.  Beams with the same logits and score tie exactly.
+ */
+#define SYMPH_BEAM_MAX 64
+int32_t symph_beam_select(const void* d_logits, int64_t row_stride, int32_t dtype, int32_t n_rows, int32_t vocab,
+                          const float* d_scores, const int32_t* d_cu_rows, const int32_t* d_cu_next, int32_t n_sessions,
+                          int32_t total_next, int32_t max_next, int32_t end_token, int32_t* d_parents, int32_t* d_tokens,
+                          float* d_next_scores, float* d_end_scores, void* d_workspace, int64_t workspace_bytes, void* stream);
+/* Scratch bytes symph_beam_select needs for these values (the same as in the call; 0 is possible).  Negative on bad input. */
+int64_t symph_beam_select_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t max_next);
+
+/*
+ * Rows that continue other rows: row j of the result (n_out rows) takes over the tokens of row p = d_parents[j] of the table (n_rows
+ * rows); any value outside 0 .. n_rows-1 makes an empty row.  A row without a child gives its blocks up.  With len = d_lens[p]:
+ *   d_lens_out[j]  = len (0 for an empty row);
+ *   d_table_out    row j: the full blocks of p are shared.  The first child of p (the lowest j) goes on in p's last block and keeps
+ *                  all that p holds; every other child gets, where len % block_size > 0, a new block in its place, the next id of
+ *                  d_free_blocks [n_free], taken in order of j from entry *d_free_begin on (NULL: from 0); -1 where the list has
+ *                  ended (or holds an id outside [0, n_blocks)).  Entries behind a row's blocks are left as they were;
+ *   d_held_out[j]  entries of the row that it holds now (may be NULL);
+ *   d_copy_src[j], d_copy_dst[j], d_copy_tokens[j]: for a row with a new block, what symph_kv_copy_blocks has to copy: p's last
+ *                  block, the new one, len % block_size; -1, -1 and 0 for the others;
+ *   d_refs_after   int32 [n_blocks]: d_refs and the changes; a block whose count has become 0 is free (symph_kv_free lists them);
+ *   d_blocks_taken int32 [1] (may be NULL): *d_free_begin + the blocks that the copies need, i.e. the next *d_free_begin; more than
+ *                  n_free says that the list was too short.
+ * Outputs must not be the inputs they belong to.  At most SYMPH_FORK_MAX_ROWS rows in and out each, else SYMPH_EUNSUPPORTED.
+ */
+#define SYMPH_FORK_MAX_ROWS 8192
+int32_t symph_kv_fork(const int32_t* d_parents, int32_t n_out, const int32_t* d_lens, const int32_t* d_held_blocks, int32_t n_rows,
+                      const int32_t* d_block_table, int32_t table_stride, int32_t block_size, int32_t n_blocks,
+                      const int32_t* d_refs, const int32_t* d_free_blocks, int32_t n_free, const int32_t* d_free_begin,
+                      int32_t* d_table_out, int32_t* d_lens_out, int32_t* d_held_out, int32_t* d_refs_after,
+                      int32_t* d_copy_src, int32_t* d_copy_dst, int32_t* d_copy_tokens, int32_t* d_blocks_taken, void* stream);
+
+/*
+ * Copies blocks of all layers, K and V: for every i with d_src_blocks[i] and d_dst_blocks[i] inside the cache, the first d_tokens[i]
+ * slots (all of them where d_tokens is NULL; at most block_size) of the one go to the other; other i are skipped and no other byte of
+ * the pools changes.  No block may be a destination twice, or a destination of one pair and a source of another: undefined.
+ * Alignment as for symph_kv_pack.
+ */
+int32_t symph_kv_copy_blocks(const symph_kv_cache* cache, const int32_t* d_src_blocks, const int32_t* d_dst_blocks,
+                             const int32_t* d_tokens, int32_t n_pairs, void* stream);
+
+/*
+ * Gives the blocks of dropped rows back and lists the free ones: row r is dropped where d_drop[r] != 0.
+ *   d_refs_after   int32 [n_blocks]: d_refs, less one for every time that a dropped row holds the block;
+ *   d_free_blocks  int32 [n_blocks]: the blocks whose count is then 0 (or less), ascending, -1 behind them; d_n_free int32 [1]: how
+ *                  many.  symph_build_tables and symph_kv_fork take the list as it is (a list with n_free = n_blocks);
+ *   d_lens_after, d_held_after int32 [n_rows] (may be NULL; may be d_lens and d_held_blocks themselves): 0 for dropped rows, else
+ *                  the row's length and the blocks it holds.
+ * n_rows may be 0: the list alone.  d_refs_after must not be d_refs.  d_workspace: at least symph_kv_free_workspace_bytes(n_blocks)
+ * bytes, 256-byte aligned; nothing has to be cleared.
+ */
+int32_t symph_kv_free(const int32_t* d_drop, const int32_t* d_lens, const int32_t* d_held_blocks, int32_t n_rows,
+                      const int32_t* d_block_table, int32_t table_stride, int32_t block_size, int32_t n_blocks,
+                      const int32_t* d_refs, int32_t* d_refs_after, int32_t* d_free_blocks, int32_t* d_n_free,
+                      int32_t* d_lens_after, int32_t* d_held_after, void* d_workspace, int64_t workspace_bytes, void* stream);
+int64_t symph_kv_free_workspace_bytes(int32_t n_blocks);
+
+/*
+ * Which blocks move so that those from n_keep on are free (Sec. 3.3, cooperative memory management: the framework's pool shrinks and
+ * grows beside the caches that are kept for later turns).  A negative n_keep: the number of blocks in use, i.e. everything moves to
+ * the front.  The k-th block in use (d_refs > 0) from n_keep on goes to the k-th block below n_keep that is not, for the first M of
+ * them: M is what there are of either, n_pairs at most.  Nothing is copied here; symph_kv_copy_blocks does that with the lists.
+ *   d_copy_src, d_copy_dst int32 [n_pairs]: the M moves, -1 behind them;
+ *   d_block_map    int32 [n_blocks]: where each block is afterwards (itself where it does not move);
+ *   d_refs_after   int32 [n_blocks]: the counts after the moves (0 for a block that was left);
+ *   d_table_out    (may be d_block_table): the blocks that each row holds after the moves; entries behind them are left as they were;
+ *   d_counts       int32 [3]: blocks in use, M, blocks in use that stay behind n_keep.
+ * d_refs_after and d_block_map must not be d_refs.  d_workspace: at least symph_kv_compact_workspace_bytes(n_blocks) bytes, 256-byte
+ * aligned; nothing has to be cleared.
+ */
+int32_t symph_kv_compact(const int32_t* d_refs, int32_t n_blocks, int32_t n_keep, const int32_t* d_lens,
+                         const int32_t* d_held_blocks, int32_t n_rows, const int32_t* d_block_table, int32_t table_stride,
+                         int32_t block_size, int32_t* d_table_out, int32_t* d_refs_after, int32_t* d_block_map,
+                         int32_t* d_copy_src, int32_t* d_copy_dst, int32_t n_pairs, int32_t* d_counts, void* d_workspace,
+                         int64_t workspace_bytes, void* stream);
+int64_t symph_kv_compact_workspace_bytes(int32_t n_blocks);
+
 /* Plain contiguous device copy with the same 16-byte-per-lane access shape as pack / unpack: the practical
  * HBM ceiling the migration kernels are compared with, and the known-size kernel used to calibrate hardware
  * traffic counters.  bytes must be a multiple of 16, pointers 16-byte aligned. */

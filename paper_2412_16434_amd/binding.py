@@ -21,7 +21,9 @@ EXPORTED_SYMBOLS = (
     "symph_prefix_prefill_attn_workspace_bytes_tuned", "symph_prefix_prefill_attn_static", "symph_debug_attn_flags", "symph_stage_to_host",
     "symph_stage_to_device", "symph_stage_layer_to_host", "symph_stage_layer_to_device", "symph_device_copy",
     "symph_build_tables", "symph_tree_mask", "symph_tree_attn", "symph_tree_attn_workspace_bytes", "symph_tree_accept",
-    "symph_kv_commit", "symph_mfma_reference", "symph_debug_check_tables",
+    "symph_kv_commit", "symph_beam_select", "symph_beam_select_workspace_bytes", "symph_kv_fork", "symph_kv_copy_blocks",
+    "symph_kv_free", "symph_kv_free_workspace_bytes", "symph_kv_compact", "symph_kv_compact_workspace_bytes",
+    "symph_mfma_reference", "symph_debug_check_tables",
     "symph_status_string",
     # symph_pool.h (host code only)
     "symph_pool_create", "symph_pool_destroy", "symph_pool_advise", "symph_pool_drop", "symph_pool_claim",
@@ -120,6 +122,21 @@ def load_library():
     lib.symph_tree_accept.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
     lib.symph_kv_commit.restype = i32
     lib.symph_kv_commit.argtypes = [cp, vp, vp, i32, vp, vp, i32, vp]
+    lib.symph_beam_select.restype = i32
+    lib.symph_beam_select.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, i64, vp]
+    lib.symph_beam_select_workspace_bytes.restype = i64
+    lib.symph_beam_select_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.symph_kv_fork.restype = i32
+    lib.symph_kv_fork.argtypes = [vp, i32, vp, vp, i32, vp, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.symph_kv_copy_blocks.restype = i32
+    lib.symph_kv_copy_blocks.argtypes = [cp, vp, vp, vp, i32, vp]
+    lib.symph_kv_free.restype = i32
+    lib.symph_kv_free.argtypes = [vp, vp, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.symph_kv_compact.restype = i32
+    lib.symph_kv_compact.argtypes = [vp, i32, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, i64, vp]
+    for fn in (lib.symph_kv_free_workspace_bytes, lib.symph_kv_compact_workspace_bytes):
+        fn.restype = i64
+        fn.argtypes = [i32]
     for fn in (lib.symph_stage_to_host, lib.symph_stage_to_device):
         fn.restype = i32
         fn.argtypes = [vp, vp, i64, vp, vp, vp]
@@ -655,6 +672,132 @@ def kv_commit(cache: KVCache, k_new, v_new, rows, slot_map, stream=None) -> None
         C.byref(st), _dev(k_new, "k_new", k.dtype), _dev(v_new, "v_new", k.dtype), k_new.shape[1],
         _vector(rows, "rows", torch.int32), _vector(slot_map, "slot_map", torch.int64, n), n, _stream_ptr(stream)),
         "symph_kv_commit")
+
+
+def beam_select_workspace_bytes(n_rows: int, vocab: int, max_next: int) -> int:
+    n = load_library().symph_beam_select_workspace_bytes(int(n_rows), int(vocab), int(max_next))
+    if n < 0:
+        raise SymphError(-1, "symph_beam_select_workspace_bytes")
+    return int(n)
+
+
+def _scratch(workspace):
+    """(pointer, bytes) of a workspace, which may be None."""
+    if workspace is None:
+        return None, 0
+    return _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
+
+
+def beam_select(logits, scores, cu_rows, cu_next, max_next: int, parents, tokens, next_scores, end_token: int = -1,
+                end_scores=None, workspace=None, stream=None) -> None:
+    """The best ``cu_next[s+1] - cu_next[s]`` continuations of every session over its beams (rows ``cu_rows[s]`` .. of ``logits``
+    [n_rows][vocab], bf16 or fp32, dense along the vocabulary) by score = ``scores`` + log-probability: ``parents`` (the beam's
+    row), ``tokens`` and ``next_scores``, best first; -1, -1 and -inf where there are fewer.  ``end_token`` never continues a beam;
+    its score goes to ``end_scores`` [n_rows] where it is among the session's best."""
+    torch = _torch()
+    i32, f32 = torch.int32, torch.float32
+    if logits.dim() != 2 or logits.dtype not in (torch.bfloat16, f32):
+        raise ValueError("logits must be a bfloat16 or float32 tensor [n_rows][vocab]")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a device tensor")
+    (rows, vocab), (row_stride, step) = logits.shape, logits.stride()
+    if (vocab > 1 and step != 1) or (rows > 1 and row_stride < vocab):
+        raise ValueError("logits must be dense along the vocabulary, rows apart")
+    n, total = cu_rows.shape[0] - 1, parents.shape[0]
+    wp, ws_bytes = _scratch(workspace)
+    _check(load_library().symph_beam_select(
+        logits.data_ptr(), max(row_stride, vocab), SYMPH_BF16 if logits.dtype == torch.bfloat16 else SYMPH_FP32, rows, vocab,
+        _vector(scores, "scores", f32, rows), _vector(cu_rows, "cu_rows", i32, 1), _vector(cu_next, "cu_next", i32, n + 1), n, total,
+        int(max_next), int(end_token), _vector(parents, "parents", i32), _vector(tokens, "tokens", i32, total),
+        _vector(next_scores, "next_scores", f32, total), _vector(end_scores, "end_scores", f32, rows, True), wp, ws_bytes,
+        _stream_ptr(stream)), "symph_beam_select")
+
+
+def _rows_table(t, name: str, rows: int, stride: Optional[int] = None):
+    """(pointer, row stride) of a block table of at least ``rows`` rows."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    tp, width = _table(t, name)
+    if t.shape[0] < rows or (stride is not None and width != stride):
+        raise ValueError(f"{name} must be [{rows}][{'max_blocks' if stride is None else stride}], not {list(t.shape)}")
+    return tp, width
+
+
+def kv_fork(parents, lens, block_table, refs, free_blocks, block_size: int, table_out, lens_out, refs_after, copy_src, copy_dst,
+            copy_tokens, held_blocks=None, held_out=None, free_begin=None, blocks_taken=None, stream=None) -> None:
+    """Rows that continue rows ``parents`` of ``block_table``: full blocks shared, the last one kept by a row's first child and
+    replaced by a block of ``free_blocks`` for the others (``copy_*``: what kv_copy_blocks has to copy); ``refs_after`` <- how many
+    rows hold each block.  A parent outside the table makes an empty row."""
+    i32 = _torch().int32
+    out, n, n_blocks = parents.shape[0], lens.shape[0], refs.shape[0]
+    tp, stride = _rows_table(block_table, "block_table", n)
+    op, _ = _rows_table(table_out, "table_out", out, stride)
+    _check(load_library().symph_kv_fork(
+        _vector(parents, "parents", i32), out, _vector(lens, "lens", i32), _vector(held_blocks, "held_blocks", i32, n, True), n, tp,
+        stride, int(block_size), n_blocks, _vector(refs, "refs", i32), _vector(free_blocks, "free_blocks", i32),
+        free_blocks.shape[0], _vector(free_begin, "free_begin", i32, 1, True), op, _vector(lens_out, "lens_out", i32, out),
+        _vector(held_out, "held_out", i32, out, True), _vector(refs_after, "refs_after", i32, n_blocks),
+        _vector(copy_src, "copy_src", i32, out), _vector(copy_dst, "copy_dst", i32, out),
+        _vector(copy_tokens, "copy_tokens", i32, out), _vector(blocks_taken, "blocks_taken", i32, 1, True), _stream_ptr(stream)),
+        "symph_kv_fork")
+
+
+def kv_copy_blocks(cache: KVCache, src_blocks, dst_blocks, tokens=None, stream=None) -> None:
+    """The first ``tokens[i]`` slots (None: all) of block ``src_blocks[i]`` of every layer into block ``dst_blocks[i]``, for every i
+    where both are blocks of the cache."""
+    st = cache.struct()
+    i32, n = _torch().int32, src_blocks.shape[0]
+    _check(load_library().symph_kv_copy_blocks(
+        C.byref(st), _vector(src_blocks, "src_blocks", i32), _vector(dst_blocks, "dst_blocks", i32, n),
+        _vector(tokens, "tokens", i32, n, True), n, _stream_ptr(stream)), "symph_kv_copy_blocks")
+
+
+def kv_free_workspace_bytes(n_blocks: int) -> int:
+    n = load_library().symph_kv_free_workspace_bytes(int(n_blocks))
+    if n < 0:
+        raise SymphError(-1, "symph_kv_free_workspace_bytes")
+    return int(n)
+
+
+def kv_free(drop, lens, block_table, refs, block_size: int, refs_after, free_blocks, n_free, held_blocks=None, lens_after=None,
+            held_after=None, workspace=None, stream=None) -> None:
+    """``refs_after`` <- ``refs`` without what rows with ``drop[r] != 0`` hold; ``free_blocks`` <- the blocks that nobody holds then,
+    ascending, -1 behind them; ``n_free`` <- how many.  ``drop``, ``lens`` and ``block_table`` may be None: the list alone."""
+    i32 = _torch().int32
+    n, n_blocks = 0 if drop is None else drop.shape[0], refs.shape[0]
+    tp, stride = _rows_table(block_table, "block_table", n) if n else (None, 0)
+    wp, ws_bytes = _scratch(workspace)
+    _check(load_library().symph_kv_free(
+        _vector(drop, "drop", i32, n, n == 0), _vector(lens, "lens", i32, n, n == 0),
+        _vector(held_blocks, "held_blocks", i32, n, True), n, tp, stride, int(block_size), n_blocks, _vector(refs, "refs", i32),
+        _vector(refs_after, "refs_after", i32, n_blocks), _vector(free_blocks, "free_blocks", i32, n_blocks),
+        _vector(n_free, "n_free", i32, 1), _vector(lens_after, "lens_after", i32, n, True),
+        _vector(held_after, "held_after", i32, n, True), wp, ws_bytes, _stream_ptr(stream)), "symph_kv_free")
+
+
+def kv_compact_workspace_bytes(n_blocks: int) -> int:
+    n = load_library().symph_kv_compact_workspace_bytes(int(n_blocks))
+    if n < 0:
+        raise SymphError(-1, "symph_kv_compact_workspace_bytes")
+    return int(n)
+
+
+def kv_compact(refs, n_keep: int, lens, block_table, block_size: int, table_out, refs_after, block_map, copy_src, copy_dst, counts,
+               held_blocks=None, workspace=None, stream=None) -> None:
+    """The moves after which the blocks from ``n_keep`` on are free (negative: all blocks in use move to the front), as lists for
+    kv_copy_blocks, and the table (``table_out`` may be ``block_table``), counts and ``block_map`` after them.  ``counts`` <- blocks
+    in use, moves, blocks that stay behind."""
+    i32 = _torch().int32
+    n, n_blocks, n_pairs = lens.shape[0], refs.shape[0], copy_src.shape[0]
+    tp, stride = _rows_table(block_table, "block_table", n)
+    op, _ = _rows_table(table_out, "table_out", n, stride)
+    wp, ws_bytes = _scratch(workspace)
+    _check(load_library().symph_kv_compact(
+        _vector(refs, "refs", i32), n_blocks, int(n_keep), _vector(lens, "lens", i32),
+        _vector(held_blocks, "held_blocks", i32, n, True), n, tp, stride, int(block_size), op,
+        _vector(refs_after, "refs_after", i32, n_blocks), _vector(block_map, "block_map", i32, n_blocks),
+        _vector(copy_src, "copy_src", i32), _vector(copy_dst, "copy_dst", i32, n_pairs), n_pairs, _vector(counts, "counts", i32, 3),
+        wp, ws_bytes, _stream_ptr(stream)), "symph_kv_compact")
 
 
 def debug_attn_flags(workspace, stream=None) -> int:

@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libsymph.so")
 # Python extension module: the attention call's marshalling (host code only).  The name says which interpreter it is for.
 CALL_LIB = os.path.join(HERE, "_attn_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ("api.hip", "kv_migrate.hip", "prefill_attn.hip", "rows_attn.hip", "attn_static.hip", "tree_attn.hip",
-           "draft_step.hip", "kv_pool.cpp")  # the last one is host code only
+           "draft_step.hip", "beam_select.hip", "kv_blocks.hip", "kv_pool.cpp")  # the last one is host code only
 # packed-fp32 instructions are switched off for every device compile
 HIPCC_FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
                "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]

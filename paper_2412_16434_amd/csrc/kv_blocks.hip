@@ -1,0 +1,598 @@
+// Blocks that rows of a table share: rows that continue other rows (fork), copies of blocks, references given back and the list
+// of free blocks, and the moves that empty a pool's end.  Beside the copies these are a few trips to memory one after another
+// over tables and counts of some megabytes at most; the copies are bound by HBM.
+#include "attn_lanes.h"
+
+#include <algorithm>
+
+namespace symph {
+
+static int shift_of(int64_t x) { return (x & (x - 1)) == 0 ? __builtin_ctzll((unsigned long long)x) : -1; }
+
+// ---- a row's blocks ----------------------------------------------------------------------------------------------
+// Of a row of `len` tokens: blocks that are full, blocks in use, blocks it holds.  A row's blocks end with its table row.
+struct RowBlocks {
+  int whole, used, held;
+};
+struct RowShape {
+  const int32_t* lens;
+  const int32_t* held;
+  int32_t stride, block_size, bs_shift;
+};
+__device__ __forceinline__ RowBlocks blocks_of(const RowShape& s, int len, int held) {
+  const unsigned n = (unsigned)max(len, 0);
+  const unsigned whole = s.bs_shift >= 0 ? n >> s.bs_shift : n / (unsigned)s.block_size;
+  const unsigned used = whole + (whole * (unsigned)s.block_size < n ? 1 : 0), end = (unsigned)s.stride;
+  RowBlocks r;
+  r.whole = (int)min(whole, end);
+  r.used = (int)min(used, end);
+  r.held = (int)min(max(used, (unsigned)max(held, 0)), end);
+  return r;
+}
+__device__ __forceinline__ RowBlocks blocks_of_row(const RowShape& s, int row) {
+  return blocks_of(s, s.lens[row], s.held ? s.held[row] : 0);
+}
+
+constexpr int kThreads = 256;
+
+// Sum over a workgroup's threads (every thread gets it); `at`: four words of LDS that no one else is using.
+__device__ __forceinline__ int group_sum(int v, int* at) {
+  const int incl = wave_inclusive_scan(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) at[threadIdx.x >> 6] = incl;
+  __syncthreads();
+  return at[0] + at[1] + at[2] + at[3];
+}
+// Sum over the threads before this one, and of all of them.
+__device__ __forceinline__ int group_before(int v, int* at, int* total) {
+  const int incl = wave_inclusive_scan(v), wave = threadIdx.x >> 6;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) at[wave] = incl;
+  __syncthreads();
+  int before = incl - v;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+    if (w < wave) before += at[w];
+  *total = at[0] + at[1] + at[2] + at[3];
+  return before;
+}
+
+// ---- fork --------------------------------------------------------------------------------------------------------
+struct ForkParams {
+  RowShape shape;
+  const int32_t* parents;
+  const int32_t* table;
+  const int32_t* refs;
+  const int32_t* free_blocks;
+  const int32_t* free_begin;
+  int32_t* table_out;
+  int32_t* lens_out;
+  int32_t* held_out;
+  int32_t* refs_after;
+  int32_t* copy_src;
+  int32_t* copy_dst;
+  int32_t* copy_tokens;
+  int32_t* blocks_taken;
+  int32_t n_out, n_rows, n_free, n_blocks;
+};
+
+// A workgroup per row of the result, and more that carry the counts over.  A row's place in the free list is the number of rows
+// before it that take a block, which every workgroup counts for itself: `first` [n_rows] holds each row's first child.
+__global__ __launch_bounds__(kThreads) void fork_rows_kernel(const ForkParams p) {
+  extern __shared__ int fork_lds[];
+  int* const first = fork_lds + 4;
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x >= p.n_out) {
+    const int64_t step = (int64_t)(gridDim.x - p.n_out) * kThreads;
+    for (int64_t b = (int64_t)(blockIdx.x - p.n_out) * kThreads + tid; b < p.n_blocks; b += step) p.refs_after[b] = p.refs[b];
+    if ((int)blockIdx.x > p.n_out || p.n_out > 0) return;
+    if (tid == 0 && p.blocks_taken) p.blocks_taken[0] = p.free_begin ? p.free_begin[0] : 0;
+    return;
+  }
+  const int row = blockIdx.x;
+  const bool last = row == p.n_out - 1;
+  for (int i = tid; i < p.n_rows; i += kThreads) first[i] = 0x7FFFFFFF;
+  __syncthreads();
+  for (int i = tid; i <= row; i += kThreads) {
+    const int up = p.parents[i];
+    if (up >= 0 && up < p.n_rows) atomicMin(first + up, i);
+  }
+  __syncthreads();
+  int before = 0;
+  for (int i = tid; i < row; i += kThreads) {
+    const int up = p.parents[i];
+    if (up < 0 || up >= p.n_rows || first[up] == i) continue;
+    const RowBlocks b = blocks_of_row(p.shape, up);
+    before += b.whole < b.used;
+  }
+  before = group_sum(before, fork_lds);
+  const int up = p.parents[row];
+  const bool valid = up >= 0 && up < p.n_rows;
+  const int len = valid ? p.shape.lens[up] : 0;
+  const RowBlocks b = blocks_of(p.shape, len, valid && p.shape.held ? p.shape.held[up] : 0);
+  const bool keeps = valid && first[up] == row, copies = valid && !keeps && b.whole < b.used;
+  const int held = !valid ? 0 : keeps ? b.held : b.used;
+  const int64_t place = (int64_t)(p.free_begin ? p.free_begin[0] : 0) + before;
+  int made = -1;
+  if (copies && place >= 0 && place < p.n_free) made = p.free_blocks[place];
+  if (made < 0 || made >= p.n_blocks) made = -1;
+  const int32_t* const from = p.table + (int64_t)(valid ? up : 0) * p.shape.stride;
+  int32_t* const to = p.table_out + (int64_t)row * p.shape.stride;
+  for (int c = tid; c < held; c += kThreads) to[c] = copies && c == b.whole ? made : from[c];
+  if (tid == 0) {
+    p.lens_out[row] = max(len, 0);
+    if (p.held_out) p.held_out[row] = held;
+    const int src = made >= 0 ? from[b.whole] : -1;
+    const bool pair = src >= 0 && src < p.n_blocks;
+    p.copy_src[row] = pair ? src : -1;
+    p.copy_dst[row] = made;
+    p.copy_tokens[row] = made >= 0 ? len - b.whole * p.shape.block_size : 0;
+    if (last && p.blocks_taken)
+      p.blocks_taken[0] = (int32_t)min(max(place + (copies ? 1 : 0), -(int64_t)0x80000000LL), (int64_t)0x7FFFFFFF);
+  }
+}
+
+// A workgroup per row of the old table: with c children its full blocks have c - 1 holders more, and what else it holds goes to
+// its first child, or to nobody.  One more workgroup counts the new blocks.  (Whole numbers: the order of the additions is free.)
+__global__ __launch_bounds__(kThreads) void fork_refs_kernel(const ForkParams p) {
+  __shared__ int sums[4];
+  const int row = blockIdx.x, tid = threadIdx.x;
+  if (row == p.n_rows) {
+    for (int i = tid; i < p.n_out; i += kThreads) {
+      const int made = p.copy_dst[i];
+      if (made >= 0) atomicAdd(p.refs_after + made, 1);
+    }
+    return;
+  }
+  int children = 0;
+  for (int i = tid; i < p.n_out; i += kThreads) children += p.parents[i] == row;
+  children = group_sum(children, sums);
+  if (children == 1) return;
+  const RowBlocks b = blocks_of_row(p.shape, row);
+  const int32_t* const from = p.table + (int64_t)row * p.shape.stride;
+  const int end = children == 0 ? b.held : b.whole;
+  for (int c = tid; c < end; c += kThreads) {
+    const int id = from[c];
+    if (id >= 0 && id < p.n_blocks) atomicAdd(p.refs_after + id, children - 1);
+  }
+}
+
+// ---- copies of blocks --------------------------------------------------------------------------------------------
+struct CopyParams {
+  char* k_base;
+  char* v_base;
+  const int32_t* src;
+  const int32_t* dst;
+  const int32_t* tokens;
+  int64_t layer_stride_b, block_stride_b;
+  int32_t vecs_per_row, block_size, n_blocks, n_pairs;
+};
+
+// A workgroup has 64 pairs of one layer, or a share of them (blockIdx.z).  The pairs that are there move to the first lanes (a
+// step of beam search leaves many rows without one) and the waves take their K and V in turn, as a contiguous piece each.
+template <typename VecT>
+__global__ __launch_bounds__(kThreads) void copy_blocks_kernel(const CopyParams p) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int i = blockIdx.x * 64 + lane;
+  int src = -1, dst = -1, n = 0;
+  if (i < p.n_pairs) {
+    src = p.src[i];
+    dst = p.dst[i];
+    n = p.tokens ? min(max(p.tokens[i], 0), p.block_size) : p.block_size;
+  }
+  const bool valid = src >= 0 && src < p.n_blocks && dst >= 0 && dst < p.n_blocks && src != dst && n > 0;
+  const uint64_t there = __ballot(valid), below = (1ull << lane) - 1;
+  const int pairs = __popcll(there);
+  const int rank = valid ? __popcll(there & below) : pairs + __popcll(~there & below);
+  src = __builtin_amdgcn_ds_permute(rank * 4, src);
+  dst = __builtin_amdgcn_ds_permute(rank * 4, dst);
+  n = __builtin_amdgcn_ds_permute(rank * 4, n);
+  const int64_t layer_b = (int64_t)blockIdx.y * p.layer_stride_b;
+  for (int unit = blockIdx.z * 4 + wave; unit < pairs * 2; unit += gridDim.z * 4) {
+    const int at = unit >> 1;
+    char* const base = (unit & 1 ? p.v_base : p.k_base) + layer_b;
+    const VecT* const from = reinterpret_cast<const VecT*>(base + (int64_t)__builtin_amdgcn_readlane(src, at) * p.block_stride_b);
+    VecT* const to = reinterpret_cast<VecT*>(base + (int64_t)__builtin_amdgcn_readlane(dst, at) * p.block_stride_b);
+    const int64_t vecs = (int64_t)__builtin_amdgcn_readlane(n, at) * p.vecs_per_row;
+    constexpr int kAhead = 8;
+    for (int64_t v = lane; v < vecs; v += 64 * kAhead) {
+      VecT x[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (v + 64 * u < vecs) x[u] = __builtin_nontemporal_load(from + v + 64 * u);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (v + 64 * u < vecs) __builtin_nontemporal_store(x[u], to + v + 64 * u);
+    }
+  }
+}
+
+// ---- free blocks and moves ---------------------------------------------------------------------------------------
+// The pool's counts in tiles of 1024, so many of them to a workgroup that there are no more workgroups than kMostGroups: each adds
+// up what the ones before it counted.
+constexpr int kEach = 4, kTile = kThreads * kEach, kMostGroups = 2048;
+struct PoolCut {
+  int32_t tiles, groups;  // tiles of a workgroup, workgroups
+};
+static PoolCut cut_pool(int32_t n_blocks) {
+  const int64_t tiles = ceil_div64(n_blocks, kTile);
+  PoolCut c;
+  c.tiles = (int32_t)ceil_div64(tiles, kMostGroups);
+  c.groups = (int32_t)ceil_div64(tiles, c.tiles);
+  return c;
+}
+static int64_t round256(int64_t n) { return (n + 255) & ~(int64_t)255; }
+
+struct FreeParams {
+  RowShape shape;
+  const int32_t* drop;
+  const int32_t* table;
+  const int32_t* refs;
+  int32_t* refs_after;
+  int32_t* free_blocks;
+  int32_t* n_free;
+  int32_t* lens_after;
+  int32_t* held_after;
+  int32_t* counts;  // per workgroup: blocks that nobody holds
+  int32_t n_rows, n_blocks, tiles;
+};
+
+__global__ __launch_bounds__(kThreads) void free_carry_kernel(const FreeParams p) {
+  __shared__ int sums[4];
+  const int64_t begin = (int64_t)blockIdx.x * p.tiles * kTile;
+  int unused = 0;
+  for (int t = 0; t < p.tiles; ++t)
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int64_t b = begin + (int64_t)t * kTile + u * kThreads + threadIdx.x;
+      if (b >= p.n_blocks) continue;
+      const int r = p.refs[b];
+      p.refs_after[b] = r;
+      unused += r <= 0;
+    }
+  unused = group_sum(unused, sums);
+  if (threadIdx.x == 0) p.counts[blockIdx.x] = unused;
+}
+
+__global__ __launch_bounds__(kThreads) void free_rows_kernel(const FreeParams p) {
+  const int row = blockIdx.x, tid = threadIdx.x;
+  const int len = p.shape.lens[row];
+  const RowBlocks b = blocks_of(p.shape, len, p.shape.held ? p.shape.held[row] : 0);
+  const bool gone = p.drop[row] != 0;
+  if (gone) {
+    const int32_t* const from = p.table + (int64_t)row * p.shape.stride;
+    for (int c = tid; c < b.held; c += kThreads) {
+      const int id = from[c];
+      if (id < 0 || id >= p.n_blocks) continue;
+      if (atomicSub(p.refs_after + id, 1) == 1) atomicAdd(p.counts + id / (p.tiles * kTile), 1);
+    }
+  }
+  __syncthreads();  // (the lengths may be written over)
+  if (tid == 0) {
+    if (p.lens_after) p.lens_after[row] = gone ? 0 : len;
+    if (p.held_after) p.held_after[row] = gone ? 0 : b.held;
+  }
+}
+
+// What the workgroups before this one counted, and all of them.
+__device__ __forceinline__ int counted_before(const int32_t* counts, int groups, int group, int* at, int* total) {
+  int before = 0, all = 0;
+  for (int g = threadIdx.x; g < groups; g += kThreads) {
+    const int n = counts[g];
+    all += n;
+    if (g < group) before += n;
+  }
+  *total = group_sum(all, at);
+  return group_sum(before, at);
+}
+
+__global__ __launch_bounds__(kThreads) void free_list_kernel(const FreeParams p) {
+  __shared__ int sums[4];
+  int total;
+  int at = counted_before(p.counts, gridDim.x, blockIdx.x, sums, &total);
+  if (blockIdx.x == 0 && threadIdx.x == 0) p.n_free[0] = total;
+  const int64_t begin = (int64_t)blockIdx.x * p.tiles * kTile;
+  for (int t = 0; t < p.tiles; ++t) {
+    const int64_t b0 = begin + (int64_t)t * kTile + threadIdx.x * kEach;
+    int unused[kEach], n = 0;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      unused[u] = b0 + u < p.n_blocks && p.refs_after[b0 + u] <= 0;
+      n += unused[u];
+    }
+    int in_tile;
+    int to = at + group_before(n, sums, &in_tile);
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      if (unused[u]) p.free_blocks[to++] = (int32_t)(b0 + u);
+      if (b0 + u >= total && b0 + u < p.n_blocks) p.free_blocks[b0 + u] = -1;  // behind the list's end
+    }
+    at += in_tile;
+  }
+}
+
+struct CompactParams {
+  RowShape shape;
+  const int32_t* refs;
+  const int32_t* table;
+  int32_t* table_out;
+  int32_t* refs_after;
+  int32_t* map;
+  int32_t* src;
+  int32_t* dst;
+  int32_t* result;  // blocks in use, moves, blocks that stay behind
+  int32_t* counts;  // per workgroup: blocks in use
+  int32_t* place;   // per block: which move it leaves or is taken by, -1: none
+  int32_t n_rows, n_blocks, n_keep, n_pairs, tiles;
+};
+
+__global__ __launch_bounds__(kThreads) void compact_count_kernel(const CompactParams p) {
+  __shared__ int sums[4];
+  const int64_t begin = (int64_t)blockIdx.x * p.tiles * kTile;
+  int used = 0;
+  for (int t = 0; t < p.tiles; ++t)
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int64_t b = begin + (int64_t)t * kTile + u * kThreads + threadIdx.x;
+      used += b < p.n_blocks && p.refs[b] > 0;
+    }
+  used = group_sum(used, sums);
+  if (threadIdx.x == 0) p.counts[blockIdx.x] = used;
+}
+
+// The k-th block in use from `keep` on goes to the k-th block below `keep` that is not.
+__global__ __launch_bounds__(kThreads) void compact_moves_kernel(const CompactParams p) {
+  __shared__ int sums[4];
+  const int tid = threadIdx.x;
+  int total;
+  int before = counted_before(p.counts, gridDim.x, blockIdx.x, sums, &total);
+  const int keep = p.n_keep < 0 ? total : min(p.n_keep, p.n_blocks);
+  // Blocks in use below `keep`: the workgroups before the one that has it, and that one's own up to it
+  const int64_t run = (int64_t)p.tiles * kTile;
+  const int edge = (int)min((int64_t)keep / run, (int64_t)gridDim.x);
+  int ignored;
+  int below = counted_before(p.counts, gridDim.x, edge, sums, &ignored);
+  {
+    int n = 0;
+    for (int64_t b = edge * run + tid; b < keep; b += kThreads) n += p.refs[b] > 0;
+    below += group_sum(n, sums);
+  }
+  const int moves = min(min(keep - below, total - below), p.n_pairs);
+  if (blockIdx.x == 0 && tid == 0) {
+    p.result[0] = total;
+    p.result[1] = moves;
+    p.result[2] = total - below - moves;
+  }
+  for (int64_t t = 0; t < p.tiles; ++t) {
+    const int64_t b0 = blockIdx.x * run + t * kTile + tid * kEach;
+    int used[kEach], n = 0;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      used[u] = b0 + u < p.n_blocks && p.refs[b0 + u] > 0;
+      n += used[u];
+    }
+    int in_tile;
+    int used_before = before + group_before(n, sums, &in_tile);
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int64_t b = b0 + u;
+      if (b < p.n_blocks) {
+        int k = -1;
+        if (used[u] && b >= keep) k = used_before - below;
+        if (!used[u] && b < keep) k = (int)(b - used_before);
+        if (k >= moves) k = -1;
+        p.place[b] = k;
+        if (k >= 0) (used[u] ? p.src : p.dst)[k] = (int32_t)b;
+      }
+      used_before += used[u];
+    }
+    before += in_tile;
+  }
+  for (int64_t k = moves + (int64_t)blockIdx.x * kThreads + tid; k < p.n_pairs; k += (int64_t)gridDim.x * kThreads) {
+    p.src[k] = -1;
+    p.dst[k] = -1;
+  }
+}
+
+// The first workgroups have the table's rows, the others the pool.
+__global__ __launch_bounds__(kThreads) void compact_apply_kernel(const CompactParams p) {
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x < p.n_rows) {
+    const int row = blockIdx.x, held = blocks_of_row(p.shape, row).held;
+    for (int c = tid; c < held; c += kThreads) {
+      const int64_t at = (int64_t)row * p.shape.stride + c;
+      int id = p.table[at];
+      if (id >= 0 && id < p.n_blocks) {
+        const int k = p.place[id];
+        if (k >= 0 && p.refs[id] > 0) id = p.dst[k];
+      }
+      p.table_out[at] = id;
+    }
+    return;
+  }
+  const int64_t step = (int64_t)(gridDim.x - p.n_rows) * kThreads;
+  for (int64_t b = (int64_t)(blockIdx.x - p.n_rows) * kThreads + tid; b < p.n_blocks; b += step) {
+    const int k = p.place[b], refs = p.refs[b];
+    const bool leaves = k >= 0 && refs > 0;
+    p.map[b] = leaves ? p.dst[k] : (int32_t)b;
+    p.refs_after[b] = leaves ? 0 : k >= 0 ? p.refs[p.src[k]] : refs;
+  }
+}
+
+// Checks that all of these share: a table of rows.  n_rows == 0 needs no arrays.
+static int32_t check_rows(const int32_t* d_lens, const int32_t* d_table, int32_t table_stride, int32_t n_rows, int32_t block_size,
+                          int32_t n_blocks) {
+  if (n_rows < 0 || table_stride < 0 || block_size <= 0 || n_blocks <= 0) return SYMPH_EINVAL;
+  if (n_rows > 0 && (!d_lens || (table_stride > 0 && !d_table))) return SYMPH_EINVAL;
+  return SYMPH_OK;
+}
+static RowShape shape_of(const int32_t* d_lens, const int32_t* d_held, int32_t table_stride, int32_t block_size) {
+  RowShape s;
+  s.lens = d_lens;
+  s.held = d_held;
+  s.stride = table_stride;
+  s.block_size = block_size;
+  s.bs_shift = shift_of(block_size);
+  return s;
+}
+static int32_t launched() { return hipGetLastError() == hipSuccess ? SYMPH_OK : SYMPH_ELAUNCH; }
+
+}  // namespace symph
+
+using namespace symph;
+
+extern "C" {
+
+int32_t symph_kv_fork(const int32_t* d_parents, int32_t n_out, const int32_t* d_lens, const int32_t* d_held_blocks, int32_t n_rows,
+                      const int32_t* d_block_table, int32_t table_stride, int32_t block_size, int32_t n_blocks,
+                      const int32_t* d_refs, const int32_t* d_free_blocks, int32_t n_free, const int32_t* d_free_begin,
+                      int32_t* d_table_out, int32_t* d_lens_out, int32_t* d_held_out, int32_t* d_refs_after,
+                      int32_t* d_copy_src, int32_t* d_copy_dst, int32_t* d_copy_tokens, int32_t* d_blocks_taken, void* stream) {
+  const int32_t rc = check_rows(d_lens, d_block_table, table_stride, n_rows, block_size, n_blocks);
+  if (rc != SYMPH_OK) return rc;
+  if (n_out < 0 || n_free < 0 || !d_refs || !d_refs_after || (n_free > 0 && !d_free_blocks)) return SYMPH_EINVAL;
+  if (n_out > 0 && (!d_parents || !d_lens_out || !d_copy_src || !d_copy_dst || !d_copy_tokens || (table_stride > 0 && !d_table_out)))
+    return SYMPH_EINVAL;
+  if (d_refs_after == d_refs || (d_blocks_taken && d_blocks_taken == d_free_begin)) return SYMPH_EINVAL;
+  if (n_out > 0 && n_rows > 0 &&
+      (d_lens_out == d_lens || (d_held_out && d_held_out == d_held_blocks) || (table_stride > 0 && d_table_out == d_block_table)))
+    return SYMPH_EINVAL;
+  if (n_rows > SYMPH_FORK_MAX_ROWS || n_out > SYMPH_FORK_MAX_ROWS) return SYMPH_EUNSUPPORTED;
+  ForkParams p;
+  p.shape = shape_of(d_lens, d_held_blocks, table_stride, block_size);
+  p.parents = d_parents;
+  p.table = d_block_table;
+  p.refs = d_refs;
+  p.free_blocks = d_free_blocks;
+  p.free_begin = d_free_begin;
+  p.table_out = d_table_out;
+  p.lens_out = d_lens_out;
+  p.held_out = d_held_out;
+  p.refs_after = d_refs_after;
+  p.copy_src = d_copy_src;
+  p.copy_dst = d_copy_dst;
+  p.copy_tokens = d_copy_tokens;
+  p.blocks_taken = d_blocks_taken;
+  p.n_out = n_out;
+  p.n_rows = n_rows;
+  p.n_free = n_free;
+  p.n_blocks = n_blocks;
+  const int64_t carry = std::min<int64_t>(ceil_div64(n_blocks, kTile), kMostGroups);
+  hipLaunchKernelGGL(fork_rows_kernel, dim3((unsigned)(n_out + carry)), dim3(kThreads), (4 + n_rows) * 4, (hipStream_t)stream, p);
+  hipLaunchKernelGGL(fork_refs_kernel, dim3((unsigned)n_rows + 1), dim3(kThreads), 0, (hipStream_t)stream, p);
+  return launched();
+}
+
+int32_t symph_kv_copy_blocks(const symph_kv_cache* cache, const int32_t* d_src_blocks, const int32_t* d_dst_blocks,
+                             const int32_t* d_tokens, int32_t n_pairs, void* stream) {
+  const int32_t rc = validate_cache(cache);
+  if (rc != SYMPH_OK) return rc;
+  if (n_pairs < 0) return SYMPH_EINVAL;
+  if (n_pairs == 0) return SYMPH_OK;
+  if (!d_src_blocks || !d_dst_blocks) return SYMPH_EINVAL;
+  const int eb = elem_bytes_of(cache->dtype);
+  const int64_t row_bytes = (int64_t)cache->n_kv_heads * cache->head_dim * eb, groups = ceil_div64(n_pairs, 64);
+  if (row_bytes > 0x7FFFFFFF || cache->n_layers > 65535 || !grid_takes(groups, kThreads)) return SYMPH_EUNSUPPORTED;
+  CopyParams p;
+  p.k_base = (char*)cache->k_base;
+  p.v_base = (char*)cache->v_base;
+  p.src = d_src_blocks;
+  p.dst = d_dst_blocks;
+  p.tokens = d_tokens;
+  p.layer_stride_b = cache->layer_stride * eb;
+  p.block_stride_b = cache->block_stride * eb;
+  const uintptr_t align_or = (uintptr_t)p.k_base | (uintptr_t)p.v_base | (uintptr_t)p.layer_stride_b | (uintptr_t)p.block_stride_b |
+                             (uintptr_t)row_bytes;
+  if (align_or & 3) return SYMPH_EUNSUPPORTED;
+  const int vec = (align_or & 15) ? 4 : 16;
+  p.vecs_per_row = (int32_t)(row_bytes / vec);
+  p.block_size = cache->block_size;
+  p.n_blocks = cache->n_blocks;
+  p.n_pairs = n_pairs;
+  const int64_t shares = std::min<int64_t>(32, std::max<int64_t>(1, 8192 / (groups * cache->n_layers)));
+  const dim3 grid((unsigned)groups, (unsigned)cache->n_layers, (unsigned)shares);
+  if (vec == 16)
+    hipLaunchKernelGGL(copy_blocks_kernel<u32x4>, grid, dim3(kThreads), 0, (hipStream_t)stream, p);
+  else
+    hipLaunchKernelGGL(copy_blocks_kernel<unsigned int>, grid, dim3(kThreads), 0, (hipStream_t)stream, p);
+  return launched();
+}
+
+int64_t symph_kv_free_workspace_bytes(int32_t n_blocks) {
+  return n_blocks <= 0 ? SYMPH_EINVAL : round256((int64_t)cut_pool(n_blocks).groups * 4);
+}
+
+int32_t symph_kv_free(const int32_t* d_drop, const int32_t* d_lens, const int32_t* d_held_blocks, int32_t n_rows,
+                      const int32_t* d_block_table, int32_t table_stride, int32_t block_size, int32_t n_blocks,
+                      const int32_t* d_refs, int32_t* d_refs_after, int32_t* d_free_blocks, int32_t* d_n_free,
+                      int32_t* d_lens_after, int32_t* d_held_after, void* d_workspace, int64_t workspace_bytes, void* stream) {
+  const int32_t rc = check_rows(d_lens, d_block_table, table_stride, n_rows, block_size, n_blocks);
+  if (rc != SYMPH_OK) return rc;
+  if (!d_refs || !d_refs_after || !d_free_blocks || !d_n_free || (n_rows > 0 && !d_drop) || workspace_bytes < 0) return SYMPH_EINVAL;
+  if (d_refs_after == d_refs || d_free_blocks == d_refs || d_free_blocks == d_refs_after) return SYMPH_EINVAL;
+  if (!grid_takes(n_rows, kThreads)) return SYMPH_EUNSUPPORTED;
+  if (!d_workspace || workspace_bytes < symph_kv_free_workspace_bytes(n_blocks)) return SYMPH_EWORKSPACE;
+  const PoolCut cut = cut_pool(n_blocks);
+  FreeParams p;
+  p.shape = shape_of(d_lens, d_held_blocks, table_stride, block_size);
+  p.drop = d_drop;
+  p.table = d_block_table;
+  p.refs = d_refs;
+  p.refs_after = d_refs_after;
+  p.free_blocks = d_free_blocks;
+  p.n_free = d_n_free;
+  p.lens_after = d_lens_after;
+  p.held_after = d_held_after;
+  p.counts = (int32_t*)d_workspace;
+  p.n_rows = n_rows;
+  p.n_blocks = n_blocks;
+  p.tiles = cut.tiles;
+  hipLaunchKernelGGL(free_carry_kernel, dim3(cut.groups), dim3(kThreads), 0, (hipStream_t)stream, p);
+  if (n_rows > 0) hipLaunchKernelGGL(free_rows_kernel, dim3((unsigned)n_rows), dim3(kThreads), 0, (hipStream_t)stream, p);
+  hipLaunchKernelGGL(free_list_kernel, dim3(cut.groups), dim3(kThreads), 0, (hipStream_t)stream, p);
+  return launched();
+}
+
+int64_t symph_kv_compact_workspace_bytes(int32_t n_blocks) {
+  return n_blocks <= 0 ? SYMPH_EINVAL : round256((int64_t)cut_pool(n_blocks).groups * 4) + round256((int64_t)n_blocks * 4);
+}
+
+int32_t symph_kv_compact(const int32_t* d_refs, int32_t n_blocks, int32_t n_keep, const int32_t* d_lens,
+                         const int32_t* d_held_blocks, int32_t n_rows, const int32_t* d_block_table, int32_t table_stride,
+                         int32_t block_size, int32_t* d_table_out, int32_t* d_refs_after, int32_t* d_block_map,
+                         int32_t* d_copy_src, int32_t* d_copy_dst, int32_t n_pairs, int32_t* d_counts, void* d_workspace,
+                         int64_t workspace_bytes, void* stream) {
+  const int32_t rc = check_rows(d_lens, d_block_table, table_stride, n_rows, block_size, n_blocks);
+  if (rc != SYMPH_OK) return rc;
+  if (!d_refs || !d_refs_after || !d_block_map || !d_counts || n_pairs < 0 || workspace_bytes < 0) return SYMPH_EINVAL;
+  if (n_pairs > 0 && (!d_copy_src || !d_copy_dst || d_copy_src == d_copy_dst)) return SYMPH_EINVAL;
+  if (n_rows > 0 && table_stride > 0 && !d_table_out) return SYMPH_EINVAL;
+  if (d_refs_after == d_refs || d_block_map == d_refs || d_block_map == d_refs_after) return SYMPH_EINVAL;
+  const PoolCut cut = cut_pool(n_blocks);
+  const int64_t groups = n_rows + (int64_t)std::min<int64_t>(ceil_div64(n_blocks, kTile), kMostGroups);
+  if (!grid_takes(groups, kThreads)) return SYMPH_EUNSUPPORTED;
+  if (!d_workspace || workspace_bytes < symph_kv_compact_workspace_bytes(n_blocks)) return SYMPH_EWORKSPACE;
+  CompactParams p;
+  p.shape = shape_of(d_lens, d_held_blocks, table_stride, block_size);
+  p.refs = d_refs;
+  p.table = d_block_table;
+  p.table_out = d_table_out;
+  p.refs_after = d_refs_after;
+  p.map = d_block_map;
+  p.src = d_copy_src;
+  p.dst = d_copy_dst;
+  p.result = d_counts;
+  p.counts = (int32_t*)d_workspace;
+  p.place = (int32_t*)((char*)d_workspace + round256((int64_t)cut.groups * 4));
+  p.n_rows = n_rows;
+  p.n_blocks = n_blocks;
+  p.n_keep = n_keep;
+  p.n_pairs = n_pairs;
+  p.tiles = cut.tiles;
+  hipLaunchKernelGGL(compact_count_kernel, dim3(cut.groups), dim3(kThreads), 0, (hipStream_t)stream, p);
+  hipLaunchKernelGGL(compact_moves_kernel, dim3(cut.groups), dim3(kThreads), 0, (hipStream_t)stream, p);
+  hipLaunchKernelGGL(compact_apply_kernel, dim3((unsigned)groups), dim3(kThreads), 0, (hipStream_t)stream, p);
+  return launched();
+}
+
+}  // extern "C"
