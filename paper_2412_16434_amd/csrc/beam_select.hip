@@ -1,8 +1,11 @@
 // The best continuations of every session over its beams and the vocabulary.  A candidate is a token t behind a beam r; its score is
 //   score(r, t) = scores[r] + x[r][t] - log sum_u exp x[r][u]
-// and candidates are ordered by score, then beam, then token.  Bound by reading the logits once.
-#include "common.h"
+// and candidates are ordered by score, then beam, then token.  Bound by reading the logits once, which the first launch does: every
+// workgroup goes over a part of a row and leaves its largest value, its sum of exponentials and its best tokens.  The second
+// launch joins them session by session.
+#include "attn_lanes.h"
 
+#include <algorithm>
 #include <float.h>
 #include <math.h>
 
@@ -17,144 +20,519 @@ struct BeamParams {
   int32_t* tokens;
   float* next_scores;
   float* end_scores;
-  double* log_sums;    // [n_rows]
-  float* cand_value;   // [n_rows][max_next]: a row's best tokens, best first
-  int32_t* cand_token; // -1: no more
+  // Of each part of a row: sum of exp(x - top), that top, its best tokens (-1: no more)
+  double* part_sum;     // [n_rows][parts]
+  float* part_top;      // [n_rows][parts]
+  float* cand_value;    // [n_rows][parts][max_next]
+  int32_t* cand_token;
+  float* end_logit;     // [n_rows]
+  double* end_value;    // [n_rows], for sessions of many beams
   int64_t row_stride;
-  int32_t n_rows, vocab, n_sessions, total_next, max_next, end_token;
+  int32_t n_rows, vocab, n_sessions, total_next, max_next, end_token, parts, part_tiles;
+  int32_t wide;  // fp32
 };
 
 __device__ __forceinline__ float clean(float x) { return x != x ? -INFINITY : fminf(x, FLT_MAX); }
-template <typename T>
-__device__ __forceinline__ float value_at(const char* row, int64_t i) {
-  return clean((float)reinterpret_cast<const T*>(row)[i]);
-}
 __device__ __forceinline__ bool alive(float score) { return fabsf(score) <= FLT_MAX; }
 
-template <typename T>
-__global__ __launch_bounds__(256) void beam_rows_kernel(const BeamParams p) {
-  __shared__ float value[256];
-  __shared__ int where[256];
-  __shared__ double sums[256];
-  const int row = blockIdx.x, tid = threadIdx.x;
-  if (!alive(p.scores[row])) return;
-  const char* const x = p.logits + (int64_t)row * p.row_stride * sizeof(T);
-  float best = -INFINITY;
-  for (int i = tid; i < p.vocab; i += 256) best = fmaxf(best, value_at<T>(x, i));
-  value[tid] = best;
-  __syncthreads();
-  for (int h = 128; h > 0; h >>= 1) {
-    if (tid < h) value[tid] = fmaxf(value[tid], value[tid + h]);
-    __syncthreads();
-  }
-  const float top = fmaxf(value[0], -FLT_MAX);
-  double sum = 0;
-  for (int i = tid; i < p.vocab; i += 256) sum += (double)expf(value_at<T>(x, i) - top);
-  sums[tid] = sum;
-  __syncthreads();
-  for (int h = 128; h > 0; h >>= 1) {
-    if (tid < h) sums[tid] += sums[tid + h];
-    __syncthreads();
-  }
-  if (tid == 0) p.log_sums[row] = (double)top + log(sums[0]);
-  float last_value = INFINITY;
-  int last = -1;
-  for (int k = 0; k < p.max_next; ++k) {
-    float v = -INFINITY;
-    int at = -1;
-    for (int i = tid; i < p.vocab; i += 256) {
-      const float y = value_at<T>(x, i);
-      if (i != p.end_token && (y < last_value || (y == last_value && i > last)) && y > v) v = y, at = i;
-    }
-    __syncthreads();
-    value[tid] = v;
-    where[tid] = at;
-    __syncthreads();
-    for (int h = 128; h > 0; h >>= 1) {
-      if (tid < h && (value[tid + h] > value[tid] || (value[tid + h] == value[tid] && (unsigned)where[tid + h] < (unsigned)where[tid])))
-        value[tid] = value[tid + h], where[tid] = where[tid + h];
-      __syncthreads();
-    }
-    last_value = value[0];
-    last = where[0];
-    if (tid == 0) {
-      p.cand_value[(int64_t)row * p.max_next + k] = last_value;
-      p.cand_token[(int64_t)row * p.max_next + k] = last;
-    }
-  }
+// ---- the best of a list ------------------------------------------------------------------------------------------
+// Values as whole numbers of the same order (zeros of both signs are equal), and back.
+__device__ __forceinline__ uint32_t key_of(float x) {
+  const int32_t b = __float_as_int(x + 0.0f);
+  return (uint32_t)(b ^ ((b >> 31) | (int32_t)0x80000000));
+}
+__device__ __forceinline__ float value_of(uint32_t k) {
+  return __int_as_float((int32_t)(k & 0x80000000u ? k ^ 0x80000000u : ~k));
+}
+__device__ __forceinline__ uint64_t key_of(double x) {
+  const int64_t b = __double_as_longlong(x + 0.0);
+  return (uint64_t)(b ^ ((b >> 63) | (int64_t)0x8000000000000000LL));
 }
 
-// A candidate, and whether one comes before another.  (Within a beam the logits decide: far from the sum's logarithm 64 bits do not
-// tell their scores apart.)
-struct Candidate {
-  double score;
-  float logit;
-  int row, token;
+// Lanes of the mask before this one
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The value of lane l ^ M.  Inside a row of 16 lanes by data-parallel moves, beyond by exchanging rows or halves.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+}
+template <int M>
+__device__ __forceinline__ uint32_t from_lane_xor(uint32_t v) {
+  static_assert(M == 1 || M == 2 || M == 3 || M == 4 || M == 7 || M == 8 || M == 15 || M == 16 || M == 31 || M == 32 || M == 63, "");
+  if constexpr (M == 1) return moved<0xB1>(v);        // quad_perm:[1,0,3,2]
+  if constexpr (M == 2) return moved<0x4E>(v);        // quad_perm:[2,3,0,1]
+  if constexpr (M == 3) return moved<0x1B>(v);        // quad_perm:[3,2,1,0]
+  if constexpr (M == 7) return moved<0x141>(v);       // row_half_mirror
+  if constexpr (M == 4) return moved<0x1B>(moved<0x141>(v));
+  if constexpr (M == 8) return moved<0x128>(v);       // row_ror:8
+  if constexpr (M == 15) return moved<0x140>(v);      // row_mirror
+  if constexpr (M == 16) {
+    uint32_t x = v, y = v;  // even rows twice, odd rows twice
+    asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+    return threadIdx.x & 16 ? x : y;
+  }
+  if constexpr (M == 32) {
+    uint32_t x = v, y = v;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+    return threadIdx.x & 32 ? x : y;
+  }
+  if constexpr (M == 31) return from_lane_xor<16>(from_lane_xor<15>(v));
+  if constexpr (M == 63) return from_lane_xor<32>(from_lane_xor<31>(v));
+  return v;
+}
+
+// An entry of WORDS words, ordered by them, the first before the others.  64 entries, one to a lane, are sorted by exchanges between
+// lanes, the largest into lane 0; no two are equal but empty ones (all words 0).  The time does not depend on the values.
+template <int WORDS>
+struct Entry {
+  uint32_t w[WORDS];
 };
-__device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) {
-  if (a.score != b.score) return a.score > b.score;
-  if (a.row != b.row) return a.row < b.row;
-  return a.logit > b.logit || (a.logit == b.logit && a.token < b.token);
+// (the fourth of four words comes along and does not count)
+template <int WORDS>
+__device__ __forceinline__ bool over(const Entry<WORDS>& a, const Entry<WORDS>& b) {
+  if constexpr (WORDS == 1) return a.w[0] > b.w[0];
+  const uint64_t x = (uint64_t)a.w[0] << 32 | a.w[WORDS > 1 ? 1 : 0], y = (uint64_t)b.w[0] << 32 | b.w[WORDS > 1 ? 1 : 0];
+  if constexpr (WORDS == 2) return x > y;
+  return x > y || (x == y && a.w[WORDS > 2 ? 2 : 0] > b.w[WORDS > 2 ? 2 : 0]);
+}
+// The larger of lane l's and lane l ^ M's goes to the lower of the two lanes
+template <int M, int WORDS>
+__device__ __forceinline__ void exchange(Entry<WORDS>& e) {
+  Entry<WORDS> o;
+#pragma unroll
+  for (int k = 0; k < WORDS; ++k) o.w[k] = from_lane_xor<M>(e.w[k]);
+  constexpr int kHigh = M & (M + 1) ? M : (M + 1) / 2;  // (the bit that tells which lane is the lower one)
+  const bool lower = (threadIdx.x & kHigh) == 0, take = over(o, e) == lower;
+#pragma unroll
+  for (int k = 0; k < WORDS; ++k) e.w[k] = take ? o.w[k] : e.w[k];
+}
+template <int WORDS>
+__device__ __forceinline__ void sort_rest(Entry<WORDS>& e) {  // sequences of 16 that rise and fall
+  exchange<8>(e);
+  exchange<4>(e);
+  exchange<2>(e);
+  exchange<1>(e);
+}
+template <int WORDS>
+__device__ __forceinline__ void sort64(Entry<WORDS>& e) {
+  exchange<1>(e);
+  exchange<3>(e);
+  exchange<1>(e);
+  exchange<7>(e);
+  exchange<2>(e);
+  exchange<1>(e);
+  exchange<15>(e);
+  exchange<4>(e);
+  exchange<2>(e);
+  exchange<1>(e);
+  exchange<31>(e);
+  sort_rest(e);
+  exchange<63>(e);
+  exchange<16>(e);
+  sort_rest(e);
+}
+// The 64 largest of two sorted sequences, sorted
+template <int WORDS>
+__device__ __forceinline__ void join64(Entry<WORDS>& e, const Entry<WORDS>& with) {
+  Entry<WORDS> o;
+#pragma unroll
+  for (int k = 0; k < WORDS; ++k) o.w[k] = from_lane_xor<63>(with.w[k]);
+  const bool take = over(o, e);
+#pragma unroll
+  for (int k = 0; k < WORDS; ++k) e.w[k] = take ? o.w[k] : e.w[k];
+  exchange<32>(e);
+  exchange<16>(e);
+  sort_rest(e);
+}
+
+// ---- parts of rows -----------------------------------------------------------------------------------------------
+constexpr int kValues = 32, kTile = 64 * kValues, kWaves = 4;  // a lane's values of a tile, a wave's tile
+
+typedef unsigned int u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));  // (rows begin at any element)
+typedef unsigned int u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T>
+struct Loads;
+template <>
+struct Loads<__bf16> {
+  typedef u32x4_at2 Vec;
+  static constexpr int kPer = 8;
+  static __device__ __forceinline__ float at(const u32x4& v, int j) {
+    return __uint_as_float(j & 1 ? v[j >> 1] & 0xFFFF0000u : v[j >> 1] << 16);
+  }
+};
+template <>
+struct Loads<float> {
+  typedef u32x4_at4 Vec;
+  static constexpr int kPer = 4;
+  static __device__ __forceinline__ float at(const u32x4& v, int j) { return __uint_as_float(v[j]); }
+};
+
+// A lane's vectors of a whole tile that begins at `from`.  Which lane has which value follows from the index alone, not from addresses:
+// equal rows have equal sums.
+template <typename T>
+__device__ __forceinline__ void load_tile(u32x4 (&raw)[kValues / Loads<T>::kPer], const T* from) {
+  constexpr int kPer = Loads<T>::kPer;
+#pragma unroll
+  for (int u = 0; u < kValues / kPer; ++u)
+    raw[u] = *reinterpret_cast<const typename Loads<T>::Vec*>(from + (u * 64 + (threadIdx.x & 63)) * kPer);
+}
+
+// (fmaxf would first quieten every operand; a signalling NaN comes out as a NaN here, which is looked for behind the sum)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+constexpr int kQueue = 384, kSortFrom = 24;  // entries that can wait, and from how many on they are sorted in behind a tile
+constexpr int kGroup = 4, kGroups = kValues / kGroup;  // values that are looked at together for candidates
+
+// exp(x - top) with the rest of log2 e: the constant's own rounding would be the same for all tokens far below the top
+__device__ __forceinline__ float exp_below(float x, float top) {
+  const float d = x - top;
+  return __builtin_amdgcn_exp2f(fmaf(d, 1.44269502e+00f, d * 1.92596300e-08f));
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void beam_sessions_kernel(const BeamParams p) {
-  __shared__ Candidate best[256], chosen[SYMPH_BEAM_MAX];
-  const int s = blockIdx.x, tid = threadIdx.x;
+__global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamParams p) {
+  __shared__ uint32_t queues[kWaves][2][kQueue];
+  __shared__ unsigned long long shared_least;  // `least` and ~`seen` of the wave whose best reach furthest
+  __shared__ float tops[kWaves];
+  __shared__ double sums[kWaves];
+  const int part = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  if (!alive(p.scores[row])) return;
+  constexpr int kPer = Loads<T>::kPer, kVecs = kValues / kPer;
+  const T* const x0 = reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.row_stride;
+  const int first = part * p.part_tiles, end = min(first + p.part_tiles, (p.vocab + kTile - 1) / kTile);
+  uint32_t (&queue)[2][kQueue] = queues[wave];
+  if (threadIdx.x == 0) shared_least = 0;
+  __syncthreads();
+
+  float top = -FLT_MAX;
+  double sum = 0;
+  Entry<2> best = {};  // the wave's best so far, sorted: key_of the value, ~token; what is still to be sorted in waits in the queue
+  int n = 0;
+  const int wanted = p.max_next;
+  // As many values as are wanted reach the key `least`, in tiles up to `seen`: later ones have to pass it (0: there are not as many yet)
+  uint32_t least = 0;
+  int seen = 0;
+  u32x4 raw[kVecs];
+  int tile = first + wave, from = 0;  // from > 0: the tile's candidates from that group on are still to be looked at
+  if ((tile + 1) * kTile <= p.vocab && tile < end) load_tile<T>(raw, x0 + tile * kTile);
+  while (tile < end) {
+    const int base = tile * kTile;
+    const bool whole = base + kTile <= p.vocab;
+    float x[kValues], most[kGroups];
+    if (whole) {
+#pragma unroll
+      for (int v = 0; v < kValues; ++v) x[v] = Loads<T>::at(raw[v / kPer], v % kPer);
+    } else {
+#pragma unroll
+      for (int v = 0; v < kValues; ++v) {
+        const float y = (float)x0[min(base + v * 64 + lane, p.vocab - 1)];
+        x[v] = base + v * 64 + lane < p.vocab ? y : -INFINITY;
+      }
+    }
+    if (base + (kWaves + 1) * kTile <= p.vocab && tile + kWaves < end) load_tile<T>(raw, x0 + base + kWaves * kTile);
+    auto index = [&](int v) { return base + (whole ? (v / kPer * 64 + lane) * kPer + v % kPer : v * 64 + lane); };
+    auto largest = [&]() {
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        most[g] = max3(x[4 * g], x[4 * g + 1], x[4 * g + 2]);
+        most[g] = max3(most[g], x[4 * g + 3], x[4 * g + 3]);
+      }
+      float m = max3(most[0], most[1], most[2]);
+      m = max3(m, most[3], most[4]);
+      m = max3(m, most[5], most[6]);
+      return max3(m, most[7], most[7]);
+    };
+    float here = largest(), above, more;
+    for (bool again = false;; again = true) {
+      above = max3(top, here, here);
+      more = 0;
+#pragma unroll
+      for (int v = 0; v < kValues; ++v) more += exp_below(x[v], above);
+      if (again || __ballot(more != more) == 0) break;
+#pragma unroll
+      for (int v = 0; v < kValues; ++v) x[v] = clean(x[v]);  // NaN or +infinity somewhere
+      here = largest();
+    }
+    if (from == 0) {
+      sum = sum * (double)exp_below(top, above) + (double)more;
+      top = above;
+    }
+    if (p.end_token >= base && p.end_token < base + kTile) {
+#pragma unroll
+      for (int v = 0; v < kValues; ++v)
+        if (index(v) == p.end_token) {
+          p.end_logit[row] = x[v];
+          x[v] = -INFINITY;
+        }
+      here = largest();
+    }
+    // What another wave's best reach counts here too: only the best of all waves go on
+    const uint64_t others = __hip_atomic_load(&shared_least, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    const uint32_t their_least = (uint32_t)__builtin_amdgcn_readfirstlane((int)(others >> 32));
+    const int their_seen = (int)~__builtin_amdgcn_readfirstlane((int)(uint32_t)others);
+    if (their_least > least || (their_least == least && their_seen < seen)) least = their_least, seen = their_seen;
+    float bar = least ? value_of(least + (tile > seen ? 1 : 0)) : -INFINITY;  // candidates reach it
+    if (least == 0 && wanted > 0) {
+      // as many lanes as are wanted reach the last of the lanes' largest that count
+      Entry<1> e = {here > -INFINITY ? key_of(here) : 0};
+      sort64(e);
+      const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)e.w[0], wanted - 1);
+      if (t) bar = value_of(t);
+    }
+    int stop = 0;
+    if (wanted > 0 && __ballot(here > -INFINITY && here >= bar) != 0) {
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        // (a tile begins with fewer than kSortFrom entries: its first group has room)
+        static_assert(kSortFrom + 64 * kGroup <= kQueue, "");
+        const uint64_t hits = __ballot(most[g] > -INFINITY && most[g] >= bar);
+        if (hits == 0 || g < from || stop > 0) continue;
+        if (n + kGroup * __popcll(hits) > kQueue) {  // what waits is sorted in first
+          stop = g;
+          continue;
+        }
+#pragma unroll
+        for (int v = g * kGroup; v < (g + 1) * kGroup; ++v) {
+          const bool better = x[v] > -INFINITY && x[v] >= bar;
+          const uint64_t mask = __ballot(better);
+          if (better) {
+            const int to = n + lanes_before(mask);
+            queue[0][to] = key_of(x[v]);
+            queue[1][to] = ~(uint32_t)index(v);
+          }
+          n += __popcll(mask);
+        }
+      }
+    }
+    from = stop;
+    if (n > 0 && (stop > 0 || least == 0 || n >= kSortFrom || tile + kWaves >= end)) {
+      wave_sync();
+#pragma unroll 1
+      for (int i = lane; i - lane < n; i += 64) {
+        Entry<2> e;
+        e.w[0] = i < n ? queue[0][i] : 0;
+        e.w[1] = i < n ? queue[1][i] : 0;
+        sort64(e);
+        join64(best, e);
+      }
+      wave_sync();
+      n = 0;
+      const uint32_t reached = (uint32_t)__builtin_amdgcn_readlane((int)best.w[0], wanted - 1);
+      if (reached > least) {
+        least = reached;
+        seen = tile;
+        if (lane == 0) atomicMax(&shared_least, (unsigned long long)least << 32 | (uint32_t)~tile);
+      }
+    }
+    if (stop == 0)
+      tile += kWaves;
+    else if (whole)
+      load_tile<T>(raw, x0 + base);
+  }
+  // The wave's sum over its lanes, then the workgroup's
+  float high = top;
+#pragma unroll
+  for (int step = 1; step < 64; step <<= 1) high = fmaxf(high, __shfl_xor(high, step));
+  sum *= (double)exp_below(top, high);
+#pragma unroll
+  for (int step = 1; step < 64; step <<= 1) sum += __shfl_xor(sum, step);
+  if (lane == 0) {
+    tops[wave] = high;
+    sums[wave] = sum;
+  }
+  queue[0][lane] = best.w[0];
+  queue[1][lane] = best.w[1];
+  __syncthreads();
+  if (wave != 0) return;
+  const int64_t at = (int64_t)row * p.parts + part;
+  if (lane == 0) {
+    for (int w = 1; w < kWaves; ++w) high = fmaxf(high, tops[w]);
+    sum = 0;
+    for (int w = 0; w < kWaves; ++w) sum += sums[w] * (double)exp_below(tops[w], high);
+    p.part_sum[at] = sum;
+    p.part_top[at] = high;
+  }
+#pragma unroll 1
+  for (int w = 1; w < kWaves && wanted > 0; ++w) {
+    const Entry<2> e = {{queues[w][0][lane], queues[w][1][lane]}};
+    join64(best, e);
+  }
+  if (lane < wanted) {
+    p.cand_value[at * wanted + lane] = value_of(best.w[0]);
+    p.cand_token[at * wanted + lane] = best.w[0] ? (int32_t)~best.w[1] : -1;
+  }
+}
+
+// ---- sessions ----------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float logit_at(const BeamParams& p, int row, int token) {
+  const int64_t at = (int64_t)row * p.row_stride + token;
+  return clean(p.wide ? reinterpret_cast<const float*>(p.logits)[at] : (float)reinterpret_cast<const __bf16*>(p.logits)[at]);
+}
+
+constexpr int kSessionWaves = 8, kRows = 256;  // kRows: rows of a session whose end scores stay in LDS
+
+// A workgroup per session, a wave per row.  A row's best are sorted by logit and token, which is the order of their scores as well (far
+// from the sum's logarithm, where 64 bits do not tell scores apart, it is the logits that count); rows are then joined by score, row
+// and place in the row.
+__global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const BeamParams p) {
+  __shared__ Entry<4> lists[kSessionWaves][64];
+  __shared__ double end_near[kRows];
+  __shared__ float end_logit_near[kRows];
+  const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(tid >> 6));
   const int r0 = min(max(p.cu_rows[s], 0), p.n_rows), r1 = max(min(p.cu_rows[s + 1], p.n_rows), r0);
   const int n0 = min(max(p.cu_next[s], 0), p.total_next), n1 = max(min(p.cu_next[s + 1], p.total_next), n0);
-  const int width = min(n1 - n0, p.max_next);
-  const int64_t n = (int64_t)(r1 - r0) * p.max_next;
-  const Candidate none{-INFINITY, -INFINITY, 0x7FFFFFFF, 0x7FFFFFFF};
-  Candidate last{INFINITY, INFINITY, -1, -1};
-  for (int k = 0; k < width; ++k) {
-    Candidate c = none;
-    for (int64_t i = tid; i < n; i += 256) {
-      const int row = r0 + (int)(i / p.max_next);
-      const float cum = p.scores[row];
-      if (!alive(cum)) continue;
-      const int64_t at = (int64_t)row * p.max_next + i % p.max_next;
-      const int token = p.cand_token[at];
-      if (token < 0) continue;
-      const float x = p.cand_value[at];
-      const Candidate y{(double)cum + ((double)x - p.log_sums[row]), x, row, token};
-      if (before(last, y) && before(y, c)) c = y;
+  const int width = min(n1 - n0, p.max_next), per_row = width > 0 ? p.parts * p.max_next : 0;
+
+  struct Asked {
+    float cum, last, top, x;
+    double sum;
+    int token;
+  };
+  auto candidate = [&](int r, int i, float* x, int* token) {
+    const bool in = i < per_row;
+    *x = in ? p.cand_value[(int64_t)r * per_row + i] : 0;
+    *token = in ? p.cand_token[(int64_t)r * per_row + i] : -1;
+  };
+  auto ask = [&](int r) {  // (of a row that is not alive this may be anything)
+    Asked a;
+    a.cum = p.scores[r];
+    a.last = p.end_token >= 0 ? p.end_logit[r] : -INFINITY;
+    a.top = lane < p.parts ? p.part_top[(int64_t)r * p.parts + lane] : -FLT_MAX;
+    a.sum = lane < p.parts ? p.part_sum[(int64_t)r * p.parts + lane] : 0;
+    candidate(r, lane, &a.x, &a.token);
+    return a;
+  };
+  Entry<4> best = {};  // sorted: the score's halves, ~(row, place in it), token
+  Asked next;
+  if (r0 + wave < r1) next = ask(r0 + wave);
+#pragma unroll 1
+  for (int r = r0 + wave; r < r1; r += kSessionWaves) {
+    const Asked a = next;
+    if (r + kSessionWaves < r1) next = ask(r + kSessionWaves);
+    double ends = -INFINITY;
+    if (alive(a.cum)) {
+      float high = a.top;
+      double sum = 0;
+      for (int q = lane + 64; q < p.parts; q += 64) high = fmaxf(high, p.part_top[(int64_t)r * p.parts + q]);
+#pragma unroll
+      for (int step = 1; step < 64; step <<= 1) high = fmaxf(high, __shfl_xor(high, step));
+      for (int q = lane; q < p.parts; q += 64) {
+        const bool first = q < 64;
+        const double part = first ? a.sum : p.part_sum[(int64_t)r * p.parts + q];
+        sum += part * exp((double)(first ? a.top : p.part_top[(int64_t)r * p.parts + q]) - (double)high);
+      }
+#pragma unroll
+      for (int step = 1; step < 64; step <<= 1) sum += __shfl_xor(sum, step);
+      const double log_sum = (double)high + log(sum);
+      if (a.last > -INFINITY) ends = (double)a.cum + ((double)a.last - log_sum);
+      Entry<2> of_row = {};
+      float x = a.x;
+      int token = a.token;
+#pragma unroll 1
+      for (int i = lane; i - lane < per_row; i += 64) {
+        Entry<2> e;
+        e.w[0] = token >= 0 ? key_of(x) : 0;
+        e.w[1] = token >= 0 ? ~(uint32_t)token : 0;
+        candidate(r, i + 64, &x, &token);
+        sort64(e);
+        join64(of_row, e);
+      }
+      const bool there = lane < width && of_row.w[0] != 0;
+      const uint64_t key = key_of((double)a.cum + ((double)value_of(of_row.w[0]) - log_sum));
+      Entry<4> e;
+      e.w[0] = there ? (uint32_t)(key >> 32) : 0;
+      e.w[1] = there ? (uint32_t)key : 0;
+      e.w[2] = there ? ~(uint32_t)((r - r0) * 64 + lane) : 0;
+      e.w[3] = ~of_row.w[1];
+      join64(best, e);
     }
-    __syncthreads();
-    best[tid] = c;
-    __syncthreads();
-    for (int h = 128; h > 0; h >>= 1) {
-      if (tid < h && before(best[tid + h], best[tid])) best[tid] = best[tid + h];
-      __syncthreads();
+    if (lane == 0) {
+      const bool near = r - r0 < kRows;
+      (near ? end_near[r - r0] : p.end_value[r]) = ends;
+      if (near) end_logit_near[r - r0] = a.last;
     }
-    last = best[0];
-    if (tid == 0) chosen[k] = last;
   }
-  __syncthreads();
-  for (int k = tid; k < n1 - n0; k += 256) {
-    const bool there = k < width && chosen[k].row != none.row;
-    p.parents[n0 + k] = there ? chosen[k].row : -1;
-    p.tokens[n0 + k] = there ? chosen[k].token : -1;
-    p.next_scores[n0 + k] = there ? (float)chosen[k].score : -INFINITY;
+  // Half of the waves join what the other half has, and so on
+#pragma unroll 1
+  for (int half = kSessionWaves / 2; half > 0; half >>= 1) {
+    if (wave >= half && wave < 2 * half) lists[wave][lane] = best;
+    __syncthreads();
+    if (wave < half) {
+      const Entry<4> e = lists[wave + half][lane];
+      join64(best, e);
+    }
+  }
+  if (wave == 0) {
+    lists[0][lane] = best;
+    const uint64_t key = (uint64_t)best.w[0] << 32 | best.w[1];
+    if (lane < width) {
+      const bool there = key != 0;
+      const double score = __longlong_as_double((long long)(key >> 63 ? key ^ 0x8000000000000000ull : ~key));
+      p.parents[n0 + lane] = there ? r0 + (int)(~best.w[2] >> 6) : -1;
+      p.tokens[n0 + lane] = there ? (int)best.w[3] : -1;
+      p.next_scores[n0 + lane] = there ? (float)score : -INFINITY;
+    }
+  }
+  for (int k = max(width, 0) + tid; k < n1 - n0; k += 64 * kSessionWaves) {
+    p.parents[n0 + k] = -1;
+    p.tokens[n0 + k] = -1;
+    p.next_scores[n0 + k] = -INFINITY;
   }
   if (!p.end_scores) return;
-  auto end_of = [&](int r) {
-    const float cum = p.scores[r];
-    if (p.end_token < 0 || !alive(cum)) return none;
-    const float x = value_at<T>(p.logits + (int64_t)r * p.row_stride * sizeof(T), p.end_token);
-    return x == -INFINITY ? none : Candidate{(double)cum + ((double)x - p.log_sums[r]), x, r, p.end_token};
-  };
-  for (int r = r0 + tid; r < r1; r += 256) {
-    const Candidate y = end_of(r);
-    int rank = 0;
-    if (y.row != none.row) {
-      for (int k = 0; k < width; ++k) rank += before(chosen[k], y);
-      for (int q = r0; q < r1 && rank < width; ++q) rank += q != r && before(end_of(q), y);
+  __syncthreads();
+  auto end_of = [&](int r) { return r - r0 < kRows ? end_near[r - r0] : p.end_value[r]; };
+  for (int r = r0 + tid; r < r1; r += 64 * kSessionWaves) {
+    const double mine = end_of(r);
+    int place = 0;
+    if (mine > -INFINITY) {
+      const uint64_t key = key_of(mine);
+      for (int k = 0; k < width; ++k) {
+        const Entry<4> e = lists[0][k];
+        const uint64_t other = (uint64_t)e.w[0] << 32 | e.w[1];
+        const int row = r0 + (int)(~e.w[2] >> 6);
+        bool before = other > key || (other == key && row < r);
+        if (other == key && row == r) {
+          const float x = r - r0 < kRows ? end_logit_near[r - r0] : p.end_logit[r], y = logit_at(p, r, (int)e.w[3]);
+          before = y > x || (y == x && (int)e.w[3] < p.end_token);
+        }
+        place += before;
+      }
+      for (int q = r0; q < r1 && place < width; ++q) {
+        const double other = end_of(q);
+        place += other > mine || (other == mine && q < r);
+      }
     }
-    p.end_scores[r] = rank < width ? (float)y.score : -INFINITY;
+    p.end_scores[r] = place < width ? (float)mine : -INFINITY;
   }
 }
 
+// How rows are cut: so many workgroups that they fill the chip, tiles for all waves in each.
+constexpr int kGroupsWanted = 1024;
+struct RowCut {
+  int32_t parts, tiles;  // parts of a row, tiles of a part
+};
+static RowCut cut_rows(int32_t n_rows, int32_t vocab) {
+  const int64_t tiles = ceil_div64(vocab, kTile);
+  const int64_t wanted = std::min(ceil_div64(kGroupsWanted, std::max(n_rows, 1)), ceil_div64(tiles, kWaves));
+  RowCut c;
+  c.tiles = (int32_t)ceil_div64(tiles, wanted);
+  c.parts = (int32_t)ceil_div64(tiles, c.tiles);
+  return c;
+}
 static int64_t round256(int64_t n) { return (n + 255) & ~(int64_t)255; }
 
 }  // namespace symph
@@ -165,7 +543,8 @@ extern "C" {
 
 int64_t symph_beam_select_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t max_next) {
   if (n_rows < 0 || vocab <= 0 || max_next < 0 || max_next > SYMPH_BEAM_MAX) return SYMPH_EINVAL;
-  return round256((int64_t)n_rows * 8) + 2 * round256((int64_t)n_rows * max_next * 4);
+  const int64_t parts = (int64_t)n_rows * cut_rows(n_rows, vocab).parts;
+  return round256((int64_t)n_rows * 4) + round256((int64_t)n_rows * 8) + round256(parts * 8) + round256(parts * 4) + 2 * round256(parts * max_next * 4);
 }
 
 int32_t symph_beam_select(const void* d_logits, int64_t row_stride, int32_t dtype, int32_t n_rows, int32_t vocab,
@@ -180,9 +559,12 @@ int32_t symph_beam_select(const void* d_logits, int64_t row_stride, int32_t dtyp
   if (!d_cu_rows || !d_cu_next || (n_rows > 0 && (!d_logits || !d_scores))) return SYMPH_EINVAL;
   if (total_next > 0 && (!d_parents || !d_tokens || !d_next_scores)) return SYMPH_EINVAL;
   if (d_next_scores && d_next_scores == d_scores) return SYMPH_EINVAL;
-  if (!grid_takes(n_rows, 256) || !grid_takes(n_sessions, 256)) return SYMPH_EUNSUPPORTED;
+  // (a grid's second axis takes 65535 workgroups; tiles are counted in 32 bits)
+  if (n_rows > 65535 || vocab > 0x7FFFFFFF - 2 * kWaves * kTile || !grid_takes(n_sessions, 64 * kSessionWaves)) return SYMPH_EUNSUPPORTED;
   if (workspace_bytes < symph_beam_select_workspace_bytes(n_rows, vocab, max_next) || (!d_workspace && n_rows > 0))
     return SYMPH_EWORKSPACE;
+  const RowCut cut = cut_rows(n_rows, vocab);
+  const int64_t parts = (int64_t)n_rows * cut.parts;
   BeamParams p;
   p.logits = (const char*)d_logits;
   p.scores = d_scores;
@@ -192,9 +574,18 @@ int32_t symph_beam_select(const void* d_logits, int64_t row_stride, int32_t dtyp
   p.tokens = d_tokens;
   p.next_scores = d_next_scores;
   p.end_scores = d_end_scores;
-  p.log_sums = (double*)d_workspace;
-  p.cand_value = (float*)((char*)d_workspace + round256((int64_t)n_rows * 8));
-  p.cand_token = (int32_t*)((char*)p.cand_value + round256((int64_t)n_rows * max_next * 4));
+  char* at = (char*)d_workspace;
+  auto take = [&](int64_t bytes) {
+    char* const here = at;
+    at += round256(bytes);
+    return here;
+  };
+  p.end_logit = (float*)take((int64_t)n_rows * 4);
+  p.end_value = (double*)take((int64_t)n_rows * 8);
+  p.part_sum = (double*)take(parts * 8);
+  p.part_top = (float*)take(parts * 4);
+  p.cand_value = (float*)take(parts * max_next * 4);
+  p.cand_token = (int32_t*)take(parts * max_next * 4);
   p.row_stride = row_stride;
   p.n_rows = n_rows;
   p.vocab = vocab;
@@ -202,14 +593,18 @@ int32_t symph_beam_select(const void* d_logits, int64_t row_stride, int32_t dtyp
   p.total_next = total_next;
   p.max_next = max_next;
   p.end_token = end_token;
+  p.parts = cut.parts;
+  p.part_tiles = cut.tiles;
+  p.wide = dtype == SYMPH_FP32;
   hipStream_t st = (hipStream_t)stream;
-  if (dtype == SYMPH_BF16) {
-    if (n_rows > 0) hipLaunchKernelGGL(beam_rows_kernel<__bf16>, dim3((unsigned)n_rows), dim3(256), 0, st, p);
-    hipLaunchKernelGGL(beam_sessions_kernel<__bf16>, dim3((unsigned)n_sessions), dim3(256), 0, st, p);
-  } else {
-    if (n_rows > 0) hipLaunchKernelGGL(beam_rows_kernel<float>, dim3((unsigned)n_rows), dim3(256), 0, st, p);
-    hipLaunchKernelGGL(beam_sessions_kernel<float>, dim3((unsigned)n_sessions), dim3(256), 0, st, p);
+  const dim3 grid((unsigned)cut.parts, (unsigned)n_rows), threads(64 * kWaves);
+  if (n_rows > 0) {
+    if (dtype == SYMPH_BF16)
+      hipLaunchKernelGGL(beam_parts_kernel<__bf16>, grid, threads, 0, st, p);
+    else
+      hipLaunchKernelGGL(beam_parts_kernel<float>, grid, threads, 0, st, p);
   }
+  hipLaunchKernelGGL(beam_sessions_kernel, dim3((unsigned)n_sessions), dim3(64 * kSessionWaves), 0, st, p);
   return hipGetLastError() == hipSuccess ? SYMPH_OK : SYMPH_ELAUNCH;
 }
 
