@@ -182,7 +182,7 @@ __device__ __forceinline__ void load_tile(u32x4 (&raw)[kValues / Loads<T>::kPer]
   constexpr int kPer = Loads<T>::kPer;
 #pragma unroll
   for (int u = 0; u < kValues / kPer; ++u)
-    raw[u] = *reinterpret_cast<const typename Loads<T>::Vec*>(from + (u * 64 + (threadIdx.x & 63)) * kPer);
+    raw[u] = __builtin_nontemporal_load(reinterpret_cast<const typename Loads<T>::Vec*>(from + (u * 64 + (threadIdx.x & 63)) * kPer));
 }
 
 // (fmaxf would first quieten every operand; a signalling NaN comes out as a NaN here, which is looked for behind the sum)
@@ -192,8 +192,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-constexpr int kQueue = 384, kSortFrom = 24;  // entries that can wait, and from how many on they are sorted in behind a tile
-constexpr int kGroup = 4, kGroups = kValues / kGroup;  // values that are looked at together for candidates
+constexpr int kQueue = 320, kSortFrom = 24;  // entries that can wait, and from how many on they are sorted in behind a tile
 
 // exp(x - top) with the rest of log2 e: the constant's own rounding would be the same for all tokens far below the top
 __device__ __forceinline__ float exp_below(float x, float top) {
@@ -201,19 +200,40 @@ __device__ __forceinline__ float exp_below(float x, float top) {
   return __builtin_amdgcn_exp2f(fmaf(d, 1.44269502e+00f, d * 1.92596300e-08f));
 }
 
+// Sum and maximum over a wave's lanes, every lane gets them
+template <int M>
+__device__ __forceinline__ double plus_xor(double v) {
+  const uint64_t b = (uint64_t)__double_as_longlong(v);
+  return v + __longlong_as_double((long long)((uint64_t)from_lane_xor<M>((uint32_t)(b >> 32)) << 32 | from_lane_xor<M>((uint32_t)b)));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+  return plus_xor<32>(plus_xor<16>(plus_xor<8>(plus_xor<4>(plus_xor<2>(plus_xor<1>(v))))));
+}
+template <int M>
+__device__ __forceinline__ float max_xor(float v) {
+  return max3(v, __uint_as_float(from_lane_xor<M>(__float_as_uint(v))), v);
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return max_xor<32>(max_xor<16>(max_xor<8>(max_xor<4>(max_xor<2>(max_xor<1>(v))))));
+}
+
 template <typename T>
 __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamParams p) {
-  __shared__ uint32_t queues[kWaves][2][kQueue];
+  __shared__ int queues[kWaves][kQueue];
+  __shared__ Entry<2> lists[kWaves][64];
   __shared__ unsigned long long shared_least;  // `least` and ~`seen` of the wave whose best reach furthest
   __shared__ float tops[kWaves];
   __shared__ double sums[kWaves];
   const int part = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  if (!alive(p.scores[row])) return;
   constexpr int kPer = Loads<T>::kPer, kVecs = kValues / kPer;
   const T* const x0 = reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.row_stride;
   const int first = part * p.part_tiles, end = min(first + p.part_tiles, (p.vocab + kTile - 1) / kTile);
-  uint32_t (&queue)[2][kQueue] = queues[wave];
+  u32x4 raw[kVecs];
+  int tile = first + wave;
+  if (tile < end && (tile + 1) * kTile <= p.vocab) load_tile<T>(raw, x0 + tile * kTile);
+  if (!alive(p.scores[row])) return;  // (asked for behind the first tile: one trip to memory less)
+  int* const queue = queues[wave];
   if (threadIdx.x == 0) shared_least = 0;
   __syncthreads();
 
@@ -225,13 +245,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
   // As many values as are wanted reach the key `least`, in tiles up to `seen`: later ones have to pass it (0: there are not as many yet)
   uint32_t least = 0;
   int seen = 0;
-  u32x4 raw[kVecs];
-  int tile = first + wave, from = 0;  // from > 0: the tile's candidates from that group on are still to be looked at
-  if ((tile + 1) * kTile <= p.vocab && tile < end) load_tile<T>(raw, x0 + tile * kTile);
-  while (tile < end) {
+  for (; tile < end; tile += kWaves) {
     const int base = tile * kTile;
     const bool whole = base + kTile <= p.vocab;
-    float x[kValues], most[kGroups];
+    float x[kValues];
     if (whole) {
 #pragma unroll
       for (int v = 0; v < kValues; ++v) x[v] = Loads<T>::at(raw[v / kPer], v % kPer);
@@ -242,18 +259,13 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
         x[v] = base + v * 64 + lane < p.vocab ? y : -INFINITY;
       }
     }
-    if (base + (kWaves + 1) * kTile <= p.vocab && tile + kWaves < end) load_tile<T>(raw, x0 + base + kWaves * kTile);
+    if (tile + kWaves < end && base + (kWaves + 1) * kTile <= p.vocab) load_tile<T>(raw, x0 + base + kWaves * kTile);
     auto index = [&](int v) { return base + (whole ? (v / kPer * 64 + lane) * kPer + v % kPer : v * 64 + lane); };
     auto largest = [&]() {
+      float a = max3(x[0], x[1], x[2]), b = max3(x[3], x[4], x[5]);
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        most[g] = max3(x[4 * g], x[4 * g + 1], x[4 * g + 2]);
-        most[g] = max3(most[g], x[4 * g + 3], x[4 * g + 3]);
-      }
-      float m = max3(most[0], most[1], most[2]);
-      m = max3(m, most[3], most[4]);
-      m = max3(m, most[5], most[6]);
-      return max3(m, most[7], most[7]);
+      for (int v = 6; v < kValues - 2; v += 4) a = max3(a, x[v], x[v + 1]), b = max3(b, x[v + 2], x[v + 3]);
+      return max3(max3(a, x[kValues - 2], x[kValues - 1]), b, b);
     };
     float here = largest(), above, more;
     for (bool again = false;; again = true) {
@@ -266,10 +278,9 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
       for (int v = 0; v < kValues; ++v) x[v] = clean(x[v]);  // NaN or +infinity somewhere
       here = largest();
     }
-    if (from == 0) {
-      sum = sum * (double)exp_below(top, above) + (double)more;
-      top = above;
-    }
+    sum = sum * (double)exp_below(top, above) + (double)more;
+    top = above;
+    if (wanted == 0) continue;
     if (p.end_token >= base && p.end_token < base + kTile) {
 #pragma unroll
       for (int v = 0; v < kValues; ++v)
@@ -284,47 +295,39 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     const uint32_t their_least = (uint32_t)__builtin_amdgcn_readfirstlane((int)(others >> 32));
     const int their_seen = (int)~__builtin_amdgcn_readfirstlane((int)(uint32_t)others);
     if (their_least > least || (their_least == least && their_seen < seen)) least = their_least, seen = their_seen;
-    float bar = least ? value_of(least + (tile > seen ? 1 : 0)) : -INFINITY;  // candidates reach it
-    if (least == 0 && wanted > 0) {
+    float bar = least ? value_of(least + (tile > seen ? 1 : 0)) : -FLT_MAX;  // candidates reach it
+    if (least == 0) {
       // as many lanes as are wanted reach the last of the lanes' largest that count
       Entry<1> e = {here > -INFINITY ? key_of(here) : 0};
       sort64(e);
       const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)e.w[0], wanted - 1);
       if (t) bar = value_of(t);
     }
-    int stop = 0;
-    if (wanted > 0 && __ballot(here > -INFINITY && here >= bar) != 0) {
+    if (__ballot(here >= bar) == 0 && (n == 0 || tile + kWaves < end)) continue;
+    uint32_t open = 0xFFFFFFFFu;  // values that have not gone to the queue, the first in the highest bit
+    for (bool more_hits = true; more_hits;) {
+      uint32_t hits = 0;
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        // (a tile begins with fewer than kSortFrom entries: its first group has room)
-        static_assert(kSortFrom + 64 * kGroup <= kQueue, "");
-        const uint64_t hits = __ballot(most[g] > -INFINITY && most[g] >= bar);
-        if (hits == 0 || g < from || stop > 0) continue;
-        if (n + kGroup * __popcll(hits) > kQueue) {  // what waits is sorted in first
-          stop = g;
-          continue;
+      for (int v = 0; v < kValues; ++v) hits = hits + hits + (x[v] >= bar ? 1 : 0);
+      hits &= open;
+      for (uint64_t mask; (mask = __ballot(hits != 0)) != 0 && n + 64 <= kQueue;) {
+        if (hits) {  // the value with the highest index first
+          const int bit = __builtin_ctz(hits), v = kValues - 1 - bit;
+          queue[n + lanes_before(mask)] = index(v);
+          hits &= hits - 1;
+          open ^= 1u << bit;
         }
-#pragma unroll
-        for (int v = g * kGroup; v < (g + 1) * kGroup; ++v) {
-          const bool better = x[v] > -INFINITY && x[v] >= bar;
-          const uint64_t mask = __ballot(better);
-          if (better) {
-            const int to = n + lanes_before(mask);
-            queue[0][to] = key_of(x[v]);
-            queue[1][to] = ~(uint32_t)index(v);
-          }
-          n += __popcll(mask);
-        }
+        n += __popcll(mask);
       }
-    }
-    from = stop;
-    if (n > 0 && (stop > 0 || least == 0 || n >= kSortFrom || tile + kWaves >= end)) {
+      more_hits = __ballot(hits != 0) != 0;
+      if (!more_hits && n < kSortFrom && least != 0 && tile + kWaves < end) break;
       wave_sync();
 #pragma unroll 1
       for (int i = lane; i - lane < n; i += 64) {
+        const int token = i < n ? queue[i] : 0;
         Entry<2> e;
-        e.w[0] = i < n ? queue[0][i] : 0;
-        e.w[1] = i < n ? queue[1][i] : 0;
+        e.w[0] = i < n ? key_of(clean((float)x0[token])) : 0;
+        e.w[1] = i < n ? ~(uint32_t)token : 0;
         sort64(e);
         join64(best, e);
       }
@@ -334,27 +337,19 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
       if (reached > least) {
         least = reached;
         seen = tile;
+        bar = value_of(least);
         if (lane == 0) atomicMax(&shared_least, (unsigned long long)least << 32 | (uint32_t)~tile);
       }
     }
-    if (stop == 0)
-      tile += kWaves;
-    else if (whole)
-      load_tile<T>(raw, x0 + base);
   }
   // The wave's sum over its lanes, then the workgroup's
-  float high = top;
-#pragma unroll
-  for (int step = 1; step < 64; step <<= 1) high = fmaxf(high, __shfl_xor(high, step));
-  sum *= (double)exp_below(top, high);
-#pragma unroll
-  for (int step = 1; step < 64; step <<= 1) sum += __shfl_xor(sum, step);
+  float high = wave_max(top);
+  sum = wave_sum(sum * (double)exp_below(top, high));
   if (lane == 0) {
     tops[wave] = high;
     sums[wave] = sum;
   }
-  queue[0][lane] = best.w[0];
-  queue[1][lane] = best.w[1];
+  lists[wave][lane] = best;
   __syncthreads();
   if (wave != 0) return;
   const int64_t at = (int64_t)row * p.parts + part;
@@ -366,10 +361,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     p.part_top[at] = high;
   }
 #pragma unroll 1
-  for (int w = 1; w < kWaves && wanted > 0; ++w) {
-    const Entry<2> e = {{queues[w][0][lane], queues[w][1][lane]}};
-    join64(best, e);
-  }
+  for (int w = 1; w < kWaves && wanted > 0; ++w) join64(best, lists[w][lane]);
   if (lane < wanted) {
     p.cand_value[at * wanted + lane] = value_of(best.w[0]);
     p.cand_token[at * wanted + lane] = best.w[0] ? (int32_t)~best.w[1] : -1;
@@ -428,15 +420,13 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
       float high = a.top;
       double sum = 0;
       for (int q = lane + 64; q < p.parts; q += 64) high = fmaxf(high, p.part_top[(int64_t)r * p.parts + q]);
-#pragma unroll
-      for (int step = 1; step < 64; step <<= 1) high = fmaxf(high, __shfl_xor(high, step));
+      high = wave_max(high);
       for (int q = lane; q < p.parts; q += 64) {
         const bool first = q < 64;
         const double part = first ? a.sum : p.part_sum[(int64_t)r * p.parts + q];
         sum += part * exp((double)(first ? a.top : p.part_top[(int64_t)r * p.parts + q]) - (double)high);
       }
-#pragma unroll
-      for (int step = 1; step < 64; step <<= 1) sum += __shfl_xor(sum, step);
+      sum = wave_sum(sum);
       const double log_sum = (double)high + log(sum);
       if (a.last > -INFINITY) ends = (double)a.cum + ((double)a.last - log_sum);
       Entry<2> of_row = {};
