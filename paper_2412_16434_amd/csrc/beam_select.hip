@@ -121,23 +121,34 @@ __device__ __forceinline__ void sort_rest(Entry<WORDS>& e) {  // sequences of 16
   exchange<2>(e);
   exchange<1>(e);
 }
+// `runs`: runs of so many lanes (a power of two) are sorted already
 template <int WORDS>
-__device__ __forceinline__ void sort64(Entry<WORDS>& e) {
-  exchange<1>(e);
-  exchange<3>(e);
-  exchange<1>(e);
-  exchange<7>(e);
-  exchange<2>(e);
-  exchange<1>(e);
-  exchange<15>(e);
-  exchange<4>(e);
-  exchange<2>(e);
-  exchange<1>(e);
-  exchange<31>(e);
-  sort_rest(e);
-  exchange<63>(e);
-  exchange<16>(e);
-  sort_rest(e);
+__device__ __forceinline__ void sort64(Entry<WORDS>& e, int runs = 1) {
+  if (runs <= 1) exchange<1>(e);
+  if (runs <= 2) {
+    exchange<3>(e);
+    exchange<1>(e);
+  }
+  if (runs <= 4) {
+    exchange<7>(e);
+    exchange<2>(e);
+    exchange<1>(e);
+  }
+  if (runs <= 8) {
+    exchange<15>(e);
+    exchange<4>(e);
+    exchange<2>(e);
+    exchange<1>(e);
+  }
+  if (runs <= 16) {
+    exchange<31>(e);
+    sort_rest(e);
+  }
+  if (runs <= 32) {
+    exchange<63>(e);
+    exchange<16>(e);
+    sort_rest(e);
+  }
 }
 // The 64 largest of two sorted sequences, sorted
 template <int WORDS>
@@ -221,6 +232,7 @@ template <typename T>
 __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamParams p) {
   __shared__ int queues[kWaves][kQueue];
   __shared__ Entry<2> lists[kWaves][64];
+  __shared__ uint32_t firsts[kWaves][64];
   __shared__ unsigned long long shared_least;  // `least` and ~`seen` of the wave whose best reach furthest
   __shared__ float tops[kWaves];
   __shared__ double sums[kWaves];
@@ -234,17 +246,43 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
   if (tile < end && (tile + 1) * kTile <= p.vocab) load_tile<T>(raw, x0 + tile * kTile);
   if (!alive(p.scores[row])) return;  // (asked for behind the first tile: one trip to memory less)
   int* const queue = queues[wave];
+  const int wanted = p.max_next;
+  auto largest = [](const float (&x)[kValues]) {
+    float a = max3(x[0], x[1], x[2]), b = max3(x[3], x[4], x[5]);
+#pragma unroll
+    for (int v = 6; v < kValues - 2; v += 4) a = max3(a, x[v], x[v + 1]), b = max3(b, x[v + 2], x[v + 3]);
+    return max3(max3(a, x[kValues - 2], x[kValues - 1]), b, b);
+  };
+  // As many values as are wanted reach the key `least`: to begin with, that many of the lanes' largest in the waves' first tiles do.
+  // (One more where one of them could be the end token.)  Where a wave's best reached it, in tiles up to `seen`, later ones have to
+  // pass it.  0: there are not as many yet.
+  uint32_t least = 0;
+  int seen = 0x7FFFFFFF;
+  const int count = wanted + (p.end_token >= 0 ? 1 : 0);
   if (threadIdx.x == 0) shared_least = 0;
-  __syncthreads();
+  if (wanted > 0 && count <= 64) {
+    Entry<1> e = {0};
+    if (tile < end && (tile + 1) * kTile <= p.vocab) {
+      float x[kValues];
+#pragma unroll
+      for (int v = 0; v < kValues; ++v) x[v] = Loads<T>::at(raw[v / kPer], v % kPer);
+      const float here = clean(largest(x));
+      e.w[0] = here > -INFINITY ? key_of(here) : 0;
+    }
+    sort64(e);
+    firsts[wave][lane] = e.w[0];
+    __syncthreads();
+#pragma unroll 1
+    for (int w = 1; w < kWaves; ++w) join64(e, Entry<1>{firsts[(wave + w) % kWaves][lane]});
+    least = (uint32_t)__builtin_amdgcn_readlane((int)e.w[0], count - 1);
+  } else {
+    __syncthreads();
+  }
 
   float top = -FLT_MAX;
   double sum = 0;
   Entry<2> best = {};  // the wave's best so far, sorted: key_of the value, ~token; what is still to be sorted in waits in the queue
   int n = 0;
-  const int wanted = p.max_next;
-  // As many values as are wanted reach the key `least`, in tiles up to `seen`: later ones have to pass it (0: there are not as many yet)
-  uint32_t least = 0;
-  int seen = 0;
   for (; tile < end; tile += kWaves) {
     const int base = tile * kTile;
     const bool whole = base + kTile <= p.vocab;
@@ -261,13 +299,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     }
     if (tile + kWaves < end && base + (kWaves + 1) * kTile <= p.vocab) load_tile<T>(raw, x0 + base + kWaves * kTile);
     auto index = [&](int v) { return base + (whole ? (v / kPer * 64 + lane) * kPer + v % kPer : v * 64 + lane); };
-    auto largest = [&]() {
-      float a = max3(x[0], x[1], x[2]), b = max3(x[3], x[4], x[5]);
-#pragma unroll
-      for (int v = 6; v < kValues - 2; v += 4) a = max3(a, x[v], x[v + 1]), b = max3(b, x[v + 2], x[v + 3]);
-      return max3(max3(a, x[kValues - 2], x[kValues - 1]), b, b);
-    };
-    float here = largest(), above, more;
+    float here = largest(x), above, more;
     for (bool again = false;; again = true) {
       above = max3(top, here, here);
       more = 0;
@@ -276,7 +308,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
       if (again || __ballot(more != more) == 0) break;
 #pragma unroll
       for (int v = 0; v < kValues; ++v) x[v] = clean(x[v]);  // NaN or +infinity somewhere
-      here = largest();
+      here = largest(x);
     }
     sum = sum * (double)exp_below(top, above) + (double)more;
     top = above;
@@ -288,7 +320,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
           p.end_logit[row] = x[v];
           x[v] = -INFINITY;
         }
-      here = largest();
+      here = largest(x);
     }
     // What another wave's best reach counts here too: only the best of all waves go on
     const uint64_t others = __hip_atomic_load(&shared_least, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
@@ -334,7 +366,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
       wave_sync();
       n = 0;
       const uint32_t reached = (uint32_t)__builtin_amdgcn_readlane((int)best.w[0], wanted - 1);
-      if (reached > least) {
+      if (reached > least || (reached == least && reached != 0 && tile < seen)) {
         least = reached;
         seen = tile;
         bar = value_of(least);
@@ -374,7 +406,7 @@ __device__ __forceinline__ float logit_at(const BeamParams& p, int row, int toke
   return clean(p.wide ? reinterpret_cast<const float*>(p.logits)[at] : (float)reinterpret_cast<const __bf16*>(p.logits)[at]);
 }
 
-constexpr int kSessionWaves = 8, kRows = 256;  // kRows: rows of a session whose end scores stay in LDS
+constexpr int kSessionWaves = 16, kRows = 256;  // kRows: rows of a session whose end scores stay in LDS
 
 // A workgroup per session, a wave per row.  A row's best are sorted by logit and token, which is the order of their scores as well (far
 // from the sum's logarithm, where 64 bits do not tell scores apart, it is the logits that count); rows are then joined by score, row
@@ -387,17 +419,23 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
   const int wave = __builtin_amdgcn_readfirstlane((int)(tid >> 6));
   const int r0 = min(max(p.cu_rows[s], 0), p.n_rows), r1 = max(min(p.cu_rows[s + 1], p.n_rows), r0);
   const int n0 = min(max(p.cu_next[s], 0), p.total_next), n1 = max(min(p.cu_next[s + 1], p.total_next), n0);
-  const int width = min(n1 - n0, p.max_next), per_row = width > 0 ? p.parts * p.max_next : 0;
+  const int width = min(n1 - n0, p.max_next);
 
   struct Asked {
     float cum, last, top, x;
     double sum;
     int token;
   };
-  auto candidate = [&](int r, int i, float* x, int* token) {
-    const bool in = i < per_row;
-    *x = in ? p.cand_value[(int64_t)r * per_row + i] : 0;
-    *token = in ? p.cand_token[(int64_t)r * per_row + i] : -1;
+  // A part's best are sorted: 2^n lanes to a part
+  int run = 1;
+  while (run < p.max_next) run <<= 1;
+  const int per_batch = width > 0 ? 64 / run : 1;
+  auto candidate = [&](int r, int first, float* x, int* token) {  // of the parts from `first` on
+    const int part = first + lane / run, place = lane & (run - 1);
+    const bool in = width > 0 && part < p.parts && place < p.max_next;
+    const int64_t at = ((int64_t)r * p.parts + part) * p.max_next + place;
+    *x = in ? p.cand_value[at] : 0;
+    *token = in ? p.cand_token[at] : -1;
   };
   auto ask = [&](int r) {  // (of a row that is not alive this may be anything)
     Asked a;
@@ -405,7 +443,7 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
     a.last = p.end_token >= 0 ? p.end_logit[r] : -INFINITY;
     a.top = lane < p.parts ? p.part_top[(int64_t)r * p.parts + lane] : -FLT_MAX;
     a.sum = lane < p.parts ? p.part_sum[(int64_t)r * p.parts + lane] : 0;
-    candidate(r, lane, &a.x, &a.token);
+    candidate(r, 0, &a.x, &a.token);
     return a;
   };
   Entry<4> best = {};  // sorted: the score's halves, ~(row, place in it), token
@@ -424,7 +462,7 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
       for (int q = lane; q < p.parts; q += 64) {
         const bool first = q < 64;
         const double part = first ? a.sum : p.part_sum[(int64_t)r * p.parts + q];
-        sum += part * exp((double)(first ? a.top : p.part_top[(int64_t)r * p.parts + q]) - (double)high);
+        sum += part * (double)exp_below(first ? a.top : p.part_top[(int64_t)r * p.parts + q], high);
       }
       sum = wave_sum(sum);
       const double log_sum = (double)high + log(sum);
@@ -433,13 +471,16 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
       float x = a.x;
       int token = a.token;
 #pragma unroll 1
-      for (int i = lane; i - lane < per_row; i += 64) {
+      for (int part = 0; part < p.parts && width > 0; part += per_batch) {
         Entry<2> e;
         e.w[0] = token >= 0 ? key_of(x) : 0;
         e.w[1] = token >= 0 ? ~(uint32_t)token : 0;
-        candidate(r, i + 64, &x, &token);
-        sort64(e);
-        join64(of_row, e);
+        if (part + per_batch < p.parts) candidate(r, part + per_batch, &x, &token);
+        sort64(e, run);
+        if (part == 0)
+          of_row = e;
+        else
+          join64(of_row, e);
       }
       const bool there = lane < width && of_row.w[0] != 0;
       const uint64_t key = key_of((double)a.cum + ((double)value_of(of_row.w[0]) - log_sum));
@@ -448,7 +489,10 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
       e.w[1] = there ? (uint32_t)key : 0;
       e.w[2] = there ? ~(uint32_t)((r - r0) * 64 + lane) : 0;
       e.w[3] = ~of_row.w[1];
-      join64(best, e);
+      if (r < r0 + kSessionWaves)
+        best = e;
+      else
+        join64(best, e);
     }
     if (lane == 0) {
       const bool near = r - r0 < kRows;
@@ -461,10 +505,7 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
   for (int half = kSessionWaves / 2; half > 0; half >>= 1) {
     if (wave >= half && wave < 2 * half) lists[wave][lane] = best;
     __syncthreads();
-    if (wave < half) {
-      const Entry<4> e = lists[wave + half][lane];
-      join64(best, e);
-    }
+    if (wave < half && r0 + wave + half < r1) join64(best, lists[wave + half][lane]);  // (the others had no row)
   }
   if (wave == 0) {
     lists[0][lane] = best;
