@@ -203,12 +203,30 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+constexpr float kLarge = 1048576.0f;
 constexpr int kQueue = 320, kSortFrom = 24;  // entries that can wait, and from how many on they are sorted in behind a tile
 
 // exp(x - top) with the rest of log2 e: the constant's own rounding would be the same for all tokens far below the top
+constexpr float kLog2e = 1.44269502e+00f, kLog2eRest = 1.92596300e-08f;
 __device__ __forceinline__ float exp_below(float x, float top) {
   const float d = x - top;
-  return __builtin_amdgcn_exp2f(fmaf(d, 1.44269502e+00f, d * 1.92596300e-08f));
+  return __builtin_amdgcn_exp2f(fmaf(d, kLog2e, d * kLog2eRest));
+}
+// The sum of exp(x - top) over a lane's values, top being at least the largest.  The vector unit bounds the launch, and one instruction
+// in front of each exponential takes a tenth less than three: x log2 e - c with c = top log2 e rounded, and what c is off by taken out
+// behind the sum.  What is left out is (x - top) 1.3e-8 of a term, nearly the same for all rows of a call.  Values that are too large
+// for that (c would be off by more than an exponential takes) go the long way.
+__device__ __forceinline__ float sum_below(const float (&x)[kValues], float top, bool large) {
+  float s = 0;
+  if (__ballot(large) == 0) {
+    const float near = fmaxf(top, -kLarge), c = near * kLog2e, off = fmaf(near, kLog2e, -c);
+#pragma unroll
+    for (int v = 0; v < kValues; ++v) s += __builtin_amdgcn_exp2f(fmaf(x[v], kLog2e, -c));
+    return s * __builtin_amdgcn_exp2f(-off);
+  }
+#pragma unroll
+  for (int v = 0; v < kValues; ++v) s += exp_below(x[v], top);
+  return s;
 }
 
 // Sum and maximum over a wave's lanes, every lane gets them
@@ -253,7 +271,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     for (int v = 6; v < kValues - 2; v += 4) a = max3(a, x[v], x[v + 1]), b = max3(b, x[v + 2], x[v + 3]);
     return max3(max3(a, x[kValues - 2], x[kValues - 1]), b, b);
   };
-  // As many values as are wanted reach the key `least`: to begin with, that many of the lanes' largest in the waves' first tiles do.
+  // As many values as are wanted reach the key `least`: to begin with, that many lanes' largest in the waves' first tiles do.
   // (One more where one of them could be the end token.)  Where a wave's best reached it, in tiles up to `seen`, later ones have to
   // pass it.  0: there are not as many yet.
   uint32_t least = 0;
@@ -269,11 +287,11 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
       const float here = clean(largest(x));
       e.w[0] = here > -INFINITY ? key_of(here) : 0;
     }
-    sort64(e);
     firsts[wave][lane] = e.w[0];
     __syncthreads();
-#pragma unroll 1
-    for (int w = 1; w < kWaves; ++w) join64(e, Entry<1>{firsts[(wave + w) % kWaves][lane]});
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) e.w[0] = max(e.w[0], firsts[w][lane]);
+    sort64(e);
     least = (uint32_t)__builtin_amdgcn_readlane((int)e.w[0], count - 1);
   } else {
     __syncthreads();
@@ -302,9 +320,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     float here = largest(x), above, more;
     for (bool again = false;; again = true) {
       above = max3(top, here, here);
-      more = 0;
-#pragma unroll
-      for (int v = 0; v < kValues; ++v) more += exp_below(x[v], above);
+      more = sum_below(x, above, here > -INFINITY && fabsf(above) > kLarge);
       if (again || __ballot(more != more) == 0) break;
 #pragma unroll
       for (int v = 0; v < kValues; ++v) x[v] = clean(x[v]);  // NaN or +infinity somewhere
