@@ -251,7 +251,9 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
   __shared__ int queues[kWaves][kQueue];
   __shared__ Entry<2> lists[kWaves][64];
   __shared__ uint32_t firsts[kWaves][64];
-  __shared__ unsigned long long shared_least;  // `least` and ~`seen` of the wave whose best reach furthest
+  // What the best of the wave that is furthest reach, and the complement of the tile up to which they were found: later ones have to pass it
+  __shared__ unsigned long long shared_least;
+  __shared__ int waiting[kWaves];
   __shared__ float tops[kWaves];
   __shared__ double sums[kWaves];
   const int part = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63;
@@ -271,11 +273,9 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     for (int v = 6; v < kValues - 2; v += 4) a = max3(a, x[v], x[v + 1]), b = max3(b, x[v + 2], x[v + 3]);
     return max3(max3(a, x[kValues - 2], x[kValues - 1]), b, b);
   };
-  // As many values as are wanted reach the key `least`: to begin with, that many lanes' largest in the waves' first tiles do.
-  // (One more where one of them could be the end token.)  Where a wave's best reached it, in tiles up to `seen`, later ones have to
-  // pass it.  0: there are not as many yet.
+  // Candidates reach the key `least`, as at least so many values as are wanted do: to begin with, that many lanes' largest in the
+  // waves' first tiles.  (One more where one of them could be the end token.)  0: that is not known yet.
   uint32_t least = 0;
-  int seen = 0x7FFFFFFF;
   const int count = wanted + (p.end_token >= 0 ? 1 : 0);
   if (threadIdx.x == 0) shared_least = 0;
   if (wanted > 0 && count <= 64) {
@@ -338,12 +338,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
         }
       here = largest(x);
     }
-    // What another wave's best reach counts here too: only the best of all waves go on
-    const uint64_t others = __hip_atomic_load(&shared_least, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    const uint32_t their_least = (uint32_t)__builtin_amdgcn_readfirstlane((int)(others >> 32));
-    const int their_seen = (int)~__builtin_amdgcn_readfirstlane((int)(uint32_t)others);
-    if (their_least > least || (their_least == least && their_seen < seen)) least = their_least, seen = their_seen;
-    float bar = least ? value_of(least + (tile > seen ? 1 : 0)) : -FLT_MAX;  // candidates reach it
+    float bar = least ? value_of(least) : -FLT_MAX;
     if (least == 0) {
       // as many lanes as are wanted reach the last of the lanes' largest that count
       Entry<1> e = {here > -INFINITY ? key_of(here) : 0};
@@ -351,7 +346,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
       const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)e.w[0], wanted - 1);
       if (t) bar = value_of(t);
     }
-    if (__ballot(here >= bar) == 0 && (n == 0 || tile + kWaves < end)) continue;
+    if (__ballot(here >= bar) == 0) continue;
     uint32_t open = 0xFFFFFFFFu;  // values that have not gone to the queue, the first in the highest bit
     for (bool more_hits = true; more_hits;) {
       uint32_t hits = 0;
@@ -368,7 +363,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
         n += __popcll(mask);
       }
       more_hits = __ballot(hits != 0) != 0;
-      if (!more_hits && n < kSortFrom && least != 0 && tile + kWaves < end) break;
+      if (!more_hits && n < kSortFrom && least != 0) break;
       wave_sync();
 #pragma unroll 1
       for (int i = lane; i - lane < n; i += 64) {
@@ -381,13 +376,17 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
       }
       wave_sync();
       n = 0;
+      // What is left of the tile has to reach the last of the best, later tiles have to pass it (and what other waves know)
       const uint32_t reached = (uint32_t)__builtin_amdgcn_readlane((int)best.w[0], wanted - 1);
-      if (reached > least || (reached == least && reached != 0 && tile < seen)) {
-        least = reached;
-        seen = tile;
-        bar = value_of(least);
-        if (lane == 0) atomicMax(&shared_least, (unsigned long long)least << 32 | (uint32_t)~tile);
-      }
+      if (reached == 0) continue;
+      bar = fmaxf(bar, value_of(reached));
+      least = max(least, reached + 1);
+      const unsigned long long mine = (unsigned long long)reached << 32 | (uint32_t)~tile;
+      unsigned long long theirs = 0;
+      if (lane == 0) theirs = atomicMax(&shared_least, mine);
+      const uint32_t their_key = (uint32_t)__builtin_amdgcn_readfirstlane((int)(theirs >> 32));
+      const int their_tile = (int)~__builtin_amdgcn_readfirstlane((int)(uint32_t)theirs);
+      least = max(least, their_key + (their_key != 0 && tile + kWaves > their_tile ? 1u : 0u));
     }
   }
   // The wave's sum over its lanes, then the workgroup's
@@ -398,6 +397,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     sums[wave] = sum;
   }
   lists[wave][lane] = best;
+  if (lane == 0) waiting[wave] = n;
   __syncthreads();
   if (wave != 0) return;
   const int64_t at = (int64_t)row * p.parts + part;
@@ -408,8 +408,31 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     p.part_sum[at] = sum;
     p.part_top[at] = high;
   }
+  if (wanted == 0) return;
+  // What still waits in all queues, laid end to end; then the lists, where there are any
+  int begin[kWaves], total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    begin[w] = total;
+    total += waiting[w];
+  }
 #pragma unroll 1
-  for (int w = 1; w < kWaves && wanted > 0; ++w) join64(best, lists[w][lane]);
+  for (int i = lane; i - lane < total; i += 64) {
+    int token = queues[0][min(i, kQueue - 1)];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w)
+      if (i >= begin[w]) token = queues[w][min(i - begin[w], kQueue - 1)];
+    Entry<2> e;
+    e.w[0] = i < total ? key_of(clean((float)x0[i < total ? token : 0])) : 0;
+    e.w[1] = i < total ? ~(uint32_t)token : 0;
+    sort64(e);
+    join64(best, e);
+  }
+#pragma unroll 1
+  for (int w = 1; w < kWaves; ++w) {
+    const Entry<2> e = lists[w][lane];
+    if (__ballot(e.w[0] != 0) != 0) join64(best, e);
+  }
   if (lane < wanted) {
     p.cand_value[at * wanted + lane] = value_of(best.w[0]);
     p.cand_token[at * wanted + lane] = best.w[0] ? (int32_t)~best.w[1] : -1;
