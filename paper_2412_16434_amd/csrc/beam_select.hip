@@ -204,7 +204,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 constexpr float kLarge = 1048576.0f;
-constexpr int kQueue = 320, kSortFrom = 24;  // entries that can wait, and from how many on they are sorted in behind a tile
+// Entries of a wave's two queues: a lane's share of a tile where one of its values may count, and tokens that do.  A wave sorts its
+// tokens in from kSortFrom on, and from kSortLast on behind its last tile; the others are sorted for all waves together.  Tiles where
+// kMany lanes or more have a token that counts are looked through at once.
+constexpr int kQueue = 256, kTokens = 128, kSortFrom = 48, kSortLast = 24, kMany = 12;
 
 // exp(x - top) with the rest of log2 e: the constant's own rounding would be the same for all tokens far below the top
 constexpr float kLog2e = 1.44269502e+00f, kLog2eRest = 1.92596300e-08f;
@@ -248,7 +251,7 @@ __device__ __forceinline__ float wave_max(float v) {
 
 template <typename T>
 __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamParams p) {
-  __shared__ int queues[kWaves][kQueue];
+  __shared__ int queues[kWaves][kQueue], tokens[kWaves][kTokens];
   __shared__ Entry<2> lists[kWaves][64];
   __shared__ uint32_t firsts[kWaves][64];
   // What the best of the wave that is furthest reach, and the complement of the tile up to which they were found: later ones have to pass it
@@ -274,9 +277,9 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     return max3(max3(a, x[kValues - 2], x[kValues - 1]), b, b);
   };
   // Candidates reach the key `least`, as at least so many values as are wanted do: to begin with, that many lanes' largest in the
-  // waves' first tiles.  (One more where one of them could be the end token.)  0: that is not known yet.
+  // waves' first tiles.  (One more where the end token is among them.)  0: that is not known yet.
   uint32_t least = 0;
-  const int count = wanted + (p.end_token >= 0 ? 1 : 0);
+  const int count = wanted + (p.end_token >= first * kTile && p.end_token < (first + kWaves) * kTile ? 1 : 0);
   if (threadIdx.x == 0) shared_least = 0;
   if (wanted > 0 && count <= 64) {
     Entry<1> e = {0};
@@ -297,97 +300,134 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     __syncthreads();
   }
 
+  if (threadIdx.x == 0 && p.end_token >= first * kTile && p.end_token < end * kTile) p.end_logit[row] = clean((float)x0[p.end_token]);
+
   float top = -FLT_MAX;
   double sum = 0;
-  Entry<2> best = {};  // the wave's best so far, sorted: key_of the value, ~token; what is still to be sorted in waits in the queue
-  int n = 0;
-  for (; tile < end; tile += kWaves) {
-    const int base = tile * kTile;
+  Entry<2> best = {};  // the wave's best so far, sorted: key_of the value, ~token
+  int n = 0, m = 0;    // entries of the two queues
+  float bar = least ? value_of(least) : -FLT_MAX;
+
+  // Sorts the waiting tokens in.  What is left of the tile `t` and earlier ones has to reach the last of the best, later tiles have to
+  // pass it (and what other waves know).
+  auto sort_in = [&](int t) {
+    wave_sync();
+#pragma unroll 1
+    for (int i = lane; i - lane < m; i += 64) {
+      const int token = i < m ? tokens[wave][i] : 0;
+      Entry<2> e;
+      e.w[0] = i < m ? key_of(clean((float)x0[token])) : 0;
+      e.w[1] = i < m ? ~(uint32_t)token : 0;
+      sort64(e);
+      join64(best, e);
+    }
+    wave_sync();
+    m = 0;
+    const uint32_t reached = (uint32_t)__builtin_amdgcn_readlane((int)best.w[0], wanted - 1);
+    if (reached == 0) return;
+    bar = fmaxf(bar, value_of(reached));
+    least = max(least, reached + 1);
+    const unsigned long long mine = (unsigned long long)reached << 32 | (uint32_t)~t;
+    unsigned long long theirs = 0;
+    if (lane == 0) theirs = atomicMax(&shared_least, mine);
+    const uint32_t their_key = (uint32_t)__builtin_amdgcn_readfirstlane((int)(theirs >> 32));
+    const int their_tile = (int)~__builtin_amdgcn_readfirstlane((int)(uint32_t)theirs);
+    least = max(least, their_key + (their_key != 0 && t + kWaves > their_tile ? 1u : 0u));
+  };
+  // A turn looks through a tile, or again through 64 lanes' shares of earlier ones.  (Few lanes of a tile have a token that counts; to
+  // look for it tile by tile took a fifth of the launch, so those lanes' values are read again, many tiles' together.)
+  int again = -1;  // the queue's first entry that is to be looked at again
+  while (tile < end) {
+    const bool fresh = again < 0, last = tile + kWaves >= end;
+    if (!fresh) wave_sync();
+    const int code = fresh ? tile * 64 + lane : again + lane < n ? queue[again + lane] : -1;
+    const int base = max(code >> 6, 0) * kTile, l = code & 63;
     const bool whole = base + kTile <= p.vocab;
+    auto index = [&](int v) { return base + (whole ? (v / kPer * 64 + l) * kPer + v % kPer : v * 64 + l); };
     float x[kValues];
     if (whole) {
+      if (!fresh) {
+        u32x4 old[kVecs];
 #pragma unroll
-      for (int v = 0; v < kValues; ++v) x[v] = Loads<T>::at(raw[v / kPer], v % kPer);
+        for (int u = 0; u < kVecs; ++u) old[u] = *reinterpret_cast<const typename Loads<T>::Vec*>(x0 + index(u * kPer));
+#pragma unroll
+        for (int v = 0; v < kValues; ++v) x[v] = Loads<T>::at(old[v / kPer], v % kPer);
+      } else {
+#pragma unroll
+        for (int v = 0; v < kValues; ++v) x[v] = Loads<T>::at(raw[v / kPer], v % kPer);
+      }
     } else {
 #pragma unroll
       for (int v = 0; v < kValues; ++v) {
-        const float y = (float)x0[min(base + v * 64 + lane, p.vocab - 1)];
-        x[v] = base + v * 64 + lane < p.vocab ? y : -INFINITY;
+        const float y = (float)x0[min(index(v), p.vocab - 1)];
+        x[v] = index(v) < p.vocab ? y : -INFINITY;
       }
     }
-    if (tile + kWaves < end && base + (kWaves + 1) * kTile <= p.vocab) load_tile<T>(raw, x0 + base + kWaves * kTile);
-    auto index = [&](int v) { return base + (whole ? (v / kPer * 64 + lane) * kPer + v % kPer : v * 64 + lane); };
-    float here = largest(x), above, more;
-    for (bool again = false;; again = true) {
-      above = max3(top, here, here);
-      more = sum_below(x, above, here > -INFINITY && fabsf(above) > kLarge);
-      if (again || __ballot(more != more) == 0) break;
+    uint32_t open = code >= 0 ? 0xFFFFFFFFu : 0;  // values that are still to be looked at, the first in the highest bit
+    bool done = !fresh && again + 64 >= n;        // with the tile, behind this turn
+    if (fresh) {
+      if (tile + kWaves < end && base + (kWaves + 1) * kTile <= p.vocab) load_tile<T>(raw, x0 + base + kWaves * kTile);
+      float here = largest(x), above, more;
+      for (bool clear = false;; clear = true) {
+        above = max3(top, here, here);
+        more = sum_below(x, above, here > -INFINITY && fabsf(above) > kLarge);
+        if (clear || __ballot(more != more) == 0) break;
 #pragma unroll
-      for (int v = 0; v < kValues; ++v) x[v] = clean(x[v]);  // NaN or +infinity somewhere
-      here = largest(x);
+        for (int v = 0; v < kValues; ++v) x[v] = clean(x[v]);  // NaN or +infinity somewhere
+        here = largest(x);
+      }
+      sum = sum * (double)exp_below(top, above) + (double)more;
+      top = above;
+      bar = least ? value_of(least) : -FLT_MAX;
+      if (least == 0 && wanted > 0 && wanted < 64) {
+        // as many lanes (and one that may have the end token) as are wanted reach the last of the lanes' largest that count
+        Entry<1> e = {here > -INFINITY ? key_of(here) : 0};
+        sort64(e);
+        const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)e.w[0], wanted);
+        if (t) bar = value_of(t);
+      }
+      const uint64_t mask = wanted > 0 ? __ballot(here >= bar) : 0;
+      const bool at_once = mask != 0 && (last || least == 0 || __popcll(mask) >= kMany);
+      if (mask != 0 && !at_once) {
+        if (mask >> lane & 1) queue[n + lanes_before(mask)] = code;
+        n += __popcll(mask);
+      }
+      done = n == 0 || !(last || n + 64 > kQueue);
+      if (!at_once) {
+        if (done)
+          tile += kWaves;
+        else
+          again = 0;
+        continue;
+      }
     }
-    sum = sum * (double)exp_below(top, above) + (double)more;
-    top = above;
-    if (wanted == 0) continue;
     if (p.end_token >= base && p.end_token < base + kTile) {
-#pragma unroll
-      for (int v = 0; v < kValues; ++v)
-        if (index(v) == p.end_token) {
-          p.end_logit[row] = x[v];
-          x[v] = -INFINITY;
-        }
-      here = largest(x);
+      const int at = p.end_token - base, v = whole ? at / (64 * kPer) * kPer + at % kPer : at >> 6;
+      if ((whole ? at / kPer : at) % 64 == l) open &= ~(0x80000000u >> v);
     }
-    float bar = least ? value_of(least) : -FLT_MAX;
-    if (least == 0) {
-      // as many lanes as are wanted reach the last of the lanes' largest that count
-      Entry<1> e = {here > -INFINITY ? key_of(here) : 0};
-      sort64(e);
-      const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)e.w[0], wanted - 1);
-      if (t) bar = value_of(t);
-    }
-    if (__ballot(here >= bar) == 0) continue;
-    uint32_t open = 0xFFFFFFFFu;  // values that have not gone to the queue, the first in the highest bit
-    for (bool more_hits = true; more_hits;) {
+    for (bool left = true; left;) {
       uint32_t hits = 0;
 #pragma unroll
       for (int v = 0; v < kValues; ++v) hits = hits + hits + (x[v] >= bar ? 1 : 0);
       hits &= open;
-      for (uint64_t mask; (mask = __ballot(hits != 0)) != 0 && n + 64 <= kQueue;) {
+      for (uint64_t mask; (mask = __ballot(hits != 0)) != 0 && m + 64 <= kTokens;) {
         if (hits) {  // the value with the highest index first
-          const int bit = __builtin_ctz(hits), v = kValues - 1 - bit;
-          queue[n + lanes_before(mask)] = index(v);
+          const int bit = __builtin_ctz(hits);
+          tokens[wave][m + lanes_before(mask)] = index(kValues - 1 - bit);
           hits &= hits - 1;
           open ^= 1u << bit;
         }
-        n += __popcll(mask);
+        m += __popcll(mask);
       }
-      more_hits = __ballot(hits != 0) != 0;
-      if (!more_hits && n < kSortFrom && least != 0) break;
-      wave_sync();
-#pragma unroll 1
-      for (int i = lane; i - lane < n; i += 64) {
-        const int token = i < n ? queue[i] : 0;
-        Entry<2> e;
-        e.w[0] = i < n ? key_of(clean((float)x0[token])) : 0;
-        e.w[1] = i < n ? ~(uint32_t)token : 0;
-        sort64(e);
-        join64(best, e);
-      }
-      wave_sync();
-      n = 0;
-      // What is left of the tile has to reach the last of the best, later tiles have to pass it (and what other waves know)
-      const uint32_t reached = (uint32_t)__builtin_amdgcn_readlane((int)best.w[0], wanted - 1);
-      if (reached == 0) continue;
-      bar = fmaxf(bar, value_of(reached));
-      least = max(least, reached + 1);
-      const unsigned long long mine = (unsigned long long)reached << 32 | (uint32_t)~tile;
-      unsigned long long theirs = 0;
-      if (lane == 0) theirs = atomicMax(&shared_least, mine);
-      const uint32_t their_key = (uint32_t)__builtin_amdgcn_readfirstlane((int)(theirs >> 32));
-      const int their_tile = (int)~__builtin_amdgcn_readfirstlane((int)(uint32_t)theirs);
-      least = max(least, their_key + (their_key != 0 && tile + kWaves > their_tile ? 1u : 0u));
+      left = __ballot(hits != 0) != 0;
+      if (left || (done && m >= (last ? kSortLast : kSortFrom)) || (least == 0 && !last)) sort_in(tile);
     }
+    if (!fresh) again = done ? -1 : again + 64;
+    if (!fresh && done) n = 0;
+    if (done)
+      tile += kWaves;
+    else if (fresh)
+      again = 0;
   }
   // The wave's sum over its lanes, then the workgroup's
   float high = wave_max(top);
@@ -397,7 +437,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     sums[wave] = sum;
   }
   lists[wave][lane] = best;
-  if (lane == 0) waiting[wave] = n;
+  if (lane == 0) waiting[wave] = m;
   __syncthreads();
   if (wave != 0) return;
   const int64_t at = (int64_t)row * p.parts + part;
@@ -409,7 +449,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     p.part_top[at] = high;
   }
   if (wanted == 0) return;
-  // What still waits in all queues, laid end to end; then the lists, where there are any
+  // The tokens that still wait, laid end to end; then the lists, where there are any
   int begin[kWaves], total = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
@@ -418,10 +458,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
   }
 #pragma unroll 1
   for (int i = lane; i - lane < total; i += 64) {
-    int token = queues[0][min(i, kQueue - 1)];
+    int token = tokens[0][min(i, kTokens - 1)];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w)
-      if (i >= begin[w]) token = queues[w][min(i - begin[w], kQueue - 1)];
+      if (i >= begin[w]) token = tokens[w][min(i - begin[w], kTokens - 1)];
     Entry<2> e;
     e.w[0] = i < total ? key_of(clean((float)x0[i < total ? token : 0])) : 0;
     e.w[1] = i < total ? ~(uint32_t)token : 0;
