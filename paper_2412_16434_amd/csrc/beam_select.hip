@@ -121,35 +121,36 @@ __device__ __forceinline__ void sort_rest(Entry<WORDS>& e) {  // sequences of 16
   exchange<2>(e);
   exchange<1>(e);
 }
-// `runs`: runs of so many lanes (a power of two) are sorted already
+// `runs`: runs of so many lanes (a power of two) are sorted already; `limit`: lanes from there on (a power of two) are empty
 template <int WORDS>
-__device__ __forceinline__ void sort64(Entry<WORDS>& e, int runs = 1) {
-  if (runs <= 1) exchange<1>(e);
-  if (runs <= 2) {
+__device__ __forceinline__ void sort64(Entry<WORDS>& e, int runs = 1, int limit = 64) {
+  if (runs <= 1 && limit > 1) exchange<1>(e);
+  if (runs <= 2 && limit > 2) {
     exchange<3>(e);
     exchange<1>(e);
   }
-  if (runs <= 4) {
+  if (runs <= 4 && limit > 4) {
     exchange<7>(e);
     exchange<2>(e);
     exchange<1>(e);
   }
-  if (runs <= 8) {
+  if (runs <= 8 && limit > 8) {
     exchange<15>(e);
     exchange<4>(e);
     exchange<2>(e);
     exchange<1>(e);
   }
-  if (runs <= 16) {
+  if (runs <= 16 && limit > 16) {
     exchange<31>(e);
     sort_rest(e);
   }
-  if (runs <= 32) {
+  if (runs <= 32 && limit > 32) {
     exchange<63>(e);
     exchange<16>(e);
     sort_rest(e);
   }
 }
+__device__ __forceinline__ int power_of_two_from(int n) { return n <= 1 ? 1 : 1 << (32 - __builtin_clz(n - 1)); }
 // The 64 largest of two sorted sequences, sorted
 template <int WORDS>
 __device__ __forceinline__ void join64(Entry<WORDS>& e, const Entry<WORDS>& with) {
@@ -318,8 +319,11 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
       Entry<2> e;
       e.w[0] = i < m ? key_of(clean((float)x0[token])) : 0;
       e.w[1] = i < m ? ~(uint32_t)token : 0;
-      sort64(e);
-      join64(best, e);
+      sort64(e, 1, min(power_of_two_from(m - (i - lane)), 64));
+      if (__ballot(best.w[0] != 0) == 0)
+        best = e;
+      else
+        join64(best, e);
     }
     wave_sync();
     m = 0;
@@ -465,8 +469,11 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     Entry<2> e;
     e.w[0] = i < total ? key_of(clean((float)x0[i < total ? token : 0])) : 0;
     e.w[1] = i < total ? ~(uint32_t)token : 0;
-    sort64(e);
-    join64(best, e);
+    sort64(e, 1, min(power_of_two_from(total - (i - lane)), 64));
+    if (__ballot(best.w[0] != 0) == 0)
+      best = e;
+    else
+      join64(best, e);
   }
 #pragma unroll 1
   for (int w = 1; w < kWaves; ++w) {
@@ -506,8 +513,7 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
     int token;
   };
   // A part's best are sorted: 2^n lanes to a part
-  int run = 1;
-  while (run < p.max_next) run <<= 1;
+  const int run = power_of_two_from(p.max_next), row_limit = min(power_of_two_from(p.parts * run), 64);
   const int per_batch = width > 0 ? 64 / run : 1;
   auto candidate = [&](int r, int first, float* x, int* token) {  // of the parts from `first` on
     const int part = first + lane / run, place = lane & (run - 1);
@@ -525,66 +531,80 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
     candidate(r, 0, &a.x, &a.token);
     return a;
   };
+  // Rows are taken as many together as there are waves.  Their lists meet in LDS, 64 entries' worth to a wave
+  const int most = min(r1 - r0, kSessionWaves), joiners = width > 0 ? (most * run + 63) / 64 : 0;
   Entry<4> best = {};  // sorted: the score's halves, ~(row, place in it), token
   Asked next;
   if (r0 + wave < r1) next = ask(r0 + wave);
 #pragma unroll 1
-  for (int r = r0 + wave; r < r1; r += kSessionWaves) {
-    const Asked a = next;
-    if (r + kSessionWaves < r1) next = ask(r + kSessionWaves);
-    double ends = -INFINITY;
-    if (alive(a.cum)) {
-      float high = a.top;
-      double sum = 0;
-      for (int q = lane + 64; q < p.parts; q += 64) high = fmaxf(high, p.part_top[(int64_t)r * p.parts + q]);
-      high = wave_max(high);
-      for (int q = lane; q < p.parts; q += 64) {
-        const bool first = q < 64;
-        const double part = first ? a.sum : p.part_sum[(int64_t)r * p.parts + q];
-        sum += part * (double)exp_below(first ? a.top : p.part_top[(int64_t)r * p.parts + q], high);
-      }
-      sum = wave_sum(sum);
-      const double log_sum = (double)high + log(sum);
-      if (a.last > -INFINITY) ends = (double)a.cum + ((double)a.last - log_sum);
-      Entry<2> of_row = {};
-      float x = a.x;
-      int token = a.token;
+  for (int c0 = r0; c0 < r1; c0 += kSessionWaves) {
+    const int r = c0 + wave;
+    Entry<4> e = {};
+    if (r < r1) {
+      const Asked a = next;
+      if (r + kSessionWaves < r1) next = ask(r + kSessionWaves);
+      double ends = -INFINITY;
+      if (alive(a.cum)) {
+        float high = a.top;
+        double sum = 0;
+        for (int q = lane + 64; q < p.parts; q += 64) high = fmaxf(high, p.part_top[(int64_t)r * p.parts + q]);
+        high = wave_max(high);
+        for (int q = lane; q < p.parts; q += 64) {
+          const bool first = q < 64;
+          const double part = first ? a.sum : p.part_sum[(int64_t)r * p.parts + q];
+          sum += part * (double)exp_below(first ? a.top : p.part_top[(int64_t)r * p.parts + q], high);
+        }
+        sum = wave_sum(sum);
+        const double log_sum = (double)high + log(sum);
+        if (a.last > -INFINITY) ends = (double)a.cum + ((double)a.last - log_sum);
+        Entry<2> of_row = {};
+        float x = a.x;
+        int token = a.token;
 #pragma unroll 1
-      for (int part = 0; part < p.parts && width > 0; part += per_batch) {
-        Entry<2> e;
-        e.w[0] = token >= 0 ? key_of(x) : 0;
-        e.w[1] = token >= 0 ? ~(uint32_t)token : 0;
-        if (part + per_batch < p.parts) candidate(r, part + per_batch, &x, &token);
-        sort64(e, run);
-        if (part == 0)
-          of_row = e;
-        else
-          join64(of_row, e);
+        for (int part = 0; part < p.parts && width > 0; part += per_batch) {
+          Entry<2> e;
+          e.w[0] = token >= 0 ? key_of(x) : 0;
+          e.w[1] = token >= 0 ? ~(uint32_t)token : 0;
+          if (part + per_batch < p.parts) candidate(r, part + per_batch, &x, &token);
+          sort64(e, run, row_limit);
+          if (part == 0)
+            of_row = e;
+          else
+            join64(of_row, e);
+        }
+        const bool there = lane < width && of_row.w[0] != 0;
+        const uint64_t key = key_of((double)a.cum + ((double)value_of(of_row.w[0]) - log_sum));
+        e.w[0] = there ? (uint32_t)(key >> 32) : 0;
+        e.w[1] = there ? (uint32_t)key : 0;
+        e.w[2] = there ? ~(uint32_t)((r - r0) * 64 + lane) : 0;
+        e.w[3] = ~of_row.w[1];
       }
-      const bool there = lane < width && of_row.w[0] != 0;
-      const uint64_t key = key_of((double)a.cum + ((double)value_of(of_row.w[0]) - log_sum));
-      Entry<4> e;
-      e.w[0] = there ? (uint32_t)(key >> 32) : 0;
-      e.w[1] = there ? (uint32_t)key : 0;
-      e.w[2] = there ? ~(uint32_t)((r - r0) * 64 + lane) : 0;
-      e.w[3] = ~of_row.w[1];
-      if (r < r0 + kSessionWaves)
-        best = e;
-      else
-        join64(best, e);
+      if (lane == 0) {
+        const bool near = r - r0 < kRows;
+        (near ? end_near[r - r0] : p.end_value[r]) = ends;
+        if (near) end_logit_near[r - r0] = a.last;
+      }
     }
-    if (lane == 0) {
-      const bool near = r - r0 < kRows;
-      (near ? end_near[r - r0] : p.end_value[r]) = ends;
-      if (near) end_logit_near[r - r0] = a.last;
-    }
-  }
-  // Half of the waves join what the other half has, and so on
-#pragma unroll 1
-  for (int half = kSessionWaves / 2; half > 0; half >>= 1) {
-    if (wave >= half && wave < 2 * half) lists[wave][lane] = best;
+    if (lane < run) lists[wave][lane] = e;
     __syncthreads();
-    if (wave < half && r0 + wave + half < r1) join64(best, lists[wave + half][lane]);  // (the others had no row)
+    if (wave < joiners) {
+      const int from = wave * per_batch + lane / run;
+      Entry<4> o = {};
+      if (from < min(r1 - c0, kSessionWaves)) o = lists[from][lane & (run - 1)];
+      sort64(o, run, min(power_of_two_from(most * run), 64));
+      if (c0 == r0)
+        best = o;
+      else
+        join64(best, o);
+    }
+    __syncthreads();
+  }
+  // Half of the joiners take what the other half has, and so on
+#pragma unroll 1
+  for (int half = power_of_two_from(joiners) / 2; half > 0; half >>= 1) {
+    if (wave >= half && wave < min(2 * half, joiners)) lists[wave][lane] = best;
+    __syncthreads();
+    if (wave < half && wave + half < joiners) join64(best, lists[wave + half][lane]);
   }
   if (wave == 0) {
     lists[0][lane] = best;
@@ -604,29 +624,32 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
   }
   if (!p.end_scores) return;
   __syncthreads();
+  // A wave per row: how many of the chosen, and how many other rows' ends, come before its end
   auto end_of = [&](int r) { return r - r0 < kRows ? end_near[r - r0] : p.end_value[r]; };
-  for (int r = r0 + tid; r < r1; r += 64 * kSessionWaves) {
+  for (int r = r0 + wave; r < r1; r += kSessionWaves) {
     const double mine = end_of(r);
-    int place = 0;
-    if (mine > -INFINITY) {
+    bool counts = mine > -INFINITY;
+    if (counts) {
       const uint64_t key = key_of(mine);
-      for (int k = 0; k < width; ++k) {
-        const Entry<4> e = lists[0][k];
+      bool before = false;
+      if (lane < width) {
+        const Entry<4> e = lists[0][lane];
         const uint64_t other = (uint64_t)e.w[0] << 32 | e.w[1];
         const int row = r0 + (int)(~e.w[2] >> 6);
-        bool before = other > key || (other == key && row < r);
+        before = other > key || (other == key && row < r);
         if (other == key && row == r) {
           const float x = r - r0 < kRows ? end_logit_near[r - r0] : p.end_logit[r], y = logit_at(p, r, (int)e.w[3]);
           before = y > x || (y == x && (int)e.w[3] < p.end_token);
         }
-        place += before;
       }
-      for (int q = r0; q < r1 && place < width; ++q) {
-        const double other = end_of(q);
-        place += other > mine || (other == mine && q < r);
+      int place = __popcll(__ballot(before));
+      for (int q0 = r0; q0 < r1 && place < width; q0 += 64) {
+        const double other = q0 + lane < r1 ? end_of(q0 + lane) : -INFINITY;
+        place += __popcll(__ballot(other > mine || (other == mine && q0 + lane < r)));
       }
+      counts = place < width;
     }
-    p.end_scores[r] = place < width ? (float)mine : -INFINITY;
+    if (lane == 0) p.end_scores[r] = counts ? (float)mine : -INFINITY;
   }
 }
 
