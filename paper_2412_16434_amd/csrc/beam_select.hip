@@ -166,7 +166,7 @@ __device__ __forceinline__ void join64(Entry<WORDS>& e, const Entry<WORDS>& with
 }
 
 // ---- parts of rows -----------------------------------------------------------------------------------------------
-constexpr int kValues = 32, kTile = 64 * kValues, kWaves = 4;  // a lane's values of a tile, a wave's tile
+constexpr int kValues = 32, kTile = 64 * kValues;  // a lane's values of a tile, a wave's tile
 
 typedef unsigned int u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));  // (rows begin at any element)
 typedef unsigned int u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
@@ -250,16 +250,17 @@ __device__ __forceinline__ float wave_max(float v) {
   return max_xor<32>(max_xor<16>(max_xor<8>(max_xor<4>(max_xor<2>(max_xor<1>(v))))));
 }
 
-template <typename T>
-__global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamParams p) {
-  __shared__ int queues[kWaves][kQueue], tokens[kWaves][kTokens];
-  __shared__ Entry<2> lists[kWaves][64];
-  __shared__ uint32_t firsts[kWaves][64];
+template <typename T, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 4) void beam_parts_kernel(const BeamParams p) {
+  __shared__ int queues[WAVES][kQueue], tokens[WAVES][kTokens];
+  __shared__ Entry<2> lists[WAVES][64];
+  __shared__ uint32_t firsts[WAVES][64];
   // What the best of the wave that is furthest reach, and the complement of the tile up to which they were found: later ones have to pass it
   __shared__ unsigned long long shared_least;
-  __shared__ int waiting[kWaves];
-  __shared__ float tops[kWaves];
-  __shared__ double sums[kWaves];
+  __shared__ int waiting, rest[WAVES * kSortLast];  // tokens that wait at the end
+  __shared__ uint32_t listed;                       // waves that have sorted some
+  __shared__ float tops[WAVES];
+  __shared__ double sums[WAVES];
   const int part = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   constexpr int kPer = Loads<T>::kPer, kVecs = kValues / kPer;
@@ -280,8 +281,12 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
   // Candidates reach the key `least`, as at least so many values as are wanted do: to begin with, that many lanes' largest in the
   // waves' first tiles.  (One more where the end token is among them.)  0: that is not known yet.
   uint32_t least = 0;
-  const int count = wanted + (p.end_token >= first * kTile && p.end_token < (first + kWaves) * kTile ? 1 : 0);
-  if (threadIdx.x == 0) shared_least = 0;
+  const int count = wanted + (p.end_token >= first * kTile && p.end_token < (first + WAVES) * kTile ? 1 : 0);
+  if (threadIdx.x == 0) {
+    shared_least = 0;
+    waiting = 0;
+    listed = 0;
+  }
   if (wanted > 0 && count <= 64) {
     Entry<1> e = {0};
     if (tile < end && (tile + 1) * kTile <= p.vocab) {
@@ -294,7 +299,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     firsts[wave][lane] = e.w[0];
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) e.w[0] = max(e.w[0], firsts[w][lane]);
+    for (int w = 0; w < WAVES; ++w) e.w[0] = max(e.w[0], firsts[w][lane]);
     sort64(e);
     least = (uint32_t)__builtin_amdgcn_readlane((int)e.w[0], count - 1);
   } else {
@@ -336,13 +341,13 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     if (lane == 0) theirs = atomicMax(&shared_least, mine);
     const uint32_t their_key = (uint32_t)__builtin_amdgcn_readfirstlane((int)(theirs >> 32));
     const int their_tile = (int)~__builtin_amdgcn_readfirstlane((int)(uint32_t)theirs);
-    least = max(least, their_key + (their_key != 0 && t + kWaves > their_tile ? 1u : 0u));
+    least = max(least, their_key + (their_key != 0 && t + WAVES > their_tile ? 1u : 0u));
   };
   // A turn looks through a tile, or again through 64 lanes' shares of earlier ones.  (Few lanes of a tile have a token that counts; to
   // look for it tile by tile took a fifth of the launch, so those lanes' values are read again, many tiles' together.)
   int again = -1;  // the queue's first entry that is to be looked at again
   while (tile < end) {
-    const bool fresh = again < 0, last = tile + kWaves >= end;
+    const bool fresh = again < 0, last = tile + WAVES >= end;
     if (!fresh) wave_sync();
     const int code = fresh ? tile * 64 + lane : again + lane < n ? queue[again + lane] : -1;
     const int base = max(code >> 6, 0) * kTile, l = code & 63;
@@ -370,7 +375,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     uint32_t open = code >= 0 ? 0xFFFFFFFFu : 0;  // values that are still to be looked at, the first in the highest bit
     bool done = !fresh && again + 64 >= n;        // with the tile, behind this turn
     if (fresh) {
-      if (tile + kWaves < end && base + (kWaves + 1) * kTile <= p.vocab) load_tile<T>(raw, x0 + base + kWaves * kTile);
+      if (tile + WAVES < end && base + (WAVES + 1) * kTile <= p.vocab) load_tile<T>(raw, x0 + base + WAVES * kTile);
       float here = largest(x), above, more;
       for (bool clear = false;; clear = true) {
         above = max3(top, here, here);
@@ -399,7 +404,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
       done = n == 0 || !(last || n + 64 > kQueue);
       if (!at_once) {
         if (done)
-          tile += kWaves;
+          tile += WAVES;
         else
           again = 0;
         continue;
@@ -429,45 +434,45 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
     if (!fresh) again = done ? -1 : again + 64;
     if (!fresh && done) n = 0;
     if (done)
-      tile += kWaves;
+      tile += WAVES;
     else if (fresh)
       again = 0;
   }
-  // The wave's sum over its lanes, then the workgroup's
-  float high = wave_max(top);
+  // The wave's sum over its lanes; its tokens that wait join the others' in any order
+  const float high = wave_max(top);
   sum = wave_sum(sum * (double)exp_below(top, high));
+  wave_sync();
+  int at = 0;
   if (lane == 0) {
     tops[wave] = high;
     sums[wave] = sum;
+    if (m > 0) at = atomicAdd(&waiting, m);
   }
-  lists[wave][lane] = best;
-  if (lane == 0) waiting[wave] = m;
+  at = __builtin_amdgcn_readfirstlane(at);
+  if (lane < m) rest[at + lane] = tokens[wave][lane];
+  if (wave > 0 && __ballot(best.w[0] != 0) != 0) {
+    lists[wave][lane] = best;
+    if (lane == 0) atomicOr(&listed, 1u << wave);
+  }
   __syncthreads();
   if (wave != 0) return;
-  const int64_t at = (int64_t)row * p.parts + part;
-  if (lane == 0) {
-    for (int w = 1; w < kWaves; ++w) high = fmaxf(high, tops[w]);
-    sum = 0;
-    for (int w = 0; w < kWaves; ++w) sum += sums[w] * (double)exp_below(tops[w], high);
-    p.part_sum[at] = sum;
-    p.part_top[at] = high;
+  const int64_t place = (int64_t)row * p.parts + part;
+  {
+    const bool in = lane < WAVES;
+    const float each = in ? tops[lane] : -FLT_MAX, all = wave_max(each);
+    const double whole = wave_sum(in ? sums[lane] * (double)exp_below(each, all) : 0.0);
+    if (lane == 0) {
+      p.part_sum[place] = whole;
+      p.part_top[place] = all;
+    }
   }
   if (wanted == 0) return;
-  // The tokens that still wait, laid end to end; then the lists, where there are any
-  int begin[kWaves], total = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    begin[w] = total;
-    total += waiting[w];
-  }
+  const int total = waiting;
 #pragma unroll 1
   for (int i = lane; i - lane < total; i += 64) {
-    int token = tokens[0][min(i, kTokens - 1)];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w)
-      if (i >= begin[w]) token = tokens[w][min(i - begin[w], kTokens - 1)];
+    const int token = i < total ? rest[i] : 0;
     Entry<2> e;
-    e.w[0] = i < total ? key_of(clean((float)x0[i < total ? token : 0])) : 0;
+    e.w[0] = i < total ? key_of(clean((float)x0[token])) : 0;
     e.w[1] = i < total ? ~(uint32_t)token : 0;
     sort64(e, 1, min(power_of_two_from(total - (i - lane)), 64));
     if (__ballot(best.w[0] != 0) == 0)
@@ -476,13 +481,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void beam_parts_kernel(const BeamPa
       join64(best, e);
   }
 #pragma unroll 1
-  for (int w = 1; w < kWaves; ++w) {
-    const Entry<2> e = lists[w][lane];
-    if (__ballot(e.w[0] != 0) != 0) join64(best, e);
-  }
+  for (uint32_t left = __builtin_amdgcn_readfirstlane((int)listed); left != 0; left &= left - 1) join64(best, lists[__builtin_ctz(left)][lane]);
   if (lane < wanted) {
-    p.cand_value[at * wanted + lane] = value_of(best.w[0]);
-    p.cand_token[at * wanted + lane] = best.w[0] ? (int32_t)~best.w[1] : -1;
+    p.cand_value[place * wanted + lane] = value_of(best.w[0]);
+    p.cand_token[place * wanted + lane] = best.w[0] ? (int32_t)~best.w[1] : -1;
   }
 }
 
@@ -653,18 +655,29 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
   }
 }
 
-// How rows are cut: so many workgroups that they fill the chip, tiles for all waves in each.
-constexpr int kGroupsWanted = 1024;
+// How rows are cut: into as many waves as there are places for (four to a SIMD; half as many: 39.6 against 36.3 us for 512 rows of
+// 128256 in bf16), a wave having a tile at least.  Up to eight waves of a row share a workgroup: what they know of each other's first
+// tiles keeps the lists short, and few parts keep the second launch short (four at most: 11.9 against 11.2 us for 32 rows, 19.0
+// against 17.8 for 90 of 50001 in fp32; up to sixteen, which wait for each other: 12.7 and 17.3).
+constexpr int kWavesWanted = 4096;
 struct RowCut {
-  int32_t parts, tiles;  // parts of a row, tiles of a part
+  int32_t parts, tiles, waves;  // parts of a row, tiles of a part, waves of a part's workgroup (4 or 8)
 };
 static RowCut cut_rows(int32_t n_rows, int32_t vocab) {
-  const int64_t tiles = ceil_div64(vocab, kTile);
-  const int64_t wanted = std::min(ceil_div64(kGroupsWanted, std::max(n_rows, 1)), ceil_div64(tiles, kWaves));
+  const int64_t tiles = ceil_div64(vocab, kTile), per_row = std::min<int64_t>(tiles, std::max(kWavesWanted / std::max(n_rows, 1), 1));
   RowCut c;
-  c.tiles = (int32_t)ceil_div64(tiles, wanted);
+  c.waves = per_row <= 4 ? 4 : 8;
+  c.tiles = (int32_t)ceil_div64(tiles, ceil_div64(per_row, c.waves));
   c.parts = (int32_t)ceil_div64(tiles, c.tiles);
   return c;
+}
+template <typename T>
+static void launch_parts(const BeamParams& p, const RowCut& cut, hipStream_t stream) {
+  const dim3 grid((unsigned)cut.parts, (unsigned)p.n_rows), threads(64 * cut.waves);
+  if (cut.waves == 4)
+    hipLaunchKernelGGL((beam_parts_kernel<T, 4>), grid, threads, 0, stream, p);
+  else
+    hipLaunchKernelGGL((beam_parts_kernel<T, 8>), grid, threads, 0, stream, p);
 }
 static int64_t round256(int64_t n) { return (n + 255) & ~(int64_t)255; }
 
@@ -693,7 +706,7 @@ int32_t symph_beam_select(const void* d_logits, int64_t row_stride, int32_t dtyp
   if (total_next > 0 && (!d_parents || !d_tokens || !d_next_scores)) return SYMPH_EINVAL;
   if (d_next_scores && d_next_scores == d_scores) return SYMPH_EINVAL;
   // (a grid's second axis takes 65535 workgroups; tiles are counted in 32 bits)
-  if (n_rows > 65535 || vocab > 0x7FFFFFFF - 2 * kWaves * kTile || !grid_takes(n_sessions, 64 * kSessionWaves)) return SYMPH_EUNSUPPORTED;
+  if (n_rows > 65535 || vocab > 0x7FFFFFFF - 16 * kTile || !grid_takes(n_sessions, 64 * kSessionWaves)) return SYMPH_EUNSUPPORTED;
   if (workspace_bytes < symph_beam_select_workspace_bytes(n_rows, vocab, max_next) || (!d_workspace && n_rows > 0))
     return SYMPH_EWORKSPACE;
   const RowCut cut = cut_rows(n_rows, vocab);
@@ -730,13 +743,8 @@ int32_t symph_beam_select(const void* d_logits, int64_t row_stride, int32_t dtyp
   p.part_tiles = cut.tiles;
   p.wide = dtype == SYMPH_FP32;
   hipStream_t st = (hipStream_t)stream;
-  const dim3 grid((unsigned)cut.parts, (unsigned)n_rows), threads(64 * kWaves);
-  if (n_rows > 0) {
-    if (dtype == SYMPH_BF16)
-      hipLaunchKernelGGL(beam_parts_kernel<__bf16>, grid, threads, 0, st, p);
-    else
-      hipLaunchKernelGGL(beam_parts_kernel<float>, grid, threads, 0, st, p);
-  }
+  if (n_rows > 0 && dtype == SYMPH_BF16) launch_parts<__bf16>(p, cut, st);
+  if (n_rows > 0 && dtype == SYMPH_FP32) launch_parts<float>(p, cut, st);
   hipLaunchKernelGGL(beam_sessions_kernel, dim3((unsigned)n_sessions), dim3(64 * kSessionWaves), 0, st, p);
   return hipGetLastError() == hipSuccess ? SYMPH_OK : SYMPH_ELAUNCH;
 }
