@@ -479,6 +479,37 @@ def _load_draft_calls():
     return _draft_calls
 
 
+_beam_calls = None  # the same for beam search
+
+
+def _load_beam_calls():
+    global _beam_calls
+    compiled = _attn_call or _load_attn_call()
+    if compiled is not _attn_call:  # (no library)
+        return False
+    _beam_calls = False
+    module = getattr(compiled, "__self__", None)
+    if hasattr(module, "bind_beam"):
+        lib = load_library()
+        module.bind_beam(*(C.cast(f, C.c_void_p).value for f in (
+            lib.symph_beam_select, lib.symph_kv_fork, lib.symph_kv_copy_blocks, lib.symph_kv_free, lib.symph_kv_compact)))
+        _beam_calls = module
+    return _beam_calls
+
+
+def _beam_call(stream):
+    return stream is None and (_load_beam_calls() if _beam_calls is None else _beam_calls)
+
+
+def _on_this_device(stream, **tensors) -> None:
+    """Without a stream the call goes to the current device's: the tensors have to be there."""
+    if stream is None:
+        torch = _torch()
+        for name, t in tensors.items():
+            if t is not None and t.is_cuda and t.get_device() != torch.cuda.current_device():
+                raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is cuda:{torch.cuda.current_device()}")
+
+
 def _load_attn_call():
     """The compiled marshalling of the ordinary attention call (``csrc/attn_call.c``), bound to the library's entry point; where
     it is not built (or not for this interpreter), or torch lacks what it needs, what leaves every call to the general path."""
@@ -694,6 +725,12 @@ def beam_select(logits, scores, cu_rows, cu_next, max_next: int, parents, tokens
     [n_rows][vocab], bf16 or fp32, dense along the vocabulary) by score = ``scores`` + log-probability: ``parents`` (the beam's
     row), ``tokens`` and ``next_scores``, best first; -1, -1 and -inf where there are fewer.  ``end_token`` never continues a beam;
     its score goes to ``end_scores`` [n_rows] where it is among the session's best."""
+    calls = _beam_call(stream)
+    if calls:
+        status = calls.select_beams(logits, scores, cu_rows, cu_next, max_next, parents, tokens, next_scores, end_token, end_scores,
+                                    workspace)
+        if status is not None:
+            return _check(status, "symph_beam_select")
     torch = _torch()
     i32, f32 = torch.int32, torch.float32
     if logits.dim() != 2 or logits.dtype not in (torch.bfloat16, f32):
@@ -703,6 +740,8 @@ def beam_select(logits, scores, cu_rows, cu_next, max_next: int, parents, tokens
     (rows, vocab), (row_stride, step) = logits.shape, logits.stride()
     if (vocab > 1 and step != 1) or (rows > 1 and row_stride < vocab):
         raise ValueError("logits must be dense along the vocabulary, rows apart")
+    _on_this_device(stream, logits=logits, scores=scores, cu_rows=cu_rows, cu_next=cu_next, parents=parents, tokens=tokens,
+                    next_scores=next_scores, end_scores=end_scores, workspace=workspace)
     n, total = cu_rows.shape[0] - 1, parents.shape[0]
     wp, ws_bytes = _scratch(workspace)
     _check(load_library().symph_beam_select(
@@ -728,6 +767,15 @@ def kv_fork(parents, lens, block_table, refs, free_blocks, block_size: int, tabl
     """Rows that continue rows ``parents`` of ``block_table``: full blocks shared, the last one kept by a row's first child and
     replaced by a block of ``free_blocks`` for the others (``copy_*``: what kv_copy_blocks has to copy); ``refs_after`` <- how many
     rows hold each block.  A parent outside the table makes an empty row."""
+    calls = _beam_call(stream)
+    if calls:
+        status = calls.fork_rows(parents, lens, block_table, refs, free_blocks, block_size, table_out, lens_out, refs_after, copy_src,
+                                 copy_dst, copy_tokens, held_blocks, held_out, free_begin, blocks_taken)
+        if status is not None:
+            return _check(status, "symph_kv_fork")
+    _on_this_device(stream, parents=parents, lens=lens, block_table=block_table, refs=refs, free_blocks=free_blocks, table_out=table_out,
+                    lens_out=lens_out, refs_after=refs_after, copy_src=copy_src, copy_dst=copy_dst, copy_tokens=copy_tokens,
+                    held_blocks=held_blocks, held_out=held_out, free_begin=free_begin, blocks_taken=blocks_taken)
     i32 = _torch().int32
     out, n, n_blocks = parents.shape[0], lens.shape[0], refs.shape[0]
     tp, stride = _rows_table(block_table, "block_table", n)
@@ -745,6 +793,14 @@ def kv_fork(parents, lens, block_table, refs, free_blocks, block_size: int, tabl
 def kv_copy_blocks(cache: KVCache, src_blocks, dst_blocks, tokens=None, stream=None) -> None:
     """The first ``tokens[i]`` slots (None: all) of block ``src_blocks[i]`` of every layer into block ``dst_blocks[i]``, for every i
     where both are blocks of the cache."""
+    calls = type(cache) is KVCache and _beam_call(stream)
+    if calls:
+        status = calls.copy_blocks(cache.k_pool, cache.v_pool, src_blocks, dst_blocks, tokens)
+        if status is not None:
+            return _check(status, "symph_kv_copy_blocks")
+    _on_this_device(stream, k_pool=cache.k_pool, v_pool=cache.v_pool, src_blocks=src_blocks, dst_blocks=dst_blocks, tokens=tokens)
+    if not (cache.k_pool.is_cuda and cache.v_pool.is_cuda):
+        raise ValueError("the pools must be device tensors")
     st = cache.struct()
     i32, n = _torch().int32, src_blocks.shape[0]
     _check(load_library().symph_kv_copy_blocks(
@@ -763,6 +819,14 @@ def kv_free(drop, lens, block_table, refs, block_size: int, refs_after, free_blo
             held_after=None, workspace=None, stream=None) -> None:
     """``refs_after`` <- ``refs`` without what rows with ``drop[r] != 0`` hold; ``free_blocks`` <- the blocks that nobody holds then,
     ascending, -1 behind them; ``n_free`` <- how many.  ``drop``, ``lens`` and ``block_table`` may be None: the list alone."""
+    calls = _beam_call(stream)
+    if calls:
+        status = calls.free_rows(drop, lens, block_table, refs, block_size, refs_after, free_blocks, n_free, held_blocks, lens_after,
+                                 held_after, workspace)
+        if status is not None:
+            return _check(status, "symph_kv_free")
+    _on_this_device(stream, drop=drop, lens=lens, block_table=block_table, refs=refs, refs_after=refs_after, free_blocks=free_blocks,
+                    n_free=n_free, held_blocks=held_blocks, lens_after=lens_after, held_after=held_after, workspace=workspace)
     i32 = _torch().int32
     n, n_blocks = 0 if drop is None else drop.shape[0], refs.shape[0]
     tp, stride = _rows_table(block_table, "block_table", n) if n else (None, 0)
@@ -787,6 +851,14 @@ def kv_compact(refs, n_keep: int, lens, block_table, block_size: int, table_out,
     """The moves after which the blocks from ``n_keep`` on are free (negative: all blocks in use move to the front), as lists for
     kv_copy_blocks, and the table (``table_out`` may be ``block_table``), counts and ``block_map`` after them.  ``counts`` <- blocks
     in use, moves, blocks that stay behind."""
+    calls = _beam_call(stream)
+    if calls:
+        status = calls.compact_pool(refs, n_keep, lens, block_table, block_size, table_out, refs_after, block_map, copy_src, copy_dst,
+                                    counts, held_blocks, workspace)
+        if status is not None:
+            return _check(status, "symph_kv_compact")
+    _on_this_device(stream, refs=refs, lens=lens, block_table=block_table, table_out=table_out, refs_after=refs_after, block_map=block_map,
+                    copy_src=copy_src, copy_dst=copy_dst, counts=counts, held_blocks=held_blocks, workspace=workspace)
     i32 = _torch().int32
     n, n_blocks, n_pairs = lens.shape[0], refs.shape[0], copy_src.shape[0]
     tp, stride = _rows_table(block_table, "block_table", n)

@@ -1,7 +1,7 @@
 // Argument checks and marshalling, compiled, of the calls that a model's step makes: what binding.py's prefix_prefill_attn
 // does with some fifty attribute reads and a ctypes call, 3.6 of the 9.2 us that a call of one launch kept the host busy; the
 // operators of a drafted step likewise (small calls, one after another: build_tables 9.3 -> 6.1 us, tree_mask 7.1 -> 4.8,
-// tree_attn 11.5 -> 10.7, tree_accept and kv_commit together 17.3 -> 11.4).  Only the ordinary call is taken (no stream or
+// tree_attn 11.5 -> 10.7, tree_accept and kv_commit together 17.3 -> 11.4); and those of a step of beam search.  Only the ordinary call is taken (no stream or
 // tuning argument, every tensor as the entry point wants it); for anything else, and for every error, the answer is None and
 // the general path decides, so that there is one place that says what is wrong.
 #define PY_SSIZE_T_CLEAN
@@ -26,16 +26,31 @@ typedef int32_t (*accept_fn)(const int32_t*, const int32_t*, const int32_t*, con
                              int32_t*, int32_t*, int32_t*, int32_t*, void*);
 typedef int32_t (*commit_fn)(const symph_kv_cache*, const void*, const void*, int32_t, const int32_t*, const int64_t*, int32_t,
                              void*);
+typedef int32_t (*select_fn)(const void*, int64_t, int32_t, int32_t, int32_t, const float*, const int32_t*, const int32_t*, int32_t,
+                             int32_t, int32_t, int32_t, int32_t*, int32_t*, float*, float*, void*, int64_t, void*);
+typedef int32_t (*fork_fn)(const int32_t*, int32_t, const int32_t*, const int32_t*, int32_t, const int32_t*, int32_t, int32_t, int32_t,
+                           const int32_t*, const int32_t*, int32_t, const int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, int32_t*,
+                           int32_t*, int32_t*, int32_t*, void*);
+typedef int32_t (*copy_fn)(const symph_kv_cache*, const int32_t*, const int32_t*, const int32_t*, int32_t, void*);
+typedef int32_t (*free_fn)(const int32_t*, const int32_t*, const int32_t*, int32_t, const int32_t*, int32_t, int32_t, int32_t,
+                           const int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, void*, int64_t, void*);
+typedef int32_t (*compact_fn)(const int32_t*, int32_t, int32_t, const int32_t*, const int32_t*, int32_t, const int32_t*, int32_t, int32_t,
+                              int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, int32_t, int32_t*, void*, int64_t, void*);
 
-// Set once, by bind() and bind_draft()
+// Set once, by bind(), bind_draft() and bind_beam()
 static attn_fn entry;
 static tables_fn tables_entry;
 static mask_fn mask_entry;
 static tree_fn tree_entry;
 static accept_fn accept_entry;
 static commit_fn commit_entry;
+static select_fn select_entry;
+static fork_fn fork_entry;
+static copy_fn copy_entry;
+static free_fn free_entry;
+static compact_fn compact_entry;
 static PyObject *t_bf16, *t_fp32, *t_int32, *t_int64, *raw_stream, *get_device;
-static PyObject *s_dtype, *s_shape, *s_is_cuda, *s_is_contiguous, *s_data_ptr, *s_stride, *s_numel, *s_element_size;
+static PyObject *s_dtype, *s_shape, *s_is_cuda, *s_is_contiguous, *s_data_ptr, *s_stride, *s_numel, *s_element_size, *s_get_device;
 
 static PyObject* bind(PyObject* self, PyObject* args) {
   unsigned long long address;
@@ -59,6 +74,16 @@ static PyObject* bind_draft(PyObject* self, PyObject* args) {
   t_int64 = i64;
   tables_entry = (tables_fn)(uintptr_t)a, mask_entry = (mask_fn)(uintptr_t)b, tree_entry = (tree_fn)(uintptr_t)c;
   accept_entry = (accept_fn)(uintptr_t)d, commit_entry = (commit_fn)(uintptr_t)e;
+  Py_RETURN_NONE;
+}
+
+// (after bind())
+static PyObject* bind_beam(PyObject* self, PyObject* args) {
+  unsigned long long a, b, c, d, e;
+  (void)self;
+  if (!PyArg_ParseTuple(args, "KKKKK", &a, &b, &c, &d, &e)) return NULL;
+  select_entry = (select_fn)(uintptr_t)a, fork_entry = (fork_fn)(uintptr_t)b, copy_entry = (copy_fn)(uintptr_t)c;
+  free_entry = (free_fn)(uintptr_t)d, compact_entry = (compact_fn)(uintptr_t)e;
   Py_RETURN_NONE;
 }
 
@@ -326,6 +351,184 @@ static PyObject* commit(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   return PyLong_FromLong(status);
 }
 
+// ---- beam search: every tensor has to be on the current device ----
+typedef struct {
+  int64_t device;
+  void* stream;
+} place;
+
+static int current_place(place* at) {
+  PyObject* device = PyObject_CallNoArgs(get_device);
+  PyObject* raw = device ? PyObject_CallOneArg(raw_stream, device) : NULL;
+  const int ok = raw && PyLong_Check(raw) && as_int(device, &at->device);
+  if (ok) at->stream = PyLong_AsVoidPtr(raw);
+  Py_XDECREF(raw);
+  Py_XDECREF(device);
+  return ok && !PyErr_Occurred();
+}
+static int dense_at(PyObject* t, PyObject* dtype, const place* at, void** ptr) {
+  int64_t device, p;
+  if (!method_int(t, s_get_device, &device) || device != at->device || (dtype && !attr_is(t, s_dtype, dtype))) return 0;
+  PyObject* r = PyObject_CallMethodNoArgs(t, s_is_contiguous);
+  const int ok = r == Py_True;
+  Py_XDECREF(r);
+  if (!ok || !method_int(t, s_data_ptr, &p)) return 0;
+  *ptr = (void*)(uintptr_t)p;
+  return 1;
+}
+static int vector_at(PyObject* t, PyObject* dtype, int64_t least, int optional, const place* at, void** ptr, int64_t* length) {
+  int64_t n;
+  if (t == Py_None) {
+    *ptr = NULL;
+    return optional;
+  }
+  if (!dims(t, s_shape, 0, 1, &n) || n < least || n > INT32_MAX || !dense_at(t, dtype, at, ptr)) return 0;
+  if (length) *length = n;
+  return 1;
+}
+// An int32 [>= rows][stride] table; stride < 0: any, which becomes it
+static int table_at(PyObject* t, int64_t rows, int64_t* stride, const place* at, void** ptr) {
+  int64_t d[2];
+  if (!dims(t, s_shape, 0, 2, d) || d[0] < rows || d[1] > INT32_MAX || (*stride >= 0 && d[1] != *stride) ||
+      !dense_at(t, t_int32, at, ptr))
+    return 0;
+  *stride = d[1];
+  return 1;
+}
+static int scratch_at(PyObject* t, const place* at, void** ptr, int64_t* bytes) {
+  int64_t n, e;
+  *ptr = NULL, *bytes = 0;
+  if (t == Py_None) return 1;
+  if (!dense_at(t, NULL, at, ptr) || !method_int(t, s_numel, &n) || !method_int(t, s_element_size, &e)) return 0;
+  *bytes = n * e;
+  return 1;
+}
+
+// (logits, scores, cu_rows, cu_next, max_next, parents, tokens, next_scores, end_token, end_scores, workspace) -> status or None
+static PyObject* select_beams(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
+  (void)self;
+  place at;
+  int64_t d[2], strides[2], n, total, device, ws_bytes, p;
+  int32_t most, end, status;
+  void *scores, *cu, *cu_next, *parents, *tokens, *best, *ends, *ws;
+  PyObject* dt = n_args == 11 ? PyObject_GetAttr(a[0], s_dtype) : NULL;
+  Py_XDECREF(dt);  // (torch's dtypes live as long as the module)
+  if (!dt || !select_entry || (dt != t_bf16 && dt != t_fp32) || !current_place(&at) || !dims(a[0], s_shape, 0, 2, d) ||
+      !dims(a[0], s_stride, 1, 2, strides) || d[0] > INT32_MAX || d[1] > INT32_MAX || (d[1] > 1 && strides[1] != 1) ||
+      (d[0] > 1 && strides[0] < d[1]) || !method_int(a[0], s_get_device, &device) || device != at.device ||
+      !method_int(a[0], s_data_ptr, &p) || !vector_at(a[1], t_fp32, d[0], 0, &at, &scores, NULL) ||
+      !vector_at(a[2], t_int32, 1, 0, &at, &cu, &n) || (n -= 1) < 0 || !vector_at(a[3], t_int32, n + 1, 0, &at, &cu_next, NULL) ||
+      !as_int32(a[4], &most) || !vector_at(a[5], t_int32, 0, 0, &at, &parents, &total) ||
+      !vector_at(a[6], t_int32, total, 0, &at, &tokens, NULL) || !vector_at(a[7], t_fp32, total, 0, &at, &best, NULL) ||
+      !as_int32(a[8], &end) || !vector_at(a[9], t_fp32, d[0], 1, &at, &ends, NULL) || !scratch_at(a[10], &at, &ws, &ws_bytes)) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  Py_BEGIN_ALLOW_THREADS
+  status = select_entry((void*)(uintptr_t)p, strides[0] < d[1] ? d[1] : strides[0], dt == t_bf16 ? SYMPH_BF16 : SYMPH_FP32, (int32_t)d[0],
+                        (int32_t)d[1], scores, cu, cu_next, (int32_t)n, (int32_t)total, most, end, parents, tokens, best, ends, ws,
+                        ws_bytes, at.stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// (parents, lens, block_table, refs, free_blocks, block_size, table_out, lens_out, refs_after, copy_src, copy_dst, copy_tokens,
+// held_blocks, held_out, free_begin, blocks_taken) -> status or None
+static PyObject* fork_rows(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
+  (void)self;
+  place at;
+  int64_t out, n, blocks, n_free, stride = -1;
+  int32_t bs, status;
+  void *parents, *lens, *table, *refs, *list, *to, *lens_out, *after, *src, *dst, *count, *held, *held_out, *begin, *taken;
+  if (n_args != 16 || !fork_entry || !current_place(&at) || !vector_at(a[0], t_int32, 0, 0, &at, &parents, &out) ||
+      !vector_at(a[1], t_int32, 0, 0, &at, &lens, &n) || !table_at(a[2], n, &stride, &at, &table) ||
+      !vector_at(a[3], t_int32, 0, 0, &at, &refs, &blocks) || !vector_at(a[4], t_int32, 0, 0, &at, &list, &n_free) ||
+      !as_int32(a[5], &bs) || !table_at(a[6], out, &stride, &at, &to) || !vector_at(a[7], t_int32, out, 0, &at, &lens_out, NULL) ||
+      !vector_at(a[8], t_int32, blocks, 0, &at, &after, NULL) || !vector_at(a[9], t_int32, out, 0, &at, &src, NULL) ||
+      !vector_at(a[10], t_int32, out, 0, &at, &dst, NULL) || !vector_at(a[11], t_int32, out, 0, &at, &count, NULL) ||
+      !vector_at(a[12], t_int32, n, 1, &at, &held, NULL) || !vector_at(a[13], t_int32, out, 1, &at, &held_out, NULL) ||
+      !vector_at(a[14], t_int32, 1, 1, &at, &begin, NULL) || !vector_at(a[15], t_int32, 1, 1, &at, &taken, NULL)) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  Py_BEGIN_ALLOW_THREADS
+  status = fork_entry(parents, (int32_t)out, lens, held, (int32_t)n, table, (int32_t)stride, bs, (int32_t)blocks, refs, list,
+                      (int32_t)n_free, begin, to, lens_out, held_out, after, src, dst, count, taken, at.stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// (k_pool, v_pool, src_blocks, dst_blocks, tokens) -> status or None
+static PyObject* copy_blocks(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
+  (void)self;
+  place at;
+  symph_kv_cache c;
+  int64_t n, device;
+  int32_t status;
+  PyObject* dt;
+  void *src, *dst, *count;
+  if (n_args != 5 || !copy_entry || !current_place(&at) || !describe(a[0], a[1], &dt, &c) ||
+      !method_int(a[0], s_get_device, &device) || device != at.device || !method_int(a[1], s_get_device, &device) ||
+      device != at.device || !vector_at(a[2], t_int32, 0, 0, &at, &src, &n) || !vector_at(a[3], t_int32, n, 0, &at, &dst, NULL) ||
+      !vector_at(a[4], t_int32, n, 1, &at, &count, NULL)) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  Py_BEGIN_ALLOW_THREADS
+  status = copy_entry(&c, src, dst, count, (int32_t)n, at.stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// (drop, lens, block_table, refs, block_size, refs_after, free_blocks, n_free, held_blocks, lens_after, held_after, workspace) ->
+// status or None
+static PyObject* free_rows(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
+  (void)self;
+  place at;
+  int64_t n, blocks, ws_bytes, stride = -1;
+  int32_t bs, status;
+  void *drop, *lens, *table, *refs, *after, *list, *count, *held, *lens_after, *held_after, *ws;
+  if (n_args != 12 || !free_entry || a[0] == Py_None || !current_place(&at) || !vector_at(a[0], t_int32, 1, 0, &at, &drop, &n) ||
+      !vector_at(a[1], t_int32, n, 0, &at, &lens, NULL) || !table_at(a[2], n, &stride, &at, &table) ||
+      !vector_at(a[3], t_int32, 0, 0, &at, &refs, &blocks) || !as_int32(a[4], &bs) ||
+      !vector_at(a[5], t_int32, blocks, 0, &at, &after, NULL) || !vector_at(a[6], t_int32, blocks, 0, &at, &list, NULL) ||
+      !vector_at(a[7], t_int32, 1, 0, &at, &count, NULL) || !vector_at(a[8], t_int32, n, 1, &at, &held, NULL) ||
+      !vector_at(a[9], t_int32, n, 1, &at, &lens_after, NULL) || !vector_at(a[10], t_int32, n, 1, &at, &held_after, NULL) ||
+      !scratch_at(a[11], &at, &ws, &ws_bytes)) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  Py_BEGIN_ALLOW_THREADS
+  status = free_entry(drop, lens, held, (int32_t)n, table, (int32_t)stride, bs, (int32_t)blocks, refs, after, list, count, lens_after,
+                      held_after, ws, ws_bytes, at.stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// (refs, n_keep, lens, block_table, block_size, table_out, refs_after, block_map, copy_src, copy_dst, counts, held_blocks, workspace)
+// -> status or None
+static PyObject* compact_pool(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
+  (void)self;
+  place at;
+  int64_t n, blocks, pairs, ws_bytes, stride = -1;
+  int32_t keep, bs, status;
+  void *refs, *lens, *table, *to, *after, *map, *src, *dst, *counts, *held, *ws;
+  if (n_args != 13 || !compact_entry || !current_place(&at) || !vector_at(a[0], t_int32, 0, 0, &at, &refs, &blocks) ||
+      !as_int32(a[1], &keep) || !vector_at(a[2], t_int32, 0, 0, &at, &lens, &n) || !table_at(a[3], n, &stride, &at, &table) ||
+      !as_int32(a[4], &bs) || !table_at(a[5], n, &stride, &at, &to) || !vector_at(a[6], t_int32, blocks, 0, &at, &after, NULL) ||
+      !vector_at(a[7], t_int32, blocks, 0, &at, &map, NULL) || !vector_at(a[8], t_int32, 0, 0, &at, &src, &pairs) ||
+      !vector_at(a[9], t_int32, pairs, 0, &at, &dst, NULL) || !vector_at(a[10], t_int32, 3, 0, &at, &counts, NULL) ||
+      !vector_at(a[11], t_int32, n, 1, &at, &held, NULL) || !scratch_at(a[12], &at, &ws, &ws_bytes)) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  Py_BEGIN_ALLOW_THREADS
+  status = compact_entry(refs, (int32_t)blocks, keep, lens, held, (int32_t)n, table, (int32_t)stride, bs, to, after, map, src, dst,
+                         (int32_t)pairs, counts, ws, ws_bytes, at.stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
 static PyMethodDef methods[] = {
     {"bind", bind, METH_VARARGS, "bind(address of the entry point, bfloat16, float32, int32, raw stream of a device, current device)"},
     {"attn", (PyCFunction)(void (*)(void))attn, METH_FASTCALL, "status of the call, or None where the general path has to make it"},
@@ -335,6 +538,12 @@ static PyMethodDef methods[] = {
     {"mask", (PyCFunction)(void (*)(void))mask, METH_FASTCALL, "tree_mask, likewise"},
     {"accept", (PyCFunction)(void (*)(void))accept, METH_FASTCALL, "tree_accept, likewise"},
     {"commit", (PyCFunction)(void (*)(void))commit, METH_FASTCALL, "kv_commit, likewise"},
+    {"bind_beam", bind_beam, METH_VARARGS, "bind_beam(addresses of beam_select, kv_fork, kv_copy_blocks, kv_free, kv_compact)"},
+    {"select_beams", (PyCFunction)(void (*)(void))select_beams, METH_FASTCALL, "beam_select, likewise"},
+    {"fork_rows", (PyCFunction)(void (*)(void))fork_rows, METH_FASTCALL, "kv_fork, likewise"},
+    {"copy_blocks", (PyCFunction)(void (*)(void))copy_blocks, METH_FASTCALL, "kv_copy_blocks, likewise"},
+    {"free_rows", (PyCFunction)(void (*)(void))free_rows, METH_FASTCALL, "kv_free, likewise"},
+    {"compact_pool", (PyCFunction)(void (*)(void))compact_pool, METH_FASTCALL, "kv_compact, likewise"},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_attn_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
@@ -347,7 +556,8 @@ PyMODINIT_FUNC PyInit__attn_call(void) {
   s_stride = PyUnicode_InternFromString("stride");
   s_numel = PyUnicode_InternFromString("numel");
   s_element_size = PyUnicode_InternFromString("element_size");
-  if (!s_dtype || !s_shape || !s_is_cuda || !s_is_contiguous || !s_data_ptr || !s_stride || !s_numel || !s_element_size)
+  s_get_device = PyUnicode_InternFromString("get_device");
+  if (!s_dtype || !s_shape || !s_is_cuda || !s_is_contiguous || !s_data_ptr || !s_stride || !s_numel || !s_element_size || !s_get_device)
     return NULL;
   return PyModule_Create(&module);
 }
