@@ -76,13 +76,75 @@ struct ForkParams {
   int32_t n_out, n_rows, n_free, n_blocks;
 };
 
+// Small calls take one launch, which is what they cost: up to so many table entries, rows and (in one workgroup) blocks.
+constexpr int kFewEntries = 16384, kFewRows = 1024, kFewBlocks = 8192;
+static bool few(int32_t n_rows, int32_t table_stride) {
+  return n_rows <= kFewRows && (int64_t)n_rows * table_stride <= kFewEntries;
+}
+constexpr int kSlice = 4096;  // blocks whose counts a workgroup of a small fork has
+
+// The counts of a slice of the pool after a small fork, every change looked for in the whole table.
+__device__ __forceinline__ void fork_slice(const ForkParams& p, int slice, int* lds) {
+  __shared__ int change[kSlice], children[kFewRows], whole[kFewRows], held[kFewRows];
+  int* const first = lds + 4;
+  const int tid = threadIdx.x, lo = slice * kSlice, n = min(p.n_blocks - lo, kSlice);
+  for (int b = tid; b < kSlice; b += kThreads) change[b] = 0;
+  for (int r = tid; r < p.n_rows; r += kThreads) {
+    const RowBlocks b = blocks_of_row(p.shape, r);
+    first[r] = 0x7FFFFFFF;
+    children[r] = 0;
+    whole[r] = b.whole;
+    held[r] = b.held | (b.whole < b.used ? 1 << 30 : 0);  // (bit 30: the last block in use is not full; a row has fewer blocks)
+  }
+  __syncthreads();
+  for (int i = tid; i < p.n_out; i += kThreads) {
+    const int up = p.parents[i];
+    if (up < 0 || up >= p.n_rows) continue;
+    atomicAdd(children + up, 1);
+    atomicMin(first + up, i);
+  }
+  __syncthreads();
+  int made = 0;
+  for (int r = tid; r < p.n_rows; r += kThreads)
+    if (held[r] >> 30) made += max(children[r] - 1, 0);
+  made = group_sum(made, lds);
+  const int entries = p.n_rows * p.shape.stride;
+  constexpr int kAhead = 4;
+  for (int e0 = tid; e0 < entries; e0 += kThreads * kAhead) {
+    int id[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) id[u] = e0 + u * kThreads < entries ? p.table[e0 + u * kThreads] : -1;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int at = id[u] - lo;
+      if (id[u] < 0 || at < 0 || at >= n) continue;
+      const int r = (e0 + u * kThreads) / p.shape.stride, c = e0 + u * kThreads - r * p.shape.stride;
+      const int more = c < whole[r] ? children[r] - 1 : c < (held[r] & 0x3FFFFFFF) && children[r] == 0 ? -1 : 0;
+      if (more != 0) atomicAdd(change + at, more);
+    }
+  }
+  const int64_t begin = p.free_begin ? p.free_begin[0] : 0;
+  for (int k = tid; k < made; k += kThreads) {
+    const int at = begin + k >= 0 && begin + k < p.n_free ? p.free_blocks[begin + k] - lo : -1;
+    if (at >= 0 && at < n) atomicAdd(change + at, 1);
+  }
+  __syncthreads();
+  for (int b = tid; b < n; b += kThreads) p.refs_after[lo + b] = p.refs[lo + b] + change[b];
+}
+
 // A workgroup per row of the result, and more that carry the counts over.  A row's place in the free list is the number of rows
 // before it that take a block, which every workgroup counts for itself: `first` [n_rows] holds each row's first child.
+template <bool FEW>
 __global__ __launch_bounds__(kThreads) void fork_rows_kernel(const ForkParams p) {
   extern __shared__ int fork_lds[];
   int* const first = fork_lds + 4;
   const int tid = threadIdx.x;
   if ((int)blockIdx.x >= p.n_out) {
+    if (FEW) {
+      fork_slice(p, blockIdx.x - p.n_out, fork_lds);
+      if (p.n_out == 0 && (int)blockIdx.x == 0 && tid == 0 && p.blocks_taken) p.blocks_taken[0] = p.free_begin ? p.free_begin[0] : 0;
+      return;
+    }
     const int64_t step = (int64_t)(gridDim.x - p.n_out) * kThreads;
     for (int64_t b = (int64_t)(blockIdx.x - p.n_out) * kThreads + tid; b < p.n_blocks; b += step) p.refs_after[b] = p.refs[b];
     if ((int)blockIdx.x > p.n_out || p.n_out > 0) return;
@@ -168,12 +230,41 @@ struct CopyParams {
   int32_t vecs_per_row, block_size, n_blocks, n_pairs;
 };
 
-// A workgroup has 64 pairs of one layer, or a share of them (blockIdx.z).  The pairs that are there move to the first lanes (a
+// A workgroup has K or V of one pair in one layer: a contiguous piece, all of it on its way before the first store for blocks of up to
+// 32 KB.  Pairs follow each other fastest, so that what runs at a time lies in few pages.  Bound by HBM: 448 blocks of all layers of the
+// 8B shape, 1.88 GB read and written, take 343 us (5.5 TB/s; a copy of the same bytes that lie in a row takes 281), with 256 threads
+// the same, waves that have such a piece each 372, workgroups that go from piece to piece with the next one's loads under way 356.
+constexpr int kCopyThreads = 512;
+constexpr int64_t kDenseMost = 1 << 17;  // workgroups
+template <typename VecT>
+__global__ __launch_bounds__(kCopyThreads) void copy_blocks_kernel(const CopyParams p) {
+  const int i = blockIdx.x >> 1, tid = threadIdx.x;
+  const int src = p.src[i], dst = p.dst[i], n = p.tokens ? min(max(p.tokens[i], 0), p.block_size) : p.block_size;
+  if (src < 0 || src >= p.n_blocks || dst < 0 || dst >= p.n_blocks || src == dst) return;
+  char* const base = (blockIdx.x & 1 ? p.v_base : p.k_base) + (int64_t)blockIdx.y * p.layer_stride_b;
+  const VecT* const from = reinterpret_cast<const VecT*>(base + (int64_t)src * p.block_stride_b);
+  VecT* const to = reinterpret_cast<VecT*>(base + (int64_t)dst * p.block_stride_b);
+  const int64_t vecs = (int64_t)n * p.vecs_per_row;
+  constexpr int kAhead = 4;
+  for (int64_t v = tid; v < vecs; v += kCopyThreads * kAhead) {
+    VecT x[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (v + kCopyThreads * u < vecs) x[u] = __builtin_nontemporal_load(from + v + kCopyThreads * u);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (v + kCopyThreads * u < vecs) __builtin_nontemporal_store(x[u], to + v + kCopyThreads * u);
+  }
+}
+
+// The same for long lists, which have few pairs in them as a rule (the moves of a compaction, in room for all there could be; 100 in
+// 4096 entries: 90 us, workgroups for every entry 113; 100 in 65536: 141 against 1762; but 1000 in 4096: 833 against 786): a workgroup has 64 pairs of one layer, or a share of them (blockIdx.z).  The pairs that are there move to the first lanes (a
 // step of beam search leaves many rows without one) and the waves take their K and V in turn, as a contiguous piece each.
 template <typename VecT>
-__global__ __launch_bounds__(kThreads) void copy_blocks_kernel(const CopyParams p) {
+__global__ __launch_bounds__(kThreads) void copy_sparse_kernel(const CopyParams p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const int i = blockIdx.x * 64 + lane;
+  // (turned from layer to layer: workgroups of the same group would meet on one part of the chip)
+  const int i = (int)((blockIdx.x + blockIdx.y + blockIdx.z) % gridDim.x) * 64 + lane;
   int src = -1, dst = -1, n = 0;
   if (i < p.n_pairs) {
     src = p.src[i];
@@ -311,6 +402,64 @@ __global__ __launch_bounds__(kThreads) void free_list_kernel(const FreeParams p)
   }
 }
 
+// ---- small pools: one workgroup ----
+constexpr int kOne = 1024, kOneEach = kFewBlocks / kOne;  // its threads, consecutive blocks of a thread
+
+// Sum over the threads before this one of a workgroup of kOne, and of all of them
+__device__ __forceinline__ int one_before(int v, int* at, int* total) {
+  const int incl = wave_inclusive_scan(v), wave = threadIdx.x >> 6;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) at[wave] = incl;
+  __syncthreads();
+  int before = incl - v, all = 0;
+#pragma unroll
+  for (int w = 0; w < kOne / 64; ++w) {
+    if (w < wave) before += at[w];
+    all += at[w];
+  }
+  *total = all;
+  return before;
+}
+
+__global__ __launch_bounds__(kOne) void free_few_kernel(const FreeParams p) {
+  __shared__ int refs[kFewBlocks], ends[kFewRows], sums[kOne / 64];
+  const int tid = threadIdx.x, entries = p.n_rows * p.shape.stride;
+  for (int b = tid; b < p.n_blocks; b += kOne) refs[b] = p.refs[b];
+  for (int r = tid; r < p.n_rows; r += kOne) {
+    const int len = p.shape.lens[r];
+    const RowBlocks b = blocks_of(p.shape, len, p.shape.held ? p.shape.held[r] : 0);
+    const bool gone = p.drop[r] != 0;
+    ends[r] = gone ? b.held : 0;
+    if (p.lens_after) p.lens_after[r] = gone ? 0 : len;
+    if (p.held_after) p.held_after[r] = gone ? 0 : b.held;
+  }
+  __syncthreads();
+  for (int e = tid; e < entries; e += kOne) {
+    const int r = e / p.shape.stride;
+    if (e - r * p.shape.stride >= ends[r]) continue;
+    const int id = p.table[e];
+    if (id >= 0 && id < p.n_blocks) atomicSub(refs + id, 1);
+  }
+  __syncthreads();
+  int unused[kOneEach], n = 0;
+#pragma unroll
+  for (int u = 0; u < kOneEach; ++u) {
+    const int b = tid * kOneEach + u;
+    unused[u] = b < p.n_blocks && refs[b] <= 0;
+    n += unused[u];
+  }
+  int total;
+  int to = one_before(n, sums, &total);
+#pragma unroll
+  for (int u = 0; u < kOneEach; ++u)
+    if (unused[u]) p.free_blocks[to++] = tid * kOneEach + u;
+  for (int b = tid; b < p.n_blocks; b += kOne) {
+    p.refs_after[b] = refs[b];
+    if (b >= total) p.free_blocks[b] = -1;
+  }
+  if (tid == 0) p.n_free[0] = total;
+}
+
 struct CompactParams {
   RowShape shape;
   const int32_t* refs;
@@ -419,6 +568,69 @@ __global__ __launch_bounds__(kThreads) void compact_apply_kernel(const CompactPa
   }
 }
 
+__global__ __launch_bounds__(kOne) void compact_few_kernel(const CompactParams p) {
+  __shared__ uint16_t to[kFewBlocks], src[kFewBlocks / 2], dst[kFewBlocks / 2];  // (there are no more moves than half of the blocks)
+  __shared__ int held[kFewRows], sums[kOne / 64];
+  const int tid = threadIdx.x, entries = p.n_rows * p.shape.stride;
+  for (int r = tid; r < p.n_rows; r += kOne) held[r] = blocks_of_row(p.shape, r).held;
+  int refs[kOneEach], n = 0;
+#pragma unroll
+  for (int u = 0; u < kOneEach; ++u) {
+    const int b = tid * kOneEach + u;
+    refs[u] = b < p.n_blocks ? p.refs[b] : 0;
+    n += refs[u] > 0;
+    to[b] = (uint16_t)b;
+  }
+  int total;
+  const int used_before = one_before(n, sums, &total);
+  const int keep = p.n_keep < 0 ? total : min(p.n_keep, p.n_blocks);
+  int below = 0;
+#pragma unroll
+  for (int u = 0; u < kOneEach; ++u) below += refs[u] > 0 && tid * kOneEach + u < keep;
+  int all_below;
+  one_before(below, sums, &all_below);
+  const int moves = min(min(keep - all_below, total - all_below), p.n_pairs);
+  int used = used_before;
+#pragma unroll
+  for (int u = 0; u < kOneEach; ++u) {
+    const int b = tid * kOneEach + u;
+    if (b >= p.n_blocks) break;
+    const int k = refs[u] > 0 ? (b >= keep ? used - all_below : moves) : (b < keep ? b - used : moves);
+    used += refs[u] > 0;
+    if (k >= moves)
+      p.refs_after[b] = refs[u];
+    else if (refs[u] > 0)
+      src[k] = (uint16_t)b;
+    else
+      dst[k] = (uint16_t)b;
+  }
+  __syncthreads();
+  for (int k = tid; k < p.n_pairs; k += kOne) {
+    const bool there = k < moves;
+    const int from = there ? src[k] : -1, into = there ? dst[k] : -1;
+    p.src[k] = from;
+    p.dst[k] = into;
+    if (there) {
+      to[from] = (uint16_t)into;
+      p.refs_after[into] = p.refs[from];
+      p.refs_after[from] = 0;
+    }
+  }
+  __syncthreads();
+  for (int b = tid; b < p.n_blocks; b += kOne) p.map[b] = to[b];
+  for (int e = tid; e < entries; e += kOne) {
+    const int r = e / p.shape.stride;
+    if (e - r * p.shape.stride >= held[r]) continue;
+    const int id = p.table[e];
+    p.table_out[e] = id >= 0 && id < p.n_blocks ? to[id] : id;
+  }
+  if (tid == 0) {
+    p.result[0] = total;
+    p.result[1] = moves;
+    p.result[2] = total - all_below - moves;
+  }
+}
+
 // Checks that all of these share: a table of rows.  n_rows == 0 needs no arrays.
 static int32_t check_rows(const int32_t* d_lens, const int32_t* d_table, int32_t table_stride, int32_t n_rows, int32_t block_size,
                           int32_t n_blocks) {
@@ -477,8 +689,14 @@ int32_t symph_kv_fork(const int32_t* d_parents, int32_t n_out, const int32_t* d_
   p.n_rows = n_rows;
   p.n_free = n_free;
   p.n_blocks = n_blocks;
+  const unsigned lds = (4 + n_rows) * 4;
+  if (few(n_rows, table_stride) && n_out <= kFewRows) {
+    hipLaunchKernelGGL(fork_rows_kernel<true>, dim3((unsigned)(n_out + ceil_div64(n_blocks, kSlice))), dim3(kThreads), lds,
+                       (hipStream_t)stream, p);
+    return launched();
+  }
   const int64_t carry = std::min<int64_t>(ceil_div64(n_blocks, kTile), kMostGroups);
-  hipLaunchKernelGGL(fork_rows_kernel, dim3((unsigned)(n_out + carry)), dim3(kThreads), (4 + n_rows) * 4, (hipStream_t)stream, p);
+  hipLaunchKernelGGL(fork_rows_kernel<false>, dim3((unsigned)(n_out + carry)), dim3(kThreads), lds, (hipStream_t)stream, p);
   hipLaunchKernelGGL(fork_refs_kernel, dim3((unsigned)n_rows + 1), dim3(kThreads), 0, (hipStream_t)stream, p);
   return launched();
 }
@@ -509,12 +727,20 @@ int32_t symph_kv_copy_blocks(const symph_kv_cache* cache, const int32_t* d_src_b
   p.block_size = cache->block_size;
   p.n_blocks = cache->n_blocks;
   p.n_pairs = n_pairs;
-  const int64_t shares = std::min<int64_t>(32, std::max<int64_t>(1, 8192 / (groups * cache->n_layers)));
-  const dim3 grid((unsigned)groups, (unsigned)cache->n_layers, (unsigned)shares);
-  if (vec == 16)
-    hipLaunchKernelGGL(copy_blocks_kernel<u32x4>, grid, dim3(kThreads), 0, (hipStream_t)stream, p);
-  else
-    hipLaunchKernelGGL(copy_blocks_kernel<unsigned int>, grid, dim3(kThreads), 0, (hipStream_t)stream, p);
+  if (2 * (int64_t)n_pairs * cache->n_layers <= kDenseMost) {
+    const dim3 grid((unsigned)n_pairs * 2, (unsigned)cache->n_layers);
+    if (vec == 16)
+      hipLaunchKernelGGL(copy_blocks_kernel<u32x4>, grid, dim3(kCopyThreads), 0, (hipStream_t)stream, p);
+    else
+      hipLaunchKernelGGL(copy_blocks_kernel<unsigned int>, grid, dim3(kCopyThreads), 0, (hipStream_t)stream, p);
+  } else {
+    const int64_t shares = std::min<int64_t>(32, std::max<int64_t>(1, kDenseMost / (groups * cache->n_layers)));
+    const dim3 grid((unsigned)groups, (unsigned)cache->n_layers, (unsigned)shares);
+    if (vec == 16)
+      hipLaunchKernelGGL(copy_sparse_kernel<u32x4>, grid, dim3(kThreads), 0, (hipStream_t)stream, p);
+    else
+      hipLaunchKernelGGL(copy_sparse_kernel<unsigned int>, grid, dim3(kThreads), 0, (hipStream_t)stream, p);
+  }
   return launched();
 }
 
@@ -547,6 +773,10 @@ int32_t symph_kv_free(const int32_t* d_drop, const int32_t* d_lens, const int32_
   p.n_rows = n_rows;
   p.n_blocks = n_blocks;
   p.tiles = cut.tiles;
+  if (n_blocks <= kFewBlocks && few(n_rows, table_stride)) {
+    hipLaunchKernelGGL(free_few_kernel, dim3(1), dim3(kOne), 0, (hipStream_t)stream, p);
+    return launched();
+  }
   hipLaunchKernelGGL(free_carry_kernel, dim3(cut.groups), dim3(kThreads), 0, (hipStream_t)stream, p);
   if (n_rows > 0) hipLaunchKernelGGL(free_rows_kernel, dim3((unsigned)n_rows), dim3(kThreads), 0, (hipStream_t)stream, p);
   hipLaunchKernelGGL(free_list_kernel, dim3(cut.groups), dim3(kThreads), 0, (hipStream_t)stream, p);
@@ -589,6 +819,10 @@ int32_t symph_kv_compact(const int32_t* d_refs, int32_t n_blocks, int32_t n_keep
   p.n_keep = n_keep;
   p.n_pairs = n_pairs;
   p.tiles = cut.tiles;
+  if (n_blocks <= kFewBlocks && few(n_rows, table_stride)) {
+    hipLaunchKernelGGL(compact_few_kernel, dim3(1), dim3(kOne), 0, (hipStream_t)stream, p);
+    return launched();
+  }
   hipLaunchKernelGGL(compact_count_kernel, dim3(cut.groups), dim3(kThreads), 0, (hipStream_t)stream, p);
   hipLaunchKernelGGL(compact_moves_kernel, dim3(cut.groups), dim3(kThreads), 0, (hipStream_t)stream, p);
   hipLaunchKernelGGL(compact_apply_kernel, dim3((unsigned)groups), dim3(kThreads), 0, (hipStream_t)stream, p);

@@ -40,12 +40,15 @@ def _fork(parents, lens, held, table, refs, free, bs, begin=0, with_held=True, w
     return got
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("bs", [1, 5, 16, 64])
 @pytest.mark.parametrize("sessions,beams,longest", [(1, 1, 1), (1, 4, 100), (7, 3, 333), (40, 8, 60), (2, 5, 5000)])
-def test_forks(sessions, beams, longest, bs):
+def test_forks(sessions, beams, longest, bs, wide):
     rs = np.random.RandomState(sessions + bs)
     lens, held, table, refs, free = R.shared_pages(rs, sessions, beams, bs, longest, 4 * sessions * beams * (longest // bs + 4))
     rows = sessions * beams
+    if wide:  # (tables of many entries take two launches)
+        table = np.pad(table, ((0, 0), (0, 16400 // rows)), constant_values=-1)
     for n_out in (rows, 1, 3 * rows + 1):
         parents = rs.randint(0, rows, size=n_out) if n_out != rows else np.arange(rows) // beams * beams + rs.randint(0, beams, size=rows)
         parents = np.where(rs.random_sample(n_out) < 0.1, -1, parents)
@@ -65,9 +68,12 @@ def test_a_prompt_becomes_beams():
     assert got["copy_tokens"].tolist() == [0, 5, 5] and got["refs_after"].tolist() == [0, 1, 3, 0, 3, 0, 0, 1, 0, 1, 0, 0]
 
 
-def test_lists_that_end_too_early_and_blocks_outside():
+@pytest.mark.parametrize("wide", [False, True])
+def test_lists_that_end_too_early_and_blocks_outside(wide):
     rs = np.random.RandomState(3)
     lens, held, table, refs, free = R.shared_pages(rs, 4, 4, 16, 200, 600)
+    if wide:
+        table = np.pad(table, ((0, 0), (0, 1100)), constant_values=-1)
     parents = np.repeat(np.arange(16), 2)
     lens[:] = np.maximum(lens, 1) | 1  # (no full last block)
     for bad, begin in ((free[:5], 0), (free[:5], 4), (free, 10_000), (free, -3), (free[:0], 0), (np.array([-1, 600, 5]), 0)):
@@ -76,7 +82,7 @@ def test_lists_that_end_too_early_and_blocks_outside():
     odd[2], odd[5, 0], odd[7, ::2] = -1, 600, 10 ** 9
     _fork(parents, lens, held, odd, refs, free, 16)
     _fork([-1, -2 ** 31, 16, 2 ** 31 - 1, 15], lens, held, table, refs, free, 16)
-    _fork(parents, lens * 100, held * 100, table, refs, free, 16)          # longer than their table rows
+    _fork(parents, lens * 1000, held * 1000, table, refs, free, 16)        # longer than their table rows
     _fork(parents, np.where(lens % 3 == 0, -lens, lens), held, table, refs, free, 16)
     _fork(parents, lens, held, table, refs, free, 16, with_held=False, with_begin=False)
     _fork(parents, np.full(16, 2 ** 31 - 1), np.full(16, 2 ** 31 - 1), table, refs, free, 2 ** 31 - 1)
@@ -128,6 +134,7 @@ def test_frees(n_blocks, bs):
     for drop in (np.zeros(len(lens), int), np.ones(len(lens), int), rs.randint(-1, 2, size=len(lens))):
         _free(drop, lens, held, table, refs, bs)
     _free(drop, lens, held, table, refs, bs, with_held=False)
+    _free(drop, lens, held, np.pad(table, ((0, 0), (0, 16400)), constant_values=0), refs, bs)   # (not the small call's kernel)
     _free(drop, lens, held, table, rs.randint(-2, 3, size=n_blocks), bs)   # counts that do not belong to the table
 
 
@@ -175,6 +182,7 @@ def test_compactions(n_blocks, in_place):
     for n_keep in (-1, 0, 1, n_blocks // 2, n_blocks - 1, n_blocks, 2 ** 31 - 1, -(2 ** 31), 1024):
         for n_pairs in (n_blocks, 5, 0):
             _compact(refs, n_keep, lens, held, table, 16, n_pairs, in_place)
+    _compact(refs, -1, lens, held, np.pad(table, ((0, 0), (0, 16400)), constant_values=0), 16, n_blocks, in_place)
 
 
 def test_compactions_of_full_empty_and_large_pools():
@@ -229,6 +237,22 @@ def test_copies(layers, bs, hkv, d, pad, pairs, dtype):
         S.kv_copy_blocks(cache, _i32(src), _i32(dst), None if filled is None else _i32(filled))
         torch.cuda.synchronize()
         assert torch.equal(raw[0], want[0]) and torch.equal(raw[1], want[1])
+
+
+@pytest.mark.parametrize("there", [0, 1, 70])
+def test_long_lists_with_few_pairs(there):
+    """The moves of a compaction in room for many more: at the front, and all over."""
+    cache, raw = _pools(2, 150, 16, 1, 64, torch.bfloat16, there)
+    ids = np.random.RandomState(there).permutation(150)
+    src, dst = np.full(70_000, -1), np.full(70_000, -1)
+    at = np.arange(there) if there < 70 else np.random.RandomState(1).permutation(70_000)[:there]
+    src[at], dst[at] = ids[:there], ids[there:2 * there]
+    want = [r.clone() for r in raw]
+    for w in want:
+        w[:, ids[there:2 * there]] = w[:, ids[:there]]
+    S.kv_copy_blocks(cache, _i32(src), _i32(dst))
+    torch.cuda.synchronize()
+    assert torch.equal(raw[0], want[0]) and torch.equal(raw[1], want[1])
 
 
 def test_copies_behind_four_gigabytes():
