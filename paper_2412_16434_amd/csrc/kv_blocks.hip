@@ -33,6 +33,12 @@ __device__ __forceinline__ RowBlocks blocks_of_row(const RowShape& s, int row) {
   return blocks_of(s, s.lens[row], s.held ? s.held[row] : 0);
 }
 
+// Entry i of n > 0 entries, `none` behind them: asked for unconditionally, so that a thread's loads wait together
+__device__ __forceinline__ int entry_or(const int32_t* list, int64_t i, int64_t n, int none) {
+  const int v = list[min(i, n - 1)];
+  return i < n ? v : none;
+}
+
 constexpr int kThreads = 256;
 
 // Sum over a workgroup's threads (every thread gets it); `at`: four words of LDS that no one else is using.
@@ -76,10 +82,12 @@ struct ForkParams {
   int32_t n_out, n_rows, n_free, n_blocks;
 };
 
-// Small calls take one launch, which is what they cost: up to so many table entries, rows and (in one workgroup) blocks.
-constexpr int kFewEntries = 16384, kFewRows = 1024, kFewBlocks = 8192;
-static bool few(int32_t n_rows, int32_t table_stride) {
-  return n_rows <= kFewRows && (int64_t)n_rows * table_stride <= kFewEntries;
+// Small calls take one launch, which is what they cost: up to so many table entries, rows and (in one workgroup) blocks.  A fork of 8
+// rows of 507 entries 8.8 us, in two launches 10.8; of 16 such rows 12.7 and 10.0.  A free of 16 rows of 71 entries 6.4, in three launches
+// 12.6; of 32 rows of 383 entries 10.7 and 11.8, a compaction of them 12.3 and 12.7.
+constexpr int kFewEntries = 16384, kFewForked = 4096, kFewRows = 1024, kFewBlocks = 8192;
+static bool few(int32_t n_rows, int32_t table_stride, int32_t entries = kFewEntries) {
+  return n_rows <= kFewRows && (int64_t)n_rows * table_stride <= entries;
 }
 constexpr int kSlice = 4096;  // blocks whose counts a workgroup of a small fork has
 
@@ -113,7 +121,7 @@ __device__ __forceinline__ void fork_slice(const ForkParams& p, int slice, int* 
   for (int e0 = tid; e0 < entries; e0 += kThreads * kAhead) {
     int id[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) id[u] = e0 + u * kThreads < entries ? p.table[e0 + u * kThreads] : -1;
+    for (int u = 0; u < kAhead; ++u) id[u] = entry_or(p.table, e0 + u * kThreads, entries, -1);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int at = id[u] - lo;
@@ -324,25 +332,30 @@ struct FreeParams {
   int32_t* n_free;
   int32_t* lens_after;
   int32_t* held_after;
-  int32_t* counts;  // per workgroup: blocks that nobody holds
-  int32_t n_rows, n_blocks, tiles;
+  int32_t* counts;  // of every run of 2^run_shift blocks: those that nobody holds
+  int32_t n_rows, n_blocks, run_shift, n_runs;
 };
 
+// Counts are kept for runs of 64 blocks, longer ones where there would be more than kMostGroups: rows that are dropped together change
+// them all over, and few counters would make them wait for each other (150 rows with 80000 blocks: 28 us; runs of 1024: 130).
+static int run_shift_of(int32_t n_blocks) {
+  int s = 6;
+  while (((int64_t)kMostGroups << s) < n_blocks) ++s;
+  return s;
+}
+
+// A wave per run
 __global__ __launch_bounds__(kThreads) void free_carry_kernel(const FreeParams p) {
-  __shared__ int sums[4];
-  const int64_t begin = (int64_t)blockIdx.x * p.tiles * kTile;
+  const int lane = threadIdx.x & 63, run = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (run >= p.n_runs) return;
   int unused = 0;
-  for (int t = 0; t < p.tiles; ++t)
-#pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-      const int64_t b = begin + (int64_t)t * kTile + u * kThreads + threadIdx.x;
-      if (b >= p.n_blocks) continue;
-      const int r = p.refs[b];
-      p.refs_after[b] = r;
-      unused += r <= 0;
-    }
-  unused = group_sum(unused, sums);
-  if (threadIdx.x == 0) p.counts[blockIdx.x] = unused;
+  for (int64_t i = lane; i < 1ll << p.run_shift; i += 64) {
+    const int64_t b = ((int64_t)run << p.run_shift) + i;
+    const int r = entry_or(p.refs, b, p.n_blocks, 1);
+    if (b < p.n_blocks) p.refs_after[b] = r;
+    unused += __popcll(__ballot(r <= 0));
+  }
+  if (lane == 0) p.counts[run] = unused;
 }
 
 __global__ __launch_bounds__(kThreads) void free_rows_kernel(const FreeParams p) {
@@ -355,7 +368,7 @@ __global__ __launch_bounds__(kThreads) void free_rows_kernel(const FreeParams p)
     for (int c = tid; c < b.held; c += kThreads) {
       const int id = from[c];
       if (id < 0 || id >= p.n_blocks) continue;
-      if (atomicSub(p.refs_after + id, 1) == 1) atomicAdd(p.counts + id / (p.tiles * kTile), 1);
+      if (atomicSub(p.refs_after + id, 1) == 1) atomicAdd(p.counts + (id >> p.run_shift), 1);
     }
   }
   __syncthreads();  // (the lengths may be written over)
@@ -377,18 +390,21 @@ __device__ __forceinline__ int counted_before(const int32_t* counts, int groups,
   return group_sum(before, at);
 }
 
+// A workgroup per kListRuns runs
+constexpr int kListRuns = kTile / 64;
 __global__ __launch_bounds__(kThreads) void free_list_kernel(const FreeParams p) {
   __shared__ int sums[4];
+  const int tiles = 1 << (p.run_shift - 6);
+  const int64_t begin = (int64_t)blockIdx.x * tiles * kTile;
   int total;
-  int at = counted_before(p.counts, gridDim.x, blockIdx.x, sums, &total);
+  int at = counted_before(p.counts, p.n_runs, blockIdx.x * kListRuns, sums, &total);
   if (blockIdx.x == 0 && threadIdx.x == 0) p.n_free[0] = total;
-  const int64_t begin = (int64_t)blockIdx.x * p.tiles * kTile;
-  for (int t = 0; t < p.tiles; ++t) {
+  for (int t = 0; t < tiles; ++t) {
     const int64_t b0 = begin + (int64_t)t * kTile + threadIdx.x * kEach;
     int unused[kEach], n = 0;
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
-      unused[u] = b0 + u < p.n_blocks && p.refs_after[b0 + u] <= 0;
+      unused[u] = entry_or(p.refs_after, b0 + u, p.n_blocks, 1) <= 0;
       n += unused[u];
     }
     int in_tile;
@@ -481,12 +497,20 @@ __global__ __launch_bounds__(kThreads) void compact_count_kernel(const CompactPa
   int used = 0;
   for (int t = 0; t < p.tiles; ++t)
 #pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-      const int64_t b = begin + (int64_t)t * kTile + u * kThreads + threadIdx.x;
-      used += b < p.n_blocks && p.refs[b] > 0;
-    }
+    for (int u = 0; u < kEach; ++u)
+      used += entry_or(p.refs, begin + (int64_t)t * kTile + u * kThreads + threadIdx.x, p.n_blocks, 0) > 0;
   used = group_sum(used, sums);
   if (threadIdx.x == 0) p.counts[blockIdx.x] = used;
+}
+
+// Which move a block leaves by, or is taken by
+__device__ __forceinline__ void place_block(const CompactParams& p, int b, bool used, int used_before, int keep, int below, int moves) {
+  int k = -1;
+  if (used && b >= keep) k = used_before - below;
+  if (!used && b < keep) k = b - used_before;
+  if (k >= moves) k = -1;
+  p.place[b] = k;
+  if (k >= 0) (used ? p.src : p.dst)[k] = b;
 }
 
 // The k-th block in use from `keep` on goes to the k-th block below `keep` that is not.
@@ -517,22 +541,14 @@ __global__ __launch_bounds__(kThreads) void compact_moves_kernel(const CompactPa
     int used[kEach], n = 0;
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
-      used[u] = b0 + u < p.n_blocks && p.refs[b0 + u] > 0;
+      used[u] = entry_or(p.refs, b0 + u, p.n_blocks, 0) > 0;
       n += used[u];
     }
     int in_tile;
     int used_before = before + group_before(n, sums, &in_tile);
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
-      const int64_t b = b0 + u;
-      if (b < p.n_blocks) {
-        int k = -1;
-        if (used[u] && b >= keep) k = used_before - below;
-        if (!used[u] && b < keep) k = (int)(b - used_before);
-        if (k >= moves) k = -1;
-        p.place[b] = k;
-        if (k >= 0) (used[u] ? p.src : p.dst)[k] = (int32_t)b;
-      }
+      if (b0 + u < p.n_blocks) place_block(p, (int)(b0 + u), used[u], used_before, keep, below, moves);
       used_before += used[u];
     }
     before += in_tile;
@@ -577,7 +593,7 @@ __global__ __launch_bounds__(kOne) void compact_few_kernel(const CompactParams p
 #pragma unroll
   for (int u = 0; u < kOneEach; ++u) {
     const int b = tid * kOneEach + u;
-    refs[u] = b < p.n_blocks ? p.refs[b] : 0;
+    refs[u] = entry_or(p.refs, b, p.n_blocks, 0);
     n += refs[u] > 0;
     to[b] = (uint16_t)b;
   }
@@ -690,7 +706,7 @@ int32_t symph_kv_fork(const int32_t* d_parents, int32_t n_out, const int32_t* d_
   p.n_free = n_free;
   p.n_blocks = n_blocks;
   const unsigned lds = (4 + n_rows) * 4;
-  if (few(n_rows, table_stride) && n_out <= kFewRows) {
+  if (few(n_rows, table_stride, kFewForked) && n_out <= kFewRows) {
     hipLaunchKernelGGL(fork_rows_kernel<true>, dim3((unsigned)(n_out + ceil_div64(n_blocks, kSlice))), dim3(kThreads), lds,
                        (hipStream_t)stream, p);
     return launched();
@@ -745,7 +761,7 @@ int32_t symph_kv_copy_blocks(const symph_kv_cache* cache, const int32_t* d_src_b
 }
 
 int64_t symph_kv_free_workspace_bytes(int32_t n_blocks) {
-  return n_blocks <= 0 ? SYMPH_EINVAL : round256((int64_t)cut_pool(n_blocks).groups * 4);
+  return n_blocks <= 0 ? SYMPH_EINVAL : round256(ceil_div64(n_blocks, 1ll << run_shift_of(n_blocks)) * 4);
 }
 
 int32_t symph_kv_free(const int32_t* d_drop, const int32_t* d_lens, const int32_t* d_held_blocks, int32_t n_rows,
@@ -758,7 +774,6 @@ int32_t symph_kv_free(const int32_t* d_drop, const int32_t* d_lens, const int32_
   if (d_refs_after == d_refs || d_free_blocks == d_refs || d_free_blocks == d_refs_after) return SYMPH_EINVAL;
   if (!grid_takes(n_rows, kThreads)) return SYMPH_EUNSUPPORTED;
   if (!d_workspace || workspace_bytes < symph_kv_free_workspace_bytes(n_blocks)) return SYMPH_EWORKSPACE;
-  const PoolCut cut = cut_pool(n_blocks);
   FreeParams p;
   p.shape = shape_of(d_lens, d_held_blocks, table_stride, block_size);
   p.drop = d_drop;
@@ -772,14 +787,15 @@ int32_t symph_kv_free(const int32_t* d_drop, const int32_t* d_lens, const int32_
   p.counts = (int32_t*)d_workspace;
   p.n_rows = n_rows;
   p.n_blocks = n_blocks;
-  p.tiles = cut.tiles;
+  p.run_shift = run_shift_of(n_blocks);
+  p.n_runs = (int32_t)ceil_div64(n_blocks, 1ll << p.run_shift);
   if (n_blocks <= kFewBlocks && few(n_rows, table_stride)) {
     hipLaunchKernelGGL(free_few_kernel, dim3(1), dim3(kOne), 0, (hipStream_t)stream, p);
     return launched();
   }
-  hipLaunchKernelGGL(free_carry_kernel, dim3(cut.groups), dim3(kThreads), 0, (hipStream_t)stream, p);
+  hipLaunchKernelGGL(free_carry_kernel, dim3((unsigned)ceil_div64(p.n_runs, 4)), dim3(kThreads), 0, (hipStream_t)stream, p);
   if (n_rows > 0) hipLaunchKernelGGL(free_rows_kernel, dim3((unsigned)n_rows), dim3(kThreads), 0, (hipStream_t)stream, p);
-  hipLaunchKernelGGL(free_list_kernel, dim3(cut.groups), dim3(kThreads), 0, (hipStream_t)stream, p);
+  hipLaunchKernelGGL(free_list_kernel, dim3((unsigned)ceil_div64(p.n_runs, kListRuns)), dim3(kThreads), 0, (hipStream_t)stream, p);
   return launched();
 }
 
