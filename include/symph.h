@@ -462,9 +462,9 @@ int32_t symph_kv_commit(const symph_kv_cache* cache, const void* d_k_new, const 
  * pursued.  Beams of a session share the blocks of the tokens that they have in common; d_refs int32 [n_blocks] holds, for every
  * block of the pool, how many rows hold it (0: free).  A step, behind the model's logits for every beam's last token, is
  *   symph_beam_select     the best continuations of every session: token, score and the beam it continues
- *   symph_kv_fork         table rows for them, reference counts, copies to make of blocks that are not full
+ *   symph_kv_free         the blocks that were taken since the last step counted, sessions that are done dropped, a new free list
+ *   symph_kv_fork         table rows for the continuations, reference counts, copies to make of blocks that are not full
  *   symph_kv_copy_blocks  those copies, all layers
- *   symph_kv_free         the free list for the next step (and rows of sessions that are done)
  *   symph_build_tables, symph_kv_append and the attention calls for the next token, a beam being a session of theirs.
  * A prompt in one row becomes several beams by a fork whose parents name the row several times.  symph_kv_compact says which blocks
  * move so that the end of a pool becomes free.  Contract on blocks: only full blocks are shared (what these calls keep); a row that
@@ -541,13 +541,18 @@ int32_t symph_kv_copy_blocks(const symph_kv_cache* cache, const int32_t* d_src_b
  *                  many.  symph_build_tables and symph_kv_fork take the list as it is (a list with n_free = n_blocks);
  *   d_lens_after, d_held_after int32 [n_rows] (may be NULL; may be d_lens and d_held_blocks themselves): 0 for dropped rows, else
  *                  the row's length and the blocks it holds.
+ * Blocks that symph_build_tables took since d_refs was made are held by a row each and not counted yet: d_taken_blocks [n_taken] (may
+ * be NULL) is the list that they came from, entries *d_taken_begin (NULL: 0) .. *d_taken_end - 1 of it, i.e. that call's
+ * *d_free_begin and *d_blocks_taken; each counts one holder more.  (It must not be the list that is written.)
  * n_rows may be 0: the list alone.  d_refs_after must not be d_refs.  d_workspace: at least symph_kv_free_workspace_bytes(n_blocks)
  * bytes, 256-byte aligned; nothing has to be cleared.
  */
 int32_t symph_kv_free(const int32_t* d_drop, const int32_t* d_lens, const int32_t* d_held_blocks, int32_t n_rows,
                       const int32_t* d_block_table, int32_t table_stride, int32_t block_size, int32_t n_blocks,
                       const int32_t* d_refs, int32_t* d_refs_after, int32_t* d_free_blocks, int32_t* d_n_free,
-                      int32_t* d_lens_after, int32_t* d_held_after, void* d_workspace, int64_t workspace_bytes, void* stream);
+                      int32_t* d_lens_after, int32_t* d_held_after, const int32_t* d_taken_blocks, int32_t n_taken,
+                      const int32_t* d_taken_begin, const int32_t* d_taken_end, void* d_workspace, int64_t workspace_bytes,
+                      void* stream);
 int64_t symph_kv_free_workspace_bytes(int32_t n_blocks);
 
 /*

@@ -131,7 +131,7 @@ def load_library():
     lib.symph_kv_copy_blocks.restype = i32
     lib.symph_kv_copy_blocks.argtypes = [cp, vp, vp, vp, i32, vp]
     lib.symph_kv_free.restype = i32
-    lib.symph_kv_free.argtypes = [vp, vp, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.symph_kv_free.argtypes = [vp, vp, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, i64, vp]
     lib.symph_kv_compact.restype = i32
     lib.symph_kv_compact.argtypes = [vp, i32, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, i64, vp]
     for fn in (lib.symph_kv_free_workspace_bytes, lib.symph_kv_compact_workspace_bytes):
@@ -816,17 +816,20 @@ def kv_free_workspace_bytes(n_blocks: int) -> int:
 
 
 def kv_free(drop, lens, block_table, refs, block_size: int, refs_after, free_blocks, n_free, held_blocks=None, lens_after=None,
-            held_after=None, workspace=None, stream=None) -> None:
+            held_after=None, workspace=None, taken_blocks=None, taken_begin=None, taken_end=None, stream=None) -> None:
     """``refs_after`` <- ``refs`` without what rows with ``drop[r] != 0`` hold; ``free_blocks`` <- the blocks that nobody holds then,
-    ascending, -1 behind them; ``n_free`` <- how many.  ``drop``, ``lens`` and ``block_table`` may be None: the list alone."""
+    ascending, -1 behind them; ``n_free`` <- how many.  ``taken_blocks``: the list that build_tables has taken entries
+    ``taken_begin`` .. ``taken_end`` - 1 of since ``refs`` was made, which then count as held by a row.  ``drop``, ``lens`` and
+    ``block_table`` may be None: the list alone."""
     calls = _beam_call(stream)
     if calls:
         status = calls.free_rows(drop, lens, block_table, refs, block_size, refs_after, free_blocks, n_free, held_blocks, lens_after,
-                                 held_after, workspace)
+                                 held_after, workspace, taken_blocks, taken_begin, taken_end)
         if status is not None:
             return _check(status, "symph_kv_free")
     _on_this_device(stream, drop=drop, lens=lens, block_table=block_table, refs=refs, refs_after=refs_after, free_blocks=free_blocks,
-                    n_free=n_free, held_blocks=held_blocks, lens_after=lens_after, held_after=held_after, workspace=workspace)
+                    n_free=n_free, held_blocks=held_blocks, lens_after=lens_after, held_after=held_after, workspace=workspace,
+                    taken_blocks=taken_blocks, taken_begin=taken_begin, taken_end=taken_end)
     i32 = _torch().int32
     n, n_blocks = 0 if drop is None else drop.shape[0], refs.shape[0]
     tp, stride = _rows_table(block_table, "block_table", n) if n else (None, 0)
@@ -836,7 +839,9 @@ def kv_free(drop, lens, block_table, refs, block_size: int, refs_after, free_blo
         _vector(held_blocks, "held_blocks", i32, n, True), n, tp, stride, int(block_size), n_blocks, _vector(refs, "refs", i32),
         _vector(refs_after, "refs_after", i32, n_blocks), _vector(free_blocks, "free_blocks", i32, n_blocks),
         _vector(n_free, "n_free", i32, 1), _vector(lens_after, "lens_after", i32, n, True),
-        _vector(held_after, "held_after", i32, n, True), wp, ws_bytes, _stream_ptr(stream)), "symph_kv_free")
+        _vector(held_after, "held_after", i32, n, True), _vector(taken_blocks, "taken_blocks", i32, None, True),
+        0 if taken_blocks is None else taken_blocks.shape[0], _vector(taken_begin, "taken_begin", i32, 1, True),
+        _vector(taken_end, "taken_end", i32, 1, taken_blocks is None), wp, ws_bytes, _stream_ptr(stream)), "symph_kv_free")
 
 
 def kv_compact_workspace_bytes(n_blocks: int) -> int:

@@ -33,7 +33,8 @@ typedef int32_t (*fork_fn)(const int32_t*, int32_t, const int32_t*, const int32_
                            int32_t*, int32_t*, int32_t*, void*);
 typedef int32_t (*copy_fn)(const symph_kv_cache*, const int32_t*, const int32_t*, const int32_t*, int32_t, void*);
 typedef int32_t (*free_fn)(const int32_t*, const int32_t*, const int32_t*, int32_t, const int32_t*, int32_t, int32_t, int32_t,
-                           const int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, void*, int64_t, void*);
+                           const int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, const int32_t*, int32_t, const int32_t*,
+                           const int32_t*, void*, int64_t, void*);
 typedef int32_t (*compact_fn)(const int32_t*, int32_t, int32_t, const int32_t*, const int32_t*, int32_t, const int32_t*, int32_t, int32_t,
                               int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, int32_t, int32_t*, void*, int64_t, void*);
 
@@ -480,27 +481,30 @@ static PyObject* copy_blocks(PyObject* self, PyObject* const* a, Py_ssize_t n_ar
   return PyLong_FromLong(status);
 }
 
-// (drop, lens, block_table, refs, block_size, refs_after, free_blocks, n_free, held_blocks, lens_after, held_after, workspace) ->
-// status or None
+// (drop, lens, block_table, refs, block_size, refs_after, free_blocks, n_free, held_blocks, lens_after, held_after, workspace,
+// taken_blocks, taken_begin, taken_end) -> status or None
 static PyObject* free_rows(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   (void)self;
   place at;
-  int64_t n, blocks, ws_bytes, stride = -1;
+  int64_t n, blocks, ws_bytes, n_taken = 0, stride = -1;
   int32_t bs, status;
+  void *taken, *taken_begin, *taken_end;
   void *drop, *lens, *table, *refs, *after, *list, *count, *held, *lens_after, *held_after, *ws;
-  if (n_args != 12 || !free_entry || a[0] == Py_None || !current_place(&at) || !vector_at(a[0], t_int32, 1, 0, &at, &drop, &n) ||
+  if (n_args != 15 || !free_entry || a[0] == Py_None || !current_place(&at) || !vector_at(a[0], t_int32, 1, 0, &at, &drop, &n) ||
       !vector_at(a[1], t_int32, n, 0, &at, &lens, NULL) || !table_at(a[2], n, &stride, &at, &table) ||
       !vector_at(a[3], t_int32, 0, 0, &at, &refs, &blocks) || !as_int32(a[4], &bs) ||
       !vector_at(a[5], t_int32, blocks, 0, &at, &after, NULL) || !vector_at(a[6], t_int32, blocks, 0, &at, &list, NULL) ||
       !vector_at(a[7], t_int32, 1, 0, &at, &count, NULL) || !vector_at(a[8], t_int32, n, 1, &at, &held, NULL) ||
       !vector_at(a[9], t_int32, n, 1, &at, &lens_after, NULL) || !vector_at(a[10], t_int32, n, 1, &at, &held_after, NULL) ||
-      !scratch_at(a[11], &at, &ws, &ws_bytes)) {
+      !scratch_at(a[11], &at, &ws, &ws_bytes) || !vector_at(a[12], t_int32, 0, 1, &at, &taken, &n_taken) ||
+      !vector_at(a[13], t_int32, 1, 1, &at, &taken_begin, NULL) ||
+      !vector_at(a[14], t_int32, 1, a[12] == Py_None, &at, &taken_end, NULL)) {
     PyErr_Clear();
     Py_RETURN_NONE;
   }
   Py_BEGIN_ALLOW_THREADS
   status = free_entry(drop, lens, held, (int32_t)n, table, (int32_t)stride, bs, (int32_t)blocks, refs, after, list, count, lens_after,
-                      held_after, ws, ws_bytes, at.stream);
+                      held_after, taken, (int32_t)n_taken, taken_begin, taken_end, ws, ws_bytes, at.stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(status);
 }

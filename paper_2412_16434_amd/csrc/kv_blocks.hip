@@ -325,6 +325,9 @@ static int64_t round256(int64_t n) { return (n + 255) & ~(int64_t)255; }
 struct FreeParams {
   RowShape shape;
   const int32_t* drop;
+  const int32_t* taken;  // a list, of which entries *taken_begin .. *taken_end - 1 were taken since the counts
+  const int32_t* taken_begin;
+  const int32_t* taken_end;
   const int32_t* table;
   const int32_t* refs;
   int32_t* refs_after;
@@ -333,7 +336,7 @@ struct FreeParams {
   int32_t* lens_after;
   int32_t* held_after;
   int32_t* counts;  // of every run of 2^run_shift blocks: those that nobody holds
-  int32_t n_rows, n_blocks, run_shift, n_runs;
+  int32_t n_rows, n_blocks, n_taken, run_shift, n_runs;
 };
 
 // Counts are kept for runs of 64 blocks, longer ones where there would be more than kMostGroups: rows that are dropped together change
@@ -358,8 +361,28 @@ __global__ __launch_bounds__(kThreads) void free_carry_kernel(const FreeParams p
   if (lane == 0) p.counts[run] = unused;
 }
 
+// The part of the list that was taken
+__device__ __forceinline__ void taken_range(const FreeParams& p, int* begin, int* end) {
+  *begin = *end = 0;
+  if (!p.taken) return;
+  *begin = max(p.taken_begin ? p.taken_begin[0] : 0, 0);
+  *end = min(p.taken_end[0], p.n_taken);
+}
+
+// A workgroup per row, and one for the blocks that were taken.  (A count that passes from 0 to 1 or back, in whatever order the changes
+// come, ends where the run's count of unused blocks says.)
 __global__ __launch_bounds__(kThreads) void free_rows_kernel(const FreeParams p) {
   const int row = blockIdx.x, tid = threadIdx.x;
+  if (row == p.n_rows) {
+    int begin, end;
+    taken_range(p, &begin, &end);
+    for (int i = begin + tid; i < end; i += kThreads) {
+      const int id = p.taken[i];
+      if (id < 0 || id >= p.n_blocks) continue;
+      if (atomicAdd(p.refs_after + id, 1) == 0) atomicSub(p.counts + (id >> p.run_shift), 1);
+    }
+    return;
+  }
   const int len = p.shape.lens[row];
   const RowBlocks b = blocks_of(p.shape, len, p.shape.held ? p.shape.held[row] : 0);
   const bool gone = p.drop[row] != 0;
@@ -455,6 +478,12 @@ __global__ __launch_bounds__(kOne) void free_few_kernel(const FreeParams p) {
     if (e - r * p.shape.stride >= ends[r]) continue;
     const int id = p.table[e];
     if (id >= 0 && id < p.n_blocks) atomicSub(refs + id, 1);
+  }
+  int begin, end;
+  taken_range(p, &begin, &end);
+  for (int i = begin + tid; i < end; i += kOne) {
+    const int id = p.taken[i];
+    if (id >= 0 && id < p.n_blocks) atomicAdd(refs + id, 1);
   }
   __syncthreads();
   int unused[kOneEach], n = 0;
@@ -767,16 +796,23 @@ int64_t symph_kv_free_workspace_bytes(int32_t n_blocks) {
 int32_t symph_kv_free(const int32_t* d_drop, const int32_t* d_lens, const int32_t* d_held_blocks, int32_t n_rows,
                       const int32_t* d_block_table, int32_t table_stride, int32_t block_size, int32_t n_blocks,
                       const int32_t* d_refs, int32_t* d_refs_after, int32_t* d_free_blocks, int32_t* d_n_free,
-                      int32_t* d_lens_after, int32_t* d_held_after, void* d_workspace, int64_t workspace_bytes, void* stream) {
+                      int32_t* d_lens_after, int32_t* d_held_after, const int32_t* d_taken_blocks, int32_t n_taken,
+                      const int32_t* d_taken_begin, const int32_t* d_taken_end, void* d_workspace, int64_t workspace_bytes,
+                      void* stream) {
   const int32_t rc = check_rows(d_lens, d_block_table, table_stride, n_rows, block_size, n_blocks);
   if (rc != SYMPH_OK) return rc;
+  if (n_taken < 0 || (d_taken_blocks && !d_taken_end) || (d_taken_blocks && d_taken_blocks == d_free_blocks)) return SYMPH_EINVAL;
   if (!d_refs || !d_refs_after || !d_free_blocks || !d_n_free || (n_rows > 0 && !d_drop) || workspace_bytes < 0) return SYMPH_EINVAL;
   if (d_refs_after == d_refs || d_free_blocks == d_refs || d_free_blocks == d_refs_after) return SYMPH_EINVAL;
-  if (!grid_takes(n_rows, kThreads)) return SYMPH_EUNSUPPORTED;
+  if (!grid_takes((int64_t)n_rows + 1, kThreads)) return SYMPH_EUNSUPPORTED;
   if (!d_workspace || workspace_bytes < symph_kv_free_workspace_bytes(n_blocks)) return SYMPH_EWORKSPACE;
   FreeParams p;
   p.shape = shape_of(d_lens, d_held_blocks, table_stride, block_size);
   p.drop = d_drop;
+  p.taken = n_taken > 0 ? d_taken_blocks : nullptr;
+  p.taken_begin = d_taken_begin;
+  p.taken_end = d_taken_end;
+  p.n_taken = n_taken;
   p.table = d_block_table;
   p.refs = d_refs;
   p.refs_after = d_refs_after;
@@ -794,7 +830,8 @@ int32_t symph_kv_free(const int32_t* d_drop, const int32_t* d_lens, const int32_
     return launched();
   }
   hipLaunchKernelGGL(free_carry_kernel, dim3((unsigned)ceil_div64(p.n_runs, 4)), dim3(kThreads), 0, (hipStream_t)stream, p);
-  if (n_rows > 0) hipLaunchKernelGGL(free_rows_kernel, dim3((unsigned)n_rows), dim3(kThreads), 0, (hipStream_t)stream, p);
+  const unsigned changes = (unsigned)n_rows + (p.taken ? 1 : 0);
+  if (changes > 0) hipLaunchKernelGGL(free_rows_kernel, dim3(changes), dim3(kThreads), 0, (hipStream_t)stream, p);
   hipLaunchKernelGGL(free_list_kernel, dim3((unsigned)ceil_div64(p.n_runs, kListRuns)), dim3(kThreads), 0, (hipStream_t)stream, p);
   return launched();
 }

@@ -91,8 +91,11 @@ def fork(parents, lens, held, table, refs, free, begin, bs, table_out):
                 copy_tokens=tokens, blocks_taken=[at])
 
 
-def free(drop, lens, held, table, refs, bs):
+def free(drop, lens, held, table, refs, bs, taken=(), begin=0, end=0):
     after, lens_after, held_after = refs.copy(), [], []
+    for b in taken[max(begin, 0):max(end, 0)]:
+        if 0 <= b < len(refs):
+            after[b] += 1
     for r in range(len(drop)):
         _, _, h = row_blocks(lens[r], held[r], table.shape[1], bs)
         if drop[r]:

@@ -63,12 +63,12 @@ def test_free_refuses():
     lib = S.load_library()
 
     def call(drop=0x10, lens=0x20, held=None, rows=4, table=0x30, stride=8, bs=16, blocks=64, refs=0x40, after=0x50, free=0x60, n_free=0x70,
-             ws=0x100, ws_bytes=BIG):
-        return lib.symph_kv_free(drop, lens, held, rows, table, stride, bs, blocks, refs, after, free, n_free, None, None, ws, ws_bytes,
-                                 None)
+             taken=None, n_taken=0, taken_end=None, ws=0x100, ws_bytes=BIG):
+        return lib.symph_kv_free(drop, lens, held, rows, table, stride, bs, blocks, refs, after, free, n_free, None, None, taken, n_taken,
+                                 None, taken_end, ws, ws_bytes, None)
     for bad in (dict(drop=None), dict(lens=None), dict(rows=-1), dict(table=None), dict(stride=-1), dict(bs=0), dict(blocks=0),
                 dict(refs=None), dict(after=None), dict(free=None), dict(n_free=None), dict(after=0x40), dict(free=0x40), dict(free=0x50),
-                dict(ws_bytes=-1)):
+                dict(ws_bytes=-1), dict(n_taken=-1), dict(taken=0x80, n_taken=4), dict(taken=0x60, n_taken=4, taken_end=0x90)):
         assert call(**bad) == EINVAL, bad
     assert call(rows=1 << 30) == EUNSUPPORTED
     assert call(ws=None) == EWORKSPACE and call(ws_bytes=3) == EWORKSPACE

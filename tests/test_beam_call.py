@@ -32,7 +32,8 @@ def _step(dev, dtype=torch.bfloat16):
                                 dst_blocks=i32([8, 2, 9]), tokens=i32([4, 16, 20])), []),
         "kv_free": (dict(drop=i32([0, 1, 0, 0]), lens=lens, block_table=table, refs=refs, block_size=16, refs_after=fill(10),
                          free_blocks=fill(10), n_free=fill(1), held_blocks=i32([2, 2, 3, 3]), lens_after=fill(4), held_after=fill(4),
-                         workspace=space), ["refs_after", "free_blocks", "n_free", "lens_after", "held_after"]),
+                         workspace=space, taken_blocks=i32([9, 8, 3]), taken_begin=i32([0]), taken_end=i32([1])),
+                    ["refs_after", "free_blocks", "n_free", "lens_after", "held_after"]),
         "kv_compact": (dict(refs=refs, n_keep=-1, lens=lens, block_table=table, block_size=16, table_out=fill(4, 3), refs_after=fill(10),
                             block_map=fill(10), copy_src=fill(5), copy_dst=fill(5), counts=fill(3), held_blocks=i32([2, 2, 3, 3]),
                             workspace=space), ["table_out", "refs_after", "block_map", "copy_src", "copy_dst", "counts"]),
@@ -109,7 +110,7 @@ def test_same_call_both_ways(name, dtype, counting):
 @pytest.mark.parametrize("name", NAMES)
 def test_what_may_be_left_out(name, counting):
     optional = dict(beam_select=["end_scores", "end_token"], kv_fork=["held_blocks", "held_out", "free_begin", "blocks_taken"],
-                    kv_copy_blocks=["tokens"], kv_free=["held_blocks", "lens_after", "held_after"], kv_compact=["held_blocks"])
+                    kv_copy_blocks=["tokens"], kv_free=["held_blocks", "lens_after", "held_after", "taken_blocks", "taken_begin", "taken_end"], kv_compact=["held_blocks"])
     a, _ = _step("cuda:0")[name]
     for k in optional[name]:
         del a[k]

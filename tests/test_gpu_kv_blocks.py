@@ -115,12 +115,14 @@ def test_many_rows():
     _same(got, dict(refs_after=counts))
 
 
-def _free(drop, lens, held, table, refs, bs, with_held=True):
+def _free(drop, lens, held, table, refs, bs, with_held=True, taken=None, begin=0, end=0):
     n, n_blocks = len(drop), len(refs)
+    more = {} if taken is None else dict(taken_blocks=_i32(taken), taken_begin=_i32([begin]), taken_end=_i32([end]))
     got = dict(refs_after=_left(n_blocks), free_blocks=_left(n_blocks), n_free=_left(1), lens_after=_left(n), held_after=_left(n))
     space = torch.full((S.kv_free_workspace_bytes(n_blocks),), 255, dtype=torch.uint8, device=DEV)
-    S.kv_free(_i32(drop), _i32(lens), _i32(table), _i32(refs), bs, held_blocks=_i32(held) if with_held else None, workspace=space, **got)
-    _same(got, R.free(drop, lens, held if with_held else np.zeros_like(held), table, refs, bs))
+    S.kv_free(_i32(drop), _i32(lens), _i32(table), _i32(refs), bs, held_blocks=_i32(held) if with_held else None, workspace=space, **got,
+              **more)
+    _same(got, R.free(drop, lens, held if with_held else np.zeros_like(held), table, refs, bs, [] if taken is None else taken, begin, end))
     return got
 
 
@@ -136,6 +138,26 @@ def test_frees(n_blocks, bs):
     _free(drop, lens, held, table, refs, bs, with_held=False)
     _free(drop, lens, held, np.pad(table, ((0, 0), (0, 16400)), constant_values=0), refs, bs)   # (not the small call's kernel)
     _free(drop, lens, held, table, rs.randint(-2, 3, size=n_blocks), bs)   # counts that do not belong to the table
+
+
+@pytest.mark.parametrize("n_blocks", [900, 20000])
+def test_blocks_that_were_taken_since(n_blocks):
+    """A list of which some entries were taken: parts of it, none, more than there are, ids outside the pool, blocks of dropped rows."""
+    rs = np.random.RandomState(4)
+    lens, held, table, refs, free = R.shared_pages(rs, 4, 3, 16, 200, n_blocks)
+    drop = rs.randint(0, 2, size=12)
+    for taken, begin, end in ((free, 0, 30), (free, 7, 8), (free, 9, 9), (free, 50, 20), (free[:20], -5, 10 ** 9), (free[:0], 0, 3),
+                              (np.array([-1, n_blocks, free[0], 10 ** 9]), 0, 4)):
+        _free(drop, lens, held, table, refs, 16, taken=taken, begin=begin, end=end)
+    row = int(np.flatnonzero((drop != 0) & (held > 0))[0])
+    fresh = refs.copy()
+    fresh[table[row, held[row] - 1]] -= 1      # (a block that a dropped row holds, and that is not counted yet)
+    _free(drop, lens, held, table, fresh, 16, taken=table[row, held[row] - 1:held[row]], begin=0, end=1)
+    ids, count, after = _left(n_blocks), _left(1), _left(n_blocks)
+    space = torch.empty(S.kv_free_workspace_bytes(n_blocks), dtype=torch.uint8, device=DEV)
+    S.kv_free(None, None, None, _i32(refs), 16, after, ids, count, workspace=space, taken_blocks=_i32(free), taken_end=_i32([5]))
+    want = R.free([], [], [], np.zeros((0, 1), int), refs, 16, free, 0, 5)
+    _same(dict(refs_after=after, free_blocks=ids, n_free=count), {k: want[k] for k in ("refs_after", "free_blocks", "n_free")})
 
 
 def test_a_list_without_rows_and_a_large_pool():
