@@ -287,7 +287,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void beam_parts_kernel(const BeamPar
     waiting = 0;
     listed = 0;
   }
-  if (wanted > 0 && count <= 64) {
+  // (a wave by itself does that with its first tile below; so does one whose row has no whole tile)
+  if (WAVES > 1 && wanted > 0 && count <= 64 && (first + 1) * kTile <= p.vocab) {
     Entry<1> e = {0};
     if (tile < end && (tile + 1) * kTile <= p.vocab) {
       float x[kValues];
@@ -312,6 +313,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void beam_parts_kernel(const BeamPar
   double sum = 0;
   Entry<2> best = {};  // the wave's best so far, sorted: key_of the value, ~token
   int n = 0, m = 0;    // entries of the two queues
+  int sorted = 0;      // tokens that were sorted in
   float bar = least ? value_of(least) : -FLT_MAX;
 
   // Sorts the waiting tokens in.  What is left of the tile `t` and earlier ones has to reach the last of the best, later tiles have to
@@ -331,6 +333,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void beam_parts_kernel(const BeamPar
         join64(best, e);
     }
     wave_sync();
+    sorted += m;
     m = 0;
     const uint32_t reached = (uint32_t)__builtin_amdgcn_readlane((int)best.w[0], wanted - 1);
     if (reached == 0) return;
@@ -429,7 +432,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void beam_parts_kernel(const BeamPar
         m += __popcll(mask);
       }
       left = __ballot(hits != 0) != 0;
-      if (left || (done && m >= (last ? kSortLast : kSortFrom)) || (least == 0 && !last)) sort_in(tile);
+      if (left || (done && m >= (last ? kSortLast : kSortFrom)) || (least == 0 && sorted + m >= wanted && !last)) sort_in(tile);
     }
     if (!fresh) again = done ? -1 : again + 64;
     if (!fresh && done) n = 0;
@@ -661,12 +664,12 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
 // against 17.8 for 90 of 50001 in fp32; up to sixteen, which wait for each other: 12.7 and 17.3).
 constexpr int kWavesWanted = 4096;
 struct RowCut {
-  int32_t parts, tiles, waves;  // parts of a row, tiles of a part, waves of a part's workgroup (4 or 8)
+  int32_t parts, tiles, waves;  // parts of a row, tiles of a part, waves of a part's workgroup (1, 2, 4 or 8)
 };
 static RowCut cut_rows(int32_t n_rows, int32_t vocab) {
   const int64_t tiles = ceil_div64(vocab, kTile), per_row = std::min<int64_t>(tiles, std::max(kWavesWanted / std::max(n_rows, 1), 1));
   RowCut c;
-  c.waves = per_row <= 4 ? 4 : 8;
+  c.waves = per_row <= 1 ? 1 : per_row <= 2 ? 2 : per_row <= 4 ? 4 : 8;
   c.tiles = (int32_t)ceil_div64(tiles, ceil_div64(per_row, c.waves));
   c.parts = (int32_t)ceil_div64(tiles, c.tiles);
   return c;
@@ -674,7 +677,11 @@ static RowCut cut_rows(int32_t n_rows, int32_t vocab) {
 template <typename T>
 static void launch_parts(const BeamParams& p, const RowCut& cut, hipStream_t stream) {
   const dim3 grid((unsigned)cut.parts, (unsigned)p.n_rows), threads(64 * cut.waves);
-  if (cut.waves == 4)
+  if (cut.waves == 1)
+    hipLaunchKernelGGL((beam_parts_kernel<T, 1>), grid, threads, 0, stream, p);
+  else if (cut.waves == 2)
+    hipLaunchKernelGGL((beam_parts_kernel<T, 2>), grid, threads, 0, stream, p);
+  else if (cut.waves == 4)
     hipLaunchKernelGGL((beam_parts_kernel<T, 4>), grid, threads, 0, stream, p);
   else
     hipLaunchKernelGGL((beam_parts_kernel<T, 8>), grid, threads, 0, stream, p);
