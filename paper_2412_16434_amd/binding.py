@@ -490,9 +490,12 @@ def _load_beam_calls():
     _beam_calls = False
     module = getattr(compiled, "__self__", None)
     if hasattr(module, "bind_beam"):
-        lib = load_library()
+        if _draft_calls is None:
+            _load_draft_calls()
+        lib, tensor = load_library(), _torch().Tensor
         module.bind_beam(*(C.cast(f, C.c_void_p).value for f in (
-            lib.symph_beam_select, lib.symph_kv_fork, lib.symph_kv_copy_blocks, lib.symph_kv_free, lib.symph_kv_compact)))
+            lib.symph_beam_select, lib.symph_kv_fork, lib.symph_kv_copy_blocks, lib.symph_kv_free, lib.symph_kv_compact)),
+            tensor, getattr(tensor, "__dlpack_c_exchange_api__", None))
         _beam_calls = module
     return _beam_calls
 

@@ -1,6 +1,7 @@
 """Compile the HIP sources into ``libsymph.so`` (gfx950 only), in-tree next to this file."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -34,8 +35,15 @@ def build_attn_call() -> bool:
         print("[build] no gcc: the attention call is marshalled in Python", file=sys.stderr)
         return False
     tmp = CALL_LIB + f".tmp{os.getpid()}"
-    subprocess.check_call([gcc, "-O2", "-std=c11", "-Wall", "-shared", "-fPIC", "-I", include, "-I",
-                           os.path.join(ROOT, "include"), os.path.join(CSRC, "attn_call.c"), "-o", tmp])
+    base = [gcc, "-O2", "-std=c11", "-Wall", "-shared", "-fPIC", "-I", include, "-I", os.path.join(ROOT, "include"),
+            os.path.join(CSRC, "attn_call.c"), "-o", tmp]
+    # With the header of torch's tensor exchange where it has one that is new enough, else without
+    spec = importlib.util.find_spec("torch")
+    exchange = os.path.join(os.path.dirname(spec.origin), "include", "ATen") if spec and spec.origin else None
+    with_exchange = exchange and os.path.exists(os.path.join(exchange, "dlpack.h")) and subprocess.run(
+        [*base, "-DSYMPH_DLPACK", "-I", exchange], stdout=subprocess.DEVNULL, stderr=subprocess.DEVNULL).returncode == 0
+    if not with_exchange:
+        subprocess.check_call(base)
     os.replace(tmp, CALL_LIB)
     return True
 

@@ -10,6 +10,12 @@
 
 #include "symph.h"
 
+// A tensor's description in one call, where this torch has the exchange interface of DLPack for C (the build passes the folder of its
+// header): a vector argument takes 0.05 us that way and 0.26 through five attributes.
+#if defined(SYMPH_DLPACK)
+#include <dlpack.h>
+#endif
+
 typedef int32_t (*attn_fn)(const symph_kv_cache*, int32_t, const void*, const void*, const void*, void*, const int32_t*,
                            const int32_t*, const int32_t*, int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, float, void*,
                            int64_t, void*);
@@ -50,6 +56,10 @@ static fork_fn fork_entry;
 static copy_fn copy_entry;
 static free_fn free_entry;
 static compact_fn compact_entry;
+#if defined(SYMPH_DLPACK)
+static const DLPackExchangeAPI* exchange;  // NULL: by attributes
+static PyTypeObject* tensor_type;
+#endif
 static PyObject *t_bf16, *t_fp32, *t_int32, *t_int64, *raw_stream, *get_device;
 static PyObject *s_dtype, *s_shape, *s_is_cuda, *s_is_contiguous, *s_data_ptr, *s_stride, *s_numel, *s_element_size, *s_get_device;
 
@@ -78,11 +88,22 @@ static PyObject* bind_draft(PyObject* self, PyObject* args) {
   Py_RETURN_NONE;
 }
 
-// (after bind())
+// (after bind() and bind_draft(), whose types these are)
 static PyObject* bind_beam(PyObject* self, PyObject* args) {
   unsigned long long a, b, c, d, e;
+  PyObject *tensor, *capsule;
   (void)self;
-  if (!PyArg_ParseTuple(args, "KKKKK", &a, &b, &c, &d, &e)) return NULL;
+  if (!PyArg_ParseTuple(args, "KKKKKOO", &a, &b, &c, &d, &e, &tensor, &capsule)) return NULL;
+#if defined(SYMPH_DLPACK)
+  exchange = NULL;
+  if (PyType_Check(tensor) && PyCapsule_IsValid(capsule, "dlpack_exchange_api")) {
+    const DLPackExchangeAPI* api = (const DLPackExchangeAPI*)PyCapsule_GetPointer(capsule, "dlpack_exchange_api");
+    if (api && api->header.version.major == DLPACK_MAJOR_VERSION && api->dltensor_from_py_object_no_sync) {
+      Py_INCREF(tensor), Py_INCREF(capsule);  // (both live as long as torch)
+      exchange = api, tensor_type = (PyTypeObject*)tensor;
+    }
+  }
+#endif
   select_entry = (select_fn)(uintptr_t)a, fork_entry = (fork_fn)(uintptr_t)b, copy_entry = (copy_fn)(uintptr_t)c;
   free_entry = (free_fn)(uintptr_t)d, compact_entry = (compact_fn)(uintptr_t)e;
   Py_RETURN_NONE;
@@ -367,41 +388,95 @@ static int current_place(place* at) {
   Py_XDECREF(device);
   return ok && !PyErr_Occurred();
 }
-static int dense_at(PyObject* t, PyObject* dtype, const place* at, void** ptr) {
-  int64_t device, p;
+// What a tensor is: its n sizes and strides (n < 0: any number, not written down), whether it is dense
+typedef struct {
+  int64_t sizes[5], strides[5], bytes;
+  void* data;
+  int dense;
+} tensor_at;
+
+#if defined(SYMPH_DLPACK)
+static int exchanged(PyObject* t, PyObject* dtype, int n, const place* at, tensor_at* out) {
+  DLTensor d;
+  if (!PyObject_TypeCheck(t, tensor_type) || exchange->dltensor_from_py_object_no_sync(t, &d) != 0) return 0;
+  if (d.device.device_type != kDLROCM || d.device.device_id != at->device || (n >= 0 && d.ndim != n) || d.dtype.lanes != 1) return 0;
+  const int bits = d.dtype.bits;
+  if (dtype && !(dtype == t_int32   ? d.dtype.code == kDLInt && bits == 32
+                 : dtype == t_int64 ? d.dtype.code == kDLInt && bits == 64
+                 : dtype == t_fp32  ? d.dtype.code == kDLFloat && bits == 32
+                 : dtype == t_bf16  ? d.dtype.code == kDLBfloat && bits == 16
+                                    : 0))
+    return 0;
+  out->dense = 1;
+  int64_t count = 1;
+  for (int i = d.ndim - 1; i >= 0; --i) {
+    if (d.strides && d.shape[i] > 1 && d.strides[i] != count) out->dense = 0;
+    if (n >= 0 && i < 5) out->sizes[i] = d.shape[i], out->strides[i] = d.strides ? d.strides[i] : count;
+    count *= d.shape[i];
+  }
+  if (count == 0) out->dense = 1;
+  out->bytes = count * ((bits + 7) / 8);
+  out->data = (char*)d.data + d.byte_offset;
+  return 1;
+}
+#endif
+
+static int look(PyObject* t, PyObject* dtype, int n, const place* at, tensor_at* out) {
+#if defined(SYMPH_DLPACK)
+  if (exchange) return exchanged(t, dtype, n, at, out);
+#endif
+  int64_t device, p, count, size;
   if (!method_int(t, s_get_device, &device) || device != at->device || (dtype && !attr_is(t, s_dtype, dtype))) return 0;
+  if (n >= 0 && (!dims(t, s_shape, 0, n, out->sizes) || !dims(t, s_stride, 1, n, out->strides))) return 0;
   PyObject* r = PyObject_CallMethodNoArgs(t, s_is_contiguous);
-  const int ok = r == Py_True;
+  out->dense = r == Py_True;
   Py_XDECREF(r);
-  if (!ok || !method_int(t, s_data_ptr, &p)) return 0;
-  *ptr = (void*)(uintptr_t)p;
+  if (!method_int(t, s_data_ptr, &p) || !method_int(t, s_numel, &count) || !method_int(t, s_element_size, &size)) return 0;
+  out->bytes = count * size;
+  out->data = (void*)(uintptr_t)p;
   return 1;
 }
 static int vector_at(PyObject* t, PyObject* dtype, int64_t least, int optional, const place* at, void** ptr, int64_t* length) {
-  int64_t n;
+  tensor_at x;
   if (t == Py_None) {
     *ptr = NULL;
     return optional;
   }
-  if (!dims(t, s_shape, 0, 1, &n) || n < least || n > INT32_MAX || !dense_at(t, dtype, at, ptr)) return 0;
-  if (length) *length = n;
+  if (!look(t, dtype, 1, at, &x) || !x.dense || x.sizes[0] < least || x.sizes[0] > INT32_MAX) return 0;
+  *ptr = x.data;
+  if (length) *length = x.sizes[0];
   return 1;
 }
 // An int32 [>= rows][stride] table; stride < 0: any, which becomes it
 static int table_at(PyObject* t, int64_t rows, int64_t* stride, const place* at, void** ptr) {
-  int64_t d[2];
-  if (!dims(t, s_shape, 0, 2, d) || d[0] < rows || d[1] > INT32_MAX || (*stride >= 0 && d[1] != *stride) ||
-      !dense_at(t, t_int32, at, ptr))
+  tensor_at x;
+  if (!look(t, t_int32, 2, at, &x) || !x.dense || x.sizes[0] < rows || x.sizes[1] > INT32_MAX || (*stride >= 0 && x.sizes[1] != *stride))
     return 0;
-  *stride = d[1];
+  *stride = x.sizes[1];
+  *ptr = x.data;
   return 1;
 }
 static int scratch_at(PyObject* t, const place* at, void** ptr, int64_t* bytes) {
-  int64_t n, e;
+  tensor_at x;
   *ptr = NULL, *bytes = 0;
   if (t == Py_None) return 1;
-  if (!dense_at(t, NULL, at, ptr) || !method_int(t, s_numel, &n) || !method_int(t, s_element_size, &e)) return 0;
-  *bytes = n * e;
+  if (!look(t, NULL, -1, at, &x) || !x.dense) return 0;
+  *ptr = x.data, *bytes = x.bytes;
+  return 1;
+}
+// The pools of a cache on the current device
+static int pools_at(PyObject* k, PyObject* v, const place* at, symph_kv_cache* c) {
+  tensor_at x, y;
+  const int wide = look(k, t_fp32, 5, at, &x);
+  if (!wide) PyErr_Clear();
+  if ((!wide && !look(k, t_bf16, 5, at, &x)) || !look(v, wide ? t_fp32 : t_bf16, 5, at, &y)) return 0;
+  for (int i = 0; i < 5; ++i)
+    if (x.sizes[i] > INT32_MAX) return 0;
+  c->k_base = x.data, c->v_base = y.data;
+  c->layer_stride = x.strides[0], c->block_stride = x.strides[1];
+  c->n_layers = (int32_t)x.sizes[0], c->n_blocks = (int32_t)x.sizes[1], c->block_size = (int32_t)x.sizes[2];
+  c->n_kv_heads = (int32_t)x.sizes[3], c->head_dim = (int32_t)x.sizes[4];
+  c->dtype = wide ? SYMPH_FP32 : SYMPH_BF16;
   return 1;
 }
 
@@ -409,25 +484,24 @@ static int scratch_at(PyObject* t, const place* at, void** ptr, int64_t* bytes) 
 static PyObject* select_beams(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   (void)self;
   place at;
-  int64_t d[2], strides[2], n, total, device, ws_bytes, p;
-  int32_t most, end, status;
+  tensor_at x;
+  int64_t n, total, ws_bytes;
+  int32_t most, end, status, wide = 0;
   void *scores, *cu, *cu_next, *parents, *tokens, *best, *ends, *ws;
-  PyObject* dt = n_args == 11 ? PyObject_GetAttr(a[0], s_dtype) : NULL;
-  Py_XDECREF(dt);  // (torch's dtypes live as long as the module)
-  if (!dt || !select_entry || (dt != t_bf16 && dt != t_fp32) || !current_place(&at) || !dims(a[0], s_shape, 0, 2, d) ||
-      !dims(a[0], s_stride, 1, 2, strides) || d[0] > INT32_MAX || d[1] > INT32_MAX || (d[1] > 1 && strides[1] != 1) ||
-      (d[0] > 1 && strides[0] < d[1]) || !method_int(a[0], s_get_device, &device) || device != at.device ||
-      !method_int(a[0], s_data_ptr, &p) || !vector_at(a[1], t_fp32, d[0], 0, &at, &scores, NULL) ||
-      !vector_at(a[2], t_int32, 1, 0, &at, &cu, &n) || (n -= 1) < 0 || !vector_at(a[3], t_int32, n + 1, 0, &at, &cu_next, NULL) ||
-      !as_int32(a[4], &most) || !vector_at(a[5], t_int32, 0, 0, &at, &parents, &total) ||
-      !vector_at(a[6], t_int32, total, 0, &at, &tokens, NULL) || !vector_at(a[7], t_fp32, total, 0, &at, &best, NULL) ||
-      !as_int32(a[8], &end) || !vector_at(a[9], t_fp32, d[0], 1, &at, &ends, NULL) || !scratch_at(a[10], &at, &ws, &ws_bytes)) {
+  if (n_args != 11 || !select_entry || !current_place(&at) ||
+      (!look(a[0], t_bf16, 2, &at, &x) && (PyErr_Clear(), !(wide = look(a[0], t_fp32, 2, &at, &x)))) || x.sizes[0] > INT32_MAX ||
+      x.sizes[1] > INT32_MAX || (x.sizes[1] > 1 && x.strides[1] != 1) || (x.sizes[0] > 1 && x.strides[0] < x.sizes[1]) ||
+      !vector_at(a[1], t_fp32, x.sizes[0], 0, &at, &scores, NULL) || !vector_at(a[2], t_int32, 1, 0, &at, &cu, &n) || (n -= 1) < 0 ||
+      !vector_at(a[3], t_int32, n + 1, 0, &at, &cu_next, NULL) || !as_int32(a[4], &most) ||
+      !vector_at(a[5], t_int32, 0, 0, &at, &parents, &total) || !vector_at(a[6], t_int32, total, 0, &at, &tokens, NULL) ||
+      !vector_at(a[7], t_fp32, total, 0, &at, &best, NULL) || !as_int32(a[8], &end) ||
+      !vector_at(a[9], t_fp32, x.sizes[0], 1, &at, &ends, NULL) || !scratch_at(a[10], &at, &ws, &ws_bytes)) {
     PyErr_Clear();
     Py_RETURN_NONE;
   }
   Py_BEGIN_ALLOW_THREADS
-  status = select_entry((void*)(uintptr_t)p, strides[0] < d[1] ? d[1] : strides[0], dt == t_bf16 ? SYMPH_BF16 : SYMPH_FP32, (int32_t)d[0],
-                        (int32_t)d[1], scores, cu, cu_next, (int32_t)n, (int32_t)total, most, end, parents, tokens, best, ends, ws,
+  status = select_entry(x.data, x.sizes[0] > 1 ? x.strides[0] : x.sizes[1], wide ? SYMPH_FP32 : SYMPH_BF16, (int32_t)x.sizes[0],
+                        (int32_t)x.sizes[1], scores, cu, cu_next, (int32_t)n, (int32_t)total, most, end, parents, tokens, best, ends, ws,
                         ws_bytes, at.stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(status);
@@ -464,13 +538,11 @@ static PyObject* copy_blocks(PyObject* self, PyObject* const* a, Py_ssize_t n_ar
   (void)self;
   place at;
   symph_kv_cache c;
-  int64_t n, device;
+  int64_t n;
   int32_t status;
-  PyObject* dt;
   void *src, *dst, *count;
-  if (n_args != 5 || !copy_entry || !current_place(&at) || !describe(a[0], a[1], &dt, &c) ||
-      !method_int(a[0], s_get_device, &device) || device != at.device || !method_int(a[1], s_get_device, &device) ||
-      device != at.device || !vector_at(a[2], t_int32, 0, 0, &at, &src, &n) || !vector_at(a[3], t_int32, n, 0, &at, &dst, NULL) ||
+  if (n_args != 5 || !copy_entry || !current_place(&at) || !pools_at(a[0], a[1], &at, &c) ||
+      !vector_at(a[2], t_int32, 0, 0, &at, &src, &n) || !vector_at(a[3], t_int32, n, 0, &at, &dst, NULL) ||
       !vector_at(a[4], t_int32, n, 1, &at, &count, NULL)) {
     PyErr_Clear();
     Py_RETURN_NONE;
@@ -542,7 +614,7 @@ static PyMethodDef methods[] = {
     {"mask", (PyCFunction)(void (*)(void))mask, METH_FASTCALL, "tree_mask, likewise"},
     {"accept", (PyCFunction)(void (*)(void))accept, METH_FASTCALL, "tree_accept, likewise"},
     {"commit", (PyCFunction)(void (*)(void))commit, METH_FASTCALL, "kv_commit, likewise"},
-    {"bind_beam", bind_beam, METH_VARARGS, "bind_beam(addresses of beam_select, kv_fork, kv_copy_blocks, kv_free, kv_compact)"},
+    {"bind_beam", bind_beam, METH_VARARGS, "bind_beam(addresses of beam_select, kv_fork, kv_copy_blocks, kv_free, kv_compact, torch.Tensor, its exchange capsule or None)"},
     {"select_beams", (PyCFunction)(void (*)(void))select_beams, METH_FASTCALL, "beam_select, likewise"},
     {"fork_rows", (PyCFunction)(void (*)(void))fork_rows, METH_FASTCALL, "kv_fork, likewise"},
     {"copy_blocks", (PyCFunction)(void (*)(void))copy_blocks, METH_FASTCALL, "kv_copy_blocks, likewise"},
