@@ -161,34 +161,46 @@ __global__ __launch_bounds__(kThreads) void fork_rows_kernel(const ForkParams p)
   }
   const int row = blockIdx.x;
   const bool last = row == p.n_out - 1;
-  for (int i = tid; i < p.n_rows; i += kThreads) first[i] = 0x7FFFFFFF;
-  __syncthreads();
-  for (int i = tid; i <= row; i += kThreads) {
-    const int up = p.parents[i];
-    if (up >= 0 && up < p.n_rows) atomicMin(first + up, i);
-  }
-  __syncthreads();
-  int before = 0;
-  for (int i = tid; i < row; i += kThreads) {
-    const int up = p.parents[i];
-    if (up < 0 || up >= p.n_rows || first[up] == i) continue;
-    const RowBlocks b = blocks_of_row(p.shape, up);
-    before += b.whole < b.used;
-  }
-  before = group_sum(before, fork_lds);
+  // What the row itself needs is on its way while the others are counted
   const int up = p.parents[row];
   const bool valid = up >= 0 && up < p.n_rows;
   const int len = valid ? p.shape.lens[up] : 0;
   const RowBlocks b = blocks_of(p.shape, len, valid && p.shape.held ? p.shape.held[up] : 0);
+  const int64_t begin = p.free_begin ? p.free_begin[0] : 0;
+  const int32_t* const from = p.table + (int64_t)(valid ? up : 0) * p.shape.stride;
+  int32_t* const to = p.table_out + (int64_t)row * p.shape.stride;
+  constexpr int kAhead = 2;
+  int ids[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) ids[u] = valid && p.shape.stride > 0 ? entry_or(from, tid + u * kThreads, p.shape.stride, -1) : -1;
+
+  for (int i = tid; i < p.n_rows; i += kThreads) first[i] = 0x7FFFFFFF;
+  __syncthreads();
+  for (int i = tid; i <= row; i += kThreads) {
+    const int other = p.parents[i];
+    if (other >= 0 && other < p.n_rows) atomicMin(first + other, i);
+  }
+  __syncthreads();
+  int before = 0;
+  for (int i = tid; i < row; i += kThreads) {
+    const int other = p.parents[i];
+    if (other < 0 || other >= p.n_rows || first[other] == i) continue;
+    const RowBlocks o = blocks_of_row(p.shape, other);
+    before += o.whole < o.used;
+  }
+  before = group_sum(before, fork_lds);
   const bool keeps = valid && first[up] == row, copies = valid && !keeps && b.whole < b.used;
   const int held = !valid ? 0 : keeps ? b.held : b.used;
-  const int64_t place = (int64_t)(p.free_begin ? p.free_begin[0] : 0) + before;
+  const int64_t place = begin + before;
   int made = -1;
   if (copies && place >= 0 && place < p.n_free) made = p.free_blocks[place];
   if (made < 0 || made >= p.n_blocks) made = -1;
-  const int32_t* const from = p.table + (int64_t)(valid ? up : 0) * p.shape.stride;
-  int32_t* const to = p.table_out + (int64_t)row * p.shape.stride;
-  for (int c = tid; c < held; c += kThreads) to[c] = copies && c == b.whole ? made : from[c];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    const int c = tid + u * kThreads;
+    if (c < held) to[c] = copies && c == b.whole ? made : ids[u];
+  }
+  for (int c = tid + kAhead * kThreads; c < held; c += kThreads) to[c] = copies && c == b.whole ? made : from[c];
   if (tid == 0) {
     p.lens_out[row] = max(len, 0);
     if (p.held_out) p.held_out[row] = held;
@@ -214,17 +226,25 @@ __global__ __launch_bounds__(kThreads) void fork_refs_kernel(const ForkParams p)
     }
     return;
   }
-  int children = 0;
-  for (int i = tid; i < p.n_out; i += kThreads) children += p.parents[i] == row;
-  children = group_sum(children, sums);
-  if (children == 1) return;
   const RowBlocks b = blocks_of_row(p.shape, row);
   const int32_t* const from = p.table + (int64_t)row * p.shape.stride;
+  constexpr int kAhead = 2;  // entries that are on their way while the children are counted
+  int ids[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) ids[u] = p.shape.stride > 0 ? entry_or(from, tid + u * kThreads, p.shape.stride, -1) : -1;
+  int children = 0;
+  for (int i0 = tid; i0 < p.n_out; i0 += 4 * kThreads)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) children += entry_or(p.parents, i0 + u * kThreads, p.n_out, -1) == row;
+  children = group_sum(children, sums);
+  if (children == 1) return;
   const int end = children == 0 ? b.held : b.whole;
-  for (int c = tid; c < end; c += kThreads) {
-    const int id = from[c];
-    if (id >= 0 && id < p.n_blocks) atomicAdd(p.refs_after + id, children - 1);
-  }
+  auto add = [&](int c, int id) {
+    if (c < end && id >= 0 && id < p.n_blocks) atomicAdd(p.refs_after + id, children - 1);
+  };
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) add(tid + u * kThreads, ids[u]);
+  for (int c = tid + kAhead * kThreads; c < end; c += kThreads) add(c, from[c]);
 }
 
 // ---- copies of blocks --------------------------------------------------------------------------------------------
@@ -388,10 +408,16 @@ __global__ __launch_bounds__(kThreads) void free_rows_kernel(const FreeParams p)
   const bool gone = p.drop[row] != 0;
   if (gone) {
     const int32_t* const from = p.table + (int64_t)row * p.shape.stride;
-    for (int c = tid; c < b.held; c += kThreads) {
-      const int id = from[c];
-      if (id < 0 || id >= p.n_blocks) continue;
-      if (atomicSub(p.refs_after + id, 1) == 1) atomicAdd(p.counts + (id >> p.run_shift), 1);
+    constexpr int kAhead = 2;
+    for (int c0 = tid; c0 < b.held; c0 += kAhead * kThreads) {
+      int id[kAhead], were[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) id[u] = entry_or(from, c0 + u * kThreads, b.held, -1);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) were[u] = id[u] >= 0 && id[u] < p.n_blocks ? atomicSub(p.refs_after + id[u], 1) : 0;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (were[u] == 1) atomicAdd(p.counts + (id[u] >> p.run_shift), 1);
     }
   }
   __syncthreads();  // (the lengths may be written over)
@@ -401,26 +427,43 @@ __global__ __launch_bounds__(kThreads) void free_rows_kernel(const FreeParams p)
   }
 }
 
-// What the workgroups before this one counted, and all of them.
-__device__ __forceinline__ int counted_before(const int32_t* counts, int groups, int group, int* at, int* total) {
-  int before = 0, all = 0;
-  for (int g = threadIdx.x; g < groups; g += kThreads) {
-    const int n = counts[g];
-    all += n;
-    if (g < group) before += n;
+// What the groups before `group`, those before `other`, and all of them counted
+struct Counted {
+  int before, other, total;
+};
+__device__ __forceinline__ Counted counted(const int32_t* counts, int groups, int group, int other, int (*at)[3]) {
+  int n[kMostGroups / kThreads], sum[3] = {0, 0, 0};
+#pragma unroll
+  for (int u = 0; u < kMostGroups / kThreads; ++u) n[u] = entry_or(counts, threadIdx.x + u * kThreads, groups, 0);
+#pragma unroll
+  for (int u = 0; u < kMostGroups / kThreads; ++u) {
+    const int g = threadIdx.x + u * kThreads;
+    sum[0] += g < group ? n[u] : 0;
+    sum[1] += g < other ? n[u] : 0;
+    sum[2] += n[u];
   }
-  *total = group_sum(all, at);
-  return group_sum(before, at);
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const int incl = wave_inclusive_scan(sum[k]);
+    if ((threadIdx.x & 63) == 63) at[threadIdx.x >> 6][k] = incl;
+  }
+  __syncthreads();
+  Counted c;
+  c.before = at[0][0] + at[1][0] + at[2][0] + at[3][0];
+  c.other = at[0][1] + at[1][1] + at[2][1] + at[3][1];
+  c.total = at[0][2] + at[1][2] + at[2][2] + at[3][2];
+  return c;
 }
 
 // A workgroup per kListRuns runs
 constexpr int kListRuns = kTile / 64;
 __global__ __launch_bounds__(kThreads) void free_list_kernel(const FreeParams p) {
-  __shared__ int sums[4];
+  __shared__ int sums[4], known[4][3];
   const int tiles = 1 << (p.run_shift - 6);
   const int64_t begin = (int64_t)blockIdx.x * tiles * kTile;
-  int total;
-  int at = counted_before(p.counts, p.n_runs, blockIdx.x * kListRuns, sums, &total);
+  const Counted all = counted(p.counts, p.n_runs, blockIdx.x * kListRuns, 0, known);
+  const int total = all.total;
+  int at = all.before;
   if (blockIdx.x == 0 && threadIdx.x == 0) p.n_free[0] = total;
   for (int t = 0; t < tiles; ++t) {
     const int64_t b0 = begin + (int64_t)t * kTile + threadIdx.x * kEach;
@@ -544,19 +587,20 @@ __device__ __forceinline__ void place_block(const CompactParams& p, int b, bool 
 
 // The k-th block in use from `keep` on goes to the k-th block below `keep` that is not.
 __global__ __launch_bounds__(kThreads) void compact_moves_kernel(const CompactParams p) {
-  __shared__ int sums[4];
+  __shared__ int sums[4], known[4][3], at_edge[4][3];
   const int tid = threadIdx.x;
-  int total;
-  int before = counted_before(p.counts, gridDim.x, blockIdx.x, sums, &total);
-  const int keep = p.n_keep < 0 ? total : min(p.n_keep, p.n_blocks);
-  // Blocks in use below `keep`: the workgroups before the one that has it, and that one's own up to it
+  // Blocks in use below `keep`: the workgroups' before the one that has it, and that one's own up to it
   const int64_t run = (int64_t)p.tiles * kTile;
-  const int edge = (int)min((int64_t)keep / run, (int64_t)gridDim.x);
-  int ignored;
-  int below = counted_before(p.counts, gridDim.x, edge, sums, &ignored);
+  const int edge_known = p.n_keep < 0 ? 0 : (int)(min(p.n_keep, p.n_blocks) / run);
+  const Counted all = counted(p.counts, gridDim.x, blockIdx.x, edge_known, known);
+  const int total = all.total, keep = p.n_keep < 0 ? total : min(p.n_keep, p.n_blocks);
+  const int edge = (int)(keep / run);
+  int before = all.before, below = p.n_keep < 0 ? counted(p.counts, gridDim.x, edge, 0, at_edge).before : all.other;
   {
     int n = 0;
-    for (int64_t b = edge * run + tid; b < keep; b += kThreads) n += p.refs[b] > 0;
+    for (int64_t b0 = edge * run + tid; b0 < keep; b0 += kEach * kThreads)
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) n += entry_or(p.refs, b0 + u * kThreads, keep, 0) > 0;
     below += group_sum(n, sums);
   }
   const int moves = min(min(keep - below, total - below), p.n_pairs);
