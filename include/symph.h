@@ -487,12 +487,13 @@ int32_t symph_kv_commit(const symph_kv_cache* cache, const void* d_k_new, const 
  * -1, -1 and -infinity where there are fewer, and from max_next on.  Written per beam, where d_end_scores (fp32 [n_rows]) is not NULL:
  * score(r, end_token) where that is among the first W_s (at most max_next) of ALL candidates of the session, else -infinity.
  * No candidates: tokens with a logit of -infinity or NaN (they add nothing to the sum), beams whose score is not finite (an ended
- * beam's is -infinity; their logits are not read).  A logit of +infinity counts as the largest fp32 number.
+ * beam's is -infinity; whatever its logits hold).  A logit of +infinity counts as the largest fp32 number.
  * max_next >= max W_s, at most SYMPH_BEAM_MAX; total_next: entries of the outputs.  row_stride in elements, any address of the type.
  * Entries behind the last session's, and rows behind its beams, are left as they were.  d_next_scores must not be d_scores.
  * d_workspace: at least symph_beam_select_workspace_bytes(...) bytes, 256-byte aligned; nothing has to be cleared.
  * Arithmetic: exponentials in fp32, their sums, the logarithm and the scores in 64 bits, so that nearly equal scores of different
- * beams keep their order to about 1e-8; scores are rounded to fp32 once.  Beams with the same logits and score tie exactly.
+ * beams keep their order to about 1e-7; scores are rounded to fp32 once.  Within a beam the logits decide.  Beams with the same logits
+ * and score tie exactly, wherever their rows lie.  Up to 65535 rows and a vocabulary below 2^31 - 32768, else SYMPH_EUNSUPPORTED.
  */
 #define SYMPH_BEAM_MAX 64
 int32_t symph_beam_select(const void* d_logits, int64_t row_stride, int32_t dtype, int32_t n_rows, int32_t vocab,

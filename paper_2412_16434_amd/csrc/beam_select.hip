@@ -257,7 +257,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void beam_parts_kernel(const BeamPar
   __shared__ uint32_t firsts[WAVES][64];
   // What the best of the wave that is furthest reach, and the complement of the tile up to which they were found: later ones have to pass it
   __shared__ unsigned long long shared_least;
-  __shared__ int waiting, rest[WAVES * kSortLast];  // tokens that wait at the end
+  // Tokens that wait at the end: fewer than kSortLast of a wave whose last tile had some, fewer than kSortFrom of one whose had none
+  __shared__ int waiting, rest[WAVES * kSortFrom];
   __shared__ uint32_t listed;                       // waves that have sorted some
   __shared__ float tops[WAVES];
   __shared__ double sums[WAVES];

@@ -78,7 +78,7 @@ def test_sizes_of_the_vocabulary(vocab, dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("beams,widths", [([1], [1]), ([1], [64]), ([64], [64]), ([64, 1, 0, 3], [3, 0, 5, 64]), ([0], [4]),
-                                          ([130], [17]), ([1] * 70, [2] * 70), ([5, 0, 0, 5], [33, 0, 1, 31])])
+                                          ([130], [17]), ([300, 2], [9, 3]), ([1] * 70, [2] * 70), ([5, 0, 0, 5], [33, 0, 1, 31])])
 def test_widths_of_sessions(beams, widths, dtype):
     rows = sum(beams)
     _check(_normal(max(rows, 1), 5003, dtype, rows), _scores(max(rows, 1), 3), beams, widths, end=17)
@@ -123,6 +123,19 @@ def test_orders_that_fill_every_list(order, dtype):
     x = {"rising": x, "falling": x.flip(0), "late peak": torch.where(torch.arange(vocab) >= vocab - 70, x, torch.zeros(())),
          "steps": torch.floor(x)}[order]
     _check(x.to(dtype).to(DEV).expand(4, vocab).contiguous(), [-1.0, -1.5, -0.5, -1.0], [4], [64], end=vocab - 1)
+
+
+@pytest.mark.parametrize("rows,tiles", [(512, 16), (820, 8), (1366, 3), (2049, 2)])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_tokens_that_wait_while_the_last_tiles_have_none(rows, tiles, dtype):
+    """Forty tokens in every tile of the first half, in as many lanes, and nothing behind: all waves bring theirs to the end at once."""
+    logits = torch.full((rows, tiles * 2048), -INF)
+    per = 8 if dtype == BF16 else 4                     # neighbouring values of a lane
+    rs = np.random.RandomState(rows)
+    for tile in range((tiles + 1) // 2):
+        tokens = tile * 2048 + (np.arange(40) + 8 * tile) % 64 * per
+        logits[:, tokens] = torch.from_numpy(rs.standard_normal((rows, 40)).astype(np.float32))
+    _check(logits.to(dtype).to(DEV), _scores(rows, 4), [1] * rows, [64] * rows, end=(per * 3) % 64)
 
 
 def test_few_tokens_left():
