@@ -385,8 +385,8 @@ __global__ __launch_bounds__(kThreads) void free_carry_kernel(const FreeParams p
 __device__ __forceinline__ void taken_range(const FreeParams& p, int* begin, int* end) {
   *begin = *end = 0;
   if (!p.taken) return;
-  *begin = max(p.taken_begin ? p.taken_begin[0] : 0, 0);
   *end = min(p.taken_end[0], p.n_taken);
+  *begin = min(max(p.taken_begin ? p.taken_begin[0] : 0, 0), max(*end, 0));
 }
 
 // A workgroup per row, and one for the blocks that were taken.  (A count that passes from 0 to 1 or back, in whatever order the changes
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(kThreads) void free_rows_kernel(const FreeParams p)
   if (row == p.n_rows) {
     int begin, end;
     taken_range(p, &begin, &end);
-    for (int i = begin + tid; i < end; i += kThreads) {
+    for (int64_t i = begin + tid; i < end; i += kThreads) {
       const int id = p.taken[i];
       if (id < 0 || id >= p.n_blocks) continue;
       if (atomicAdd(p.refs_after + id, 1) == 0) atomicSub(p.counts + (id >> p.run_shift), 1);
@@ -524,7 +524,7 @@ __global__ __launch_bounds__(kOne) void free_few_kernel(const FreeParams p) {
   }
   int begin, end;
   taken_range(p, &begin, &end);
-  for (int i = begin + tid; i < end; i += kOne) {
+  for (int64_t i = begin + tid; i < end; i += kOne) {
     const int id = p.taken[i];
     if (id >= 0 && id < p.n_blocks) atomicAdd(refs + id, 1);
   }

@@ -147,7 +147,7 @@ def test_blocks_that_were_taken_since(n_blocks):
     lens, held, table, refs, free = R.shared_pages(rs, 4, 3, 16, 200, n_blocks)
     drop = rs.randint(0, 2, size=12)
     for taken, begin, end in ((free, 0, 30), (free, 7, 8), (free, 9, 9), (free, 50, 20), (free[:20], -5, 10 ** 9), (free[:0], 0, 3),
-                              (np.array([-1, n_blocks, free[0], 10 ** 9]), 0, 4)):
+                              (free, 2 ** 31 - 1, 2 ** 31 - 1), (np.array([-1, n_blocks, free[0], 10 ** 9]), 0, 4)):
         _free(drop, lens, held, table, refs, 16, taken=taken, begin=begin, end=end)
     row = int(np.flatnonzero((drop != 0) & (held > 0))[0])
     fresh = refs.copy()
