@@ -509,7 +509,7 @@ constexpr int kSessionWaves = 16, kRows = 256;  // kRows: rows of a session whos
 
 // A workgroup per session, a wave per row.  A row's best are sorted by logit and token, which is the order of their scores as well (far
 // from the sum's logarithm, where 64 bits do not tell scores apart, it is the logits that count); rows are then joined by score, row
-// and place in the row.  A chain of trips to memory: 64 sessions of 8 rows 5 us, 7 of 1 to 24 rows and parts 10 to 12.  (A first bar from
+// and place in the row.  A chain of trips to memory: 64 sessions of 8 rows 5 us, 7 of 2 to 24 rows of four parts 10 to 12.  (A first bar from
 // the rows' largest, so that fewer entries are sorted: 17.6, the bar has to be agreed on first.)
 __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const BeamParams p) {
   __shared__ Entry<4> lists[kSessionWaves][64];
@@ -670,7 +670,7 @@ __global__ __launch_bounds__(64 * kSessionWaves) void beam_sessions_kernel(const
 // How rows are cut: into as many waves as there are places for (four to a SIMD; half as many: 39.6 against 36.3 us for 512 rows of
 // 128256 in bf16), a wave having a tile at least.  Up to eight waves of a row share a workgroup: what they know of each other's first
 // tiles keeps the lists short, and few parts keep the second launch short (four at most: 11.9 against 11.2 us for 32 rows, 19.0
-// against 17.8 for 90 of 50001 in fp32; up to sixteen, which wait for each other: 12.7 and 17.3).
+// against 17.8 for 72 of 50001 in fp32; up to sixteen, which wait for each other: 12.7 and 17.3).
 constexpr int kWavesWanted = 4096;
 struct RowCut {
   int32_t parts, tiles, waves;  // parts of a row, tiles of a part, waves of a part's workgroup (1, 2, 4 or 8)
