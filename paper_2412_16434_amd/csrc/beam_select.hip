@@ -325,8 +325,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void beam_parts_kernel(const BeamPar
   float bar = least ? value_of(least) : -FLT_MAX;
 
   // Sorts the waiting tokens in.  What is left of the tile `t` and earlier ones has to reach the last of the best, later tiles have to
-  // pass it (and what other waves know).
-  auto sort_in = [&](int t) {
+  // pass it (and what other waves know), or to reach it as well while shares of earlier tiles are left in the queue (`shares`).
+  auto sort_in = [&](int t, bool shares) {
     wave_sync();
 #pragma unroll 1
     for (int i = lane; i - lane < m; i += 64) {
@@ -346,13 +346,13 @@ __global__ __launch_bounds__(64 * WAVES, 4) void beam_parts_kernel(const BeamPar
     const uint32_t reached = (uint32_t)__builtin_amdgcn_readlane((int)best.w[0], wanted - 1);
     if (reached == 0) return;
     bar = fmaxf(bar, value_of(reached));
-    least = max(least, reached + 1);
+    least = max(least, reached + (shares ? 0u : 1u));
     const unsigned long long mine = (unsigned long long)reached << 32 | (uint32_t)~t;
     unsigned long long theirs = 0;
     if (lane == 0) theirs = atomicMax(&shared_least, mine);
     const uint32_t their_key = (uint32_t)__builtin_amdgcn_readfirstlane((int)(theirs >> 32));
     const int their_tile = (int)~__builtin_amdgcn_readfirstlane((int)(uint32_t)theirs);
-    least = max(least, their_key + (their_key != 0 && t + WAVES > their_tile ? 1u : 0u));
+    least = max(least, their_key + (their_key != 0 && !shares && t + WAVES > their_tile ? 1u : 0u));
   };
   // A turn looks through a tile, or again through 64 lanes' shares of earlier ones.  (Few lanes of a tile have a token that counts; to
   // look for it tile by tile took a fifth of the launch, so those lanes' values are read again, many tiles' together.)
@@ -440,7 +440,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void beam_parts_kernel(const BeamPar
         m += __popcll(mask);
       }
       left = __ballot(hits != 0) != 0;
-      if (left || (done && m >= (last ? kSortLast : kSortFrom)) || (least == 0 && sorted + m >= wanted && !last)) sort_in(tile);
+      if (left || (done && m >= (last ? kSortLast : kSortFrom)) || (least == 0 && sorted + m >= wanted && !last)) sort_in(tile, fresh && done && n > 0);
     }
     if (!fresh) again = done ? -1 : again + 64;
     if (!fresh && done) n = 0;

@@ -138,6 +138,22 @@ def test_tokens_that_wait_while_the_last_tiles_have_none(rows, tiles, dtype):
     _check(logits.to(dtype).to(DEV), _scores(rows, 4), [1] * rows, [64] * rows, end=(per * 3) % 64)
 
 
+@pytest.mark.parametrize("rows,waves", [(512, 8), (820, 4), (1366, 2), (2049, 1)])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_equal_values_that_are_looked_at_late(rows, waves, dtype):
+    """A wave's second tile has three tokens (few: they are looked at together with later ones) and its third fifty (many: at once), all of
+    one value: the three come first.  In the last row another wave's tiles have the same value behind them."""
+    tile = 2048
+    logits = torch.full((rows, 5 * waves * tile), -INF)
+    per = 8 if dtype == BF16 else 4                     # neighbouring values of a lane
+    lanes = torch.arange(64) * per
+    logits[:, lanes[:20]] = 1.0
+    logits[:, waves * tile + lanes[[5, 9, 40]]] = 2.0
+    logits[:, 2 * waves * tile + lanes[:50]] = 2.0
+    logits[-1, (waves + 1) * tile + lanes[:50]] = 2.0
+    _check(logits.to(dtype).to(DEV), _scores(rows, 6), [1] * rows, [8] * rows, end=waves * tile + 9 * per)
+
+
 def test_few_tokens_left():
     """Fewer candidates than are wanted: what there is, then nothing."""
     logits = torch.full((4, 3000), -INF, device=DEV)
