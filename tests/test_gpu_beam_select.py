@@ -154,6 +154,23 @@ def test_equal_values_that_are_looked_at_late(rows, waves, dtype):
     _check(logits.to(dtype).to(DEV), _scores(rows, 6), [1] * rows, [8] * rows, end=waves * tile + 9 * per)
 
 
+@pytest.mark.parametrize("rows,waves,beams", [(513, 7, 1), (820, 4, 4), (1366, 2, 2), (2049, 1, 3)])
+@pytest.mark.parametrize("seed", range(4))
+def test_few_values_and_many_tiles(rows, waves, beams, seed):
+    """Tiles of a few tokens, of many and of none by chance, of values that many share, for parts of several tiles a wave."""
+    rs, tile = np.random.RandomState(seed), 2048
+    vocab = 6 * waves * tile + int(rs.randint(tile))
+    kinds, levels = 24, int(rs.choice([1, 2, 5, 40]))
+    drawn = np.full((kinds, vocab), -np.inf, np.float32)
+    for k in range(kinds):
+        for t in range(0, vocab, tile):
+            there = rs.random_sample(min(tile, vocab - t)) < rs.choice([0, 0.0005, 0.002, 0.006, 0.02, 0.05])
+            drawn[k, t:t + there.size][there] = np.floor(rs.random_sample(int(there.sum())) * levels + t * rs.choice([0, 1]) / vocab * levels)
+    logits = torch.from_numpy(drawn).to(BF16 if seed % 2 else FP32).to(DEV)[torch.arange(rows, device=DEV) % kinds]
+    sessions = [beams] * (rows // beams) + ([rows % beams] if rows % beams else [])
+    _check(logits, rs.choice([-1.0, -2.0, -3.5], rows), sessions, rs.choice([1, 4, 9, 30, 64], len(sessions)).tolist(), end=vocab // 3)
+
+
 def test_few_tokens_left():
     """Fewer candidates than are wanted: what there is, then nothing."""
     logits = torch.full((4, 3000), -INF, device=DEV)
