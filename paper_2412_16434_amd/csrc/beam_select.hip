@@ -2,8 +2,8 @@
 //   score(r, t) = scores[r] + x[r][t] - log sum_u exp x[r][u]
 // and candidates are ordered by score, then beam, then token.  Bound by reading the logits once, which the first launch does: every
 // workgroup goes over a part of a row and leaves its largest value, its sum of exponentials and its best tokens.  The second
-// launch joins them session by session.  512 rows of 128256 in bf16, 131 MB: 30 us and 5 us (HBM alone 20), the vector unit 75 % busy with
-// maxima, exponentials and sums.  Four rows of 32000 in fp32: 6.3 and 3.8 us, trips to memory one after another.
+// launch joins them session by session.  512 rows of 128256 in bf16, 131 MB: 30 us and 5 us (HBM alone 20), the vector unit 76 % busy with
+// maxima, exponentials and sums, the memory idle under the workgroups' first bars and last sortings.  Four rows of 32000 in fp32: 6.3 and 3.8 us, trips to memory one after another.
 #include "attn_lanes.h"
 
 #include <algorithm>
@@ -217,8 +217,8 @@ __device__ __forceinline__ float exp_below(float x, float top) {
   const float d = x - top;
   return __builtin_amdgcn_exp2f(fmaf(d, kLog2e, d * kLog2eRest));
 }
-// The sum of exp(x - top) over a lane's values, top being at least the largest.  The vector unit bounds the launch, and one instruction
-// in front of each exponential takes a tenth less than three: x log2 e - c with c = top log2 e rounded, and what c is off by taken out
+// The sum of exp(x - top) over a lane's values, top being at least the largest.  One instruction in front of each
+// exponential takes a tenth less of the launch than three: x log2 e - c with c = top log2 e rounded, and what c is off by taken out
 // behind the sum.  What is left out is (x - top) 1.3e-8 of a term, nearly the same for all rows of a call.  Values that are too large
 // for that (c would be off by more than an exponential takes) go the long way.
 __device__ __forceinline__ float sum_below(const float (&x)[kValues], float top, bool large) {

@@ -76,6 +76,11 @@ def test_sizes_of_the_vocabulary(vocab, dtype):
     _check(_normal(9, vocab, dtype, vocab), _scores(9, vocab), [4, 2, 3], [4, 5, 1], end=vocab // 2)
 
 
+@pytest.mark.parametrize("vocab,width", [(1_300_007, 5), (3_000_001, 64), (3_000_001, 1)])
+def test_rows_of_more_than_64_parts(vocab, width):
+    _check(_normal(2, vocab, BF16, width), _scores(2, 5), [2], [width], end=7)
+
+
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("beams,widths", [([1], [1]), ([1], [64]), ([64], [64]), ([64, 1, 0, 3], [3, 0, 5, 64]), ([0], [4]),
                                           ([130], [17]), ([300, 2], [9, 3]), ([1] * 70, [2] * 70), ([5, 0, 0, 5], [33, 0, 1, 31])])
