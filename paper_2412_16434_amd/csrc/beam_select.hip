@@ -220,11 +220,12 @@ __device__ __forceinline__ float exp_below(float x, float top) {
 // The sum of exp(x - top) over a lane's values, top being at least the largest.  One instruction in front of each
 // exponential takes a tenth less of the launch than three: x log2 e - c with c = top log2 e rounded, and what c is off by taken out
 // behind the sum.  What is left out is (x - top) 1.3e-8 of a term, nearly the same for all rows of a call.  Values that are too large
-// for that (c would be off by more than an exponential takes) go the long way.
+// for that (c would be off by more than an exponential takes) go the long way.  A lane that brings none but -infinity stays on this one, whatever
+// largest value it carries from earlier tiles: its terms are 0, and c is held to where `off` is small, or 0 would be multiplied by infinity.
 __device__ __forceinline__ float sum_below(const float (&x)[kValues], float top, bool large) {
   float s = 0;
   if (__ballot(large) == 0) {
-    const float near = fmaxf(top, -kLarge), c = near * kLog2e, off = fmaf(near, kLog2e, -c);
+    const float near = __builtin_amdgcn_fmed3f(top, -kLarge, kLarge), c = near * kLog2e, off = fmaf(near, kLog2e, -c);
 #pragma unroll
     for (int v = 0; v < kValues; ++v) s += __builtin_amdgcn_exp2f(fmaf(x[v], kLog2e, -c));
     return s * __builtin_amdgcn_exp2f(-off);
