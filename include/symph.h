@@ -466,9 +466,13 @@ int32_t symph_kv_commit(const symph_kv_cache* cache, const void* d_k_new, const 
  *   symph_kv_fork         table rows for the continuations, reference counts, copies to make of blocks that are not full
  *   symph_kv_copy_blocks  those copies, all layers
  *   symph_build_tables, symph_kv_append and the attention calls for the next token, a beam being a session of theirs.
- * A prompt in one row becomes several beams by a fork whose parents name the row several times.  symph_kv_compact says which blocks
- * move so that the end of a pool becomes free.  Contract on blocks: only full blocks are shared (what these calls keep); a row that
- * holds blocks behind those in use (symph_build_tables' d_held_blocks) holds them alone.
+ * Each call takes the counts, lengths, blocks held and free list that the one before it wrote: symph_kv_fork those of symph_kv_free
+ * (d_lens_after and d_held_after too where rows were dropped: with the old lengths a dropped row, which no row continues, would give
+ * its blocks up twice; a row that names it as its parent is empty), the next step's symph_kv_free those of symph_kv_fork and, as blocks
+ * that were taken, symph_build_tables' part of the list.  A prompt in one row becomes several beams by a fork whose parents name the
+ * row several times.  symph_kv_compact says which blocks move so that the end of a pool becomes free.  Contract on blocks: only full
+ * blocks are shared (what these calls keep); a row that holds blocks behind those in use (symph_build_tables' d_held_blocks) holds
+ * them alone.
  * symph_kv_fork, symph_kv_free and symph_kv_compact write new tables and counts and leave the ones they read as they were, so a step
  * that found too few free blocks is undone by dropping its outputs.  They do no work in memory but in what they are given; results
  * are the same from call to call.  A row's blocks are the first H entries of its table row: ceil(len / block_size), or its entry of

@@ -769,7 +769,8 @@ def kv_fork(parents, lens, block_table, refs, free_blocks, block_size: int, tabl
             copy_tokens, held_blocks=None, held_out=None, free_begin=None, blocks_taken=None, stream=None) -> None:
     """Rows that continue rows ``parents`` of ``block_table``: full blocks shared, the last one kept by a row's first child and
     replaced by a block of ``free_blocks`` for the others (``copy_*``: what kv_copy_blocks has to copy); ``refs_after`` <- how many
-    rows hold each block.  A parent outside the table makes an empty row."""
+    rows hold each block.  A parent outside the table makes an empty row.  Behind a kv_free that dropped rows: its ``lens_after`` and
+    ``held_after``, or those rows give their blocks up again."""
     calls = _beam_call(stream)
     if calls:
         status = calls.fork_rows(parents, lens, block_table, refs, free_blocks, block_size, table_out, lens_out, refs_after, copy_src,
