@@ -494,7 +494,8 @@ int32_t symph_kv_commit(const symph_kv_cache* cache, const void* d_k_new, const 
  * beam's is -infinity; whatever its logits hold).  A logit of +infinity counts as the largest fp32 number.
  * max_next >= max W_s, at most SYMPH_BEAM_MAX; total_next: entries of the outputs.  row_stride in elements, any address of the type.
  * Entries behind the last session's, and rows behind its beams, are left as they were.  d_next_scores must not be d_scores.
- * d_workspace: at least symph_beam_select_workspace_bytes(...) bytes, 256-byte aligned; nothing has to be cleared.
+ * d_workspace: at least symph_beam_select_workspace_bytes(...) bytes, 256-byte aligned (else SYMPH_EUNSUPPORTED); nothing has to be
+ * cleared.
  * Arithmetic: exponentials in fp32, their sums, the logarithm and the scores in 64 bits, so that nearly equal scores of different
  * beams keep their order to about 1e-7; scores are rounded to fp32 once.  Within a beam the logits decide.  Beams with the same logits
  * and score tie exactly, wherever their rows lie.  Up to 65535 rows and a vocabulary below 2^31 - 32768, else SYMPH_EUNSUPPORTED.
@@ -550,7 +551,7 @@ int32_t symph_kv_copy_blocks(const symph_kv_cache* cache, const int32_t* d_src_b
  * be NULL) is the list that they came from, entries *d_taken_begin (NULL: 0) .. *d_taken_end - 1 of it, i.e. that call's
  * *d_free_begin and *d_blocks_taken; each counts one holder more.  (It must not be the list that is written.)
  * n_rows may be 0: the list alone.  d_refs_after must not be d_refs.  d_workspace: at least symph_kv_free_workspace_bytes(n_blocks)
- * bytes, 256-byte aligned; nothing has to be cleared.
+ * bytes, 256-byte aligned (else SYMPH_EUNSUPPORTED); nothing has to be cleared.
  */
 int32_t symph_kv_free(const int32_t* d_drop, const int32_t* d_lens, const int32_t* d_held_blocks, int32_t n_rows,
                       const int32_t* d_block_table, int32_t table_stride, int32_t block_size, int32_t n_blocks,
@@ -571,7 +572,7 @@ int64_t symph_kv_free_workspace_bytes(int32_t n_blocks);
  *   d_table_out    (may be d_block_table): the blocks that each row holds after the moves; entries behind them are left as they were;
  *   d_counts       int32 [3]: blocks in use, M, blocks in use that stay behind n_keep.
  * d_refs_after and d_block_map must not be d_refs.  d_workspace: at least symph_kv_compact_workspace_bytes(n_blocks) bytes, 256-byte
- * aligned; nothing has to be cleared.
+ * aligned (else SYMPH_EUNSUPPORTED); nothing has to be cleared.
  */
 int32_t symph_kv_compact(const int32_t* d_refs, int32_t n_blocks, int32_t n_keep, const int32_t* d_lens,
                          const int32_t* d_held_blocks, int32_t n_rows, const int32_t* d_block_table, int32_t table_stride,

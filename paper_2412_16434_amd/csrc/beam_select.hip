@@ -726,6 +726,7 @@ int32_t symph_beam_select(const void* d_logits, int64_t row_stride, int32_t dtyp
   if (n_rows > 65535 || vocab > 0x7FFFFFFF - 16 * kTile || !grid_takes(n_sessions, 64 * kSessionWaves)) return SYMPH_EUNSUPPORTED;
   if (workspace_bytes < symph_beam_select_workspace_bytes(n_rows, vocab, max_next) || (!d_workspace && n_rows > 0))
     return SYMPH_EWORKSPACE;
+  if (n_rows > 0 && ((uintptr_t)d_workspace & 255) != 0) return SYMPH_EUNSUPPORTED;
   const RowCut cut = cut_rows(n_rows, vocab);
   const int64_t parts = (int64_t)n_rows * cut.parts;
   BeamParams p;

@@ -853,6 +853,7 @@ int32_t symph_kv_free(const int32_t* d_drop, const int32_t* d_lens, const int32_
   if (d_refs_after == d_refs || d_free_blocks == d_refs || d_free_blocks == d_refs_after) return SYMPH_EINVAL;
   if (!grid_takes((int64_t)n_rows + 1, kThreads)) return SYMPH_EUNSUPPORTED;
   if (!d_workspace || workspace_bytes < symph_kv_free_workspace_bytes(n_blocks)) return SYMPH_EWORKSPACE;
+  if (((uintptr_t)d_workspace & 255) != 0) return SYMPH_EUNSUPPORTED;
   FreeParams p;
   p.shape = shape_of(d_lens, d_held_blocks, table_stride, block_size);
   p.drop = d_drop;
@@ -902,6 +903,7 @@ int32_t symph_kv_compact(const int32_t* d_refs, int32_t n_blocks, int32_t n_keep
   const int64_t groups = n_rows + (int64_t)std::min<int64_t>(ceil_div64(n_blocks, kTile), kMostGroups);
   if (!grid_takes(groups, kThreads)) return SYMPH_EUNSUPPORTED;
   if (!d_workspace || workspace_bytes < symph_kv_compact_workspace_bytes(n_blocks)) return SYMPH_EWORKSPACE;
+  if (((uintptr_t)d_workspace & 255) != 0) return SYMPH_EUNSUPPORTED;
   CompactParams p;
   p.shape = shape_of(d_lens, d_held_blocks, table_stride, block_size);
   p.refs = d_refs;
