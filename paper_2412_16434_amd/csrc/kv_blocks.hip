@@ -94,12 +94,10 @@ constexpr int kSlice = 4096;  // blocks whose counts a workgroup of a small fork
 // The counts of a slice of the pool after a small fork, every change looked for in the whole table.
 __device__ __forceinline__ void fork_slice(const ForkParams& p, int slice, int* lds) {
   __shared__ int change[kSlice], children[kFewRows], whole[kFewRows], held[kFewRows];
-  int* const first = lds + 4;
   const int tid = threadIdx.x, lo = slice * kSlice, n = min(p.n_blocks - lo, kSlice);
   for (int b = tid; b < kSlice; b += kThreads) change[b] = 0;
   for (int r = tid; r < p.n_rows; r += kThreads) {
     const RowBlocks b = blocks_of_row(p.shape, r);
-    first[r] = 0x7FFFFFFF;
     children[r] = 0;
     whole[r] = b.whole;
     held[r] = b.held | (b.whole < b.used ? 1 << 30 : 0);  // (bit 30: the last block in use is not full; a row has fewer blocks)
@@ -107,9 +105,7 @@ __device__ __forceinline__ void fork_slice(const ForkParams& p, int slice, int* 
   __syncthreads();
   for (int i = tid; i < p.n_out; i += kThreads) {
     const int up = p.parents[i];
-    if (up < 0 || up >= p.n_rows) continue;
-    atomicAdd(children + up, 1);
-    atomicMin(first + up, i);
+    if (up >= 0 && up < p.n_rows) atomicAdd(children + up, 1);
   }
   __syncthreads();
   int made = 0;
