@@ -82,12 +82,19 @@ struct ForkParams {
   int32_t n_out, n_rows, n_free, n_blocks;
 };
 
-// Small calls take one launch, which is what they cost: up to so many table entries, rows and (in one workgroup) blocks.  A fork of 8
-// rows of 507 entries 8.8 us, in two launches 10.8; of 16 such rows 12.7 and 10.0.  A free of 16 rows of 71 entries 6.4, in three launches
-// 12.6; of 32 rows of 383 entries 10.7 and 11.8, a compaction of them 12.3 and 12.7.
-constexpr int kFewEntries = 16384, kFewForked = 4096, kFewRows = 1024, kFewBlocks = 8192;
+// Small calls take one launch, which is what they cost: up to so many table entries, rows (what the LDS arrays hold; a free of 2048 rows
+// of 8 entries 10.8 us so, 11.5 in three launches) and, in one workgroup, blocks.  A fork of 8 rows of 507 entries 8.8 us, in two
+// launches 10.8; of 16 such rows 12.7 and 10.0.  A free in a pool of 8192 blocks, in one launch and in three: 4096 entries 7.0 and 11.4 us,
+// 16384 8.5 and 11.6, 32768 11.5 and 11.8, 65536 17.2 and 14.0; in a pool of 16384 blocks (arrays of twice the size) 14.4 and 11.5.
+// A compaction's workgroup goes over its arrays more often, and entries and blocks count together: 2048 blocks and 16384 entries 8.7 us
+// and in three launches 10.4; 4096 blocks and 12288 entries 9.6 and 10.4, 16384 10.7 and 10.5; 8192 blocks and 4096 entries 10.3 and
+// 11.8, 8192 11.6 and 12.1, 16384 14.1 and 12.2.
+constexpr int kFewEntries = 16384, kFewForked = 4096, kFewRows = 1024, kFewBlocks = 8192, kFewMoved = 24 * 1024;
 static bool few(int32_t n_rows, int32_t table_stride, int32_t entries = kFewEntries) {
   return n_rows <= kFewRows && (int64_t)n_rows * table_stride <= entries;
+}
+static bool few_to_compact(int32_t n_rows, int32_t table_stride, int32_t n_blocks) {
+  return n_blocks <= kFewBlocks && few(n_rows, table_stride) && n_rows * table_stride + 2 * n_blocks <= kFewMoved;
 }
 constexpr int kSlice = 4096;  // blocks whose counts a workgroup of a small fork has
 
@@ -917,7 +924,7 @@ int32_t symph_kv_compact(const int32_t* d_refs, int32_t n_blocks, int32_t n_keep
   p.n_keep = n_keep;
   p.n_pairs = n_pairs;
   p.tiles = cut.tiles;
-  if (n_blocks <= kFewBlocks && few(n_rows, table_stride)) {
+  if (few_to_compact(n_rows, table_stride, n_blocks)) {
     hipLaunchKernelGGL(compact_few_kernel, dim3(1), dim3(kOne), 0, (hipStream_t)stream, p);
     return launched();
   }
