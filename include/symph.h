@@ -496,9 +496,11 @@ int32_t symph_kv_commit(const symph_kv_cache* cache, const void* d_k_new, const 
  * Entries behind the last session's, and rows behind its beams, are left as they were.  d_next_scores must not be d_scores.
  * d_workspace: at least symph_beam_select_workspace_bytes(...) bytes, 256-byte aligned (else SYMPH_EUNSUPPORTED); nothing has to be
  * cleared.
- * Arithmetic: exponentials in fp32, their sums, the logarithm and the scores in 64 bits, so that nearly equal scores of different
- * beams keep their order to about 1e-7; scores are rounded to fp32 once.  Within a beam the logits decide.  Beams with the same logits
- * and score tie exactly, wherever their rows lie.  Up to 65535 rows and a vocabulary below 2^31 - 32768, else SYMPH_EUNSUPPORTED.
+ * Arithmetic: exponentials in fp32; sums of up to 32 of them in fp32, the sums of those, the logarithm and the scores in 64 bits; scores
+ * are rounded to fp32 once.  Nearly equal scores of different beams keep their order to about 1e-7 on logits as models give them; where
+ * one token outweighs all others, what lies beside it in its sum of 32 loses up to 31 half steps, 1.9e-6 of the sum.  Within a beam the
+ * logits decide.  Beams with the same logits and score tie exactly, wherever their rows lie.  Up to 65535 rows and a vocabulary below
+ * 2^31 - 32768, else SYMPH_EUNSUPPORTED.
  */
 #define SYMPH_BEAM_MAX 64
 int32_t symph_beam_select(const void* d_logits, int64_t row_stride, int32_t dtype, int32_t n_rows, int32_t vocab,

@@ -208,7 +208,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 constexpr float kLarge = 1048576.0f;
 // Entries of a wave's two queues: a lane's share of a tile where one of its values may count, and tokens that do.  A wave sorts its
 // tokens in from kSortFrom on, and from kSortLast on behind its last tile; the others are sorted for all waves together.  Tiles where
-// kMany lanes or more have a token that counts are looked through at once.
+// kMany lanes or more have a token that counts are looked through at once.  (The call over 512 rows of 128256 in bf16 takes 34.6 us; kMany 4
+// takes 36, 24 and 48 the same, and with 90 % of the tokens masked 34.4 for 33.0; kSortFrom 32 takes 35.2, 64 the same; kSortLast 8 takes
+// 35.7, in fp32 55.7 for 54.8, 48 the same.)
 constexpr int kQueue = 256, kTokens = 128, kSortFrom = 48, kSortLast = 24, kMany = 12;
 
 // exp(x - top) with the rest of log2 e: the constant's own rounding would be the same for all tokens far below the top
